@@ -75,6 +75,12 @@ typedef enum {
   /* elementwise, binary: O[x] = f(I1[x], I2[x]); implicit broadcast (right-aligned,
      size-1 dims stretch), or f(I1[x], scalar) when attrs.has_scalar */
   KORCH_ADD = 32, KORCH_SUB, KORCH_MUL, KORCH_DIV, KORCH_MAX, KORCH_MIN,
+  /* comparisons: 1 where I1[x] < (<=, >, >=, ==) I2[x], else 0 (NaN compares false) */
+  KORCH_LT, KORCH_LE, KORCH_GT, KORCH_GE, KORCH_EQ,
+  /* elementwise choice: O[x] = C[x] != 0 ? I1[x] : I2[x] (inputs C, I1, I2, broadcast like
+     the binary ones), or I2 = scalar when attrs.has_scalar (inputs C, I1).  The value that is
+     not chosen has no effect (it may be NaN). */
+  KORCH_SELECT = 48,
   /* reduce along attrs.axis (sum / mean = sum/n / max), keepdim per attrs;
      broadcast to attrs.shape */
   KORCH_REDUCE_SUM = 64, KORCH_REDUCE_MEAN, KORCH_REDUCE_MAX, KORCH_BROADCAST,
@@ -87,6 +93,16 @@ typedef enum {
   KORCH_FILL,            /* no operands: a constant tensor of shape attrs.shape (attrs.rank dims)
                             whose every element is attrs.scalar (the ones tensor of the
                             reduction-as-product transformation, Section 3)              */
+  KORCH_IOTA,            /* no operands: a tensor of shape attrs.shape (attrs.rank dims, at most 2^24
+                            long along attrs.axis) whose element is its index along attrs.axis      */
+  KORCH_GATHER,          /* a layout transformation whose map is data: I1 [..., T] is looked up along its
+                            last axis, O[x] = I1[x', clamp(I2[x], 0, T-1)], I2 whole numbers (a NaN looks
+                            up 0); x' is x without I1's size-1 dims: O's shape is I1's shape without
+                            its last axis and I2's, broadcast                                        */
+  KORCH_BIN_SUM,         /* the gather's adjoint: attrs.shape [..., T] (attrs.rank dims) is the result's
+                            shape, O[x', k] = sum of I1[x] over the x with clamp(I2[x], 0, T-1) = k and over
+                            every dim where attrs.shape without its last axis has size 1 (leading dims
+                            that it lacks count as size 1); T at most 4096                           */
   /* linear */
   KORCH_MATMUL = 128,    /* [..., M, K] x [..., K, N] -> [..., M, N], batch dims broadcast */
   KORCH_CONV2D           /* NHWC x HWIO cross-correlation, zero pad attrs.pad, stride attrs.stride */
@@ -125,7 +141,11 @@ typedef enum {
   KORCH_FAM_GEMM = 4,        /* MFMA matrix product with fused prologue / epilogue */
   KORCH_FAM_CONV = 5,        /* implicit-GEMM NHWC convolution + epilogue         */
   KORCH_FAM_ATTENTION = 6,   /* scores, row softmax and second product in one kernel */
-  KORCH_FAM_SPLITK = 7       /* long-contraction product split over workgroups, deterministic */
+  KORCH_FAM_SPLITK = 7,      /* long-contraction product split over workgroups, deterministic */
+  KORCH_FAM_PLANE = 8,       /* products that meet in a plane of scores kept in registers: attention of
+                                any length (softmax in one pass, masks, biases) and its gradients   */
+  KORCH_FAM_ROWCOL = 9,      /* a row program with sums over the rows (LayerNorm's gradient)       */
+  KORCH_FAM_BINSUM = 10      /* a sum by bins on its own                                           */
 } korch_family;
 
 const char* korch_last_error(void);

@@ -3,8 +3,8 @@
 Host C++ sources are compiled with g++ against the HIP runtime headers, the
 HIP source with hipcc for gfx950, and everything is linked with hipcc.  The
 runtime compiler helper `korch_rtc` (csrc/tools) is built next to the library.  The
-device prelude that generated kernels include at run time is embedded into
-the library as a string.
+device sources that generated kernels include at run time are embedded into
+the library as strings.
 
 Usage:  python -m paper_2406_09465_amd.build   (or build() from Python)
 """
@@ -32,12 +32,16 @@ CXX_FLAGS = ["-O2", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function", "-Wn
 
 
 def _embed_device_sources():
-    src = open(os.path.join(CSRC, "device", "prelude.h")).read()
-    if ")KORCHSRC\"" in src:
-        raise RuntimeError("delimiter collision in device prelude")
     out = os.path.join(BUILD, "device_src.cpp")
-    text = ("// generated from csrc/device/prelude.h\nnamespace korch {\n"
-            f"extern const char* k_device_prelude;\nconst char* k_device_prelude = R\"KORCHSRC({src})KORCHSRC\";\n}}\n")
+    text = "// generated from csrc/device\nnamespace korch {\n"
+    for name in ("prelude", "plane"):
+        src = open(os.path.join(CSRC, "device", name + ".h")).read()
+        if ")KORCHSRC\"" in src:
+            raise RuntimeError(f"delimiter collision in device/{name}.h")
+        parts = [src[i:i + 15000] for i in range(0, len(src), 15000)]
+        literal = " ".join(f"R\"KORCHSRC({p})KORCHSRC\"" for p in parts)
+        text += f"extern const char* k_device_{name};\nconst char* k_device_{name} = {literal};\n"
+    text += "}\n"
     if not os.path.exists(out) or open(out).read() != text:
         with open(out, "w") as f:
             f.write(text)

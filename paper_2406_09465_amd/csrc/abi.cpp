@@ -165,7 +165,7 @@ int korch_graph_node_attrs(const korch_graph* g, int32_t node, korch_attrs* attr
     if (node < 0 || node >= (int)g->g.nodes.size()) fail(KORCH_E_ARG, "node id out of range");
     const Node& n = g->g.nodes[node];
     *attrs = n.attrs;
-    if (op_kind(n.op) == Kind::Reduce || n.op == KORCH_CONCAT) attrs->axis = n.axis;
+    if (op_kind(n.op) == Kind::Reduce || n.op == KORCH_CONCAT || n.op == KORCH_IOTA) attrs->axis = n.axis;
   });
 }
 

@@ -200,6 +200,11 @@ std::string binary_expr(int op, const std::string& x, const std::string& y) {
     case KORCH_DIV: return g_fast_math ? "f_div(" + x + ", " + y + ")" : "(" + x + " / " + y + ")";
     case KORCH_MAX: return "k_max(" + x + ", " + y + ")";
     case KORCH_MIN: return "k_min(" + x + ", " + y + ")";
+    case KORCH_LT: return "(" + x + " < " + y + " ? 1.0f : 0.0f)";
+    case KORCH_LE: return "(" + x + " <= " + y + " ? 1.0f : 0.0f)";
+    case KORCH_GT: return "(" + x + " > " + y + " ? 1.0f : 0.0f)";
+    case KORCH_GE: return "(" + x + " >= " + y + " ? 1.0f : 0.0f)";
+    case KORCH_EQ: return "(" + x + " == " + y + " ? 1.0f : 0.0f)";
   }
   fail(KORCH_E_UNSUPPORTED, std::string("no binary expression for ") + op_name(op));
 }
@@ -462,12 +467,33 @@ std::string Emitter::value(int node, const std::vector<Ix>& idx) {
       body << "    const float " << out << " = " << binary_expr(n.op, x, y) << ";\n";
       break;
     }
+    case Kind::Select: {
+      const std::string c = value(n.in[0], broadcast_index(in_shape(0), n.shape, idx));
+      const std::string x = value(n.in[1], broadcast_index(in_shape(1), n.shape, idx));
+      const std::string y = n.attrs.has_scalar ? flit(n.attrs.scalar) : value(n.in[2], broadcast_index(in_shape(2), n.shape, idx));
+      out = fresh("t");
+      body << "    const float " << out << " = " << c << " != 0.0f ? " << x << " : " << y << ";\n";
+      break;
+    }
+    case Kind::Gather: {
+      const Shape& ts = in_shape(0);
+      const std::string k = value(n.in[1], broadcast_index(in_shape(1), n.shape, idx));
+      const std::string at = fresh("k");
+      // fmax and fmin drop a NaN, so the index lies in the table whatever the value is
+      body << "    const int " << at << " = (int)k_min(k_max(" << k << ", 0.0f), " << flit((double)(ts.back() - 1)) << ");\n";
+      std::vector<Ix> src = broadcast_index(Shape(ts.begin(), ts.end() - 1), n.shape, idx);
+      src.push_back(nonaffine(at));
+      out = value(n.in[0], src);
+      break;
+    }
     case Kind::Broadcast:
       out = value(n.in[0], broadcast_index(in_shape(0), n.shape, idx));
       break;
     case Kind::Layout: {
       if (n.op == KORCH_FILL) {
         out = flit(n.attrs.scalar);
+      } else if (n.op == KORCH_IOTA) {
+        out = "((float)" + idx[n.axis].at() + ")";
       } else if (n.op == KORCH_TRANSPOSE) {
         std::vector<Ix> src(idx.size());
         for (size_t d = 0; d < idx.size(); ++d) src[n.attrs.perm[d]] = idx[d];

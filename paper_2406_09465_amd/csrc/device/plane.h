@@ -1,0 +1,765 @@
+// Device skeleton of the plane family: products that meet in a plane of
+// scores, which never leaves the registers.
+//
+// The plane has an owned and a streamed axis.  A wave owns 32 indices of the
+// owned axis, one per lane pair (lane & 31), and walks over the streamed axis
+// in tiles of TS.  For every subtile of 32 streamed indices:
+//   scores  x_p = A_p . B_p       A_p: streamed rows (LDS), B_p: owned rows (registers)
+//   plane   X_o = f(x, vectors)   the kernel's own elementwise expression
+//   outputs acc_o += W_o^T . X_o  W_o: streamed rows (LDS)
+// The 32 x 32 matrix instructions put the streamed index in an accumulator's
+// register and the owned index in its lane, which is the layout that the
+// second product takes as its right operand (for 16-bit types two groups of
+// four registers make one operand of eight; the left operand's rows are read
+// in the same order).  So the plane needs no pass through LDS and no shuffle.
+// With a softmax the row maximum and sum run along (one pass over the data);
+// the reference of the exponentials only moves when the maximum has grown by
+// more than kLazy, which keeps the rescaling of the accumulators rare and the
+// exponentials below 2^8 (half-precision products stay far from overflow);
+// the results are brought to the true maximum at the end.
+//
+// Tiles whose mask is false for every pair are never loaded: the mask's value
+// range over a tile follows from the ranges of its vectors (interval
+// arithmetic), and the tiles with work are listed first.  The same ranges tell
+// tiles without a masked pair, which skip the mask.
+//
+// P (generated) describes the kernel; see the constants and functions used.
+
+typedef f16 f16x4 __attribute__((ext_vector_type(4)));
+typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
+
+static constexpr float kLog2e = 1.4426950408889634f;
+static constexpr float kLazy = 5.5f;  // natural units: 2^8
+static constexpr int kListCap = 2048;
+
+template <typename T> struct Mma;
+template <> struct Mma<f16> {
+  static constexpr int VL = 8, KU = 16;  // elements of a 16-byte vector; contraction covered by one fragment
+  typedef f16x8 Frag;
+  static __device__ __forceinline__ f32x16 run(Frag a, Frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+template <> struct Mma<bf16> {
+  static constexpr int VL = 8, KU = 16;
+  typedef bf16x8 Frag;
+  static __device__ __forceinline__ f32x16 run(Frag a, Frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Mma<float> {
+  static constexpr int VL = 4, KU = 8;
+  typedef f32x4 Frag;
+  static __device__ __forceinline__ f32x16 run(Frag a, Frag b, f32x16 c) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+  }
+};
+
+constexpr int round_up(int x, int m) { return (x + m - 1) / m * m; }
+
+// Geometry of a policy's LDS.
+template <class P> struct Geo {
+  typedef typename P::T T;
+  static constexpr int VL = Mma<T>::VL, KU = Mma<T>::KU;
+  static constexpr int NT = P::NW * 64;                 // threads of the workgroup
+  static constexpr int GT = P::WSPLIT ? 64 : NT;        // threads that share a streamed tile
+  static constexpr int NG = P::WSPLIT ? P::NW : 1;      // such groups
+  static constexpr int OT = P::WSPLIT ? 32 : 32 * P::NW;  // owned indices of the workgroup
+  static constexpr int NSUB = P::TS / 32;
+  static constexpr int width(int t) { return round_up(P::sw(t), 32); }
+  static constexpr int pitch(int t) { return width(t) + VL; }
+  static constexpr int tile_off(int t) {  // bytes, within one stage
+    int o = 0;
+    for (int i = 0; i < t; ++i) o += P::TS * pitch(i) * (int)sizeof(T);
+    return o;
+  }
+  static constexpr int tab_off = tile_off(P::NST);
+  static constexpr int stage_bytes = tab_off + P::NTAB * P::TS * 4;
+  static constexpr int group_bytes = P::STAGES * stage_bytes;
+  static constexpr int tiles_bytes = NG * group_bytes;
+  static constexpr int nreg() {  // accumulator registers of a lane
+    int n = 0;
+    for (int o = 0; o < P::NOP; ++o) n += width(P::ost(o)) / 2;
+    return n;
+  }
+  static constexpr int merge_bytes = P::WSPLIT ? P::NW * (nreg() + 2) * 64 * 4 : 0;
+  static constexpr int bin_bytes = P::NW * P::NBIN * 64 * 4;
+  static constexpr int main_bytes = tiles_bytes > merge_bytes ? tiles_bytes : merge_bytes;
+  static constexpr int list_off = main_bytes;
+  static constexpr int range_off = list_off + kListCap * 2;             // own ranges: [wave][NOV][2]
+  static constexpr int misc_off = range_off + (P::NW * P::NOV * 2 + 8) * 4;
+  static constexpr int bin_off = (misc_off + 64 + 15) / 16 * 16;
+  static constexpr int bytes = bin_off + bin_bytes;
+};
+
+template <int V> struct ic {
+  static constexpr int value = V;
+};
+
+template <int N, int I = 0, class F> __device__ __forceinline__ void static_for(F&& f) {
+  if constexpr (I < N) {
+    f(ic<I>{});
+    static_for<N, I + 1>(f);
+  }
+}
+
+template <int GT> __device__ __forceinline__ void group_sync() {
+  if constexpr (GT > 64) {
+    __syncthreads();
+  } else {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  }
+}
+
+__device__ __forceinline__ float wave_min(float v) {
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) v = k_min(v, __shfl_xor(v, m, 64));
+  return v;
+}
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) v = k_max(v, __shfl_xor(v, m, 64));
+  return v;
+}
+
+// Interval arithmetic on value ranges (rounding is monotone, so a range of
+// rounded operations holds the rounded values).
+struct Range {
+  float lo, hi;
+};
+__device__ __forceinline__ Range r_pt(float v) { return {v, v}; }
+__device__ __forceinline__ Range r_all() { return {-__builtin_huge_valf(), __builtin_huge_valf()}; }
+__device__ __forceinline__ Range r_add(Range a, Range b) { return {a.lo + b.lo, a.hi + b.hi}; }
+__device__ __forceinline__ Range r_sub(Range a, Range b) { return {a.lo - b.hi, a.hi - b.lo}; }
+__device__ __forceinline__ Range r_neg(Range a) { return {-a.hi, -a.lo}; }
+__device__ __forceinline__ Range r_max(Range a, Range b) { return {k_max(a.lo, b.lo), k_max(a.hi, b.hi)}; }
+__device__ __forceinline__ Range r_min(Range a, Range b) { return {k_min(a.lo, b.lo), k_min(a.hi, b.hi)}; }
+__device__ __forceinline__ Range r_mul(Range a, Range b) {
+  const float p = a.lo * b.lo, q = a.lo * b.hi, r = a.hi * b.lo, s = a.hi * b.hi;
+  // an infinite end times zero says nothing
+  if (!(p - p == 0.0f && q - q == 0.0f && r - r == 0.0f && s - s == 0.0f)) return r_all();
+  return {k_min(k_min(p, q), k_min(r, s)), k_max(k_max(p, q), k_max(r, s))};
+}
+__device__ __forceinline__ Range r_abs(Range a) {
+  const float p = __builtin_fabsf(a.lo), q = __builtin_fabsf(a.hi);
+  return {a.lo <= 0.0f && a.hi >= 0.0f ? 0.0f : k_min(p, q), k_max(p, q)};
+}
+__device__ __forceinline__ Range r_lt(Range a, Range b) { return {a.hi < b.lo ? 1.0f : 0.0f, a.lo < b.hi ? 1.0f : 0.0f}; }
+__device__ __forceinline__ Range r_le(Range a, Range b) { return {a.hi <= b.lo ? 1.0f : 0.0f, a.lo <= b.hi ? 1.0f : 0.0f}; }
+__device__ __forceinline__ Range r_eq(Range a, Range b) {
+  return {a.lo == a.hi && b.lo == b.hi && a.lo == b.lo ? 1.0f : 0.0f, a.lo <= b.hi && b.lo <= a.hi ? 1.0f : 0.0f};
+}
+
+__device__ __forceinline__ bool not_number(float v) { return !(v == v); }
+
+template <class P> struct Plane {
+  typedef typename P::T T;
+  typedef Geo<P> G;
+  typedef Mma<T> M;
+  typedef typename M::Frag Frag;
+  static constexpr int VL = M::VL, KU = M::KU;
+  typedef vec_t<VL, T> V16;
+  static constexpr int NREG = G::nreg();
+
+  static constexpr int vpt(int t) { return (P::TS * (P::sw(t) / VL) + G::GT - 1) / G::GT; }  // staging vectors of a thread
+  static constexpr int vtot() {
+    int n = 0;
+    for (int t = 0; t < P::NST; ++t) n += vpt(t);
+    return n > 0 ? n : 1;
+  }
+  static constexpr int vbase(int t) {
+    int n = 0;
+    for (int i = 0; i < t; ++i) n += vpt(i);
+    return n;
+  }
+  static constexpr int kfrag(int p) { return (P::sw(P::sst(p)) + KU - 1) / KU; }
+  static constexpr int fbase(int p) {
+    int n = 0;
+    for (int i = 0; i < p; ++i) n += kfrag(i);
+    return n;
+  }
+  static constexpr int NF = fbase(P::NSP);
+  static constexpr int abase(int o) {  // first 32-wide accumulator tile of output product o
+    int n = 0;
+    for (int i = 0; i < o; ++i) n += G::width(P::ost(i)) / 32;
+    return n;
+  }
+  static constexpr int NA = abase(P::NOP);
+  static constexpr int TABV = (P::NTAB * P::TS + G::GT - 1) / G::GT;
+
+  const KArgs& a;
+  typename P::B b;
+  char* smem;
+  int tid, wave, lane, l32, h, gt, gtid;
+  i64 own0;     // first owned index of the workgroup
+  i64 own;      // this lane's owned index, clamped to the axis
+  bool own_ok;  // it exists
+  float ov[P::NOV > 0 ? P::NOV : 1];
+  Frag bf[NF];
+  f32x16 acc[NA > 0 ? NA : 1];
+  float mref, mtrue, lsum;
+  V16 st[vtot()];
+  float stab[TABV > 0 ? TABV : 1];
+
+  __device__ __forceinline__ Plane(const KArgs& a_, char* s) : a(a_), smem(s) {}
+
+  __device__ __forceinline__ char* stage(int s) const { return smem + (P::WSPLIT ? wave * G::group_bytes : 0) + s * G::stage_bytes; }
+
+  // ---- loads of one streamed tile into registers, and from there to LDS ----
+  __device__ __forceinline__ void fetch(i64 s0) {
+    const bool whole = s0 + P::TS <= P::NSTR;
+    static_for<P::NST>([&](auto ti) {
+      constexpr int t = decltype(ti)::value;
+      constexpr int CV = P::sw(t) / VL;
+#pragma unroll
+      for (int i = 0; i < vpt(t); ++i) {
+        const int e = gtid + i * G::GT;
+        const int row = e / CV, c = e % CV;
+        const bool in = (P::TS * CV) % G::GT == 0 || e < P::TS * CV;
+        const i64 r = s0 + row;
+        const i64 rc = r < P::NSTR ? r : P::NSTR - 1;
+        V16 v = *(const V16*)(P::template srow<t>(a, b, in ? rc : P::NSTR - 1) + c * VL);
+        if constexpr (P::row_mask(t)) {
+          if (!(in && r < P::NSTR && P::template srow_ok<t>(a, b, rc))) v = V16{};
+        } else {
+          if (!whole && r >= P::NSTR) v = V16{};
+        }
+        st[vbase(t) + i] = v;
+      }
+    });
+    if constexpr (P::NTAB > 0) {
+#pragma unroll
+      for (int i = 0; i < TABV; ++i) {
+        const int e = gtid + i * G::GT;
+        const int k = e / P::TS;
+        const i64 r = s0 + e % P::TS, rc = r < P::NSTR ? r : P::NSTR - 1;
+        stab[i] = k < P::NTAB ? P::tab(a, b, k, rc) : 0.0f;
+      }
+    }
+  }
+  __device__ __forceinline__ void put(int s) {
+    char* base = stage(s);
+    static_for<P::NST>([&](auto ti) {
+      constexpr int t = decltype(ti)::value;
+      constexpr int CV = P::sw(t) / VL;
+#pragma unroll
+      for (int i = 0; i < vpt(t); ++i) {
+        const int e = gtid + i * G::GT;
+        const int row = e / CV, c = e % CV;
+        if ((P::TS * CV) % G::GT == 0 || e < P::TS * CV)
+          *(V16*)((T*)(base + G::tile_off(t)) + row * G::pitch(t) + c * VL) = st[vbase(t) + i];
+      }
+    });
+    if constexpr (P::NTAB > 0) {
+#pragma unroll
+      for (int i = 0; i < TABV; ++i) {
+        const int e = gtid + i * G::GT;
+        if (e < P::NTAB * P::TS) ((float*)(base + G::tab_off))[e] = stab[i];
+      }
+    }
+  }
+  // Columns past a tensor's width take part in the score products: zeros.
+  __device__ __forceinline__ void clear_pads() {
+    static_for<P::NST>([&](auto ti) {
+      constexpr int t = decltype(ti)::value;
+      constexpr int PV = (G::pitch(t) - P::sw(t)) / VL;
+      for (int s = 0; s < P::STAGES; ++s)
+        for (int e = gtid; e < P::TS * PV; e += G::GT)
+          *(V16*)((T*)(stage(s) + G::tile_off(t)) + (e / PV) * G::pitch(t) + P::sw(t) + (e % PV) * VL) = V16{};
+    });
+  }
+
+  // ---- products --------------------------------------------------------------
+  template <int p> __device__ __forceinline__ f32x16 score(const char* base, int sub) const {
+    constexpr int t = P::sst(p);
+    f32x16 c = {};
+    const T* q = (const T*)(base + G::tile_off(t)) + (sub * 32 + l32) * G::pitch(t) + h * (KU / 2);
+#pragma unroll
+    for (int k = 0; k < kfrag(p); ++k) c = M::run(*(const Frag*)(q + k * KU), bf[fbase(p) + k], c);
+    return c;
+  }
+  template <int o> __device__ __forceinline__ void output(const char* base, int sub, const float* X) {
+    constexpr int t = P::ost(o);
+    constexpr int ND = G::width(t) / 32;
+    const T* w = (const T*)(base + G::tile_off(t));
+    if constexpr (sizeof(T) == 2) {
+      typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        Frag x;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = fromf<T>(X[8 * kk + j]);
+        const T* r0 = w + (sub * 32 + kk * 16 + 4 * h + ((lane & 15) >> 2)) * G::pitch(t) + ((lane >> 4) & 1) * 16 + 4 * (lane & 3);
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(r0 + d * 32));
+          s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(r0 + 8 * G::pitch(t) + d * 32));
+          acc[abase(o) + d] = M::run(__builtin_bit_cast(Frag, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)), x, acc[abase(o) + d]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const T* r0 = w + (sub * 32 + 8 * (i / 4) + 4 * h + i % 4) * G::pitch(t) + l32;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+          acc[abase(o) + d] = __builtin_amdgcn_mfma_f32_32x32x2f32(r0[d * 32], X[i], acc[abase(o) + d], 0, 0, 0);
+      }
+    }
+  }
+
+  // Streamed index (within its tile) of register i of subtile sub.
+  __device__ __forceinline__ int sidx(int sub, int i) const { return sub * 32 + 8 * (i / 4) + 4 * h + i % 4; }
+
+  template <bool CHECK, class F> __device__ __forceinline__ void elements(const char* base, i64 s0, int sub, F&& f) {
+    const float* tab = (const float*)(base + G::tab_off);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      f32x4 tv4[P::NTAB > 0 ? P::NTAB : 1];
+#pragma unroll
+      for (int k = 0; k < P::NTAB; ++k) tv4[k] = *(const f32x4*)(tab + k * P::TS + sub * 32 + 8 * g + 4 * h);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float tv[P::NTAB > 0 ? P::NTAB : 1];
+#pragma unroll
+        for (int k = 0; k < P::NTAB; ++k) tv[k] = tv4[k][r];
+        const i64 s = s0 + sidx(sub, 4 * g + r);
+        f(4 * g + r, tv, s < P::NSTR ? s : P::NSTR - 1, s < P::NSTR);
+      }
+    }
+  }
+
+  // ---- one tile ---------------------------------------------------------------
+  template <bool CHECK> __device__ __forceinline__ void tile(int s, i64 s0) {
+    const char* base = stage(s);
+    if constexpr (P::SOFTMAX) {
+      f32x16 x[G::NSUB];
+      unsigned keep[G::NSUB];
+      float top = -__builtin_huge_valf();
+#pragma unroll
+      for (int sub = 0; sub < G::NSUB; ++sub) x[sub] = score<0>(base, sub);
+#pragma unroll
+      for (int sub = 0; sub < G::NSUB; ++sub) {
+        keep[sub] = 0;
+        elements<CHECK>(base, s0, sub, [&](int i, const float* tv, i64 sc, bool ok) {
+          float v, xs[1] = {x[sub][i]};
+          bool k = true;
+          P::template logit<CHECK>(a, b, ov, tv, own, sc, xs, v, k);
+          if (CHECK) {
+            k = k && ok;
+            keep[sub] |= k ? 1u << i : 0u;
+            top = k_max(top, k ? v : -__builtin_huge_valf());
+          } else {
+            top = k_max(top, v);
+          }
+          x[sub][i] = v;
+        });
+      }
+      top = k_max(top, __shfl_xor(top, 32, 64));
+      mtrue = k_max(mtrue, top);
+      if (__any(mtrue > mref + kLazy)) {
+        const float f = mref == mtrue ? 1.0f : __builtin_amdgcn_exp2f((mref - mtrue) * kLog2e);
+        mref = mtrue;
+        lsum *= f;
+#pragma unroll
+        for (int d = 0; d < NA; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[d][i] *= f;
+      }
+      const float mz = mref == -__builtin_huge_valf() ? 0.0f : mref;
+      const float mc = -mz * kLog2e;
+#pragma unroll
+      for (int sub = 0; sub < G::NSUB; ++sub) {
+        float X[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float p;
+          if constexpr (sizeof(T) == 2)
+            p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[sub][i], kLog2e, mc));
+          else
+            p = expf(x[sub][i] - mz);
+          if (CHECK) p = (keep[sub] >> i) & 1u ? p : 0.0f;
+          lsum += p;
+          X[i] = p;
+        }
+        static_for<P::NOP>([&](auto oi) { output<decltype(oi)::value>(base, sub, X); });
+      }
+    } else {
+#pragma unroll
+      for (int sub = 0; sub < G::NSUB; ++sub) {
+        f32x16 x[P::NSP];
+        static_for<P::NSP>([&](auto pi) { x[decltype(pi)::value] = score<decltype(pi)::value>(base, sub); });
+        float X[P::NX][16];
+        elements<CHECK>(base, s0, sub, [&](int i, const float* tv, i64 sc, bool ok) {
+          float xs[P::NSP], out[P::NX];
+#pragma unroll
+          for (int p = 0; p < P::NSP; ++p) xs[p] = x[p][i];
+          P::template plane<CHECK>(a, b, ov, tv, own, sc, xs, out);
+#pragma unroll
+          for (int k = 0; k < P::NX; ++k) X[k][i] = CHECK && !ok ? 0.0f : out[k];
+        });
+        static_for<P::NOP>([&](auto oi) { output<decltype(oi)::value>(base, sub, X[P::ox(decltype(oi)::value)]); });
+        if constexpr (P::NBIN > 0) bins(base, s0, sub, X[P::XBIN]);
+      }
+    }
+  }
+
+  // ---- sums of plane values by bin -----------------------------------------------
+  // Every lane adds its values to bins of its own in LDS ([bin][lane]): no two
+  // lanes meet at an address and a lane's additions keep their order, so the
+  // sums do not depend on timing.  The lanes are summed at the end.
+  __device__ __forceinline__ void bins(const char* base, i64 s0, int sub, const float* X) {
+    float* mine = (float*)(smem + G::bin_off) + wave * (P::NBIN * 64) + lane;
+    elements<true>(base, s0, sub, [&](int i, const float* tv, i64 sc, bool ok) {
+      const int k = (int)P::bin(a, b, ov, tv, own, sc);
+      if (own_ok && ok) mine[k * 64] += X[i];
+    });
+  }
+
+  // ---- the kernel --------------------------------------------------------------
+  __device__ __forceinline__ void run() {
+    tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l32 = lane & 31, h = lane >> 5;
+    gtid = P::WSPLIT ? lane : tid;
+    // Workgroups are dealt to the eight XCDs in turn; consecutive work of one
+    // XCD shares a batch entry, whose streamed rows then stay in that XCD's L2.
+    // Within a batch entry the last owned tiles come first (under a causal mask
+    // they are the longest).
+    int w = blockIdx.x;
+    constexpr int total = P::OTILES * P::NB;
+    if constexpr (total % 8 == 0) w = (w & 7) * (total / 8) + (w >> 3);
+    const int bl = w / P::OTILES, ot = P::OTILES - 1 - w % P::OTILES;
+    const int z = blockIdx.y;
+    b = P::batch(bl);
+    own0 = (i64)ot * G::OT;
+    const i64 o = own0 + (P::WSPLIT ? 0 : wave * 32) + l32;
+    own_ok = o < P::NOWN;
+    own = own_ok ? o : P::NOWN - 1;
+#pragma unroll
+    for (int k = 0; k < P::NOV; ++k) ov[k] = P::own(a, b, k, own);
+    // owned fragments
+    static_for<P::NSP>([&](auto pi) {
+      constexpr int p = decltype(pi)::value;
+      const T* r = P::template orow<p>(a, b, own);
+      bool ok = own_ok;
+      if constexpr (P::own_mask(p)) ok = ok && P::template orow_ok<p>(a, b, own);
+#pragma unroll
+      for (int k = 0; k < kfrag(p); ++k) {
+        const int c = k * KU + h * (KU / 2);
+        Frag v = {};
+        if (ok && c < P::sw(P::sst(p))) v = *(const Frag*)(r + c);
+        bf[fbase(p) + k] = v;
+      }
+    });
+#pragma unroll
+    for (int d = 0; d < NA; ++d) acc[d] = f32x16{};
+    mref = mtrue = P::MINIT;
+    lsum = 0.0f;
+    if constexpr (P::NBIN > 0)
+      for (int k = 0; k < P::NBIN; ++k) ((float*)(smem + G::bin_off))[(wave * P::NBIN + k) * 64 + lane] = 0.0f;
+    clear_pads();
+    // ranges of the owned vectors, over the workgroup and over the wave
+    float* rng = (float*)(smem + G::range_off);
+    Range wr[P::NOV > 0 ? P::NOV : 1], gr[P::NOV > 0 ? P::NOV : 1];
+    if constexpr (P::MASK) {
+#pragma unroll
+      for (int k = 0; k < P::NOV; ++k) {
+        const bool bad = __any(not_number(ov[k]));
+        wr[k] = bad ? r_all() : Range{wave_min(ov[k]), wave_max(ov[k])};
+        if (lane == 0) rng[(wave * P::NOV + k) * 2] = wr[k].lo, rng[(wave * P::NOV + k) * 2 + 1] = wr[k].hi;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < P::NOV; ++k) {
+        gr[k] = wr[k];
+        for (int v = 0; v < P::NW; ++v) {
+          gr[k].lo = k_min(gr[k].lo, rng[(v * P::NOV + k) * 2]);
+          gr[k].hi = k_max(gr[k].hi, rng[(v * P::NOV + k) * 2 + 1]);
+        }
+      }
+    }
+    unsigned short* list = (unsigned short*)(smem + G::list_off);
+    int* misc = (int*)(smem + G::misc_off);
+    constexpr int ntiles = (int)((P::NSTR + P::TS - 1) / P::TS);
+    for (int c0 = 0; c0 < ntiles; c0 += kListCap) {
+      const int cn = ntiles - c0 < kListCap ? ntiles - c0 : kListCap;
+      int n = cn;
+      if constexpr (P::MASK) {
+        __syncthreads();  // the previous chunk's list is no longer read
+        // state of each tile: 0 no pair, 1 some, 2 all; a group of TS / 4 lanes
+        // reads the tile's vectors
+        constexpr int GL = P::TS / 4;
+        for (int t0 = 0; t0 < cn; t0 += P::NRV ? G::NT / GL : G::NT) {
+          const int t = t0 + (P::NRV ? tid / GL : tid);
+          const i64 s0 = (i64)(c0 + (t < cn ? t : cn - 1)) * P::TS;
+          Range rv[P::NRV > 0 ? P::NRV : 1];
+          if constexpr (P::NRV > 0) {
+#pragma unroll
+            for (int k = 0; k < P::NRV; ++k) {
+              float lo = __builtin_huge_valf(), hi = -lo;
+              bool bad = false;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const i64 r = s0 + (tid % GL) * 4 + j;
+                const float v = P::rvec(a, b, k, r < P::NSTR ? r : P::NSTR - 1);
+                bad = bad || not_number(v);
+                lo = k_min(lo, v), hi = k_max(hi, v);
+              }
+              if (bad) lo = -__builtin_huge_valf(), hi = __builtin_huge_valf();
+#pragma unroll
+              for (int m = GL / 2; m >= 1; m >>= 1) lo = k_min(lo, __shfl_xor(lo, m, 64)), hi = k_max(hi, __shfl_xor(hi, m, 64));
+              rv[k] = {lo, hi};
+            }
+          }
+          const i64 s1 = s0 + P::TS - 1 < P::NSTR - 1 ? s0 + P::TS - 1 : P::NSTR - 1;
+          const Range c = P::mask_range(a, b, gr, rv, (float)s0, (float)s1);
+          const int state = c.hi == 0.0f ? 0 : (c.lo > 0.0f && s0 + P::TS <= P::NSTR ? 2 : 1);
+          if (t < cn && (!P::NRV || tid % GL == 0)) list[t] = (unsigned short)state;
+        }
+        __syncthreads();
+        // compaction by one wave, in order (entries move towards the front)
+        if (wave == 0) {
+          int m = 0;
+          for (int t0 = 0; t0 < cn; t0 += 64) {
+            const int state = t0 + lane < cn ? list[t0 + lane] : 0;
+            const unsigned long long act = __ballot(state != 0);
+            const int at = m + __popcll(act & ((1ull << lane) - 1ull));
+            if (state) list[at] = (unsigned short)((t0 + lane) | (state == 2 ? 0x8000 : 0));
+            m += __popcll(act);
+          }
+          if (lane == 0) misc[0] = m;
+        }
+        __syncthreads();
+        n = misc[0];
+      }
+      auto entry = [&](int e, i64& s0, bool& full) {
+        if constexpr (P::MASK) {
+          const int v = __builtin_amdgcn_readfirstlane((int)list[e]);
+          s0 = (i64)(c0 + (v & 0x7fff)) * P::TS;
+          full = (v & 0x8000) != 0;
+        } else {
+          s0 = (i64)(c0 + e) * P::TS;
+          full = s0 + P::TS <= P::NSTR;
+        }
+      };
+      // entries e = first, first + step, ...: over the splits and, when the
+      // waves split the streamed axis, over the waves
+      const int step = P::SPLIT * G::NG, first = z * G::NG + (P::WSPLIT ? wave : 0);
+      i64 s0 = 0, sn = 0;
+      bool full = false, fulln = false;
+      int e = __builtin_amdgcn_readfirstlane(first);
+      if (c0 > 0) group_sync<G::GT>();
+      if (e < n) {
+        entry(e, s0, full);
+        fetch(s0);
+        put(0);
+      }
+      group_sync<G::GT>();
+      int s = 0;
+      for (; e < n; e += step) {
+        const bool more = e + step < n;
+        if (more) {
+          entry(e + step, sn, fulln);
+          fetch(sn);
+        }
+        if (full)
+          tile<false>(s, s0);
+        else
+          tile<true>(s, s0);
+        if constexpr (P::STAGES == 1) group_sync<G::GT>();
+        if (more) put(P::STAGES == 1 ? 0 : s ^ 1);
+        group_sync<G::GT>();
+        if constexpr (P::STAGES == 2) s ^= 1;
+        s0 = sn, full = fulln;
+      }
+    }
+    finish(bl, ot, z);
+  }
+
+  // ---- joining the waves and the splits, and the results -------------------------
+  __device__ __forceinline__ void store_group(int at, f32x4 v) {  // register group `at` (4 registers) of the lane
+    static_for<P::NOP>([&](auto oi) {
+      constexpr int o = decltype(oi)::value;
+      constexpr int lo = abase(o) * 4, hi = abase(o + 1) * 4;
+      if (at >= lo && at < hi) {
+        const int dim = ((at - lo) / 4) * 32 + 8 * ((at - lo) % 4) + 4 * h;
+        if (own_ok && dim < P::sw(P::ost(o))) P::template store<o>(a, b, own, dim, mtrue, lsum, v);
+      }
+    });
+  }
+
+  __device__ __forceinline__ void finish(int bl, int ot, int z) {
+    constexpr int NGRP = NREG / 4;
+    if constexpr (P::NBIN > 0) join_bins(bl, ot, z);
+    if constexpr (P::SOFTMAX) {
+      lsum += __shfl_xor(lsum, 32, 64);
+      // to the true maximum
+      const float f = mref == mtrue ? 1.0f : __builtin_amdgcn_exp2f((mref - mtrue) * kLog2e);
+      lsum *= f;
+#pragma unroll
+      for (int d = 0; d < NA; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[d][i] *= f;
+    }
+    if constexpr (!P::WSPLIT && P::SPLIT == 1) {
+#pragma unroll
+      for (int g = 0; g < NGRP; ++g) {
+        f32x4 v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = acc[g / 4][(g % 4) * 4 + r];
+        store_group(g, v);
+      }
+      if constexpr (P::SOFTMAX)
+        if (own_ok && h == 0) P::stats(a, b, own, mtrue, lsum);
+    } else {
+      constexpr int NM = NGRP + 1;  // groups of four registers, then (m, l)
+      float* lds = (float*)smem;
+      f32x4 v[NGRP > 0 ? NGRP : 1];
+      constexpr int share = P::WSPLIT ? (NGRP + P::NW - 1) / P::NW : NGRP;
+      const int g0 = P::WSPLIT ? wave * share : 0;
+      if constexpr (P::WSPLIT) {
+        __syncthreads();  // the tiles are no longer read
+#pragma unroll
+        for (int g = 0; g < NGRP; ++g) {
+          f32x4 x;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) x[r] = acc[g / 4][(g % 4) * 4 + r];
+          *(f32x4*)(lds + ((wave * NGRP + g) * 64 + lane) * 4) = x;
+        }
+        float* ml = lds + P::NW * NGRP * 256;
+        if constexpr (P::SOFTMAX) ml[(wave * 2) * 64 + lane] = mtrue, ml[(wave * 2 + 1) * 64 + lane] = lsum;
+        __syncthreads();
+        float f[P::NW];
+        if constexpr (P::SOFTMAX) {
+          float m = P::MINIT, l = 0.0f;
+#pragma unroll
+          for (int v2 = 0; v2 < P::NW; ++v2) m = k_max(m, ml[v2 * 128 + lane]);
+#pragma unroll
+          for (int v2 = 0; v2 < P::NW; ++v2) {
+            const float mv = ml[v2 * 128 + lane];
+            f[v2] = mv == m ? 1.0f : __builtin_amdgcn_exp2f((mv - m) * kLog2e);
+            l += ml[v2 * 128 + 64 + lane] * f[v2];
+          }
+          mtrue = m, lsum = l;
+        }
+#pragma unroll
+        for (int g = 0; g < share; ++g) {
+          f32x4 s = {};
+          if (g0 + g < NGRP)
+#pragma unroll
+            for (int v2 = 0; v2 < P::NW; ++v2) {
+              const f32x4 x = *(const f32x4*)(lds + ((v2 * NGRP + g0 + g) * 64 + lane) * 4);
+              if constexpr (P::SOFTMAX) s += x * f[v2];
+              else s += x;
+            }
+          v[g] = s;
+        }
+      } else {
+#pragma unroll
+        for (int g = 0; g < NGRP; ++g)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[g][r] = acc[g / 4][(g % 4) * 4 + r];
+      }
+      if constexpr (P::SPLIT > 1) {
+        // partial results, [batch and owned tile][split][wave][group][lane]
+        constexpr int WV = P::WSPLIT ? 1 : P::NW;
+        const int wv = P::WSPLIT ? 0 : wave;
+        const i64 cell = (i64)bl * P::OTILES + ot;
+        float* part = (float*)a.p[P::SCR] + cell * ((i64)P::SPLIT * WV * NM * 256);
+        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(part, 0, (int)(P::SPLIT * WV * NM * 1024), 0x00020000);
+        auto at = [&](int zz, int g) { return (unsigned)((((zz * WV + wv) * NM + g) * 64 + lane) * 16); };
+#pragma unroll
+        for (int g = 0; g < share; ++g)
+          if (g0 + g < NGRP) coherent_store4(rs, at(z, g0 + g), float4{v[g][0], v[g][1], v[g][2], v[g][3]});
+        if constexpr (P::SOFTMAX)
+          if (!P::WSPLIT || wave == 0) coherent_store4(rs, at(z, NGRP), float4{mtrue, lsum, 0.0f, 0.0f});
+        __builtin_amdgcn_s_waitcnt(0);  // this wave's partial stores are performed
+        __syncthreads();
+        int* misc = (int*)(smem + G::misc_off);
+        if (tid == 0) {
+          int* cnt = (int*)a.p[P::CNT] + cell * 32;
+          const int old = __hip_atomic_fetch_add(cnt, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          misc[1] = old == P::SPLIT - 1;
+          if (old == P::SPLIT - 1) __hip_atomic_store(cnt, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        __syncthreads();
+        if (!misc[1]) return;
+        float f[P::SPLIT];
+        if constexpr (P::SOFTMAX) {
+          float mz[P::SPLIT], lz[P::SPLIT];
+#pragma unroll
+          for (int zz = 0; zz < P::SPLIT; ++zz) {
+            const float4 q = coherent_load4(rs, at(zz, NGRP));
+            mz[zz] = q.x, lz[zz] = q.y;
+          }
+          float m = P::MINIT, l = 0.0f;
+#pragma unroll
+          for (int zz = 0; zz < P::SPLIT; ++zz) m = k_max(m, mz[zz]);
+#pragma unroll
+          for (int zz = 0; zz < P::SPLIT; ++zz) {
+            f[zz] = mz[zz] == m ? 1.0f : __builtin_amdgcn_exp2f((mz[zz] - m) * kLog2e);
+            l += lz[zz] * f[zz];
+          }
+          mtrue = m, lsum = l;
+        }
+#pragma unroll
+        for (int g = 0; g < share; ++g) {
+          if (g0 + g >= NGRP) continue;
+          f32x4 s = {};
+#pragma unroll
+          for (int zz = 0; zz < P::SPLIT; ++zz) {
+            const float4 q = coherent_load4(rs, at(zz, g0 + g));
+            const f32x4 x = {q.x, q.y, q.z, q.w};
+            if constexpr (P::SOFTMAX) s += x * f[zz];
+            else s += x;
+          }
+          v[g] = s;
+        }
+      }
+#pragma unroll
+      for (int g = 0; g < share; ++g)
+        if (g0 + g < NGRP) store_group(g0 + g, v[g]);
+      if constexpr (P::SOFTMAX)
+        if (own_ok && h == 0 && (!P::WSPLIT || wave == 0)) P::stats(a, b, own, mtrue, lsum);
+    }
+  }
+
+  // Bins of all workgroups of one table row: partial sums in a fixed order.
+  __device__ __forceinline__ void join_bins(int bl, int ot, int z) {
+    const int row = P::bin_row(b), member = (P::bin_member(b) * P::OTILES + ot) * P::SPLIT + z;
+    constexpr int members = P::BIN_MEMBERS * P::OTILES * P::SPLIT;
+    float* part = (float*)a.p[P::BSCR] + (i64)row * members * P::NBIN;
+    const float* all = (const float*)(smem + G::bin_off);
+    __syncthreads();
+    // a wave per bin: the lanes' sums of every wave, then over the lanes
+    for (int k = wave; k < P::NBIN; k += P::NW) {
+      float s = 0.0f;
+      for (int v = 0; v < P::NW; ++v) s += all[(v * P::NBIN + k) * 64 + lane];
+      s = group_sum<64>(s);
+      if (lane == 0) coherent_store(&part[(i64)member * P::NBIN + k], s);
+    }
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    int* misc = (int*)(smem + G::misc_off);
+    if (tid == 0) {
+      int* cnt = (int*)a.p[P::BCNT] + row * 32;
+      const int old = __hip_atomic_fetch_add(cnt, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      misc[2] = old == members - 1;
+      if (old == members - 1) __hip_atomic_store(cnt, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (!misc[2]) return;
+    float* red = (float*)smem;  // [groups][NBIN]
+    constexpr int NG2 = P::NBIN < G::NT ? G::NT / P::NBIN : 1;
+    for (int k = tid % (P::NBIN < G::NT ? P::NBIN : G::NT), g = P::NBIN < G::NT ? tid / P::NBIN : 0; k < P::NBIN && g < NG2; k += G::NT) {
+      float s = 0.0f;
+      for (int m = g; m < members; m += NG2) s += coherent_load(&part[(i64)m * P::NBIN + k]);
+      red[g * P::NBIN + k] = s;
+    }
+    __syncthreads();
+    for (int k = tid; k < P::NBIN; k += G::NT) {
+      float s = red[k];
+      for (int g = 1; g < NG2; ++g) s += red[g * P::NBIN + k];
+      P::store_bin(a, row, k, s);
+    }
+  }
+};

@@ -1,0 +1,807 @@
+// Plane family: score products that meet in a plane [.., N, M], elementwise
+// primitives on the plane, and products of the plane with streamed operands,
+// in one kernel that never stores the plane: attention of any length with its
+// score chain (caps, biases, masks) and a softmax in one pass, and attention's
+// gradients, which evaluate the scores again (redundant execution, Korch
+// Section 4.2).
+//
+// A kernel is accepted when
+//   * every product without another product among its ancestors in the kernel
+//     is a score product A . B^T whose operands are stored tensors seen through
+//     layout primitives (or a select with zero along their rows);
+//   * the other products are output products P . W (the plane's rows are owned,
+//     its columns streamed) or P^T . W (columns owned, rows streamed), all of
+//     one kind, W stored like the scores' operands;
+//   * at most one softmax: m = max over a row, e = exp(s - m) (or 0 where a mask
+//     is false), l = sum of e; then P is e or e / l;
+//   * every output is an elementwise function of one output product and of row
+//     statistics, a row statistic of the softmax, or a sum by bins of the plane.
+#include <algorithm>
+#include <cmath>
+#include <cstdlib>
+#include <memory>
+
+#include "families.h"
+
+namespace korch {
+
+extern const char* k_device_plane;
+
+namespace {
+
+enum PlaneCls { CONSTV, ROWV, COLV, FULLP };
+
+// An operand stored in memory: rows of `width` consecutive elements.
+struct Operand {
+  int node = -1;            // node as read by the product
+  int mask = -1;            // select's condition along the rows (or -1)
+  int source = -1;          // node below the select
+  bool transposed = false;  // read as [.., k, row]
+  Shape shape;              // of `source`
+  std::string key;          // identity of the address map
+  std::string off;          // element offset of a row (variables b*, r)
+  int root = -1;
+};
+
+struct PlaneGen {
+  const KInfo& ki;
+  const Graph& g;
+  std::map<int, int> slot;
+  Shape PS;                 // plane shape [batch.., N, M]
+  int R = 0;                // its rank
+  int64_t N = 0, M = 0;
+  bool rows_owned = true;
+  int dtype = KORCH_F16;
+  std::vector<int> scores, outs_p;    // score products, output products
+  std::vector<Operand> sc_own, sc_str, out_w;
+  std::vector<Operand> streamed;      // distinct streamed tensors
+  std::vector<int> sst, ost;          // score / output product -> streamed tensor
+  std::vector<int> xnodes, ox;        // distinct plane operands of output products (and bins)
+  int xbin = -1, bin_node = -1, bin_out = -1;
+  int nm = -1, nl = -1, ne = -1, nexp = -1, nsfinal = -1;  // softmax
+  int cond = -1;                      // mask
+  double low = -INFINITY;
+  std::vector<int> ovs, tvs, rvs;     // owned vectors, streamed vectors, streamed vectors whose range is read
+  std::map<int, int> prod_of;         // output -> output product index
+  std::map<int, bool> has_score_memo;
+
+  explicit PlaneGen(const KInfo& k) : ki(k), g(k.g) {}
+
+  [[noreturn]] void bad(const std::string& m) const { fail(KORCH_E_UNSUPPORTED, "plane: " + m); }
+  bool in(int v) const { return ki.in.count(v) > 0; }
+  const Node& nd(int v) const { return g.nodes[v]; }
+
+  bool depends(int v, int on) const { return v == on || ki.ancestor(on, v); }
+  bool has_score(int v) const {
+    if (!in(v)) return false;
+    for (int s : scores)
+      if (depends(v, s)) return true;
+    return false;
+  }
+
+  PlaneCls cls(int v) const {
+    const Shape& s = nd(v).shape;
+    const int r = (int)s.size();
+    if (r > R) return FULLP;
+    const bool col = r >= 1 && s[r - 1] > 1, row = r >= 2 && s[r - 2] > 1;
+    if (has_score(v) || (row && col)) return FULLP;
+    return row ? ROWV : col ? COLV : CONSTV;
+  }
+  bool is_owned(PlaneCls c) const { return c == CONSTV || c == (rows_owned ? ROWV : COLV); }
+  bool is_streamed(PlaneCls c) const { return c == (rows_owned ? COLV : ROWV); }
+
+  // ---- analysis ------------------------------------------------------------
+
+  // Follows a product's operand to a stored tensor.  `batch` are the product's
+  // batch dims; the operand is read at [batch, r, k] (or [batch, k, r]).
+  Operand operand(int v, bool kfirst, const Shape& batch, const char* what) {
+    Operand o;
+    o.node = v;
+    const Shape& vs = nd(v).shape;
+    const int rk = (int)vs.size();
+    std::vector<Ix> idx(rk);
+    const int nb = (int)batch.size();
+    for (int d = 0; d < rk - 2; ++d) {
+      const int j = d + nb - (rk - 2);
+      idx[d] = vs[d] == 1 ? Ix::k(0) : Ix::var("b.c[" + std::to_string(j) + "]");
+    }
+    const int VL = 16 / dtype_bytes(nd(v).dtype);
+    idx[rk - (kfirst ? 1 : 2)] = Ix::var("r");
+    idx[rk - (kfirst ? 2 : 1)] = Ix::var("0", 1, VL);
+    idx[rk - (kfirst ? 2 : 1)].konst = true;
+    const int64_t width = vs[rk - (kfirst ? 2 : 1)];
+    if (width % VL) bad(std::string(what) + ": the contraction or output width is not a multiple of 16 bytes");
+    // VL consecutive elements are read as one vector: layout maps must keep
+    // them together, so indices split with the vector's lanes in mind
+    int cur = v;
+    while (in(cur)) {
+      const Node& n = nd(cur);
+      if (n.op == KORCH_TRANSPOSE) {
+        std::vector<Ix> src(idx.size());
+        for (size_t d = 0; d < idx.size(); ++d) src[n.attrs.perm[d]] = idx[d];
+        idx = src;
+        cur = n.in[0];
+      } else if (n.op == KORCH_SELECT && n.attrs.has_scalar && n.attrs.scalar == 0.0 && o.mask < 0 && nd(n.in[1]).shape == n.shape) {
+        // the condition must not vary along the contraction
+        const Shape& cs = nd(n.in[0]).shape;
+        const Shape& ns = n.shape;
+        std::vector<Ix> ci = broadcast_index(cs, ns, idx);
+        for (auto& x : ci)
+          if (x.c != 0) bad(std::string(what) + ": a select varies along the contraction");
+        o.mask = n.in[0];
+        mask_idx[v] = ci;
+        cur = n.in[1];
+      } else if (n.op == KORCH_RESHAPE || n.op == KORCH_SLICE || n.op == KORCH_BROADCAST) {
+        bad(std::string(what) + ": layout primitive not folded");
+      } else {
+        bad(std::string(what) + ": computed inside the kernel");
+      }
+    }
+    o.root = cur;
+    const Node& n = nd(cur);
+    auto st = strides_of(n.shape);
+    Ix off = Ix::k(0);
+    for (size_t d = 0; d < n.shape.size(); ++d) off = ix_add(off, ix_mulk(idx[d], st[d], VL));
+    if (!off.affine || off.c != 1 || off.al % VL) {
+      // alignment is known when every other stride is a multiple of the vector
+      bool ok = off.affine && off.c == 1;
+      for (size_t d = 0; ok && d < n.shape.size(); ++d)
+        if (idx[d].c == 0 && n.shape[d] > 1 && st[d] % VL) ok = false;
+      if (!ok) bad(std::string(what) + ": rows are not 16-byte aligned runs of elements");
+    }
+    o.off = off.b;
+    o.key = std::to_string(cur) + ":" + off.b + ":" + std::to_string(o.mask);
+    o.shape = {width};
+    return o;
+  }
+  std::map<int, std::vector<Ix>> mask_idx;
+
+  int add_streamed(const Operand& o) {
+    for (size_t i = 0; i < streamed.size(); ++i)
+      if (streamed[i].key == o.key && streamed[i].shape == o.shape) return (int)i;
+    streamed.push_back(o);
+    return (int)streamed.size() - 1;
+  }
+
+  int strip_identity(int v) const {
+    while (in(v) && nd(v).op == KORCH_IDENTITY) v = nd(v).in[0];
+    return v;
+  }
+  // x = select(cond, y, 0): cond, else -1
+  int zero_select(int v) const {
+    v = strip_identity(v);
+    if (!in(v)) return -1;
+    const Node& n = nd(v);
+    if (n.op != KORCH_SELECT || !n.attrs.has_scalar || n.attrs.scalar != 0.0 || !in(n.in[0])) return -1;
+    return n.in[0];
+  }
+
+  void analyze() {
+    if (ki.linear.empty()) bad("no product");
+    for (int v : ki.linear)
+      if (nd(v).op != KORCH_MATMUL) bad("a product is not a matrix product");
+    for (int v : ki.linear) {
+      bool inner = false;
+      for (int u : ki.linear)
+        if (u != v && ki.ancestor(u, v)) inner = true;
+      (inner ? outs_p : scores).push_back(v);
+    }
+    for (int v : ki.k.prims)
+      if (nd(v).op == KORCH_BIN_SUM) {
+        if (bin_node >= 0) bad("more than one sum by bins");
+        bin_node = v;
+      }
+    if (outs_p.empty() && bin_node < 0) bad("no product reads the plane");
+    if (scores.size() > 2) bad("more than two score products");
+    if (outs_p.size() > 2) bad("more than two output products");
+    PS = nd(scores[0]).shape;
+    R = (int)PS.size();
+    N = PS[R - 2], M = PS[R - 1];
+    for (int s : scores)
+      if (nd(s).shape != PS) bad("score products differ in shape");
+    // orientation and plane operands
+    std::vector<int> xs;
+    bool first = true;
+    for (int o : outs_p) {
+      int x = nd(o).in[0];
+      if (!in(x) || in(nd(o).in[1])) {
+        // the right operand may be a layout view or a select of a stored tensor
+        if (!in(x)) bad("an output product's left operand is not the plane");
+      }
+      bool tr = false;
+      if (nd(x).op == KORCH_TRANSPOSE && nd(nd(x).in[0]).shape == PS && in(nd(x).in[0])) {
+        const korch_attrs& a = nd(x).attrs;
+        bool last2 = a.perm[R - 2] == R - 1 && a.perm[R - 1] == R - 2;
+        for (int d = 0; d < R - 2; ++d) last2 = last2 && a.perm[d] == d;
+        if (!last2) bad("the plane's transpose must swap its last two axes");
+        tr = true;
+        x = nd(x).in[0];
+      }
+      if (nd(x).shape != PS) bad("an output product's left operand is not the plane");
+      if (!first && tr == rows_owned) bad("output products contract different axes");
+      rows_owned = !tr;
+      first = false;
+      if (nd(x).dtype != nd(nd(o).in[1]).dtype) bad("the plane's dtype differs from the operand it is multiplied with");
+      xs.push_back(x);
+    }
+    dtype = nd(nd(scores[0]).in[0]).dtype;
+    const Shape batch(PS.begin(), PS.end() - 2);
+    for (int s : scores) {
+      const Node& n = nd(s);
+      if (nd(n.in[0]).dtype != dtype || nd(n.in[1]).dtype != dtype) bad("operand dtypes differ");
+      Operand a = operand(n.in[0], false, batch, "left score operand");
+      Operand b = operand(n.in[1], true, batch, "right score operand");
+      sc_own.push_back(rows_owned ? a : b);
+      sc_str.push_back(rows_owned ? b : a);
+      sst.push_back(add_streamed(rows_owned ? b : a));
+    }
+    for (size_t i = 0; i < outs_p.size(); ++i) {
+      const Node& n = nd(outs_p[i]);
+      if (nd(n.in[1]).dtype != dtype) bad("operand dtypes differ");
+      Shape os = batch;
+      os.push_back(rows_owned ? N : M);
+      os.push_back(n.shape.back());
+      if (n.shape != os) bad("output products differ in batch dims");
+      Operand w = operand(n.in[1], false, batch, "output operand");
+      out_w.push_back(w);
+      ost.push_back(add_streamed(w));
+    }
+    // softmax
+    if (!ki.reduces.empty()) {
+      if (ki.reduces.size() != 2 || !rows_owned || scores.size() != 1) bad("reductions other than one row softmax");
+      for (int r : ki.reduces) {
+        const Node& n = nd(r);
+        if (n.axis != R - 1 || !n.attrs.keepdim || nd(n.in[0]).shape != PS) bad("a reduction is not along the plane's rows");
+        if (n.op == KORCH_REDUCE_MAX) nm = r;
+        if (n.op == KORCH_REDUCE_SUM) nl = r;
+      }
+      if (nm < 0 || nl < 0) bad("the softmax needs a row maximum and a row sum");
+      ne = nd(nl).in[0];
+      int c2 = zero_select(ne);
+      nexp = c2 >= 0 ? nd(strip_identity(ne)).in[1] : ne;
+      if (!in(nexp) || nd(nexp).op != KORCH_EXP) bad("the row sum is not over exponentials");
+      int z = nd(nexp).in[0];
+      if (!in(z) || nd(z).op != KORCH_SUB || nd(z).attrs.has_scalar || nd(z).in[1] != nm) bad("the exponent is not s - max");
+      nsfinal = nd(z).in[0];
+      int top = nd(nm).in[0];
+      if (c2 >= 0) {
+        const Node& t = nd(top);
+        if (!in(top) || t.op != KORCH_SELECT || !t.attrs.has_scalar || t.in[0] != c2 || t.in[1] != nsfinal)
+          bad("the row maximum must be over select(mask, s, low)");
+        low = t.attrs.scalar;
+        cond = c2;
+      } else if (top != nsfinal) {
+        bad("the row maximum is not over the exponent's scores");
+      }
+      for (size_t i = 0; i < xs.size(); ++i) {
+        int x = strip_identity(xs[i]);
+        if (in(x) && nd(x).op == KORCH_DIV && !nd(x).attrs.has_scalar && nd(x).in[1] == nl) {
+          divided = true;
+          x = strip_identity(nd(x).in[0]);
+        }
+        if (x != ne) bad("the softmax's product must read its exponentials");
+      }
+      if (outs_p.size() != 1 || bin_node >= 0) bad("a softmax kernel has one output product");
+      ox.push_back(0);
+    } else {
+      std::vector<int> all = xs;
+      if (bin_node >= 0) all.push_back(nd(bin_node).in[0]);
+      bool same = true;
+      for (size_t i = 0; i < all.size(); ++i) {
+        if (!in(all[i]) || nd(all[i]).shape != PS) bad("plane operand outside the kernel");
+        const int c = zero_select(all[i]);
+        if (i == 0) cond = c;
+        if (c != cond) same = false;
+        int k = (int)(std::find(xnodes.begin(), xnodes.end(), all[i]) - xnodes.begin());
+        if (k == (int)xnodes.size()) xnodes.push_back(all[i]);
+        if (i < xs.size())
+          ox.push_back(k);
+        else
+          xbin = k;
+      }
+      if (!same) cond = -1;
+    }
+    if (bin_node >= 0) {
+      if (!rows_owned && !outs_p.empty()) bad("a sum by bins goes with row-owned products");
+      const Node& n = nd(bin_node);
+      const int tr = (int)n.shape.size();
+      // result dims [.., 1, 1, T] or fewer leading ones: rows and columns are summed
+      for (int d = 0; d < tr - 1; ++d) {
+        const int j = d + R - (tr - 1);
+        if (j >= R - 2 && n.shape[d] != 1) bad("bins along a plane axis");
+      }
+      if (!in(n.in[1]) || has_score(n.in[1])) bad("the bins are not computed in the kernel, or from the scores");
+    }
+    for (auto& w : streamed)
+      if (w.shape[0] > 256) bad("an operand is wider than 256");
+    // registers of a lane that live through the walk: accumulators and owned operands
+    int64_t regs = 0;
+    for (auto& w : out_w) regs += (w.shape[0] + 31) / 32 * 16;
+    for (auto& o : sc_own) regs += (o.shape[0] + 31) / 32 * 32 * dtype_bytes(dtype) / 8;
+    if (regs > 256) bad("owned operands and output products fill the registers");
+    // outputs
+    for (int o : ki.k.outs) {
+      if (below(o) == bin_node) {
+        bin_out = o;
+        continue;
+      }
+      int p = -1;
+      for (size_t i = 0; i < outs_p.size(); ++i)
+        if (depends(o, outs_p[i])) {
+          if (p >= 0) bad("an output reads two output products");
+          p = (int)i;
+        }
+      if (p >= 0) {
+        prod_of[o] = p;
+      } else {
+        if (nm < 0 || !(depends(o, nm) || depends(o, nl))) bad("an output is neither a product's nor a row statistic");
+        const Shape& s = nd(below(o)).shape;
+        Shape want(PS.begin(), PS.end() - 1);
+        want.push_back(1);
+        if (s != want) bad("a row statistic's shape");
+      }
+    }
+    if (bin_node >= 0 && bin_out < 0) bad("a sum by bins that is not an output");
+    for (size_t i = 0; i < outs_p.size(); ++i) {
+      bool used = false;
+      for (auto& [o, p] : prod_of) used = used || p == (int)i;
+      if (!used) bad("an output product without an output");
+    }
+  }
+  bool divided = false;
+
+  // Node below the reshapes that end an output (its elements are stored in the same order).
+  int below(int o) const {
+    while (in(o) && nd(o).op == KORCH_RESHAPE) o = nd(o).in[0];
+    return o;
+  }
+
+  // ---- emission --------------------------------------------------------------
+
+  std::vector<Ix> plane_index() const {
+    std::vector<Ix> it(R);
+    for (int d = 0; d < R - 2; ++d) it[d] = Ix::var("b.c[" + std::to_string(d) + "]");
+    it[R - 2] = Ix::var(rows_owned ? "ro" : "rs");
+    it[R - 1] = Ix::var(rows_owned ? "rs" : "ro");
+    return it;
+  }
+  int vec_id(std::vector<int>& list, int v) {
+    auto f = std::find(list.begin(), list.end(), v);
+    if (f == list.end()) {
+      list.push_back(v);
+      return (int)list.size() - 1;
+    }
+    return (int)(f - list.begin());
+  }
+  std::string std_key(int node, const std::vector<Ix>& it) const {
+    return Emitter::key(node, broadcast_index(nd(node).shape, PS, it));
+  }
+
+  std::unique_ptr<Emitter> emitter() const {
+    auto e = std::make_unique<Emitter>(g);
+    e->inset = ki.in;
+    e->argslot = slot;
+    e->vec = 1;
+    return e;
+  }
+
+  // Body of a function that evaluates plane nodes `want` into `dst`; `full`:
+  // the mask is known to hold.
+  std::string plane_body(const std::vector<std::pair<int, std::string>>& want, bool full) {
+    auto it = plane_index();
+    auto e = emitter();
+    e->provide = [&](int node, const std::vector<Ix>& idx, std::string* out) {
+      for (size_t s = 0; s < scores.size(); ++s)
+        if (node == scores[s]) {
+          if (Emitter::key(node, idx) != std_key(node, it)) bad("a score is read at another index");
+          *out = "xs[" + std::to_string(s) + "]";
+          return true;
+        }
+      if (full && node == cond) {
+        *out = "(1.0f)";
+        return true;
+      }
+      const PlaneCls c = cls(node);
+      if (c == FULLP) return false;
+      if ((int)nd(node).shape.size() > R) return false;
+      std::string k;
+      try {
+        k = std_key(node, it);
+      } catch (Error&) {
+        return false;
+      }
+      if (Emitter::key(node, idx) != k) return false;
+      if (in(node) && nd(node).op == KORCH_FILL) return false;
+      if (is_owned(c))
+        *out = "ov[" + std::to_string(vec_id(ovs, node)) + "]";
+      else
+        *out = "tv[" + std::to_string(vec_id(tvs, node)) + "]";
+      return true;
+    };
+    std::string res;
+    for (auto& [node, dst] : want) {
+      const std::string v = e->value(node, broadcast_index(nd(node).shape, PS, it));
+      e->body << "    " << dst << " = " << v << ";\n";
+    }
+    return e->pre.str() + e->body.str();
+  }
+
+  // Value of a vector node at owned / streamed index variable `r`.
+  std::string vector_value(int node, bool owned, std::string* stmts) {
+    std::vector<Ix> it(R);
+    for (int d = 0; d < R - 2; ++d) it[d] = Ix::var("b.c[" + std::to_string(d) + "]");
+    const bool rows = owned == rows_owned;
+    it[R - 2] = rows ? Ix::var("r") : Ix::k(0);
+    it[R - 1] = rows ? Ix::k(0) : Ix::var("r");
+    auto e = emitter();
+    // The other axis' index is not used by a vector (its size there is 1).
+    const Shape& s = nd(node).shape;
+    std::vector<Ix> idx(s.size());
+    for (size_t d = 0; d < s.size(); ++d) {
+      const size_t j = d + R - s.size();
+      idx[d] = s[d] == 1 ? Ix::k(0) : it[j];
+    }
+    const std::string v = e->value(node, idx);
+    *stmts = e->pre.str() + e->body.str();
+    return v;
+  }
+
+  // Range of a node over a tile: expression of Range functions.
+  std::string range(int v) {
+    const Node& n = nd(v);
+    const PlaneCls c = cls(v);
+    if (in(v) && n.op == KORCH_FILL) return "r_pt(" + flit(n.attrs.scalar) + ")";
+    if (c != FULLP && is_owned(c)) return "ow[" + std::to_string(vec_id(ovs, v)) + "]";
+    if (in(v)) {
+      auto two = [&](const char* f) {
+        return std::string(f) + "(" + range(n.in[0]) + ", " + (n.attrs.has_scalar ? "r_pt(" + flit(n.attrs.scalar) + ")" : range(n.in[1])) +
+               ")";
+      };
+      auto swapped = [&](const char* f) {
+        return std::string(f) + "(" + (n.attrs.has_scalar ? "r_pt(" + flit(n.attrs.scalar) + ")" : range(n.in[1])) + ", " + range(n.in[0]) +
+               ")";
+      };
+      switch (n.op) {
+        case KORCH_ADD: return two("r_add");
+        case KORCH_SUB: return two("r_sub");
+        case KORCH_MUL: return two("r_mul");
+        case KORCH_MAX: return two("r_max");
+        case KORCH_MIN: return two("r_min");
+        case KORCH_LT: return two("r_lt");
+        case KORCH_LE: return two("r_le");
+        case KORCH_GT: return swapped("r_lt");
+        case KORCH_GE: return swapped("r_le");
+        case KORCH_EQ: return two("r_eq");
+        case KORCH_NEG: return "r_neg(" + range(n.in[0]) + ")";
+        case KORCH_ABS: return "r_abs(" + range(n.in[0]) + ")";
+        case KORCH_IDENTITY: return range(n.in[0]);
+        default: break;
+      }
+    }
+    if (c == FULLP) return "r_all()";
+    // a streamed vector: an index along the streamed axis is known, others are read
+    if (in(v) && n.op == KORCH_IOTA && (int)n.shape.size() - n.axis == (rows_owned ? 1 : 2)) return "Range{s0, s1}";
+    return "rv[" + std::to_string(vec_id(rvs, v)) + "]";
+  }
+
+  // Splits of the streamed axis and geometry.
+  int NW = 4, TS = 64, SPLIT = 1, STAGES = 2;
+  bool WSPLIT = false;
+  int64_t OTILES = 1, NB = 1;
+
+  size_t lds_bytes() const {
+    const int es = dtype_bytes(dtype), VL = 16 / es;
+    size_t tile = 0;
+    int nreg = 0;
+    for (auto& w : streamed) tile += (size_t)TS * ((w.shape[0] + 31) / 32 * 32 + VL) * es;
+    for (auto& w : out_w) nreg += (int)((w.shape[0] + 31) / 32 * 32) / 2;
+    tile += (size_t)tvs.size() * TS * 4;
+    size_t tiles = tile * STAGES * (WSPLIT ? NW : 1);
+    size_t merge = WSPLIT ? (size_t)NW * (nreg + 2) * 256 : 0;
+    size_t bins = bin_node >= 0 ? (size_t)NW * nd(bin_node).shape.back() * 256 : 0;
+    return std::max(tiles, merge) + 4096 + (NW * ovs.size() * 2 + 8) * 4 + 80 + bins;
+  }
+
+  void geometry() {
+    NB = 1;
+    for (int d = 0; d < R - 2; ++d) NB *= PS[d];
+    const int64_t nown = rows_owned ? N : M, nstr = rows_owned ? M : N;
+    const bool f32 = dtype == KORCH_F32;
+    int aw = 0, ow = 0;
+    for (auto& w : out_w) aw += (int)((w.shape[0] + 31) / 32 * 32);
+    for (auto& o : sc_own) ow += (int)((o.shape[0] + 31) / 32 * 32);
+    TS = 64;
+    NW = 4;
+    // Few owned indices: the waves share them and split the streamed axis.
+    WSPLIT = nown <= 32;
+    if (f32) TS = 32;
+    if (WSPLIT) STAGES = 1;
+    while (lds_bytes() > 160 * 1024 && TS > 32) TS /= 2;
+    while (lds_bytes() > 160 * 1024 && NW > 1) NW /= 2;
+    while (lds_bytes() > 160 * 1024 && STAGES > 1) STAGES = 1;
+    if (lds_bytes() > 160 * 1024) bad("operands exceed the 160 KiB of LDS");
+    const int OT = WSPLIT ? 32 : 32 * NW;
+    OTILES = (nown + OT - 1) / OT;
+    const int64_t wgs = OTILES * NB, tiles = (nstr + TS - 1) / TS, per = WSPLIT ? NW : 1;
+    SPLIT = 1;
+    if (workgroup_splits() && wgs < 256) {
+      // enough workgroups for two per compute unit, at least two tiles each
+      int64_t want = (512 + wgs - 1) / wgs;
+      want = std::min<int64_t>(want, std::max<int64_t>(1, tiles / (2 * per)));
+      SPLIT = (int)std::min<int64_t>(want, 32);
+    }
+    if (wgs > (int64_t)1 << 30) bad("too many workgroups");
+    (void)aw, (void)ow;
+  }
+
+  GenKernel generate(int index) {
+    const bool f32 = dtype == KORCH_F32;
+    set_fast_math(!f32);
+    GenKernel gk;
+    gk.family = KORCH_FAM_PLANE;
+    gk.name = kernel_name(index, "plane");
+    ki.assign_args(gk, slot);
+    const std::string T = ctype(dtype);
+    const bool softmax = nm >= 0;
+    // functions on the plane (both variants allocate the vectors they read)
+    std::string fn[2];
+    for (int full = 0; full < 2; ++full) {
+      std::vector<std::pair<int, std::string>> want;
+      if (softmax) {
+        want.push_back({nsfinal, "v"});
+        if (cond >= 0 && !full) want.push_back({cond, "const float kc_"});
+      } else {
+        for (size_t i = 0; i < xnodes.size(); ++i) want.push_back({xnodes[i], "out[" + std::to_string(i) + "]"});
+      }
+      fn[full] = plane_body(want, full != 0);
+      if (softmax && cond >= 0 && !full) fn[full] += "    k = kc_ != 0.0f;\n";
+    }
+    std::string bin_fn;
+    if (bin_node >= 0) bin_fn = plane_body({{nd(bin_node).in[1], "const float id_"}}, false);
+    std::string mask_expr = cond >= 0 ? range(cond) : "";
+    geometry();
+    // vectors
+    std::ostringstream p;
+    const int64_t nown = rows_owned ? N : M, nstr = rows_owned ? M : N;
+    p << "struct Pol {\n  typedef " << T << " T;\n  struct B {\n    i64 c[" << std::max(1, R - 2) << "];\n  };\n";
+    p << "  static constexpr bool SOFTMAX = " << softmax << ", MASK = " << (cond >= 0) << ", WSPLIT = " << WSPLIT << ";\n";
+    p << "  static constexpr i64 NOWN = " << nown << "LL, NSTR = " << nstr << "LL;\n";
+    p << "  static constexpr int NW = " << NW << ", TS = " << TS << ", STAGES = " << STAGES << ", SPLIT = " << SPLIT << ", OTILES = " << OTILES
+      << ", NB = " << NB << ";\n";
+    const int64_t nbin = bin_node >= 0 ? nd(bin_node).shape.back() : 0;
+    p << "  static constexpr int NSP = " << scores.size() << ", NST = " << streamed.size() << ", NOP = " << outs_p.size() << ", NX = "
+      << std::max<size_t>(1, xnodes.size()) << ", NBIN = " << nbin << ", XBIN = " << std::max(0, xbin) << ";\n";
+    p << "  static constexpr int NTAB = " << tvs.size() << ", NOV = " << ovs.size() << ", NRV = " << rvs.size() << ";\n";
+    p << "  static constexpr float MINIT = " << flit(softmax && cond >= 0 ? low : -INFINITY) << ";\n";
+    auto table = [&](const char* name, const std::vector<int>& v) {
+      p << "  static constexpr int " << name << "(int i) {\n    constexpr int t[] = {";
+      for (int x : v) p << x << ", ";
+      p << "0};\n    return t[i];\n  }\n";
+    };
+    std::vector<int> sw;
+    for (auto& w : streamed) sw.push_back((int)w.shape[0]);
+    table("sw", sw);
+    table("sst", sst);
+    table("ost", ost);
+    table("ox", ox);
+    std::vector<int> rm, om;
+    for (auto& w : streamed) rm.push_back(w.mask >= 0);
+    for (auto& w : sc_own) om.push_back(w.mask >= 0);
+    p << "  static constexpr bool row_mask(int i) {\n    constexpr bool t[] = {";
+    for (int x : rm) p << x << ", ";
+    p << "0};\n    return t[i];\n  }\n  static constexpr bool own_mask(int i) {\n    constexpr bool t[] = {";
+    for (int x : om) p << x << ", ";
+    p << "0};\n    return t[i];\n  }\n";
+    // batch coordinates
+    p << "  static __device__ __forceinline__ B batch(int l) {\n    B b;\n    i64 q = l;\n";
+    for (int d = R - 3; d >= 0; --d)
+      p << "    b.c[" << d << "] = q % " << PS[d] << "; q /= " << PS[d] << ";\n";
+    if (R == 2) p << "    b.c[0] = q;\n";
+    p << "    return b;\n  }\n";
+    // operand rows
+    auto rows = [&](const char* fnn, const std::vector<Operand>& v, const char* okn) {
+      p << "  template <int t> static __device__ __forceinline__ const T* " << fnn << "(const KArgs& a, const B& b, i64 r) {\n";
+      for (size_t i = 0; i < v.size(); ++i)
+        p << "    if constexpr (t == " << i << ") return (const T*)a.p[" << slot.at(v[i].root) << "] + " << v[i].off << ";\n";
+      p << "  }\n";
+      p << "  template <int t> static __device__ __forceinline__ bool " << okn << "(const KArgs& a, const B& b, i64 r) {\n";
+      for (size_t i = 0; i < v.size(); ++i) {
+        if (v[i].mask < 0) continue;
+        auto e = emitter();
+        const std::string x = e->value(v[i].mask, mask_idx.at(v[i].node));
+        p << "    if constexpr (t == " << i << ") {\n" << e->pre.str() << e->body.str() << "    return " << x << " != 0.0f;\n    }\n";
+      }
+      p << "    return true;\n  }\n";
+    };
+    rows("srow", streamed, "srow_ok");
+    rows("orow", sc_own, "orow_ok");
+    auto vectors = [&](const char* name, const std::vector<int>& v, bool owned) {
+      p << "  static __device__ __forceinline__ float " << name << "(const KArgs& a, const B& b, int k, i64 r) {\n";
+      for (size_t i = 0; i < v.size(); ++i) {
+        std::string st;
+        const std::string x = vector_value(v[i], owned, &st);
+        p << "    if (k == " << i << ") {\n" << st << "    return " << x << ";\n    }\n";
+      }
+      p << "    return 0.0f;\n  }\n";
+    };
+    vectors("own", ovs, true);
+    vectors("tab", tvs, false);
+    vectors("rvec", rvs, false);
+    p << "  static __device__ __forceinline__ Range mask_range(const KArgs& a, const B& b, const Range* ow, const Range* rv, float s0, float s1) {\n";
+    p << "    return " << (cond >= 0 ? mask_expr : "r_pt(1.0f)") << ";\n  }\n";
+    const char* sig = softmax ? "logit(const KArgs& a, const B& b, const float* ov, const float* tv, i64 ro, i64 rs, const float* xs, float& v, bool& k)"
+                              : "plane(const KArgs& a, const B& b, const float* ov, const float* tv, i64 ro, i64 rs, const float* xs, float* out)";
+    p << "  template <bool CHECK> static __device__ __forceinline__ void " << sig << " {\n    if constexpr (CHECK) {\n" << fn[0]
+      << "    } else {\n" << fn[1] << "    }\n  }\n";
+    if (bin_node >= 0)
+      p << "  static __device__ __forceinline__ float bin(const KArgs& a, const B& b, const float* ov, const float* tv, i64 ro, i64 rs) {\n"
+        << "    const float xs[2] = {};\n" << bin_fn << "    return k_min(k_max(id_, 0.0f), " << flit((double)(nbin - 1)) << ");\n  }\n";
+    // results
+    p << "  template <int o> static __device__ __forceinline__ void store(const KArgs& a, const B& b, i64 ro, int dim, float m, float l, f32x4 v) {\n";
+    for (size_t i = 0; i < outs_p.size(); ++i) {
+      p << "    if constexpr (o == " << i << ") {\n";
+      for (auto& [o, pi] : prod_of)
+        if (pi == (int)i) p << store_code(o, (int)i);
+      p << "    }\n";
+    }
+    p << "  }\n";
+    p << "  static __device__ __forceinline__ void stats(const KArgs& a, const B& b, i64 ro, float m, float l) {\n";
+    for (int o : ki.k.outs) {
+      if (o == bin_out || prod_of.count(o)) continue;
+      auto e = emitter();
+      std::vector<Ix> it(R);
+      for (int d = 0; d < R - 2; ++d) it[d] = Ix::var("b.c[" + std::to_string(d) + "]");
+      it[R - 2] = Ix::var("ro");
+      it[R - 1] = Ix::k(0);
+      e->provide = [&](int node, const std::vector<Ix>&, std::string* out) {
+        if (node == nm) return *out = "m", true;
+        if (node == nl) return *out = "l", true;
+        return false;
+      };
+      const std::string v = e->value(below(o), it);
+      auto st = strides_of(nd(below(o)).shape);
+      Ix off = Ix::k(0);
+      for (int d = 0; d < R; ++d) off = ix_add(off, ix_mulk(it[d], st[d], 1));
+      p << "    {\n" << e->pre.str() << e->body.str() << "    st1((" << ctype(nd(o).dtype) << "*)a.p[" << ki.out_slot(o) << "] + " << off.b
+        << ", " << v << ");\n    }\n";
+    }
+    p << "  }\n";
+    if (bin_node >= 0) {
+      const Node& n = nd(bin_node);
+      const int tr = (int)n.shape.size();
+      std::string row = "0", member = "0";
+      int64_t members = 1, rows_n = 1;
+      for (int d = 0; d < R - 2; ++d) {
+        const int j = d - (R - (tr - 1));
+        const bool kept = j >= 0 && n.shape[j] != 1;
+        std::string c = "b.c[" + std::to_string(d) + "]";
+        if (kept)
+          row = "(" + row + " * " + std::to_string(PS[d]) + " + " + c + ")", rows_n *= PS[d];
+        else
+          member = "(" + member + " * " + std::to_string(PS[d]) + " + " + c + ")", members *= PS[d];
+      }
+      p << "  static constexpr int BIN_MEMBERS = " << members << ";\n";
+      p << "  static __device__ __forceinline__ int bin_row(const B& b) { return (int)" << row << "; }\n";
+      p << "  static __device__ __forceinline__ int bin_member(const B& b) { return (int)" << member << "; }\n";
+      p << "  static __device__ __forceinline__ void store_bin(const KArgs& a, int row, int k, float v) { st1((" << ctype(nd(bin_out).dtype) << "*)a.p["
+        << ki.out_slot(bin_out) << "] + (i64)row * " << nbin << " + k, v); }\n";
+      ArgRef scr;
+      scr.kind = ArgRef::Scratch;
+      scr.bytes = (size_t)(rows_n * members * OTILES * SPLIT * nbin) * 4;
+      p << "  static constexpr int BSCR = " << gk.args.size() << ";\n";
+      gk.args.push_back(scr);
+      ArgRef cnt;
+      cnt.kind = ArgRef::Counter;
+      cnt.bytes = (size_t)rows_n * 128;
+      p << "  static constexpr int BCNT = " << gk.args.size() << ";\n";
+      gk.args.push_back(cnt);
+    }
+    if (SPLIT > 1) {
+      int nreg = 0;
+      for (auto& w : out_w) nreg += (int)((w.shape[0] + 31) / 32 * 32) / 2;
+      ArgRef scr;
+      scr.kind = ArgRef::Scratch;
+      scr.bytes = (size_t)(NB * OTILES) * SPLIT * (WSPLIT ? 1 : NW) * (nreg / 4 + 1) * 1024;
+      p << "  static constexpr int SCR = " << gk.args.size() << ";\n";
+      gk.args.push_back(scr);
+      ArgRef cnt;
+      cnt.kind = ArgRef::Counter;
+      cnt.bytes = (size_t)(NB * OTILES) * 128;
+      p << "  static constexpr int CNT = " << gk.args.size() << ";\n";
+      gk.args.push_back(cnt);
+      gk.wg_split = true;
+    }
+    p << "};\n";
+    std::ostringstream src;
+    src << source_header((int)gk.args.size()) << k_device_plane << "\n" << p.str();
+    src << "extern \"C\" __global__ void __launch_bounds__(" << NW * 64 << ") " << gk.name << "(KArgs a) {\n";
+    src << "  __shared__ __attribute__((aligned(16))) char smem[Geo<Pol>::bytes];\n  Plane<Pol> k(a, smem);\n  k.run();\n}\n";
+    gk.source = src.str();
+    gk.grid[0] = (int)(OTILES * NB);
+    gk.grid[1] = SPLIT;
+    gk.block[0] = NW * 64;
+    gk.lds_bytes = (int)lds_bytes();
+    ki.fill_cost(gk);
+    return gk;
+  }
+
+  // Epilogue of output `o` (product i): four consecutive elements of a row.
+  std::string store_code(int o, int i) {
+    const Shape& os = nd(outs_p[i]).shape;  // [batch.., own, width]
+    const int r = (int)os.size();
+    std::vector<Ix> it(r);
+    for (int d = 0; d < r - 2; ++d) it[d] = Ix::var("b.c[" + std::to_string(d) + "]");
+    it[r - 2] = Ix::var("ro");
+    it[r - 1] = Ix::var("dim", 1, 4);
+    // a transpose that ends the output changes where its elements are stored
+    const int top = below(o);
+    int v = top;
+    std::vector<int> perm(r);
+    for (int d = 0; d < r; ++d) perm[d] = d;
+    while (in(v) && nd(v).op == KORCH_TRANSPOSE && v != outs_p[i]) {
+      std::vector<int> q(r);
+      if (nd(v).attrs.rank != r) bad("an output's transpose changes its rank");
+      for (int d = 0; d < r; ++d) q[d] = nd(v).attrs.perm[perm[d]];
+      perm = q;
+      v = nd(v).in[0];
+    }
+    if (nd(v).shape != os) bad("an output's shape differs from its product's");
+    auto e = emitter();
+    e->vec = 4;
+    const std::string key = Emitter::key(outs_p[i], it);
+    e->provide = [&](int node, const std::vector<Ix>& idx, std::string* out) {
+      if (node == outs_p[i]) {
+        if (Emitter::key(node, idx) != key) bad("an output product is read at another index");
+        *out = divided ? binary_expr(KORCH_DIV, "v[e]", "l") : "v[e]";
+        return true;
+      }
+      if (node == nm && nm >= 0) return *out = "m", true;
+      if (node == nl && nl >= 0) return *out = "l", true;
+      return false;
+    };
+    const std::string x = e->value(v, it);
+    auto st = strides_of(nd(top).shape);
+    Ix off = Ix::k(0);
+    // stored element [i_0, ..] of o is v's element with index it[perm]
+    for (int d = 0; d < r; ++d) off = ix_add(off, ix_mulk(it[perm[d]], st[d], 4));
+    if (!off.affine || off.c != 1) bad("an output's rows are not consecutive");
+    bool al = true;
+    for (int d = 0; d < r; ++d)
+      if (perm[d] != r - 1 && nd(top).shape[d] > 1 && st[d] % 4) al = false;
+    std::ostringstream s;
+    s << "      {\n" << e->pre.str() << "      float y[4];\n#pragma unroll\n      for (int e = 0; e < 4; ++e) {\n" << e->body.str()
+      << "      y[e] = " << x << ";\n      }\n";
+    const std::string P = "((" + ctype(nd(o).dtype) + "*)a.p[" + std::to_string(ki.out_slot(o)) + "])";
+    if (!al) bad("an output's rows are not aligned");
+    s << "      " << out_store(g, o, P, off.b, 4, "y") << ";\n      }\n";
+    return s.str();
+  }
+};
+
+}  // namespace
+
+bool match_plane(const KInfo& ki, std::string* why) {
+  if (ki.linear.size() < 2) {
+    *why = "plane: fewer than two products";
+    bool bins = false;
+    for (int v : ki.k.prims) bins = bins || ki.g.nodes[v].op == KORCH_BIN_SUM;
+    if (!bins || ki.linear.empty()) return false;
+  }
+  try {
+    PlaneGen p(ki);
+    p.analyze();
+    p.generate(0);
+  } catch (Error& e) {
+    *why = e.what();
+    return false;
+  }
+  return true;
+}
+
+GenKernel gen_plane(const KInfo& ki, int index) {
+  PlaneGen p(ki);
+  p.analyze();
+  return p.generate(index);
+}
+
+}  // namespace korch

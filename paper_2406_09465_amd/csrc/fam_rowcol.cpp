@@ -1,0 +1,455 @@
+// Row programs with column sums: a kernel whose nodes are full rows [R, L] and
+// row statistics [R, 1], as in the row family, and that also sums full rows
+// over axis 0 (LayerNorm's gradient: the input's gradient needs two row means,
+// the weight's and the bias's are sums over the rows; one pass reads the rows
+// once for all of them).  Also the sum by bins on its own.
+//
+// HBM bound: every row tensor is read once and every row output written once.
+// A workgroup walks over rows (the next row's loads go out before the current
+// row's arithmetic), keeps the column sums of its lanes' columns in fp32
+// registers, and hands its sums over through scratch; the last workgroup of a
+// group adds the group's partial sums in order, the last group's those of the
+// groups (deterministic; no floating-point atomics).  Row programs without
+// column sums come here when a row is longer than a wavefront's registers: the
+// waves of a workgroup share it.
+#include <algorithm>
+
+#include "families.h"
+
+namespace korch {
+
+namespace {
+
+struct RowCol {
+  int64_t R = 0, L = 0;
+  std::vector<int> cols;      // column reductions
+  std::map<int, int> cls;     // 0 full row, 1 row statistic
+};
+
+bool analyze_rowcol(const KInfo& ki, RowCol& rc, std::string* why) {
+  const Graph& g = ki.g;
+  auto bad = [&](const char* m) {
+    *why = std::string("rowcol: ") + m;
+    return false;
+  };
+  if (!ki.linear.empty()) return bad("has linear primitives");
+  Shape F;
+  for (int r : ki.reduces) {
+    const Node& n = g.nodes[r];
+    const Shape& s = g.nodes[n.in[0]].shape;
+    if (s.size() != 2) return bad("a reduced tensor is not [rows, columns]");
+    if (F.empty()) F = s;
+    if (F != s) return bad("reductions over different shapes");
+    if (n.axis == 0) {
+      if (n.op == KORCH_REDUCE_MAX) return bad("a column maximum");
+      rc.cols.push_back(r);
+    } else if (!n.attrs.keepdim) {
+      return bad("a row reduction without keepdim");
+    }
+  }
+  if (ki.reduces.empty()) return bad("no reduction");
+  rc.R = F[0], rc.L = F[1];
+  if (rc.L < 2) return bad("rows shorter than 2");
+  const Shape S = {F[0], 1};
+  for (int v : ki.k.prims) {
+    const Node& n = g.nodes[v];
+    const Kind kd = op_kind(n.op);
+    if (kd != Kind::Unary && kd != Kind::Binary && kd != Kind::Reduce) return bad("a primitive that is neither elementwise nor a reduction");
+    if (std::find(rc.cols.begin(), rc.cols.end(), v) != rc.cols.end()) {
+      if (std::find(ki.k.outs.begin(), ki.k.outs.end(), v) == ki.k.outs.end()) return bad("a column sum that is not an output");
+      for (int c : g.consumers[v])
+        if (ki.in.count(c)) return bad("a column sum is read in the kernel");
+      continue;
+    }
+    if (kd != Kind::Reduce && n.shape == F)
+      rc.cls[v] = 0;
+    else if (n.shape == S)
+      rc.cls[v] = 1;
+    else
+      return bad("a node is neither a row nor a row statistic");
+    if (kd == Kind::Binary && !n.attrs.has_scalar)
+      for (int u : n.in)
+        if (ki.in.count(u) && rc.cls.count(u) && rc.cls[u] == 0 && rc.cls[v] == 1) return bad("incompatible operands");
+  }
+  for (int v : ki.k.prims)
+    if (op_kind(g.nodes[v].op) == Kind::Reduce) {
+      const int u = g.nodes[v].in[0];
+      if (ki.in.count(u) && (!rc.cls.count(u) || rc.cls[u] != 0)) return bad("a reduction's operand is not a full row");
+    }
+  return true;
+}
+
+// Lanes per row G, vector VEC, vectors per lane NC; false when a row is too long.
+bool rowcol_geometry(int64_t L, int eb, int& G, int& VEC, int& NC) {
+  VEC = 16 / eb;
+  while (L % VEC) VEC /= 2;
+  // up to 16 elements of every row tensor per lane: two row tensors, their
+  // sums and the weights stay well below the registers of eight waves per SIMD
+  const int64_t n = L / VEC;
+  G = 1;
+  while (G < 1024 && (n + G - 1) / G * VEC > 16) G *= 2;
+  NC = (int)((n + G - 1) / G);
+  return NC * VEC <= 64;
+}
+
+}  // namespace
+
+bool match_rowcol(const KInfo& ki, std::string* why) {
+  RowCol rc;
+  if (!analyze_rowcol(ki, rc, why)) return false;
+  int G, VEC, NC;
+  if (!rowcol_geometry(rc.L, 2, G, VEC, NC) || !rowcol_geometry(rc.L, 4, G, VEC, NC)) {
+    *why = "rowcol: rows longer than the registers of a workgroup";
+    return false;
+  }
+  return true;
+}
+
+GenKernel gen_rowcol(const KInfo& ki, int index) {
+  const Graph& g = ki.g;
+  RowCol rc;
+  std::string why;
+  if (!analyze_rowcol(ki, rc, &why)) fail(KORCH_E_UNSUPPORTED, why);
+  GenKernel gk;
+  gk.family = KORCH_FAM_ROWCOL;
+  gk.name = kernel_name(index, "rowcol");
+  std::map<int, int> slot;
+  ki.assign_args(gk, slot);
+  const Shape F = {rc.R, rc.L}, S = {rc.R, 1};
+  int eb = 2;
+  for (int u : ki.ext)
+    if (g.nodes[u].shape == F) eb = std::max(eb, dtype_bytes(g.nodes[u].dtype));
+  for (int o : ki.k.outs)
+    if (g.nodes[o].shape == F) eb = std::max(eb, dtype_bytes(g.nodes[o].dtype));
+  int G, VEC, NC;
+  if (!rowcol_geometry(rc.L, eb, G, VEC, NC)) fail(KORCH_E_UNSUPPORTED, "rowcol: rows too long");
+  const int NT = std::max(256, G), RPB = NT / G, WR = G > 64 ? G / 64 : 1;
+  const int64_t blocks = (rc.R + RPB - 1) / RPB;
+  const int64_t NWG = std::min<int64_t>(blocks, NT == 256 ? 512 : 256);
+  const int64_t NS = (int64_t)rc.cols.size(), C = NS * rc.L;
+  const bool ragged = (rc.L / VEC) % G != 0;  // the last vector of some lanes is past the row
+  auto guard = [&](int j) { return j == NC - 1 && ragged ? "c" + std::to_string(j) + "_ok" : std::string(); };
+  std::ostringstream decl, load, conv, store;
+  std::map<int, std::string> full;  // external tensors: value in `for e` at chunk j
+  // Row tensors are loaded one row ahead, in their own type.
+  auto ext_full = [&](int u) -> std::string {
+    auto f = full.find(u);
+    if (f != full.end()) return f->second;
+    const Node& n = g.nodes[u];
+    const std::string T = ctype(n.dtype), P = "((const " + T + "*)a.p[" + std::to_string(slot.at(u)) + "])";
+    const std::string id = std::to_string(u);
+    const Shape s2 = n.shape.size() == 2 ? n.shape : n.shape.size() == 1 ? Shape{1, n.shape[0]} : Shape{1, 1};
+    if (n.shape.size() > 2) fail(KORCH_E_UNSUPPORTED, "rowcol: operand rank");
+    const bool byrow = s2[0] > 1, bycol = s2[1] > 1;
+    if (!bycol) {  // one value per row, or one value
+      decl << "  float e" << id << " = ld1(" << P << (byrow ? " + row" : "") << ");\n";
+      if (byrow) {
+        decl << "  float n" << id << ";\n";
+        load << "    n" << id << " = ld1(" << P << " + nrow);\n";
+        store << "    e" << id << " = n" << id << ";\n";
+      }
+      return full[u] = "e" + id;
+    }
+    if (byrow) {
+      const std::string VT = "vec_t<" + std::to_string(VEC) + ", " + T + ">";
+      decl << "  " << VT << " r" << id << "[" << NC << "], n" << id << "[" << NC << "];\n";
+      for (int j = 0; j < NC; ++j) {
+        const std::string at = " + row * " + std::to_string(rc.L) + "LL + c" + std::to_string(j) + ")";
+        const std::string an = " + nrow * " + std::to_string(rc.L) + "LL + c" + std::to_string(j) + ")";
+        decl << "  r" << id << "[" << j << "] = *(const " << VT << "*)(" << P << at << ";\n";
+        load << "    n" << id << "[" << j << "] = *(const " << VT << "*)(" << P << an << ";\n";
+      }
+      store << "#pragma unroll\n    for (int j = 0; j < " << NC << "; ++j) r" << id << "[j] = n" << id << "[j];\n";
+      conv << "    float e" << id << "[" << NC << "][" << VEC << "];\n#pragma unroll\n    for (int j = 0; j < " << NC << "; ++j)\n#pragma unroll\n"
+           << "      for (int e = 0; e < " << VEC << "; ++e) e" << id << "[j][e] = tof(" << (VEC == 1 ? "r" + id + "[j]" : "r" + id + "[j][e]")
+           << ");\n";
+    } else {
+      decl << "  float e" << id << "[" << NC << "][" << VEC << "];\n";
+      for (int j = 0; j < NC; ++j) decl << "  ldv<" << VEC << ">(e" << id << "[" << j << "], " << P << " + c" << j << ");\n";
+    }
+    return full[u] = "e" + id + "[j][e]";
+  };
+  std::vector<int> pending;  // row reductions whose lanes are not yet summed
+  std::ostringstream body;
+  auto flush = [&]() {
+    if (pending.empty()) return;
+    for (int v : pending) {
+      const bool mx = g.nodes[v].op == KORCH_REDUCE_MAX;
+      body << "    s" << v << " = " << (mx ? "group_max<" : "group_sum<") << std::min(G, 64) << ">(s" << v << ");\n";
+    }
+    if (G > 64) {
+      // one barrier per exchange: buffers alternate
+      const int NP = (int)pending.size();
+      body << "    {\n      float* x_ = xch + (par & 1) * " << 8 * NT / 64 << ";\n      par ^= 1;\n";
+      for (int i = 0; i < NP; ++i) body << "      if ((tid & 63) == 0) x_[" << i * (NT / 64) << " + (tid >> 6)] = s" << pending[i] << ";\n";
+      body << "      __syncthreads();\n";
+      for (int i = 0; i < NP; ++i) {
+        const int v = pending[i];
+        const bool mx = g.nodes[v].op == KORCH_REDUCE_MAX;
+        body << "      s" << v << " = x_[" << i * (NT / 64) << " + w0_];\n#pragma unroll\n      for (int w = 1; w < " << WR << "; ++w) s" << v << " = "
+             << (mx ? "k_max(s" + std::to_string(v) + ", " : "s" + std::to_string(v) + " + (") << "x_[" << i * (NT / 64) << " + w0_ + w]);\n";
+      }
+      body << "    }\n";
+    }
+    for (int v : pending)
+      if (g.nodes[v].op == KORCH_REDUCE_MEAN) body << "    s" << v << " = s" << v << " / " << flit((double)rc.L) << ";\n";
+    pending.clear();
+  };
+  auto operand = [&](int u, bool row) -> std::string {
+    if (!ki.in.count(u)) {
+      const Node& n = g.nodes[u];
+      if (!row && n.shape != S && numel(n.shape) != 1) fail(KORCH_E_UNSUPPORTED, "rowcol: a statistic reads a row");
+      return ext_full(u);
+    }
+    if (rc.cls.at(u) == 0) return "v" + std::to_string(u) + "[j][e]";
+    if (std::find(pending.begin(), pending.end(), u) != pending.end()) flush();
+    return "s" + std::to_string(u);
+  };
+  auto each = [&](const std::string& stmt, bool guarded) {
+    for (int j = 0; j < NC; ++j) {
+      const std::string gd = guarded ? guard(j) : "";
+      body << "    " << (gd.empty() ? "" : "if (" + gd + ") ") << "{\n      constexpr int j = " << j << ";\n#pragma unroll\n      for (int e = 0; e < "
+           << VEC << "; ++e) " << stmt << ";\n    }\n";
+    }
+  };
+  for (int v : ki.k.prims) {
+    const Node& n = g.nodes[v];
+    const Kind kd = op_kind(n.op);
+    const std::string V = std::to_string(v);
+    if (std::find(rc.cols.begin(), rc.cols.end(), v) != rc.cols.end()) {
+      const std::string x = operand(n.in[0], true);
+      each("k" + V + "[j][e] += live ? " + x + " : 0.0f", true);
+      continue;
+    }
+    if (kd == Kind::Reduce) {
+      const bool mx = n.op == KORCH_REDUCE_MAX;
+      const std::string x = operand(n.in[0], true);
+      body << "    float s" << V << " = " << (mx ? "-__builtin_huge_valf()" : "0.0f") << ";\n";
+      each("s" + V + " = " + (mx ? "k_max(s" + V + ", " + x + ")" : "s" + V + " + " + x), true);
+      pending.push_back(v);
+      if (pending.size() == 8) flush();
+      continue;
+    }
+    const bool row = rc.cls.at(v) == 0;
+    const std::string x = operand(n.in[0], row);
+    const std::string y = kd == Kind::Unary ? "" : n.attrs.has_scalar ? flit(n.attrs.scalar) : operand(n.in[1], row);
+    const std::string ex = kd == Kind::Unary ? unary_expr(n.op, x) : binary_expr(n.op, x, y);
+    if (row) {
+      body << "    float v" << V << "[" << NC << "][" << VEC << "];\n";
+      each("v" + V + "[j][e] = " + ex, false);
+    } else {
+      body << "    const float s" << V << " = " << ex << ";\n";
+    }
+  }
+  flush();
+  for (int o : ki.k.outs) {
+    if (std::find(rc.cols.begin(), rc.cols.end(), o) != rc.cols.end()) continue;
+    const Node& on = g.nodes[o];
+    const std::string P = "((" + ctype(on.dtype) + "*)a.p[" + std::to_string(ki.out_slot(o)) + "])";
+    if (rc.cls.at(o) == 0) {
+      for (int j = 0; j < NC; ++j) {
+        const std::string gd = guard(j);
+        body << "    if (live" << (gd.empty() ? "" : " && " + gd) << ") "
+             << out_store(g, o, P, "row * " + std::to_string(rc.L) + "LL + c" + std::to_string(j), VEC, "v" + std::to_string(o) + "[" + std::to_string(j) + "]")
+             << ";\n";
+      }
+    } else {
+      body << "    if (live && lane == 0) " << out_store(g, o, P, "row", 0, "s" + std::to_string(o)) << ";\n";
+    }
+  }
+  // hand-over of the column sums
+  int64_t GS = 1, NG = 1;
+  int scr = -1, cnt = -1;
+  if (NWG > 1 && NS > 0) {
+    GS = NWG;
+    if (NWG > 32) {
+      GS = 8;
+      while (GS * GS < NWG) ++GS;
+    }
+    NG = (NWG + GS - 1) / GS;
+    ArgRef a;
+    a.kind = ArgRef::Scratch;
+    a.bytes = (size_t)((NWG + (NG > 1 ? NG : 0)) * C) * 4;
+    scr = (int)gk.args.size();
+    gk.args.push_back(a);
+    a.kind = ArgRef::Counter;
+    a.bytes = (size_t)(NG + 1) * 128;
+    cnt = (int)gk.args.size();
+    gk.args.push_back(a);
+  }
+  std::ostringstream s;
+  s << source_header((int)gk.args.size());
+  s << "extern \"C\" __global__ void __launch_bounds__(" << NT << ") " << gk.name << "(KArgs a) {\n";
+  const int64_t LP = (int64_t)G * NC * VEC;  // columns that the lanes of a row cover
+  if (RPB > 1 && NS > 0) s << "  __shared__ float red[" << RPB * LP << "];\n";
+  if (G > 64) s << "  __shared__ float xch[" << 2 * 8 * NT / 64 << "];\n  int par = 0;\n";
+  const bool hand = NWG > 1 && NS > 0;
+  if (hand) s << "  __shared__ int last_;\n";
+  s << "  const int tid = threadIdx.x, lane = tid % " << G << ", sub = tid / " << G << ";\n";
+  if (G > 64) s << "  const int w0_ = sub * " << WR << ";\n";
+  for (int j = 0; j < NC; ++j) {
+    s << "  const i64 cc" << j << " = ((i64)" << j << " * " << G << " + lane) * " << VEC << ";\n";
+    s << "  const bool c" << j << "_ok = cc" << j << " < " << rc.L << "LL;\n";
+    // lanes past the row read its first elements (their values are not used)
+    s << "  const i64 c" << j << " = c" << j << "_ok ? cc" << j << " : 0;\n";
+  }
+  s << "  i64 blk = blockIdx.x;\n";
+  s << "  const i64 row0 = blk * " << RPB << " + sub;\n  i64 row = row0 < " << rc.R << "LL ? row0 : " << rc.R - 1 << "LL;\n";
+  s << decl.str();
+  for (int v : rc.cols) s << "  float k" << v << "[" << NC << "][" << VEC << "] = {};\n";
+  s << "#pragma unroll 1\n  for (; blk < " << blocks << "LL; blk += " << NWG << ") {\n";
+  s << "    const bool live = blk * " << RPB << " + sub < " << rc.R << "LL;\n";
+  s << "    const i64 nr_ = (blk + " << NWG << ") * " << RPB << " + sub, nrow = nr_ < " << rc.R << "LL ? nr_ : " << rc.R - 1 << "LL;\n";
+  s << load.str() << conv.str() << body.str() << store.str() << "    row = nrow;\n  }\n";
+  auto final_value = [&](int v, const std::string& x) {
+    return g.nodes[v].op == KORCH_REDUCE_MEAN ? "(" + x + ") / " + flit((double)rc.R) : x;
+  };
+  auto out_ptr = [&](int v) { return "((" + ctype(g.nodes[v].dtype) + "*)a.p[" + std::to_string(ki.out_slot(v)) + "])"; };
+  // the workgroup's rows: groups of lanes with the same columns, in order
+  if (hand) s << "  float* part = (float*)a.p[" << scr << "] + (i64)blockIdx.x * " << C << "LL;\n";
+  for (size_t i = 0; i < rc.cols.size(); ++i) {
+    const int v = rc.cols[i];
+    const std::string V = std::to_string(v);
+    auto put = [&](const std::string& col, const std::string& x) {
+      if (NWG > 1) return "coherent_store(&part[" + std::to_string(i * rc.L) + "LL + " + col + "], " + x + ")";
+      return "st1(" + out_ptr(v) + " + " + col + ", " + final_value(v, x) + ")";
+    };
+    if (RPB > 1) {
+      if (i) s << "  __syncthreads();\n";
+      for (int j = 0; j < NC; ++j)
+        s << "#pragma unroll\n  for (int e = 0; e < " << VEC << "; ++e) red[sub * " << LP << " + " << j * G * VEC << " + lane * " << VEC
+          << " + e] = k" << V << "[" << j << "][e];\n";
+      s << "  __syncthreads();\n";
+      s << "  for (int c = tid; c < " << rc.L << "; c += " << NT << ") {\n    float x_ = red[c];\n#pragma unroll\n    for (int q = 1; q < " << RPB
+        << "; ++q) x_ += red[q * " << LP << " + c];\n    " << put("c", "x_") << ";\n  }\n";
+    } else {
+      for (int j = 0; j < NC; ++j)
+        s << "  if (c" << j << "_ok)\n#pragma unroll\n    for (int e = 0; e < " << VEC << "; ++e) " << put("c" + std::to_string(j) + " + e", "k" + V + "[" + std::to_string(j) + "][e]")
+          << ";\n";
+    }
+  }
+  if (hand) {
+    s << "  __builtin_amdgcn_s_waitcnt(0);  // this wave's partial stores are performed\n  __syncthreads();\n";
+    s << "  int* cnt = (int*)a.p[" << cnt << "];\n";
+    const std::string base = "((float*)a.p[" + std::to_string(scr) + "])";
+    auto arrive = [&](const std::string& c, const std::string& n) {
+      s << "  if (tid == 0) {\n    int* c_ = cnt + (" << c << ") * 32;\n";
+      s << "    const int n_ = " << n << ";\n";
+      s << "    last_ = __hip_atomic_fetch_add(c_, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == n_ - 1;\n";
+      s << "    if (last_) __hip_atomic_store(c_, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);\n  }\n  __syncthreads();\n  if (!last_) return;\n";
+    };
+    // sums of partial rows [z0, z1) of `from`, four columns of a thread at a time
+    const int CV = C % 4 == 0 && rc.L % 4 == 0 ? 4 : 1;
+    auto add_up = [&](const std::string& from, const std::string& count, const std::function<void(const std::string&, const std::string&)>& sink) {
+      s << "  {\n    float* f_ = " << from << ";\n    const int m_ = " << count << ";\n";
+      s << "    for (i64 c = (i64)tid * " << CV << "; c < " << C << "LL; c += " << (int64_t)NT * CV << ") {\n";
+      if (CV == 4) {
+        s << "      const __amdgpu_buffer_rsrc_t r_ = __builtin_amdgcn_make_buffer_rsrc(f_, 0, 0x7fffffff, 0x00020000);\n";
+        s << "      f32x4 x_ = {};\n#pragma unroll 8\n      for (int z = 0; z < m_; ++z) {\n        const float4 q_ = coherent_load4(r_, (unsigned)(((i64)z * " << C
+          << "LL + c) * 4));\n        x_ += f32x4{q_.x, q_.y, q_.z, q_.w};\n      }\n";
+        s << "#pragma unroll\n      for (int e = 0; e < 4; ++e) {\n        const i64 ce = c + e;\n        const float y_ = x_[e];\n";
+      } else {
+        s << "      float x_ = 0.0f;\n#pragma unroll 8\n      for (int z = 0; z < m_; ++z) x_ += coherent_load(&f_[(i64)z * " << C << "LL + c]);\n";
+        s << "      {\n        const i64 ce = c;\n        const float y_ = x_;\n";
+      }
+      sink("ce", "y_");
+      s << "      }\n    }\n  }\n";
+    };
+    auto outputs = [&](const std::string& c, const std::string& y) {
+      for (size_t i = 0; i < rc.cols.size(); ++i)
+        s << "        if (" << c << " >= " << i * rc.L << "LL && " << c << " < " << (i + 1) * rc.L << "LL) st1(" << out_ptr(rc.cols[i]) << " + (" << c << " - "
+          << i * rc.L << "LL), " << final_value(rc.cols[i], y) << ");\n";
+    };
+    if (NG > 1) {
+      s << "  const int grp = blockIdx.x / " << GS << ";\n  const int gsz = " << NWG << " - grp * " << GS << " < " << GS << " ? " << NWG << " - grp * " << GS << " : " << GS
+        << ";\n";
+      arrive("1 + grp", "gsz");
+      const std::string to = "(" + base + " + " + std::to_string(NWG * C) + "LL)";
+      add_up(base + " + (i64)grp * " + std::to_string(GS * C) + "LL", "gsz", [&](const std::string& c, const std::string& y) {
+        s << "        coherent_store(&" << to << "[(i64)grp * " << C << "LL + " << c << "], " << y << ");\n";
+      });
+      s << "  __builtin_amdgcn_s_waitcnt(0);\n  __syncthreads();\n";
+      arrive("0", std::to_string(NG));
+      add_up(to, std::to_string(NG), outputs);
+    } else {
+      arrive("0", std::to_string(NWG));
+      add_up(base, std::to_string(NWG), outputs);
+    }
+  }
+  s << "}\n";
+  gk.source = s.str();
+  gk.grid[0] = (int)NWG;
+  gk.block[0] = NT;
+  gk.wg_split = false;
+  ki.fill_cost(gk);
+  return gk;
+}
+
+// ---------------------------------------------------------------------------
+// A sum by bins on its own (a plan that stores the summed tensor): a workgroup
+// per result element adds the matching values in a fixed order.
+// ---------------------------------------------------------------------------
+
+bool match_binsum(const KInfo& ki, std::string* why) {
+  int b = -1;
+  for (int v : ki.k.prims) {
+    const Kind kd = op_kind(ki.g.nodes[v].op);
+    if (kd == Kind::BinSum) {
+      if (b >= 0) return *why = "binsum: more than one sum by bins", false;
+      b = v;
+    } else if (kd == Kind::Reduce || kd == Kind::Linear) {
+      return *why = "binsum: a reduction or a product", false;
+    }
+  }
+  if (b < 0 || ki.k.outs.size() != 1 || ki.k.outs[0] != b) return *why = "binsum: the only output must be the sum by bins", false;
+  for (int v : ki.k.prims)
+    if (v != b && !ki.ancestor(v, b)) return *why = "binsum: a node that the sum does not read", false;
+  return true;
+}
+
+GenKernel gen_binsum(const KInfo& ki, int index) {
+  const Graph& g = ki.g;
+  GenKernel gk;
+  gk.family = KORCH_FAM_BINSUM;
+  gk.name = kernel_name(index, "binsum");
+  std::map<int, int> slot;
+  ki.assign_args(gk, slot);
+  const int o = ki.k.outs[0];
+  const Node& n = g.nodes[o];
+  const Shape& X = g.nodes[n.in[0]].shape;
+  const int R = (int)X.size(), tr = (int)n.shape.size();
+  const int64_t T = n.shape.back();
+  Emitter em(g);
+  em.inset = ki.in;
+  em.argslot = slot;
+  em.vec = 1;
+  em.force_gather = true;
+  std::vector<Ix> it(R);
+  for (int d = 0; d < R; ++d) it[d] = Ix::var("i" + std::to_string(d));
+  const std::string x = em.value(n.in[0], it);
+  const std::string k = em.value(n.in[1], broadcast_index(g.nodes[n.in[1]].shape, X, it));
+  int64_t inner = 1;
+  std::ostringstream kept, summed;
+  for (int d = R - 1; d >= 0; --d) {
+    const int j = d - (R - (tr - 1));
+    const bool keep = j >= 0 && n.shape[j] != 1;
+    std::ostringstream& to = keep ? kept : summed;
+    to << (keep ? "  " : "    ") << "const i64 i" << d << " = " << (keep ? "w_" : "q_") << " % " << X[d] << "LL; " << (keep ? "w_" : "q_") << " /= " << X[d]
+       << "LL;\n";
+    if (!keep) inner *= X[d];
+  }
+  std::ostringstream s;
+  s << source_header((int)gk.args.size());
+  s << "extern \"C\" __global__ void __launch_bounds__(256) " << gk.name << "(KArgs a) {\n  __shared__ float red[4];\n";
+  s << "  const float bin = (float)(blockIdx.x % " << T << ");\n  i64 w_ = blockIdx.x / " << T << ";\n" << kept.str();
+  s << "  float sum = 0.0f;\n  for (i64 t = threadIdx.x; t < " << inner << "LL; t += 256) {\n    i64 q_ = t;\n" << summed.str() << em.pre.str() << em.body.str();
+  s << "    sum += k_min(k_max(" << k << ", 0.0f), " << flit((double)(T - 1)) << ") == bin ? " << x << " : 0.0f;\n  }\n";
+  s << "  sum = group_sum<64>(sum);\n  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = sum;\n  __syncthreads();\n";
+  s << "  if (threadIdx.x == 0) st1((" << ctype(n.dtype) << "*)a.p[" << ki.out_slot(o) << "] + (i64)blockIdx.x, ((red[0] + red[1]) + red[2]) + red[3]);\n}\n";
+  gk.source = s.str();
+  gk.grid[0] = (int)numel(n.shape);
+  ki.fill_cost(gk);
+  return gk;
+}
+
+}  // namespace korch

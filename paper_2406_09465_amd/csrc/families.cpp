@@ -284,6 +284,14 @@ static bool row_shapes(const KInfo& ki, RowShape& rs, std::map<int, int>& cls, s
   return true;
 }
 
+// Widest element of a row program's tensors.
+static int row_elem_bytes(const KInfo& ki) {
+  int eb = 2;
+  for (int v : ki.k.prims) eb = std::max(eb, dtype_bytes(ki.g.nodes[v].dtype));
+  for (int u : ki.ext) eb = std::max(eb, dtype_bytes(ki.g.nodes[u].dtype));
+  return eb;
+}
+
 bool match_row(const KInfo& ki, std::string* why) {
   if (!ki.linear.empty()) {
     *why = "row: has linear primitives";
@@ -292,6 +300,12 @@ bool match_row(const KInfo& ki, std::string* why) {
   RowShape rs;
   std::map<int, int> cls;
   if (!row_shapes(ki, rs, cls, why)) return false;
+  int G, VEC, NC;
+  choose_row_geometry(rs.L, row_elem_bytes(ki), G, VEC, NC);
+  if (NC * VEC > 64) {
+    *why = "row: row too long for one wavefront's registers";
+    return false;
+  }
   return true;
 }
 
@@ -340,11 +354,8 @@ GenKernel gen_row(const KInfo& ki, int index) {
   gk.name = kernel_name(index, "row");
   std::map<int, int> slot;
   ki.assign_args(gk, slot);
-  int eb = 2;
-  for (int v : ki.k.prims) eb = std::max(eb, dtype_bytes(g.nodes[v].dtype));
-  for (int u : ki.ext) eb = std::max(eb, dtype_bytes(g.nodes[u].dtype));
   int G, VEC, NC;
-  choose_row_geometry(rs.L, eb, G, VEC, NC);
+  choose_row_geometry(rs.L, row_elem_bytes(ki), G, VEC, NC);
   if (NC * VEC > 64) fail(KORCH_E_UNSUPPORTED, "row: row too long for one wavefront's registers");
   int RPB = 256 / G;
   int RD = (int)rs.F.size() - 1;  // number of row dims
@@ -1183,14 +1194,22 @@ static int match_family_canonical(const Graph& g, const KernelDesc& k, std::stri
     KInfo ki(g, k);
     // A constant tensor is evaluated inline by the pointwise emitter and by
     // product prologues; the row programs take only computed operands.
-    bool has_fill = false;
-    for (int v : k.prims)
-      if (g.nodes[v].op == KORCH_FILL) has_fill = true;
+    bool has_fill = false, has_bins = false;
+    for (int v : k.prims) {
+      if (g.nodes[v].op == KORCH_FILL || g.nodes[v].op == KORCH_IOTA) has_fill = true;
+      if (g.nodes[v].op == KORCH_BIN_SUM) has_bins = true;
+    }
+    if (has_bins) {
+      if (!ki.linear.empty() ? match_plane(ki, why) : match_binsum(ki, why))
+        return ki.linear.empty() ? KORCH_FAM_BINSUM : KORCH_FAM_PLANE;
+      return KORCH_FAM_NONE;
+    }
     if (!ki.linear.empty()) {
       if (match_attention(ki, why)) return KORCH_FAM_ATTENTION;
       if (match_conv(ki, why)) return KORCH_FAM_CONV;
       if (match_splitk(ki, why)) return KORCH_FAM_SPLITK;
       if (match_gemm(ki, why)) return KORCH_FAM_GEMM;
+      if (match_plane(ki, why)) return KORCH_FAM_PLANE;
       return KORCH_FAM_NONE;
     }
     if (!ki.reduces.empty()) {
@@ -1200,6 +1219,7 @@ static int match_family_canonical(const Graph& g, const KernelDesc& k, std::stri
       }
       if (match_row(ki, why)) return KORCH_FAM_ROW;
       if (match_colreduce(ki, why)) return KORCH_FAM_COLREDUCE;
+      if (match_rowcol(ki, why)) return KORCH_FAM_ROWCOL;
       return KORCH_FAM_NONE;
     }
     if (match_pointwise(ki, why)) return KORCH_FAM_POINTWISE;
@@ -1234,6 +1254,9 @@ static GenKernel generate_canonical(const Graph& g, const KernelDesc& k, int ind
     case KORCH_FAM_CONV: return gen_gemm(ki, index);
     case KORCH_FAM_SPLITK: return gen_splitk(ki, index);
     case KORCH_FAM_ATTENTION: return gen_attention(ki, index);
+    case KORCH_FAM_PLANE: return gen_plane(ki, index);
+    case KORCH_FAM_ROWCOL: return gen_rowcol(ki, index);
+    case KORCH_FAM_BINSUM: return gen_binsum(ki, index);
   }
   fail(KORCH_E_UNSUPPORTED, "kernel " + std::to_string(index) + ": no family implements it (" + why + ")");
 }

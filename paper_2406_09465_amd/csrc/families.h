@@ -37,6 +37,9 @@ bool match_gemm(const KInfo& ki, std::string* why);
 bool match_conv(const KInfo& ki, std::string* why);
 bool match_splitk(const KInfo& ki, std::string* why);
 bool match_attention(const KInfo& ki, std::string* why);
+bool match_plane(const KInfo& ki, std::string* why);
+bool match_rowcol(const KInfo& ki, std::string* why);
+bool match_binsum(const KInfo& ki, std::string* why);
 
 GenKernel gen_pointwise(const KInfo& ki, int index);
 GenKernel gen_row(const KInfo& ki, int index);
@@ -44,5 +47,8 @@ GenKernel gen_colreduce(const KInfo& ki, int index);
 GenKernel gen_gemm(const KInfo& ki, int index);
 GenKernel gen_splitk(const KInfo& ki, int index);
 GenKernel gen_attention(const KInfo& ki, int index);
+GenKernel gen_plane(const KInfo& ki, int index);
+GenKernel gen_rowcol(const KInfo& ki, int index);
+GenKernel gen_binsum(const KInfo& ki, int index);
 
 }  // namespace korch

@@ -36,17 +36,20 @@ const char* dtype_name(int dtype) {
 Kind op_kind(int op) {
   if (op == KORCH_INPUT) return Kind::Input;
   if (op >= KORCH_NEG && op <= KORCH_IDENTITY) return Kind::Unary;
-  if (op >= KORCH_ADD && op <= KORCH_MIN) return Kind::Binary;
+  if (op >= KORCH_ADD && op <= KORCH_EQ) return Kind::Binary;
+  if (op == KORCH_SELECT) return Kind::Select;
   if (op >= KORCH_REDUCE_SUM && op <= KORCH_REDUCE_MAX) return Kind::Reduce;
   if (op == KORCH_BROADCAST) return Kind::Broadcast;
-  if (op >= KORCH_TRANSPOSE && op <= KORCH_FILL) return Kind::Layout;
+  if (op >= KORCH_TRANSPOSE && op <= KORCH_IOTA) return Kind::Layout;
+  if (op == KORCH_GATHER) return Kind::Gather;
+  if (op == KORCH_BIN_SUM) return Kind::BinSum;
   if (op == KORCH_MATMUL || op == KORCH_CONV2D) return Kind::Linear;
   fail(KORCH_E_ARG, "unknown op code " + std::to_string(op));
 }
 
 bool is_elementwise(int op) {
   Kind k = op_kind(op);
-  return k == Kind::Unary || k == Kind::Binary;
+  return k == Kind::Unary || k == Kind::Binary || k == Kind::Select;
 }
 
 const char* op_name(int op) {
@@ -70,6 +73,12 @@ const char* op_name(int op) {
     case KORCH_DIV: return "div";
     case KORCH_MAX: return "max";
     case KORCH_MIN: return "min";
+    case KORCH_LT: return "lt";
+    case KORCH_LE: return "le";
+    case KORCH_GT: return "gt";
+    case KORCH_GE: return "ge";
+    case KORCH_EQ: return "eq";
+    case KORCH_SELECT: return "select";
     case KORCH_REDUCE_SUM: return "reduce_sum";
     case KORCH_REDUCE_MEAN: return "reduce_mean";
     case KORCH_REDUCE_MAX: return "reduce_max";
@@ -80,6 +89,9 @@ const char* op_name(int op) {
     case KORCH_PAD: return "pad";
     case KORCH_CONCAT: return "concat";
     case KORCH_FILL: return "fill";
+    case KORCH_IOTA: return "iota";
+    case KORCH_GATHER: return "gather";
+    case KORCH_BIN_SUM: return "bin_sum";
     case KORCH_MATMUL: return "matmul";
     case KORCH_CONV2D: return "conv2d";
   }
@@ -147,6 +159,34 @@ int Graph::add_op(int op, const std::vector<int>& in, const korch_attrs* attrs, 
         n.shape = broadcast_shapes(sh(0), sh(1));
       }
       break;
+    case Kind::Select:
+      need(a.has_scalar ? 2 : 3);
+      n.shape = broadcast_shapes(sh(0), sh(1));
+      if (!a.has_scalar) n.shape = broadcast_shapes(n.shape, sh(2));
+      break;
+    case Kind::Gather: {
+      need(2);
+      if (sh(0).empty()) fail(KORCH_E_SHAPE, "gather of a scalar");
+      if (sh(0).back() > (1 << 24)) fail(KORCH_E_SHAPE, "gather table longer than 2^24 (indices are exact in fp32 up to there)");
+      n.shape = broadcast_shapes(Shape(sh(0).begin(), sh(0).end() - 1), sh(1));
+      break;
+    }
+    case Kind::BinSum: {
+      need(2);
+      if (a.rank < 1 || a.rank > KORCH_MAX_RANK) fail(KORCH_E_SHAPE, "bad rank");
+      n.shape.assign(a.shape, a.shape + a.rank);
+      for (auto d : n.shape)
+        if (d <= 0) fail(KORCH_E_SHAPE, "bin_sum dims must be positive");
+      if (n.shape.back() > 4096) fail(KORCH_E_SHAPE, "bin_sum has more than 4096 bins");
+      const Shape x = broadcast_shapes(sh(0), sh(1));
+      if (x != sh(0)) fail(KORCH_E_SHAPE, "bin_sum: the bins' shape does not broadcast to the values'");
+      const Shape lead(n.shape.begin(), n.shape.end() - 1);
+      if (lead.size() > x.size()) fail(KORCH_E_SHAPE, "bin_sum: more result dims than value dims");
+      for (size_t d = 0; d < lead.size(); ++d)
+        if (lead[d] != 1 && lead[d] != x[d + x.size() - lead.size()])
+          fail(KORCH_E_SHAPE, "bin_sum: a result dim is neither 1 nor the values'");
+      break;
+    }
     case Kind::Reduce: {
       need(1);
       int r = (int)sh(0).size();
@@ -171,12 +211,18 @@ int Graph::add_op(int op, const std::vector<int>& in, const korch_attrs* attrs, 
       break;
     }
     case Kind::Layout: {
-      if (op == KORCH_FILL) {
+      if (op == KORCH_FILL || op == KORCH_IOTA) {
         need(0);
         if (a.rank < 0 || a.rank > KORCH_MAX_RANK) fail(KORCH_E_SHAPE, "bad rank");
         n.shape.assign(a.shape, a.shape + a.rank);
         for (auto d : n.shape)
-          if (d <= 0) fail(KORCH_E_SHAPE, "fill dims must be positive");
+          if (d <= 0) fail(KORCH_E_SHAPE, std::string(op_name(op)) + " dims must be positive");
+        if (op == KORCH_IOTA) {
+          int ax = a.axis < 0 ? a.axis + a.rank : a.axis;
+          if (ax < 0 || ax >= a.rank) fail(KORCH_E_SHAPE, "iota axis out of range");
+          if (n.shape[ax] > (1 << 24)) fail(KORCH_E_SHAPE, "iota axis longer than 2^24 (its indices are exact in fp32 up to there)");
+          n.axis = ax;
+        }
         break;
       }
       if (op == KORCH_CONCAT) {

@@ -30,7 +30,7 @@ std::string shape_str(const Shape& s);
 int dtype_bytes(int dtype);
 const char* dtype_name(int dtype);
 
-enum class Kind { Input, Unary, Binary, Reduce, Broadcast, Layout, Linear };
+enum class Kind { Input, Unary, Binary, Select, Reduce, Broadcast, Layout, Gather, BinSum, Linear };
 Kind op_kind(int op);
 const char* op_name(int op);
 bool is_elementwise(int op);

@@ -57,13 +57,13 @@ class _B:
         self.ids = {}
         self.inputs = []
 
-    def inp(self, name, shape):
-        self.ids[name] = self.g.input(self.dtype, shape)
+    def inp(self, name, shape, dtype=None):
+        self.ids[name] = self.g.input(dtype or self.dtype, shape)
         self.inputs.append(name)
         return self.ids[name]
 
-    def op(self, name, op, ins, **attrs):
-        self.ids[name] = self.g.op(op, [self.ids[i] for i in ins], self.dtype, **attrs)
+    def op(self, name, op, ins, dtype=None, **attrs):
+        self.ids[name] = self.g.op(op, [self.ids[i] for i in ins], dtype or self.dtype, **attrs)
         return self.ids[name]
 
 
@@ -258,6 +258,362 @@ def instnorm(hh=224, ww=224, c=32, dtype="f16", eps=1e-5, extra_outputs=()):
     return w
 
 
+def layernorm(m=4096, d=768, dtype="f16", eps=1e-5, extra_outputs=()):
+    """LayerNorm of the rows of X that keeps what its gradient needs: the row
+    means ``mu`` and reciprocal deviations ``r`` (fp32)."""
+    b = _B(dtype)
+    b.inp("X", (m, d))
+    b.inp("gamma", (d,))
+    b.inp("beta", (d,))
+    b.op("mu", "reduce_mean", ["X"], "f32", axis=-1, keepdim=True)
+    b.op("D", "sub", ["X", "mu"], "f32")
+    b.op("D2", "square", ["D"], "f32")
+    b.op("var", "reduce_mean", ["D2"], "f32", axis=-1, keepdim=True)
+    b.op("ve", "add", ["var"], "f32", scalar=eps)
+    b.op("r", "rsqrt", ["ve"], "f32")
+    b.op("Xh", "mul", ["D", "r"], "f32")
+    b.op("Yg", "mul", ["Xh", "gamma"], "f32")
+    b.op("Y", "add", ["Yg", "beta"])
+    w = _finish(b, "layernorm", ["Y", "mu", "r"], dict(m=m, d=d), extra_outputs)
+    w.plans["fused"] = [(["mu", "D", "D2", "var", "ve", "r", "Xh", "Yg", "Y"], ["Y", "mu", "r"])]
+    return w
+
+
+def layernorm_grad(m=4096, d=768, dtype="f16", eps=1e-5, extra_outputs=()):
+    """LayerNorm's gradient from dY and the saved row statistics: dX, and the
+    sums over the rows dgamma = sum dY Xh and dbeta = sum dY.  With
+    g = dY gamma and Xh = (X - mu) r,  dX = r (g - mean(g) - Xh mean(g Xh)).
+    (``eps`` is in the saved r.)"""
+    b = _B(dtype)
+    b.inp("X", (m, d))
+    b.inp("gamma", (d,))
+    b.inp("mu", (m, 1), "f32")
+    b.inp("r", (m, 1), "f32")
+    b.inp("dY", (m, d))
+    b.op("D", "sub", ["X", "mu"], "f32")
+    b.op("Xh", "mul", ["D", "r"], "f32")
+    b.op("dYXh", "mul", ["dY", "Xh"], "f32")
+    b.op("dgamma", "reduce_sum", ["dYXh"], axis=0, keepdim=False)
+    b.op("dbeta", "reduce_sum", ["dY"], axis=0, keepdim=False)
+    b.op("g", "mul", ["dY", "gamma"], "f32")
+    b.op("gXh", "mul", ["dYXh", "gamma"], "f32")
+    b.op("c1", "reduce_mean", ["g"], "f32", axis=-1, keepdim=True)
+    b.op("c2", "reduce_mean", ["gXh"], "f32", axis=-1, keepdim=True)
+    b.op("G1", "sub", ["g", "c1"], "f32")
+    b.op("Xc", "mul", ["Xh", "c2"], "f32")
+    b.op("G2", "sub", ["G1", "Xc"], "f32")
+    b.op("dX", "mul", ["G2", "r"])
+    w = _finish(b, "layernorm_grad", ["dX", "dgamma", "dbeta"], dict(m=m, d=d), extra_outputs)
+    w.plans["fused"] = [(["D", "Xh", "dYXh", "dgamma", "dbeta", "g", "gXh", "c1", "c2", "G1", "Xc", "G2", "dX"],
+                         ["dX", "dgamma", "dbeta"])]
+    # the row program and the two column sums apart
+    w.plans["layered"] = [(["D", "Xh", "dYXh", "g", "gXh", "c1", "c2", "G1", "Xc", "G2", "dX"], ["dX"]),
+                          (["D", "Xh", "dYXh", "dgamma"], ["dgamma"]), (["dbeta"], ["dbeta"])]
+    return w
+
+
+LOW = -1e30   # the score of a masked pair in a row's maximum
+TINY = 1e-30  # the divisor of a row whose mask leaves nothing: its result is 0
+
+
+class _Attention:
+    """The score plane that attention and its gradient share: operands, scores,
+    caps, biases and the mask, as primitives of a builder.
+
+    Query heads that share a key head are rows of one product: Q [batch, heads,
+    n, d] is read as [batch, kv_heads, group * n, d] (a view), so the sums over
+    a group in the gradients are the products' own.  With a bias table, which
+    differs from head to head, a group is a batch axis instead."""
+
+    def __init__(self, b, batch, heads, kv_heads, n, m, d, cap, slopes, causal, prefix, documents, lengths, radius, buckets):
+        kv_heads = heads if kv_heads is None else kv_heads
+        m = n if m is None else m
+        if min(batch, heads, kv_heads, n, m, d) < 1 or heads % kv_heads:
+            raise ValueError("heads must be a positive multiple of kv_heads, and every size positive")
+        if n > m:
+            raise ValueError("the queries are the last n of m positions: n must not exceed m")
+        if prefix and not causal:
+            raise ValueError("a prefix extends a causal mask: causal must be set")
+        if bool(buckets) != bool(radius) or buckets < 0 or radius < 0:
+            raise ValueError("radius and buckets go together")
+        if cap < 0:
+            raise ValueError("cap must not be negative (0: none)")
+        self.b, self.sizes = b, dict(batch=batch, heads=heads, kv_heads=kv_heads, n=n, m=m, d=d, cap=cap, slopes=slopes,
+                                     causal=causal, prefix=prefix, documents=documents, lengths=lengths, radius=radius,
+                                     buckets=buckets)
+        group = heads // kv_heads
+        self.batch, self.heads, self.kv, self.group, self.n, self.m, self.d = batch, heads, kv_heads, group, n, m, d
+        self.cap, self.scale = cap, 1.0 / math.sqrt(d)
+        self.apart = bool(buckets) and group > 1  # a group as a batch axis
+        self.fold = group > 1 and not self.apart
+        self.rows = group * n if self.fold else n
+        # leading dims of query-side and key-side tensors
+        self.qlead = (batch, kv_heads, group) if self.apart else (batch, kv_heads)
+        self.klead = (batch, kv_heads, 1) if self.apart else (batch, kv_heads)
+        self.prims = []
+        b.inp("Q", (batch, heads, n, d))
+        b.inp("K", (batch, kv_heads, m, d))
+        b.inp("V", (batch, kv_heads, m, d))
+
+    def op(self, name, op, ins, dtype="f32", **attrs):
+        """A primitive of the plane, part of every kernel that evaluates it."""
+        self.b.op(name, op, ins, dtype, **attrs)
+        self.prims.append(name)
+        return name
+
+    def view(self, name, src, shape, dtype=None):
+        """A view of a stored tensor (no kernel computes it)."""
+        if self.b.g.node_info(self.b.ids[src])[2] == tuple(shape):
+            return src
+        self.b.op(name, "reshape", [src], dtype, shape=shape)
+        return name
+
+    def per_row(self, name, src, lead, dtype="f32"):
+        """[.., n] -> [.., rows, 1]: one value per row of the plane, repeated for the heads of a group."""
+        b = self.b
+        if self.fold:
+            self.op(name + "_g", "broadcast", [src], dtype, shape=lead + (self.group, self.n))
+            return self.op(name, "reshape", [name + "_g"], dtype, shape=lead + (self.rows, 1))
+        return self.op(name, "reshape", [src], dtype, shape=lead + (self.n, 1))
+
+    def vectors(self, slopes, causal, prefix, documents, lengths, radius, buckets):
+        """The inputs beside Q, K and V."""
+        b, ones = self.b, (1,) * (len(self.qlead) - 1)
+        if slopes:
+            b.inp("slopes", (self.heads,), "f32")
+        if lengths:
+            b.inp("lengths", (self.batch,), "f32")
+        if prefix:
+            b.inp("prefix", (self.batch,), "f32")
+        if documents:
+            b.inp("documents", (self.batch, self.m), "f32")
+        if buckets:
+            b.inp("bucket", (2 * radius + 1,), "f32")
+            b.inp("table", (self.heads, buckets))
+        # positions of keys and queries (the last n positions in use)
+        self.op("key", "iota", [], shape=(1, self.m), axis=1)
+        self.op("row", "iota", [], shape=(self.group, self.n) if self.fold else (1, self.n), axis=1)
+        self.op("row_i", "reshape", ["row"], shape=(self.rows, 1))
+        if lengths:
+            end = self.view("end", "lengths", (self.batch,) + ones + (1, 1), "f32")
+            self.op("first", "sub", [end], scalar=float(self.n))
+            self.op("pos", "add", ["row_i", "first"])
+            # rows of K and V past a sequence's length are read as zeros
+            self.op("key_r", "iota", [], shape=(self.m, 1), axis=0)
+            self.op("used", "lt", ["key_r", end])
+        elif self.m != self.n:
+            self.op("pos", "add", ["row_i"], scalar=float(self.m - self.n))
+        else:
+            self.b.ids["pos"] = self.b.ids["row_i"]
+        if slopes or buckets:
+            self.op("rel", "sub", ["key", "pos"])
+        mask = None
+
+        def both(x):
+            nonlocal mask
+            mask = x if mask is None else self.op(f"mask{len(self.prims)}", "mul", [mask, x])
+
+        if causal:
+            self.op("seen", "le", ["key", "pos"])
+            if prefix:
+                pre = self.view("pre", "prefix", (self.batch,) + ones + (1, 1), "f32")
+                self.op("inpre", "lt", ["key", pre])
+                self.op("seenp", "max", ["seen", "inpre"])
+            both("seenp" if prefix else "seen")
+        if documents:
+            doc = self.view("doc", "documents", (self.batch,) + ones + (1, self.m), "f32")
+            tab = self.view("doc_t", "documents", (self.batch,) + ones + (1, 1, self.m), "f32")
+            self.op("docq", "gather", [tab, "pos"])
+            both(self.op("samedoc", "eq", ["docq", doc]))
+        if lengths:
+            both(self.op("inuse", "lt", ["key", "end" if "end" in self.b.ids else "lengths"]))
+        self.mask = mask
+        self.lengths, self.slopes, self.buckets = lengths, slopes, buckets
+
+    def operands(self):
+        b = self.b
+        self.q = self.view("Q4", "Q", self.qlead + (self.rows, self.d))
+        self.k = self.view("K4", "K", self.klead + (self.m, self.d))
+        self.v = self.view("V4", "V", self.klead + (self.m, self.d))
+        if self.lengths:
+            self.k = self.op("Km", "select", ["used", self.k], b.dtype, scalar=0.0)
+            self.v = self.op("Vm", "select", ["used", self.v], b.dtype, scalar=0.0)
+
+    def swap(self):
+        r = len(self.qlead) + 2
+        return tuple(range(r - 2)) + (r - 1, r - 2)
+
+    def scores(self):
+        """S [.., rows, m] (fp32); with a cap, ``t`` = tanh(scale Q K^T / cap)."""
+        b = self.b
+        self.op("KT", "transpose", [self.k], b.dtype, perm=self.swap())
+        self.op("S0", "matmul", [self.q, "KT"])
+        if self.cap:
+            self.op("Sx", "mul", ["S0"], scalar=self.scale / self.cap)
+            self.op("t", "tanh", ["Sx"])
+            s = self.op("Sc", "mul", ["t"], scalar=self.cap)
+        else:
+            s = self.op("Sc", "mul", ["S0"], scalar=self.scale)
+        if self.slopes:
+            if self.fold:
+                lead = self.view("slope_h", "slopes", (self.kv, self.group, 1), "f32")
+                self.op("slope_g", "broadcast", [lead], shape=(self.kv, self.group, self.n))
+                self.op("slope", "reshape", ["slope_g"], shape=(self.kv, self.rows, 1))
+            else:
+                self.view("slope", "slopes", self.qlead[1:] + (1, 1), "f32")
+            self.op("dist", "abs", ["rel"])
+            self.op("bias_d", "mul", ["dist", "slope"])
+            s = self.op("Sd", "sub", [s, "bias_d"])
+        if self.buckets:
+            self.op("at", "add", ["rel"], scalar=float(self.sizes["radius"]))
+            self.op("which", "gather", ["bucket", "at"])
+            tab = self.view("table_h", "table", self.qlead[1:] + (1, 1, self.buckets))
+            self.op("bias_b", "gather", [tab, "which"])
+            s = self.op("Sb", "add", [s, "bias_b"])
+        self.s = s
+
+    def masked(self, name, x, value=0.0):
+        return x if self.mask is None else self.op(name, "select", [self.mask, x], scalar=value)
+
+    def out(self, name, src, shape, dtype=None):
+        """A result in the caller's shape (the last primitive of its kernel)."""
+        self.b.op(name, "reshape", [src], dtype, shape=shape)
+        return name
+
+
+def mha(batch=1, heads=8, kv_heads=None, n=1024, m=None, d=64, dtype="bf16", cap=0.0, slopes=False, causal=False, prefix=False,
+        documents=False, lengths=False, radius=0, buckets=0, extra_outputs=()):
+    """Attention of any length in one kernel: O = softmax(S) V and the row's
+    log-sum-exp L (fp32, 0 for a row whose mask leaves nothing; its O is 0).
+
+      S = scale Q K^T, capped by cap tanh(S / cap) if ``cap``,
+        - slopes[h] |j - i|           if ``slopes``   (input ``slopes`` [heads], fp32)
+        + table[h, bucket[j - i]]     if ``buckets``  (inputs ``table`` [heads, buckets] and ``bucket``
+                                                       [2 radius + 1], fp32 whole numbers: the bucket of
+                                                       distances -radius .. radius; farther ones take the ends')
+
+    Q is [batch, heads, n, d], K and V are [batch, kv_heads, m, d]; query head h
+    reads key head h // (heads / kv_heads).  The queries are the last n of m
+    positions (n = 1: the next token over a cache of m - 1).  Masks, all of
+    which must hold: ``causal`` (j <= i; with ``prefix`` [batch] also j <
+    prefix), ``documents`` [batch, m] (equal document numbers), ``lengths``
+    [batch] (the first lengths[b] >= n of the m positions are in use, the
+    queries are the last n of those; K and V past them are never used and may hold
+    anything).  Numbers are fp32 whole numbers below 2^24."""
+    b = _B(dtype)
+    a = _Attention(b, batch, heads, kv_heads, n, m, d, cap, slopes, causal, prefix, documents, lengths, radius, buckets)
+    a.vectors(slopes, causal, prefix, documents, lengths, radius, buckets)
+    a.operands()
+    a.scores()
+    top = a.masked("Sm", a.s, LOW)
+    a.op("mx", "reduce_max", [top], axis=-1, keepdim=True)
+    a.op("Z", "sub", [a.s, "mx"])
+    a.op("Ex", "exp", ["Z"])
+    e = a.masked("E", "Ex")
+    a.op("l", "reduce_sum", [e], axis=-1, keepdim=True)
+    # the exponentials are rounded to the operands' type for the product (at
+    # most 1, so a half step of that type each); their sum is fp32
+    ec = e if dtype == "f32" else a.op("Ec", "identity", [e], dtype)
+    a.op("Ov", "matmul", [ec, a.v])
+    a.op("lt", "max", ["l"], scalar=TINY)
+    a.op("On", "div", ["Ov", "lt"], dtype)
+    a.op("lg", "log", ["lt"])
+    a.op("ml", "add", ["mx", "lg"])
+    a.op("some", "gt", ["l"], scalar=0.0)
+    a.op("Ln", "select", ["some", "ml"], scalar=0.0)
+    a.out("O", "On", (batch, heads, n, d))
+    a.out("L", "Ln", (batch, heads, n, 1), "f32")
+    w = _finish(b, "mha", ["O", "L"], a.sizes, extra_outputs)
+    w.plans["fused"] = [(a.prims + ["O", "L"], ["O", "L"])]
+    return w
+
+
+def mha_grad(batch=1, heads=8, kv_heads=None, n=1024, m=None, d=64, dtype="bf16", cap=0.0, slopes=False, causal=False, prefix=False,
+             documents=False, lengths=False, radius=0, buckets=0, extra_outputs=()):
+    """The gradient of ``mha`` (same arguments) from dO and the forward pass's O
+    and L: dQ, dK, dV, and with ``buckets`` the table's gradient dT.
+
+      P = exp(S - L), dP = dO V^T, delta = rowsum(dO O), dS = P (dP - delta),
+      dX = dS (1 - t^2) scale,  dQ = dX K, dK = dX^T Q, dV = P^T dO,
+      dT[h, k] = sum of dS over the batch and the pairs of bucket k.
+
+    The scores are evaluated again by the kernel that owns the queries (dQ, dT)
+    and by the one that owns the keys (dK, dV): every sum is taken by one
+    workgroup in a fixed order."""
+    b = _B(dtype)
+    a = _Attention(b, batch, heads, kv_heads, n, m, d, cap, slopes, causal, prefix, documents, lengths, radius, buckets)
+    b.inp("dO", (batch, heads, n, d))
+    b.inp("O", (batch, heads, n, d))
+    b.inp("L", (batch, heads, n, 1), "f32")
+    a.vectors(slopes, causal, prefix, documents, lengths, radius, buckets)
+    b.op("dOO", "mul", ["dO", "O"], "f32")
+    b.op("delta", "reduce_sum", ["dOO"], "f32", axis=-1, keepdim=True)
+    a.operands()
+    a.scores()
+    lse = a.view("L4", "L", a.qlead + (a.rows, 1), "f32")
+    delta = a.view("delta4", "delta", a.qlead + (a.rows, 1), "f32")
+    do = a.view("dO4", "dO", a.qlead + (a.rows, d))
+    a.op("Z", "sub", [a.s, lse])
+    a.op("Ex", "exp", ["Z"])
+    p = a.masked("P", "Ex")
+    rest = list(a.prims)
+    a.prims.clear()
+    a.op("VT", "transpose", [a.v], dtype, perm=a.swap())
+    a.op("dP", "matmul", [do, "VT"])
+    a.op("dD", "sub", ["dP", delta])
+    a.op("dS", "mul", [p, "dD"])
+    ds = a.masked("dSm", "dS")
+    dx = ds
+    if cap:
+        a.op("t2", "square", ["t"])
+        a.op("nt2", "neg", ["t2"])
+        a.op("dt", "add", ["nt2"], scalar=1.0)
+        a.op("dU", "mul", [ds, "dt"])
+        dx = a.masked("dX", "dU")
+    # P and dX are rounded to the operands' type for the products
+    xc = dx if dtype == "f32" else a.op("Xc", "identity", [dx], dtype)
+    plane = list(a.prims)
+    b.op("dQ0", "matmul", [xc, a.k], "f32")
+    b.op("dQ1", "mul", ["dQ0"], scalar=a.scale)
+    a.out("dQ", "dQ1", (batch, heads, n, d))
+    rows, rows_out = ["dQ0", "dQ1", "dQ"], ["dQ"]
+    if buckets:
+        b.op("dT0", "bin_sum", [ds, "which"], shape=a.qlead[1:] + (1, 1, buckets))
+        a.out("dT", "dT0", (heads, buckets))
+        rows, rows_out = rows + ["dT0", "dT"], rows_out + ["dT"]
+    b.op("XT", "transpose", [xc], perm=a.swap())
+    b.op("dK0", "matmul", ["XT", a.q], "f32")
+    pc = p
+    cols_p = []
+    if dtype != "f32":
+        b.op("Pc", "identity", [p])
+        pc, cols_p = "Pc", ["Pc"]
+    b.op("PT", "transpose", [pc], perm=a.swap())
+    cols_p += ["PT"]
+    b.op("dV0", "matmul", ["PT", do], "f32")
+    after = []
+    if a.apart:
+        for x in ("K", "V"):
+            b.op(f"d{x}g", "reduce_sum", [f"d{x}0"], "f32", axis=2, keepdim=False)
+            b.op(f"d{x}", "mul" if x == "K" else "identity", [f"d{x}g"], **(dict(scalar=a.scale) if x == "K" else {}))
+            after.append(([f"d{x}g", f"d{x}"], [f"d{x}"]))
+        ko, vo = ["dK0"], ["dV0"]
+    else:
+        b.op("dK1", "mul", ["dK0"], scalar=a.scale)
+        b.op("dV1", "identity", ["dV0"])
+        a.out("dK", "dK1", (batch, a.kv, a.m, d))
+        a.out("dV", "dV1", (batch, a.kv, a.m, d))
+        ko, vo = ["dK0", "dK1", "dK"], ["dV0", "dV1", "dV"]
+    outs = ["dQ", "dK", "dV"] + (["dT"] if buckets else [])
+    w = _finish(b, "mha_grad", outs, a.sizes, extra_outputs)
+    kout, vout = ko[-1:], vo[-1:]
+    dk = rest + plane + ["XT"] + ko
+    dv = rest + cols_p + vo
+    cols = [(sorted(set(dk + dv)), kout + vout)] if d <= 128 else [(dk, kout), (dv, vout)]
+    w.plans["fused"] = [(["dOO", "delta"], ["delta"]), (rest + plane + rows, rows_out)] + cols + after
+    return w
+
+
 def layout_probe(op, dtype, shapes, **attrs):
     """A graph of one layout primitive (transpose, slice, pad or concat) on
     graph inputs of the given shapes; a concat whose ``fill`` attribute is set
@@ -282,6 +638,8 @@ def layout_probe(op, dtype, shapes, **attrs):
 
 
 BUILDERS = {"attention": attention, "mlp": mlp, "sra": sra, "conv": conv, "linattn": linattn, "instnorm": instnorm}
+# Operators of a transformer layer's training and serving, built by name like the workloads.
+OPERATORS = {"layernorm": layernorm, "layernorm_grad": layernorm_grad, "mha": mha, "mha_grad": mha_grad}
 
 
 def rewritten(w: Workload, rules=None):
@@ -347,4 +705,4 @@ def plan_from_record(w: Workload, rec):
 
 
 def build(workload: str, **sizes) -> Workload:
-    return BUILDERS[workload](**sizes)
+    return (BUILDERS.get(workload) or OPERATORS[workload])(**sizes)

@@ -52,7 +52,8 @@ class PlanRunner:
 
     def set_inputs(self, storage: dict):
         """storage: {input name: storage array} (synthetic.make_inputs output)."""
-        self.ins = [to_device(storage[n], self.w.dtype, self.device) for n in self.w.input_names]
+        g = self.w.graph
+        self.ins = [to_device(storage[n], g.node_info(i)[1], self.device) for n, i in zip(self.w.input_names, g.inputs())]
 
     def _ptrs(self):
         """ctypes pointer arrays of the current input and output tensors (rebuilt
