@@ -83,9 +83,9 @@ bool analyze_rowcol(const KInfo& ki, RowCol& rc, std::string* why) {
 bool rowcol_geometry(int64_t L, int eb, int& G, int& VEC, int& NC) {
   VEC = 16 / eb;
   while (L % VEC) VEC /= 2;
-  // up to 16 elements of every row tensor per lane: two row tensors, their
-  // sums and the weights stay well below the registers of eight waves per SIMD
   const int64_t n = L / VEC;
+  // up to 16 elements of every row tensor per lane: two row tensors, their
+  // sums and the weights then leave two workgroups of eight waves per compute unit
   G = 1;
   while (G < 1024 && (n + G - 1) / G * VEC > 16) G *= 2;
   NC = (int)((n + G - 1) / G);
@@ -123,15 +123,22 @@ GenKernel gen_rowcol(const KInfo& ki, int index) {
     if (g.nodes[o].shape == F) eb = std::max(eb, dtype_bytes(g.nodes[o].dtype));
   int G, VEC, NC;
   if (!rowcol_geometry(rc.L, eb, G, VEC, NC)) fail(KORCH_E_UNSUPPORTED, "rowcol: rows too long");
-  const int NT = std::max(256, G), RPB = NT / G, WR = G > 64 ? G / 64 : 1;
+  // Eight waves per workgroup and a workgroup per compute unit (16384 x 4096
+  // bf16, three row tensors: 84 us, four waves and 512 workgroups 96; sixteen
+  // waves 97).  Rows past 4096 take sixteen waves, whose hand-over of the sums
+  // is the wider one (500 x 8192 fp16: 32 us, with eight 55).
+  const int NT = std::max(rc.L > 4096 ? 1024 : 512, G);
+  const int RPB = NT / G, WR = G > 64 ? G / 64 : 1;
   const int64_t blocks = (rc.R + RPB - 1) / RPB;
-  const int64_t NWG = std::min<int64_t>(blocks, NT == 256 ? 512 : 256);
-  const int64_t NS = (int64_t)rc.cols.size(), C = NS * rc.L;
+  const int64_t NWG = std::min<int64_t>(blocks, 256);
+  const int64_t NS = (int64_t)rc.cols.size(), LQ = (rc.L + 3) / 4 * 4, C = NS * LQ;  // partial sums, rows of whole 16-byte vectors
   const bool ragged = (rc.L / VEC) % G != 0;  // the last vector of some lanes is past the row
   auto guard = [&](int j) { return j == NC - 1 && ragged ? "c" + std::to_string(j) + "_ok" : std::string(); };
-  std::ostringstream decl, load, conv, store;
+  // Row tensors are loaded one row ahead in their own type, into the registers
+  // that the conversion to fp32 has just freed (two or three rows ahead gained
+  // nothing: 84.9 and 87.2 us against 83.8).
+  std::ostringstream decl, raw, load, conv;
   std::map<int, std::string> full;  // external tensors: value in `for e` at chunk j
-  // Row tensors are loaded one row ahead, in their own type.
   auto ext_full = [&](int u) -> std::string {
     auto f = full.find(u);
     if (f != full.end()) return f->second;
@@ -142,26 +149,22 @@ GenKernel gen_rowcol(const KInfo& ki, int index) {
     if (n.shape.size() > 2) fail(KORCH_E_UNSUPPORTED, "rowcol: operand rank");
     const bool byrow = s2[0] > 1, bycol = s2[1] > 1;
     if (!bycol) {  // one value per row, or one value
-      decl << "  float e" << id << " = ld1(" << P << (byrow ? " + row" : "") << ");\n";
       if (byrow) {
-        decl << "  float n" << id << ";\n";
-        load << "    n" << id << " = ld1(" << P << " + nrow);\n";
-        store << "    e" << id << " = n" << id << ";\n";
+        raw << "    " << T << " r" << id << ";\n";
+        load << "    q.r" << id << " = " << P << "[row];\n";
+        conv << "    const float e" << id << " = tof(q_.r" << id << ");\n";
+      } else {
+        decl << "  const float e" << id << " = ld1(" << P << ");\n";
       }
       return full[u] = "e" + id;
     }
     if (byrow) {
       const std::string VT = "vec_t<" + std::to_string(VEC) + ", " + T + ">";
-      decl << "  " << VT << " r" << id << "[" << NC << "], n" << id << "[" << NC << "];\n";
-      for (int j = 0; j < NC; ++j) {
-        const std::string at = " + row * " + std::to_string(rc.L) + "LL + c" + std::to_string(j) + ")";
-        const std::string an = " + nrow * " + std::to_string(rc.L) + "LL + c" + std::to_string(j) + ")";
-        decl << "  r" << id << "[" << j << "] = *(const " << VT << "*)(" << P << at << ";\n";
-        load << "    n" << id << "[" << j << "] = *(const " << VT << "*)(" << P << an << ";\n";
-      }
-      store << "#pragma unroll\n    for (int j = 0; j < " << NC << "; ++j) r" << id << "[j] = n" << id << "[j];\n";
+      raw << "    " << VT << " r" << id << "[" << NC << "];\n";
+      for (int j = 0; j < NC; ++j)
+        load << "    q.r" << id << "[" << j << "] = *(const " << VT << "*)(" << P << " + row * " << rc.L << "LL + c" << j << ");\n";
       conv << "    float e" << id << "[" << NC << "][" << VEC << "];\n#pragma unroll\n    for (int j = 0; j < " << NC << "; ++j)\n#pragma unroll\n"
-           << "      for (int e = 0; e < " << VEC << "; ++e) e" << id << "[j][e] = tof(" << (VEC == 1 ? "r" + id + "[j]" : "r" + id + "[j][e]")
+           << "      for (int e = 0; e < " << VEC << "; ++e) e" << id << "[j][e] = tof(" << (VEC == 1 ? "q_.r" + id + "[j]" : "q_.r" + id + "[j][e]")
            << ");\n";
     } else {
       decl << "  float e" << id << "[" << NC << "][" << VEC << "];\n";
@@ -260,12 +263,9 @@ GenKernel gen_rowcol(const KInfo& ki, int index) {
   // hand-over of the column sums
   int64_t GS = 1, NG = 1;
   int scr = -1, cnt = -1;
-  if (NWG > 1 && NS > 0) {
-    GS = NWG;
-    if (NWG > 32) {
-      GS = 8;
-      while (GS * GS < NWG) ++GS;
-    }
+  const bool hand = NWG > 1 && NS > 0;
+  if (hand) {
+    GS = NWG <= 32 ? NWG : 16;
     NG = (NWG + GS - 1) / GS;
     ArgRef a;
     a.kind = ArgRef::Scratch;
@@ -281,9 +281,13 @@ GenKernel gen_rowcol(const KInfo& ki, int index) {
   s << source_header((int)gk.args.size());
   s << "extern \"C\" __global__ void __launch_bounds__(" << NT << ") " << gk.name << "(KArgs a) {\n";
   const int64_t LP = (int64_t)G * NC * VEC;  // columns that the lanes of a row cover
-  if (RPB > 1 && NS > 0) s << "  __shared__ float red[" << RPB * LP << "];\n";
+  const int64_t CQ = C / 4;                  // 16-byte vectors of a partial row
+  // slices of the partial rows that a workgroup adds side by side
+  int64_t ZS = 1;
+  while (ZS < 16 && 2 * ZS * CQ <= NT) ZS *= 2;
+  const int64_t red_floats = std::max(RPB > 1 && NS > 0 ? RPB * LP : 0, hand && ZS > 1 ? ZS * C : 0);
+  if (red_floats) s << "  __shared__ __attribute__((aligned(16))) float red[" << red_floats << "];\n";
   if (G > 64) s << "  __shared__ float xch[" << 2 * 8 * NT / 64 << "];\n  int par = 0;\n";
-  const bool hand = NWG > 1 && NS > 0;
   if (hand) s << "  __shared__ int last_;\n";
   s << "  const int tid = threadIdx.x, lane = tid % " << G << ", sub = tid / " << G << ";\n";
   if (G > 64) s << "  const int w0_ = sub * " << WR << ";\n";
@@ -293,14 +297,16 @@ GenKernel gen_rowcol(const KInfo& ki, int index) {
     // lanes past the row read its first elements (their values are not used)
     s << "  const i64 c" << j << " = c" << j << "_ok ? cc" << j << " : 0;\n";
   }
-  s << "  i64 blk = blockIdx.x;\n";
-  s << "  const i64 row0 = blk * " << RPB << " + sub;\n  i64 row = row0 < " << rc.R << "LL ? row0 : " << rc.R - 1 << "LL;\n";
+  s << "  struct Raw {\n" << raw.str() << "  };\n  Raw q_;\n";
+  s << "  auto fetch = [&](Raw& q, i64 blk) {\n    const i64 w_ = blk * " << RPB << " + sub, row = w_ < " << rc.R << "LL ? w_ : " << rc.R - 1
+    << "LL;\n" << load.str() << "  };\n";
   s << decl.str();
   for (int v : rc.cols) s << "  float k" << v << "[" << NC << "][" << VEC << "] = {};\n";
-  s << "#pragma unroll 1\n  for (; blk < " << blocks << "LL; blk += " << NWG << ") {\n";
-  s << "    const bool live = blk * " << RPB << " + sub < " << rc.R << "LL;\n";
-  s << "    const i64 nr_ = (blk + " << NWG << ") * " << RPB << " + sub, nrow = nr_ < " << rc.R << "LL ? nr_ : " << rc.R - 1 << "LL;\n";
-  s << load.str() << conv.str() << body.str() << store.str() << "    row = nrow;\n  }\n";
+  s << "  fetch(q_, blockIdx.x);\n";
+  s << "#pragma unroll 1\n  for (i64 blk = blockIdx.x; blk < " << blocks << "LL; blk += " << NWG << ") {\n";
+  s << "    const i64 w_ = blk * " << RPB << " + sub;\n    const bool live = w_ < " << rc.R << "LL;\n    const i64 row = live ? w_ : " << rc.R - 1
+    << "LL;\n";
+  s << conv.str() << "    fetch(q_, blk + " << NWG << "LL);\n" << body.str() << "  }\n";
   auto final_value = [&](int v, const std::string& x) {
     return g.nodes[v].op == KORCH_REDUCE_MEAN ? "(" + x + ") / " + flit((double)rc.R) : x;
   };
@@ -311,7 +317,7 @@ GenKernel gen_rowcol(const KInfo& ki, int index) {
     const int v = rc.cols[i];
     const std::string V = std::to_string(v);
     auto put = [&](const std::string& col, const std::string& x) {
-      if (NWG > 1) return "coherent_store(&part[" + std::to_string(i * rc.L) + "LL + " + col + "], " + x + ")";
+      if (hand) return "coherent_store(&part[" + std::to_string(i * LQ) + "LL + " + col + "], " + x + ")";
       return "st1(" + out_ptr(v) + " + " + col + ", " + final_value(v, x) + ")";
     };
     if (RPB > 1) {
@@ -338,42 +344,49 @@ GenKernel gen_rowcol(const KInfo& ki, int index) {
       s << "    last_ = __hip_atomic_fetch_add(c_, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == n_ - 1;\n";
       s << "    if (last_) __hip_atomic_store(c_, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);\n  }\n  __syncthreads();\n  if (!last_) return;\n";
     };
-    // sums of partial rows [z0, z1) of `from`, four columns of a thread at a time
-    const int CV = C % 4 == 0 && rc.L % 4 == 0 ? 4 : 1;
-    auto add_up = [&](const std::string& from, const std::string& count, const std::function<void(const std::string&, const std::string&)>& sink) {
-      s << "  {\n    float* f_ = " << from << ";\n    const int m_ = " << count << ";\n";
-      s << "    for (i64 c = (i64)tid * " << CV << "; c < " << C << "LL; c += " << (int64_t)NT * CV << ") {\n";
-      if (CV == 4) {
-        s << "      const __amdgpu_buffer_rsrc_t r_ = __builtin_amdgcn_make_buffer_rsrc(f_, 0, 0x7fffffff, 0x00020000);\n";
-        s << "      f32x4 x_ = {};\n#pragma unroll 8\n      for (int z = 0; z < m_; ++z) {\n        const float4 q_ = coherent_load4(r_, (unsigned)(((i64)z * " << C
-          << "LL + c) * 4));\n        x_ += f32x4{q_.x, q_.y, q_.z, q_.w};\n      }\n";
-        s << "#pragma unroll\n      for (int e = 0; e < 4; ++e) {\n        const i64 ce = c + e;\n        const float y_ = x_[e];\n";
-      } else {
-        s << "      float x_ = 0.0f;\n#pragma unroll 8\n      for (int z = 0; z < m_; ++z) x_ += coherent_load(&f_[(i64)z * " << C << "LL + c]);\n";
-        s << "      {\n        const i64 ce = c;\n        const float y_ = x_;\n";
+    // Adds partial rows 0 .. m-1 (m <= maxn) of `from`: a thread per 16-byte
+    // vector and slice of the rows, every load of a thread in flight together;
+    // then the slices, in order.
+    auto add_up = [&](const std::string& from, const std::string& count, int64_t maxn, const std::function<void(const std::string&, const std::string&)>& sink) {
+      const int64_t per = (maxn + ZS - 1) / ZS, step = std::min<int64_t>(CQ * ZS, NT) / ZS;
+      s << "  {\n    const __amdgpu_buffer_rsrc_t r_ = __builtin_amdgcn_make_buffer_rsrc(" << from << ", 0, 0x7fffffff, 0x00020000);\n    const int m_ = "
+        << count << ";\n";
+      s << "    const int zs = tid / " << step << ";\n    for (int v = tid % " << step << "; v < " << CQ << " && zs < " << ZS << "; v += " << step << ") {\n";
+      s << "      float4 q_[" << per << "];\n#pragma unroll\n      for (int z = 0; z < " << per << "; ++z) {\n        const int zz = zs * " << per
+        << " + z;\n        q_[z] = coherent_load4(r_, (unsigned)((zz < m_ ? zz : m_ - 1) * " << C * 4 << " + v * 16));\n      }\n";
+      s << "      f32x4 x_ = {};\n#pragma unroll\n      for (int z = 0; z < " << per << "; ++z)\n        if (zs * " << per
+        << " + z < m_) x_ += f32x4{q_[z].x, q_[z].y, q_[z].z, q_[z].w};\n";
+      if (ZS > 1) {
+        s << "      *(f32x4*)(red + zs * " << C << " + v * 4) = x_;\n    }\n    __syncthreads();\n";
+        s << "    for (int v = tid; v < " << CQ << "; v += " << NT << ") {\n      f32x4 x_ = *(const f32x4*)(red + v * 4);\n#pragma unroll\n      for (int z = 1; z < "
+          << ZS << "; ++z) x_ += *(const f32x4*)(red + z * " << C << " + v * 4);\n";
       }
-      sink("ce", "y_");
-      s << "      }\n    }\n  }\n";
+      sink("v", "x_");
+      s << "    }\n  }\n";
     };
-    auto outputs = [&](const std::string& c, const std::string& y) {
-      for (size_t i = 0; i < rc.cols.size(); ++i)
-        s << "        if (" << c << " >= " << i * rc.L << "LL && " << c << " < " << (i + 1) * rc.L << "LL) st1(" << out_ptr(rc.cols[i]) << " + (" << c << " - "
-          << i * rc.L << "LL), " << final_value(rc.cols[i], y) << ");\n";
+    auto outputs = [&](const std::string& v, const std::string& x) {
+      for (size_t i = 0; i < rc.cols.size(); ++i) {
+        s << "      if (" << v << " >= " << i * LQ / 4 << " && " << v << " < " << (i + 1) * LQ / 4 << ")\n#pragma unroll\n        for (int e = 0; e < 4; ++e)\n";
+        s << "          if ((" << v << " - " << i * LQ / 4 << ") * 4 + e < " << rc.L << ") st1(" << out_ptr(rc.cols[i]) << " + ((" << v << " - " << i * LQ / 4
+          << ") * 4 + e), " << final_value(rc.cols[i], x + "[e]") << ");\n";
+      }
     };
+    if (ZS > 1) s << "  __syncthreads();\n";
     if (NG > 1) {
       s << "  const int grp = blockIdx.x / " << GS << ";\n  const int gsz = " << NWG << " - grp * " << GS << " < " << GS << " ? " << NWG << " - grp * " << GS << " : " << GS
         << ";\n";
       arrive("1 + grp", "gsz");
       const std::string to = "(" + base + " + " + std::to_string(NWG * C) + "LL)";
-      add_up(base + " + (i64)grp * " + std::to_string(GS * C) + "LL", "gsz", [&](const std::string& c, const std::string& y) {
-        s << "        coherent_store(&" << to << "[(i64)grp * " << C << "LL + " << c << "], " << y << ");\n";
+      add_up("(" + base + " + (i64)grp * " + std::to_string(GS * C) + "LL)", "gsz", GS, [&](const std::string& v, const std::string& x) {
+        s << "      coherent_store4(__builtin_amdgcn_make_buffer_rsrc(" << to << " + (i64)grp * " << C << "LL, 0, 0x7fffffff, 0x00020000), (unsigned)(" << v
+          << " * 16), float4{" << x << "[0], " << x << "[1], " << x << "[2], " << x << "[3]});\n";
       });
       s << "  __builtin_amdgcn_s_waitcnt(0);\n  __syncthreads();\n";
       arrive("0", std::to_string(NG));
-      add_up(to, std::to_string(NG), outputs);
+      add_up(to, std::to_string(NG), NG, outputs);
     } else {
       arrive("0", std::to_string(NWG));
-      add_up(base, std::to_string(NWG), outputs);
+      add_up(base, std::to_string(NWG), NWG, outputs);
     }
   }
   s << "}\n";
