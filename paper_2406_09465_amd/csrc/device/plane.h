@@ -25,8 +25,7 @@
 //
 // P (generated) describes the kernel; see the constants and functions used.
 
-typedef f16 f16x4 __attribute__((ext_vector_type(4)));
-typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 static constexpr float kLog2e = 1.4426950408889634f;
 static constexpr float kLazy = 5.5f;  // natural units: 2^8
@@ -63,9 +62,21 @@ template <class P> struct Geo {
   static constexpr int GT = P::WSPLIT ? 64 : NT;        // threads that share a streamed tile
   static constexpr int NG = P::WSPLIT ? P::NW : 1;      // such groups
   static constexpr int OT = P::WSPLIT ? 32 : 32 * P::NW;  // owned indices of the workgroup
+  static constexpr bool DMA = !P::WSPLIT;               // tiles go straight to LDS
   static constexpr int NSUB = P::TS / 32;
   static constexpr int width(int t) { return round_up(P::sw(t), 32); }
-  static constexpr int pitch(int t) { return width(t) + VL; }
+  // Rows lie back to back; a row's 16-byte chunk c is stored at chunk c ^ swz(row).
+  // The score products read one chunk of 32 rows at a time, the output products
+  // 64 consecutive bytes of four rows (transposed); with the chunks of the 16
+  // rows that share their address modulo the 256 bytes of all banks permuted
+  // like this, neither meets a bank twice.
+  static constexpr int pitch(int t) { return width(t); }
+  static constexpr int chunks(int t) { return width(t) / VL; }  // of a row
+  template <int t> static __device__ __forceinline__ int swz(int r) {
+    if constexpr (chunks(t) % 16 == 0) return ((r & 3) << 2) | ((r >> 2) & 3);
+    else if constexpr (chunks(t) % 8 == 0) return ((r & 2) << 1) | ((r >> 2) & 3);
+    else return (r >> 2) & 3;
+  }
   static constexpr int tile_off(int t) {  // bytes, within one stage
     int o = 0;
     for (int i = 0; i < t; ++i) o += P::TS * pitch(i) * (int)sizeof(T);
@@ -86,9 +97,27 @@ template <class P> struct Geo {
   static constexpr int list_off = main_bytes;
   static constexpr int range_off = list_off + kListCap * 2;             // own ranges: [wave][NOV][2]
   static constexpr int misc_off = range_off + (P::NW * P::NOV * 2 + 8) * 4;
-  static constexpr int bin_off = (misc_off + 64 + 15) / 16 * 16;
+  static constexpr int lut_off = (misc_off + 64 + 15) / 16 * 16;
+  static constexpr int bin_off = lut_off + (P::LUT + 3) / 4 * 16;
   static constexpr int bytes = bin_off + bin_bytes;
 };
+
+// Values that a rarely taken block of vector code starts from: what depends on
+// them cannot be evaluated ahead of the block (the compiler would evaluate all
+// of it always and select the results afterwards).
+__device__ __forceinline__ float rare(float v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
+// tanh with the fp32 accuracy that scores need (absolute: a few 2^-24), as one
+// exponential and one reciprocal: 1 - 2 / (e^{2x} + 1).
+// pl_ctanh: c tanh(a x) without the products by a and c.
+__device__ __forceinline__ float pl_ctanh(float x, float a, float c) {
+  return __builtin_fmaf(-2.0f * c, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * (a * 2.0f * kLog2e)) + 1.0f), c);
+}
+__device__ __forceinline__ float pl_tanh(float x) { return pl_ctanh(x, 1.0f, 1.0f); }
+__device__ __forceinline__ float pl_exp(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
 template <int V> struct ic {
   static constexpr int value = V;
@@ -120,6 +149,10 @@ __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
   for (int m = 32; m >= 1; m >>= 1) v = k_max(v, __shfl_xor(v, m, 64));
   return v;
+}
+
+__device__ __forceinline__ float uniform(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v)));
 }
 
 // Interval arithmetic on value ranges (rounding is monotone, so a range of
@@ -164,6 +197,7 @@ template <class P> struct Plane {
   static constexpr int vpt(int t) { return (P::TS * (P::sw(t) / VL) + G::GT - 1) / G::GT; }  // staging vectors of a thread
   static constexpr int vtot() {
     int n = 0;
+    if (G::DMA) return 1;
     for (int t = 0; t < P::NST; ++t) n += vpt(t);
     return n > 0 ? n : 1;
   }
@@ -192,39 +226,73 @@ template <class P> struct Plane {
   char* smem;
   int tid, wave, lane, l32, h, gt, gtid;
   i64 own0;     // first owned index of the workgroup
-  i64 own;      // this lane's owned index, clamped to the axis
-  bool own_ok;  // it exists
   float ov[P::NOV > 0 ? P::NOV : 1];
   Frag bf[NF];
   f32x16 acc[NA > 0 ? NA : 1];
   float mref, mtrue, lsum;
+  Range wr[P::NOV > 0 ? P::NOV : 1];  // ranges of the owned vectors over the wave
   V16 st[vtot()];
   float stab[TABV > 0 ? TABV : 1];
 
   __device__ __forceinline__ Plane(const KArgs& a_, char* s) : a(a_), smem(s) {}
 
+  // This lane's owned index (clamped to the axis), and whether it exists.
+  __device__ __forceinline__ i64 own_raw() const { return own0 + (P::WSPLIT ? 0 : wave * 32) + l32; }
+  __device__ __forceinline__ i64 own() const { return own_raw() < P::NOWN ? own_raw() : P::NOWN - 1; }
+  __device__ __forceinline__ bool own_ok() const { return own_raw() < P::NOWN; }
+
   __device__ __forceinline__ char* stage(int s) const { return smem + (P::WSPLIT ? wave * G::group_bytes : 0) + s * G::stage_bytes; }
 
-  // ---- loads of one streamed tile into registers, and from there to LDS ----
-  __device__ __forceinline__ void fetch(i64 s0) {
-    const bool whole = s0 + P::TS <= P::NSTR;
+  // ---- loads of one streamed tile ------------------------------------------------
+  // Rows are read through a buffer descriptor of the tile's rows that exist:
+  // reads past it return zero (rows past the axis, columns past a tensor's
+  // width, rows that the operand's own condition excludes).
+  template <int t> __device__ __forceinline__ i32x4 tile_rows(i64 s0) const {
+    const int rows = P::NSTR - s0 < P::TS ? (int)(P::NSTR - s0) : P::TS;
+    const unsigned long long p = (unsigned long long)P::template srow<t>(a, b, s0);
+    // in scalar registers, as the loads in assembly need it
+    return i32x4{__builtin_amdgcn_readfirstlane((int)(unsigned)p), __builtin_amdgcn_readfirstlane((int)((p >> 32) & 0xffff)),
+                 __builtin_amdgcn_readfirstlane(((rows - 1) * P::srs(t) + P::sw(t)) * (int)sizeof(T)), 0x00020000};
+  }
+  // Byte offset of chunk c of a tile's row, or one past the rows.
+  template <int t> __device__ __forceinline__ unsigned tile_offset(i64 s0, int row, int c, bool in) const {
+    if constexpr (P::row_mask(t)) {
+      const i64 r = s0 + row;
+      in = in && P::template srow_ok<t>(a, b, r < P::NSTR ? r : P::NSTR - 1);
+    }
+    return in ? (unsigned)(row * P::srs(t) * (int)sizeof(T) + c * 16) : 0x80000000u;
+  }
+  // DMA (the workgroup shares a tile): straight into the LDS of stage s, 64
+  // consecutive chunks per instruction; a lane fetches the chunk that its place
+  // holds.  The workgroup waits for the loads before its next barrier (landed()).
+  // Otherwise into registers, and from there to LDS when the tile before has been read.
+  __device__ __forceinline__ void fetch(int s, i64 s0) {
     static_for<P::NST>([&](auto ti) {
       constexpr int t = decltype(ti)::value;
-      constexpr int CV = P::sw(t) / VL;
+      const i32x4 rs = tile_rows<t>(s0);
+      if constexpr (G::DMA) {
+        constexpr int CH = G::chunks(t), NI = P::TS * CH / 64;
+        typedef __attribute__((address_space(3))) char lds_char;
+        const unsigned to = (unsigned)(unsigned long long)(lds_char*)(stage(s) + G::tile_off(t));
 #pragma unroll
-      for (int i = 0; i < vpt(t); ++i) {
-        const int e = gtid + i * G::GT;
-        const int row = e / CV, c = e % CV;
-        const bool in = (P::TS * CV) % G::GT == 0 || e < P::TS * CV;
-        const i64 r = s0 + row;
-        const i64 rc = r < P::NSTR ? r : P::NSTR - 1;
-        V16 v = *(const V16*)(P::template srow<t>(a, b, in ? rc : P::NSTR - 1) + c * VL);
-        if constexpr (P::row_mask(t)) {
-          if (!(in && r < P::NSTR && P::template srow_ok<t>(a, b, rc))) v = V16{};
-        } else {
-          if (!whole && r >= P::NSTR) v = V16{};
+        for (int i = 0; i < NI; i += P::NW) {
+          if (NI % P::NW == 0 || i + wave < NI) {
+            const int u = (i + wave) * 64 + lane, row = u / CH, c = (u % CH) ^ G::template swz<t>(row);
+            const unsigned off = tile_offset<t>(s0, row, c, c < P::sw(t) / VL);
+            const unsigned la = __builtin_amdgcn_readfirstlane(to + (i + wave) * 1024);
+            // (the descriptor may come straight from vector instructions: five wait states)
+            asm volatile("s_mov_b32 m0, %1\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %2, 0 offen lds" ::"v"(off), "s"(la), "s"(rs) : "memory", "m0");
+          }
         }
-        st[vbase(t) + i] = v;
+      } else {
+        constexpr int CV = P::sw(t) / VL;
+        const __amdgpu_buffer_rsrc_t rr = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(P::template srow<t>(a, b, s0)), 0, rs[2], 0x00020000);
+#pragma unroll
+        for (int i = 0; i < vpt(t); ++i) {
+          const int e = gtid + i * G::GT, row = e / CV, c = e % CV;
+          const bool in = (P::TS * CV) % G::GT == 0 || e < P::TS * CV;
+          st[vbase(t) + i] = __builtin_bit_cast(V16, __builtin_amdgcn_raw_buffer_load_b128(rr, tile_offset<t>(s0, row, c, in), 0, 0));
+        }
       }
     });
     if constexpr (P::NTAB > 0) {
@@ -239,17 +307,17 @@ template <class P> struct Plane {
   }
   __device__ __forceinline__ void put(int s) {
     char* base = stage(s);
-    static_for<P::NST>([&](auto ti) {
-      constexpr int t = decltype(ti)::value;
-      constexpr int CV = P::sw(t) / VL;
+    if constexpr (!G::DMA)
+      static_for<P::NST>([&](auto ti) {
+        constexpr int t = decltype(ti)::value;
+        constexpr int CV = P::sw(t) / VL;
 #pragma unroll
-      for (int i = 0; i < vpt(t); ++i) {
-        const int e = gtid + i * G::GT;
-        const int row = e / CV, c = e % CV;
-        if ((P::TS * CV) % G::GT == 0 || e < P::TS * CV)
-          *(V16*)((T*)(base + G::tile_off(t)) + row * G::pitch(t) + c * VL) = st[vbase(t) + i];
-      }
-    });
+        for (int i = 0; i < vpt(t); ++i) {
+          const int e = gtid + i * G::GT, row = e / CV, c = e % CV;
+          if ((P::TS * CV) % G::GT == 0 || e < P::TS * CV)
+            *(V16*)((T*)(base + G::tile_off(t)) + row * G::pitch(t) + (c ^ G::template swz<t>(row)) * VL) = st[vbase(t) + i];
+        }
+      });
     if constexpr (P::NTAB > 0) {
 #pragma unroll
       for (int i = 0; i < TABV; ++i) {
@@ -258,24 +326,32 @@ template <class P> struct Plane {
       }
     }
   }
-  // Columns past a tensor's width take part in the score products: zeros.
+  // This wave's direct loads have arrived.
+  __device__ __forceinline__ void landed() const {
+    if constexpr (G::DMA) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  }
+  // Columns past a tensor's width take part in the score products: zeros
+  // (direct loads write them with every tile).
   __device__ __forceinline__ void clear_pads() {
-    static_for<P::NST>([&](auto ti) {
-      constexpr int t = decltype(ti)::value;
-      constexpr int PV = (G::pitch(t) - P::sw(t)) / VL;
-      for (int s = 0; s < P::STAGES; ++s)
-        for (int e = gtid; e < P::TS * PV; e += G::GT)
-          *(V16*)((T*)(stage(s) + G::tile_off(t)) + (e / PV) * G::pitch(t) + P::sw(t) + (e % PV) * VL) = V16{};
-    });
+    if constexpr (!G::DMA)
+      static_for<P::NST>([&](auto ti) {
+        constexpr int t = decltype(ti)::value;
+        constexpr int PV = (G::width(t) - P::sw(t)) / VL;
+        if constexpr (PV > 0)
+          for (int s = 0; s < P::STAGES; ++s)
+            for (int e = gtid; e < P::TS * PV; e += G::GT)
+              *(V16*)((T*)(stage(s) + G::tile_off(t)) + (e / PV) * G::pitch(t) + ((P::sw(t) / VL + e % PV) ^ G::template swz<t>(e / PV)) * VL) = V16{};
+      });
   }
 
   // ---- products --------------------------------------------------------------
   template <int p> __device__ __forceinline__ f32x16 score(const char* base, int sub) const {
     constexpr int t = P::sst(p);
     f32x16 c = {};
-    const T* q = (const T*)(base + G::tile_off(t)) + (sub * 32 + l32) * G::pitch(t) + h * (KU / 2);
+    const T* q = (const T*)(base + G::tile_off(t)) + (sub * 32 + l32) * G::pitch(t);
+    const int z = h ^ G::template swz<t>(l32);
 #pragma unroll
-    for (int k = 0; k < kfrag(p); ++k) c = M::run(*(const Frag*)(q + k * KU), bf[fbase(p) + k], c);
+    for (int k = 0; k < kfrag(p); ++k) c = M::run(*(const Frag*)(q + ((2 * k) ^ z) * VL), bf[fbase(p) + k], c);
     return c;
   }
   template <int o> __device__ __forceinline__ void output(const char* base, int sub, const float* X) {
@@ -289,21 +365,26 @@ template <class P> struct Plane {
         Frag x;
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = fromf<T>(X[8 * kk + j]);
-        const T* r0 = w + (sub * 32 + kk * 16 + 4 * h + ((lane & 15) >> 2)) * G::pitch(t) + ((lane >> 4) & 1) * 16 + 4 * (lane & 3);
+        // this lane's part of a read: row r (and r + 8), columns 8 c + 4 (lane & 1) .. + 3 of 32
+        const int r = 4 * h + ((lane & 15) >> 2), c = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+        const T* r0 = w + (sub * 32 + kk * 16 + r) * G::pitch(t) + 4 * (lane & 1);
+        const int z0 = c ^ G::template swz<t>(r), z1 = c ^ G::template swz<t>(r + 8);
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
-          s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(r0 + d * 32));
-          s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(r0 + 8 * G::pitch(t) + d * 32));
+          s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(r0 + ((4 * d) ^ z0) * VL));
+          s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(r0 + 8 * G::pitch(t) + ((4 * d) ^ z1) * VL));
           acc[abase(o) + d] = M::run(__builtin_bit_cast(Frag, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)), x, acc[abase(o) + d]);
         }
       }
     } else {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const T* r0 = w + (sub * 32 + 8 * (i / 4) + 4 * h + i % 4) * G::pitch(t) + l32;
+        const int r = 8 * (i / 4) + 4 * h + i % 4;
+        const T* r0 = w + (sub * 32 + r) * G::pitch(t) + l32 % 4;
+        const int z = (l32 / 4) ^ G::template swz<t>(r);
 #pragma unroll
         for (int d = 0; d < ND; ++d)
-          acc[abase(o) + d] = __builtin_amdgcn_mfma_f32_32x32x2f32(r0[d * 32], X[i], acc[abase(o) + d], 0, 0, 0);
+          acc[abase(o) + d] = __builtin_amdgcn_mfma_f32_32x32x2f32(r0[((8 * d) ^ z) * VL], X[i], acc[abase(o) + d], 0, 0, 0);
       }
     }
   }
@@ -311,8 +392,10 @@ template <class P> struct Plane {
   // Streamed index (within its tile) of register i of subtile sub.
   __device__ __forceinline__ int sidx(int sub, int i) const { return sub * 32 + 8 * (i / 4) + 4 * h + i % 4; }
 
-  template <bool CHECK, class F> __device__ __forceinline__ void elements(const char* base, i64 s0, int sub, F&& f) {
+  // f(i, values of the streamed vectors, streamed index (clamped), it exists) for the registers of a subtile.
+  template <class F> __device__ __forceinline__ void elements(const char* base, i64 s0, int sub, F&& f) {
     const float* tab = (const float*)(base + G::tab_off);
+    const int rows = P::NSTR - s0 < P::TS ? (int)(P::NSTR - s0) : P::TS;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       f32x4 tv4[P::NTAB > 0 ? P::NTAB : 1];
@@ -323,42 +406,48 @@ template <class P> struct Plane {
         float tv[P::NTAB > 0 ? P::NTAB : 1];
 #pragma unroll
         for (int k = 0; k < P::NTAB; ++k) tv[k] = tv4[k][r];
-        const i64 s = s0 + sidx(sub, 4 * g + r);
-        f(4 * g + r, tv, s < P::NSTR ? s : P::NSTR - 1, s < P::NSTR);
+        const int s = sidx(sub, 4 * g + r);
+        f(4 * g + r, tv, s0 + (s < rows ? s : rows - 1), s < rows);
       }
     }
   }
 
   // ---- one tile ---------------------------------------------------------------
-  template <bool CHECK> __device__ __forceinline__ void tile(int s, i64 s0) {
+  // `full`: no pair of the tile is masked and every streamed index exists.  The
+  // mask is a step of its own, so that both kinds of tiles share the products.
+  __device__ __forceinline__ void tile(int s, i64 s0, bool full) {
     const char* base = stage(s);
+    const float* lut = (const float*)(smem + G::lut_off);
     if constexpr (P::SOFTMAX) {
       f32x16 x[G::NSUB];
-      unsigned keep[G::NSUB];
-      float top = -__builtin_huge_valf();
 #pragma unroll
       for (int sub = 0; sub < G::NSUB; ++sub) x[sub] = score<0>(base, sub);
 #pragma unroll
-      for (int sub = 0; sub < G::NSUB; ++sub) {
-        keep[sub] = 0;
-        elements<CHECK>(base, s0, sub, [&](int i, const float* tv, i64 sc, bool ok) {
-          float v, xs[1] = {x[sub][i]};
-          bool k = true;
-          P::template logit<CHECK>(a, b, ov, tv, own, sc, xs, v, k);
-          if (CHECK) {
-            k = k && ok;
-            keep[sub] |= k ? 1u << i : 0u;
-            top = k_max(top, k ? v : -__builtin_huge_valf());
-          } else {
-            top = k_max(top, v);
-          }
-          x[sub][i] = v;
+      for (int sub = 0; sub < G::NSUB; ++sub)
+        elements(base, s0, sub, [&](int i, const float* tv, i64 sc, bool) {
+          float xs[1] = {x[sub][i]};
+          x[sub][i] = P::logit(a, b, ov, tv, lut, own(), sc, xs);
         });
+      if (!full) {
+        float om[P::NOV > 0 ? P::NOV : 1];
+        for (int k = 0; k < P::NOV; ++k) om[k] = rare(ov[k]);
+        const float minus = rare(-__builtin_huge_valf());
+        // a masked pair's score is -inf: its exponential is 0 whatever the maximum
+#pragma unroll
+        for (int sub = 0; sub < G::NSUB; ++sub)
+          elements(base, s0, sub, [&](int i, const float* tv, i64 sc, bool ok) {
+            x[sub][i] = ok && P::keep(a, b, om, tv, lut, own(), sc) ? x[sub][i] : minus;
+          });
       }
+      float top = x[0][0];
+#pragma unroll
+      for (int sub = 0; sub < G::NSUB; ++sub)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = k_max(top, x[sub][i]);
       top = k_max(top, __shfl_xor(top, 32, 64));
       mtrue = k_max(mtrue, top);
-      if (__any(mtrue > mref + kLazy)) {
-        const float f = mref == mtrue ? 1.0f : __builtin_amdgcn_exp2f((mref - mtrue) * kLog2e);
+      if (__any(mtrue > mref + kLazy / P::FOLD)) {
+        const float f = rare(mref) == mtrue ? 1.0f : __builtin_amdgcn_exp2f((mref - mtrue) * (P::FOLD * kLog2e));
         mref = mtrue;
         lsum *= f;
 #pragma unroll
@@ -367,37 +456,44 @@ template <class P> struct Plane {
           for (int i = 0; i < 16; ++i) acc[d][i] *= f;
       }
       const float mz = mref == -__builtin_huge_valf() ? 0.0f : mref;
-      const float mc = -mz * kLog2e;
+      const float mc = -mz * (P::FOLD * kLog2e);
 #pragma unroll
       for (int sub = 0; sub < G::NSUB; ++sub) {
         float X[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          float p;
           if constexpr (sizeof(T) == 2)
-            p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[sub][i], kLog2e, mc));
+            X[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[sub][i], P::FOLD * kLog2e, mc));
           else
-            p = expf(x[sub][i] - mz);
-          if (CHECK) p = (keep[sub] >> i) & 1u ? p : 0.0f;
-          lsum += p;
-          X[i] = p;
+            X[i] = expf((x[sub][i] - mz) * P::FOLD);
+          lsum += X[i];
         }
         static_for<P::NOP>([&](auto oi) { output<decltype(oi)::value>(base, sub, X); });
       }
     } else {
-#pragma unroll
+#pragma unroll 1
       for (int sub = 0; sub < G::NSUB; ++sub) {
         f32x16 x[P::NSP];
         static_for<P::NSP>([&](auto pi) { x[decltype(pi)::value] = score<decltype(pi)::value>(base, sub); });
         float X[P::NX][16];
-        elements<CHECK>(base, s0, sub, [&](int i, const float* tv, i64 sc, bool ok) {
+        elements(base, s0, sub, [&](int i, const float* tv, i64 sc, bool) {
           float xs[P::NSP], out[P::NX];
 #pragma unroll
           for (int p = 0; p < P::NSP; ++p) xs[p] = x[p][i];
-          P::template plane<CHECK>(a, b, ov, tv, own, sc, xs, out);
+          P::plane(a, b, ov, tv, lut, own(), sc, xs, out);
 #pragma unroll
-          for (int k = 0; k < P::NX; ++k) X[k][i] = CHECK && !ok ? 0.0f : out[k];
+          for (int k = 0; k < P::NX; ++k) X[k][i] = out[k];
         });
+        if (!full) {
+          float om[P::NOV > 0 ? P::NOV : 1];
+          for (int k = 0; k < P::NOV; ++k) om[k] = rare(ov[k]);
+          const float zero = rare(0.0f);
+          elements(base, s0, sub, [&](int i, const float* tv, i64 sc, bool ok) {
+            const bool k1 = ok && P::keep(a, b, om, tv, lut, own(), sc);
+#pragma unroll
+            for (int k = 0; k < P::NX; ++k) X[k][i] = k1 ? X[k][i] : zero;
+          });
+        }
         static_for<P::NOP>([&](auto oi) { output<decltype(oi)::value>(base, sub, X[P::ox(decltype(oi)::value)]); });
         if constexpr (P::NBIN > 0) bins(base, s0, sub, X[P::XBIN]);
       }
@@ -407,41 +503,74 @@ template <class P> struct Plane {
   // ---- sums of plane values by bin -----------------------------------------------
   // Every lane adds its values to bins of its own in LDS ([bin][lane]): no two
   // lanes meet at an address and a lane's additions keep their order, so the
-  // sums do not depend on timing.  The lanes are summed at the end.
+  // sums do not depend on timing.  The lanes are summed at the end.  Four values
+  // are added at a time (their old sums are read together; values that share a
+  // bin add up first, and all of them write the same sum), so a subtile waits
+  // for LDS four times, not sixteen (8 x 12 heads of 512 x 512, width 64: 45 us
+  // against 56; LDS atomic additions took 191).  Where the index lies past one end of its
+  // table for every pair, as far from the diagonal, there is one bin.
   __device__ __forceinline__ void bins(const char* base, i64 s0, int sub, const float* X) {
     float* mine = (float*)(smem + G::bin_off) + wave * (P::NBIN * 64) + lane;
-    elements<true>(base, s0, sub, [&](int i, const float* tv, i64 sc, bool ok) {
-      const int k = (int)P::bin(a, b, ov, tv, own, sc);
-      if (own_ok && ok) mine[k * 64] += X[i];
-    });
+    const float* lut = (const float*)(smem + G::lut_off);
+    const Range e = P::bin_range(a, b, wr, (float)(s0 + sub * 32), (float)(s0 + sub * 32 + 31));
+    const bool live = own_ok();
+    if (e.lo >= (float)(P::BIN_T - 1) || e.hi <= 0.0f) {
+      const int k = (int)P::bin_end(lut, e.hi > 0.0f);
+      float sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sum += X[i];  // zero past the axis
+      mine[k * 64] += live ? sum : 0.0f;
+      return;
+    }
+    int id[16];
+    elements(base, s0, sub, [&](int i, const float* tv, i64 sc, bool) { id[i] = (int)P::bin(a, b, ov, tv, lut, own(), sc) * 64; });
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      float old[4], add[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) old[i] = mine[id[4 * g + i]];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        add[i] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) add[i] += id[4 * g + j] == id[4 * g + i] ? X[4 * g + j] : 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mine[id[4 * g + i]] = old[i] + (live ? add[i] : 0.0f);
+    }
   }
 
   // ---- the kernel --------------------------------------------------------------
   __device__ __forceinline__ void run() {
-    tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l32 = lane & 31, h = lane >> 5;
+    tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, h = lane >> 5;
     gtid = P::WSPLIT ? lane : tid;
-    // Workgroups are dealt to the eight XCDs in turn; consecutive work of one
-    // XCD shares a batch entry, whose streamed rows then stay in that XCD's L2.
-    // Within a batch entry the last owned tiles come first (under a causal mask
-    // they are the longest).
-    int w = blockIdx.x;
-    constexpr int total = P::OTILES * P::NB;
-    if constexpr (total % 8 == 0) w = (w & 7) * (total / 8) + (w >> 3);
-    const int bl = w / P::OTILES, ot = P::OTILES - 1 - w % P::OTILES;
-    const int z = blockIdx.y;
+    // Order of the work.  An owned axis is made of blocks of TP tiles (the
+    // positions of one head) along which a mask usually changes the work
+    // steadily.  The longest tiles of all blocks come first; of the workgroups
+    // that are resident from the start (OCC per compute unit) every second round
+    // over the compute units runs backwards, so that a long and a short one
+    // share a compute unit.  Workgroups are dealt to
+    // the eight XCDs in turn: with whole blocks for each, a block's streamed rows
+    // stay in one XCD's L2.
+    constexpr int NBLK = P::NB * (P::OTILES / P::TP);
+    constexpr bool by_xcd = NBLK % 8 == 0;
+    constexpr int NX = by_xcd ? NBLK / 8 : NBLK, CHUNK = by_xcd ? 32 : 256, ITEMS = NX * P::TP * P::SPLIT;
+    const int x0 = by_xcd ? (blockIdx.x & 7) * NX : 0;
+    int w = by_xcd ? blockIdx.x >> 3 : blockIdx.x;
+    const int round = w / CHUNK;
+    if (round < P::OCC && (round & 1)) w = round * CHUNK + (ITEMS - round * CHUNK < CHUNK ? ITEMS - round * CHUNK : CHUNK) - 1 - w % CHUNK;
+    const int z = w % P::SPLIT, blk = x0 + w / P::SPLIT % NX, rank = w / P::SPLIT / NX;
+    const int bl = blk / (P::OTILES / P::TP), ot = blk % (P::OTILES / P::TP) * P::TP + (P::LAST_FIRST ? P::TP - 1 - rank : rank);
     b = P::batch(bl);
     own0 = (i64)ot * G::OT;
-    const i64 o = own0 + (P::WSPLIT ? 0 : wave * 32) + l32;
-    own_ok = o < P::NOWN;
-    own = own_ok ? o : P::NOWN - 1;
 #pragma unroll
-    for (int k = 0; k < P::NOV; ++k) ov[k] = P::own(a, b, k, own);
+    for (int k = 0; k < P::NOV; ++k) ov[k] = P::own(a, b, k, own());
     // owned fragments
     static_for<P::NSP>([&](auto pi) {
       constexpr int p = decltype(pi)::value;
-      const T* r = P::template orow<p>(a, b, own);
-      bool ok = own_ok;
-      if constexpr (P::own_mask(p)) ok = ok && P::template orow_ok<p>(a, b, own);
+      const T* r = P::template orow<p>(a, b, own());
+      bool ok = own_ok();
+      if constexpr (P::own_mask(p)) ok = ok && P::template orow_ok<p>(a, b, own());
 #pragma unroll
       for (int k = 0; k < kfrag(p); ++k) {
         const int c = k * KU + h * (KU / 2);
@@ -457,14 +586,19 @@ template <class P> struct Plane {
     if constexpr (P::NBIN > 0)
       for (int k = 0; k < P::NBIN; ++k) ((float*)(smem + G::bin_off))[(wave * P::NBIN + k) * 64 + lane] = 0.0f;
     clear_pads();
+    // tables that the plane looks up, as the values it reads
+    if constexpr (P::LUT > 0) {
+      for (int k = tid; k < P::LUT; k += G::NT) ((float*)(smem + G::lut_off))[k] = P::lut_value(a, b, k);
+      __syncthreads();
+    }
     // ranges of the owned vectors, over the workgroup and over the wave
     float* rng = (float*)(smem + G::range_off);
-    Range wr[P::NOV > 0 ? P::NOV : 1], gr[P::NOV > 0 ? P::NOV : 1];
-    if constexpr (P::MASK) {
+    Range gr[P::NOV > 0 ? P::NOV : 1];
+    if constexpr (P::MASK || P::NBIN > 0) {
 #pragma unroll
       for (int k = 0; k < P::NOV; ++k) {
         const bool bad = __any(not_number(ov[k]));
-        wr[k] = bad ? r_all() : Range{wave_min(ov[k]), wave_max(ov[k])};
+        wr[k] = bad ? r_all() : Range{uniform(wave_min(ov[k])), uniform(wave_max(ov[k]))};
         if (lane == 0) rng[(wave * P::NOV + k) * 2] = wr[k].lo, rng[(wave * P::NOV + k) * 2 + 1] = wr[k].hi;
       }
       __syncthreads();
@@ -550,23 +684,27 @@ template <class P> struct Plane {
       if (c0 > 0) group_sync<G::GT>();
       if (e < n) {
         entry(e, s0, full);
-        fetch(s0);
+        fetch(0, s0);
         put(0);
+        landed();
       }
       group_sync<G::GT>();
       int s = 0;
       for (; e < n; e += step) {
         const bool more = e + step < n;
+        // a stage of its own, or registers: the next tile's loads go out before this tile's work
+        constexpr bool ahead = P::STAGES == 2 || !G::DMA;
         if (more) {
           entry(e + step, sn, fulln);
-          fetch(sn);
+          if constexpr (ahead) fetch(s ^ 1, sn);
         }
-        if (full)
-          tile<false>(s, s0);
-        else
-          tile<true>(s, s0);
+        tile(s, s0, full);
         if constexpr (P::STAGES == 1) group_sync<G::GT>();
-        if (more) put(P::STAGES == 1 ? 0 : s ^ 1);
+        if (more) {
+          if constexpr (!ahead) fetch(0, sn);
+          put(P::STAGES == 1 ? 0 : s ^ 1);
+          landed();
+        }
         group_sync<G::GT>();
         if constexpr (P::STAGES == 2) s ^= 1;
         s0 = sn, full = fulln;
@@ -582,7 +720,7 @@ template <class P> struct Plane {
       constexpr int lo = abase(o) * 4, hi = abase(o + 1) * 4;
       if (at >= lo && at < hi) {
         const int dim = ((at - lo) / 4) * 32 + 8 * ((at - lo) % 4) + 4 * h;
-        if (own_ok && dim < P::sw(P::ost(o))) P::template store<o>(a, b, own, dim, mtrue, lsum, v);
+        if (own_ok() && dim < P::sw(P::ost(o))) P::template store<o>(a, b, own(), dim, mtrue * P::FOLD, lsum, v);
       }
     });
   }
@@ -593,7 +731,7 @@ template <class P> struct Plane {
     if constexpr (P::SOFTMAX) {
       lsum += __shfl_xor(lsum, 32, 64);
       // to the true maximum
-      const float f = mref == mtrue ? 1.0f : __builtin_amdgcn_exp2f((mref - mtrue) * kLog2e);
+      const float f = mref == mtrue ? 1.0f : __builtin_amdgcn_exp2f((mref - mtrue) * (P::FOLD * kLog2e));
       lsum *= f;
 #pragma unroll
       for (int d = 0; d < NA; ++d)
@@ -609,7 +747,7 @@ template <class P> struct Plane {
         store_group(g, v);
       }
       if constexpr (P::SOFTMAX)
-        if (own_ok && h == 0) P::stats(a, b, own, mtrue, lsum);
+        if (own_ok() && h == 0) P::stats(a, b, own(), mtrue * P::FOLD, lsum);
     } else {
       constexpr int NM = NGRP + 1;  // groups of four registers, then (m, l)
       float* lds = (float*)smem;
@@ -636,7 +774,7 @@ template <class P> struct Plane {
 #pragma unroll
           for (int v2 = 0; v2 < P::NW; ++v2) {
             const float mv = ml[v2 * 128 + lane];
-            f[v2] = mv == m ? 1.0f : __builtin_amdgcn_exp2f((mv - m) * kLog2e);
+            f[v2] = mv == m ? 1.0f : __builtin_amdgcn_exp2f((mv - m) * (P::FOLD * kLog2e));
             l += ml[v2 * 128 + 64 + lane] * f[v2];
           }
           mtrue = m, lsum = l;
@@ -696,7 +834,7 @@ template <class P> struct Plane {
           for (int zz = 0; zz < P::SPLIT; ++zz) m = k_max(m, mz[zz]);
 #pragma unroll
           for (int zz = 0; zz < P::SPLIT; ++zz) {
-            f[zz] = mz[zz] == m ? 1.0f : __builtin_amdgcn_exp2f((mz[zz] - m) * kLog2e);
+            f[zz] = mz[zz] == m ? 1.0f : __builtin_amdgcn_exp2f((mz[zz] - m) * (P::FOLD * kLog2e));
             l += lz[zz] * f[zz];
           }
           mtrue = m, lsum = l;
@@ -719,7 +857,7 @@ template <class P> struct Plane {
       for (int g = 0; g < share; ++g)
         if (g0 + g < NGRP) store_group(g0 + g, v[g]);
       if constexpr (P::SOFTMAX)
-        if (own_ok && h == 0 && (!P::WSPLIT || wave == 0)) P::stats(a, b, own, mtrue, lsum);
+        if (own_ok() && h == 0 && (!P::WSPLIT || wave == 0)) P::stats(a, b, own(), mtrue * P::FOLD, lsum);
     }
   }
 

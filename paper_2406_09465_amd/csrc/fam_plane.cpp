@@ -18,7 +18,6 @@
 //     statistics, a row statistic of the softmax, or a sum by bins of the plane.
 #include <algorithm>
 #include <cmath>
-#include <cstdlib>
 #include <memory>
 
 #include "families.h"
@@ -41,6 +40,7 @@ struct Operand {
   std::string key;          // identity of the address map
   std::string off;          // element offset of a row (variables b*, r)
   int root = -1;
+  int64_t stride = 0;       // elements from row to row
 };
 
 struct PlaneGen {
@@ -62,6 +62,16 @@ struct PlaneGen {
   int cond = -1;                      // mask
   double low = -INFINITY;
   std::vector<int> ovs, tvs, rvs;     // owned vectors, streamed vectors, streamed vectors whose range is read
+  // A gather whose table varies from batch entry to batch entry only, by an index
+  // computed on the plane (or a gather of such a gather): the values over the
+  // innermost index are a table of the workgroup's own, kept in LDS.
+  struct Lut {
+    int node, index;  // gather, plane node that indexes (innermost)
+    int64_t size;
+    int at;           // first element
+  };
+  std::vector<Lut> luts;
+  int64_t lut_size = 0;
   std::map<int, int> prod_of;         // output -> output product index
   std::map<int, bool> has_score_memo;
 
@@ -141,7 +151,10 @@ struct PlaneGen {
     const Node& n = nd(cur);
     auto st = strides_of(n.shape);
     Ix off = Ix::k(0);
-    for (size_t d = 0; d < n.shape.size(); ++d) off = ix_add(off, ix_mulk(idx[d], st[d], VL));
+    for (size_t d = 0; d < n.shape.size(); ++d) {
+      off = ix_add(off, ix_mulk(idx[d], st[d], VL));
+      if (idx[d].b == "r") o.stride = st[d];
+    }
     if (!off.affine || off.c != 1 || off.al % VL) {
       // alignment is known when every other stride is a multiple of the vector
       bool ok = off.affine && off.c == 1;
@@ -341,6 +354,7 @@ struct PlaneGen {
         if (s != want) bad("a row statistic's shape");
       }
     }
+    if (cond >= 0 && has_score(cond)) bad("a mask computed from scores");
     if (bin_node >= 0 && bin_out < 0) bad("a sum by bins that is not an output");
     for (size_t i = 0; i < outs_p.size(); ++i) {
       bool used = false;
@@ -385,11 +399,50 @@ struct PlaneGen {
     return e;
   }
 
+  // node = c tanh(a x) on the plane, each product optional.
+  bool tanh_chain(int node, int* x, double* a, double* c) const {
+    *a = *c = 1.0;
+    auto scaled = [&](int v) { return in(v) && nd(v).op == KORCH_MUL && nd(v).attrs.has_scalar && nd(v).shape == PS; };
+    int v = node;
+    if (scaled(v)) *c = nd(v).attrs.scalar, v = nd(v).in[0];
+    if (!in(v) || nd(v).op != KORCH_TANH || nd(v).shape != PS) return false;
+    v = nd(v).in[0];
+    if (scaled(v)) *a = nd(v).attrs.scalar, v = nd(v).in[0];
+    *x = v;
+    return true;
+  }
+
+  static constexpr int64_t kLutMost = 4096;  // floats of all tables: 16 KiB of LDS
+
+  // The table for gather `node`, or null.
+  const Lut* lut_for(int node) {
+    for (auto& l : luts)
+      if (l.node == node) return &l;
+    int v = node;
+    int64_t size = 0;
+    while (in(v) && nd(v).op == KORCH_GATHER) {
+      const int t = nd(v).in[0];
+      const Shape& ts = nd(t).shape;
+      if (in(t)) return nullptr;
+      // the table's leading dims: batch only (they align with the plane's, below its last axis)
+      const int lr = (int)ts.size() - 1;
+      if (lr > R || (lr >= 1 && ts[lr - 1] != 1) || (lr >= 2 && ts[lr - 2] != 1)) return nullptr;
+      size = ts.back();
+      v = nd(v).in[1];
+    }
+    if (v == node || cls(v) != FULLP || has_score(v) || lut_size + size > kLutMost) return nullptr;
+    luts.push_back({node, v, size, (int)lut_size});
+    lut_size += size;
+    return &luts.back();
+  }
+
   // Body of a function that evaluates plane nodes `want` into `dst`; `full`:
-  // the mask is known to hold.
+  // where the mask holds.
   std::string plane_body(const std::vector<std::pair<int, std::string>>& want, bool full) {
     auto it = plane_index();
     auto e = emitter();
+    int x0 = -1;
+    double ca = 1, cc = 1;
     e->provide = [&](int node, const std::vector<Ix>& idx, std::string* out) {
       for (size_t s = 0; s < scores.size(); ++s)
         if (node == scores[s]) {
@@ -401,8 +454,25 @@ struct PlaneGen {
         *out = "(1.0f)";
         return true;
       }
+      if (fast_math() && tanh_chain(node, &x0, &ca, &cc)) {
+        const std::string x = e->value(x0, broadcast_index(nd(x0).shape, PS, it));
+        *out = e->fresh("t");
+        e->body << "    const float " << *out << " = pl_ctanh(" << x << ", " << flit(ca) << ", " << flit(cc) << ");\n";
+        return true;
+      }
       const PlaneCls c = cls(node);
-      if (c == FULLP) return false;
+      if (c == FULLP) {
+        if (!in(node) || nd(node).op != KORCH_GATHER) return false;
+        if (Emitter::key(node, idx) != std_key(node, it)) return false;
+        const Lut* l = lut_for(node);
+        if (!l) return false;
+        const int at = l->at, index = l->index;
+        const int64_t size = l->size;
+        const std::string x = e->value(index, broadcast_index(nd(index).shape, PS, it));
+        *out = e->fresh("t");
+        e->body << "    const float " << *out << " = lut[" << at << " + (int)k_min(k_max(" << x << ", 0.0f), " << flit((double)(size - 1)) << ")];\n";
+        return true;
+      }
       if ((int)nd(node).shape.size() > R) return false;
       std::string k;
       try {
@@ -423,7 +493,11 @@ struct PlaneGen {
       const std::string v = e->value(node, broadcast_index(nd(node).shape, PS, it));
       e->body << "    " << dst << " = " << v << ";\n";
     }
-    return e->pre.str() + e->body.str();
+    std::string code = e->pre.str() + e->body.str();
+    // the exponential and tanh of scores: fewer instructions than the shared ones
+    for (auto& [from, to] : {std::pair<std::string, std::string>{" f_tanh(", " pl_tanh("}, {" f_exp(", " pl_exp("}})
+      for (size_t at = code.find(from); at != std::string::npos; at = code.find(from, at + to.size())) code.replace(at, from.size(), to);
+    return code;
   }
 
   // Value of a vector node at owned / streamed index variable `r`.
@@ -485,21 +559,21 @@ struct PlaneGen {
   }
 
   // Splits of the streamed axis and geometry.
-  int NW = 4, TS = 64, SPLIT = 1, STAGES = 2;
+  int NW = 4, TS = 64, SPLIT = 1, STAGES = 2, WPE = 1, OCC = 1;
   bool WSPLIT = false;
-  int64_t OTILES = 1, NB = 1;
+  int64_t OTILES = 1, NB = 1, TP = 1;
 
   size_t lds_bytes() const {
-    const int es = dtype_bytes(dtype), VL = 16 / es;
+    const int es = dtype_bytes(dtype);
     size_t tile = 0;
     int nreg = 0;
-    for (auto& w : streamed) tile += (size_t)TS * ((w.shape[0] + 31) / 32 * 32 + VL) * es;
+    for (auto& w : streamed) tile += (size_t)TS * ((w.shape[0] + 31) / 32 * 32) * es;
     for (auto& w : out_w) nreg += (int)((w.shape[0] + 31) / 32 * 32) / 2;
     tile += (size_t)tvs.size() * TS * 4;
     size_t tiles = tile * STAGES * (WSPLIT ? NW : 1);
     size_t merge = WSPLIT ? (size_t)NW * (nreg + 2) * 256 : 0;
     size_t bins = bin_node >= 0 ? (size_t)NW * nd(bin_node).shape.back() * 256 : 0;
-    return std::max(tiles, merge) + 4096 + (NW * ovs.size() * 2 + 8) * 4 + 80 + bins;
+    return std::max(tiles, merge) + 4096 + (NW * ovs.size() * 2 + 8) * 4 + 80 + (lut_size + 3) / 4 * 16 + bins;
   }
 
   void geometry() {
@@ -507,31 +581,55 @@ struct PlaneGen {
     for (int d = 0; d < R - 2; ++d) NB *= PS[d];
     const int64_t nown = rows_owned ? N : M, nstr = rows_owned ? M : N;
     const bool f32 = dtype == KORCH_F32;
-    int aw = 0, ow = 0;
-    for (auto& w : out_w) aw += (int)((w.shape[0] + 31) / 32 * 32);
-    for (auto& o : sc_own) ow += (int)((o.shape[0] + 31) / 32 * 32);
-    TS = 64;
-    NW = 4;
+    // Registers that live through the walk.  With up to 160 of them two waves fit
+    // a SIMD; one computes while the other loads, reduces or waits (n = m = 4096,
+    // head width 128, bf16: 363 us against 431 with one).  Gradients of the keys
+    // at width 128 hold 192: one wave per SIMD (730 us; two spill, 837).
+    int live = 0;
+    for (auto& w : out_w) live += (int)((w.shape[0] + 31) / 32 * 16);
+    for (auto& o : sc_own) live += (int)((o.shape[0] + 31) / 32 * 32 * dtype_bytes(dtype) / 8);
+    WPE = live > 160 || reg_relief() > 0 ? 1 : 2;
     // Few owned indices: the waves share them and split the streamed axis.
     WSPLIT = nown <= 32;
-    if (f32) TS = 32;
-    if (WSPLIT) STAGES = 1;
-    while (lds_bytes() > 160 * 1024 && TS > 32) TS /= 2;
-    while (lds_bytes() > 160 * 1024 && NW > 1) NW /= 2;
-    while (lds_bytes() > 160 * 1024 && STAGES > 1) STAGES = 1;
-    if (lds_bytes() > 160 * 1024) bad("operands exceed the 160 KiB of LDS");
+    // Streamed rows of a tile: 64, or 32 where registers are short (two score
+    // planes at two waves per SIMD: 406 us against 444; a wave's own tiles, whose
+    // rows it loads alone: 62 us against 210 for 16 caches of up to 8192, width 128).
+    TS = f32 || WSPLIT || (nm < 0 && WPE == 2) ? 32 : 64;
+    NW = 4;
+    STAGES = WSPLIT ? 1 : 2;
+    const size_t lds_most = 160 * 1024;
+    while (lds_bytes() > lds_most && TS > 32) TS /= 2;
+    while (lds_bytes() > lds_most && NW > 1) NW /= 2;
+    while (lds_bytes() > lds_most && STAGES > 1) STAGES = 1;
+    if (lds_bytes() > lds_most) bad("operands exceed the 160 KiB of LDS");
     const int OT = WSPLIT ? 32 : 32 * NW;
     OTILES = (nown + OT - 1) / OT;
+    OCC = (int)std::max<int64_t>(1, std::min<int64_t>(WPE * 4 / NW, (int64_t)(lds_most / lds_bytes())));
     const int64_t wgs = OTILES * NB, tiles = (nstr + TS - 1) / TS, per = WSPLIT ? NW : 1;
+    // Fewer workgroups than compute units split the streamed axis, until there
+    // are two for each or every one has a tile.  A split costs its partial
+    // results (about 15 us per 512 workgroups of 128 rows of width 128), so
+    // workgroups that fill the chip once only split when a mask of positions makes
+    // them unequal and they are long: 16 heads of 4096 causal rows of width 128
+    // take 133 us in two splits, 167 in one; 32 of 2048 rows 84 and 83.  (A mask
+    // that reads data, as documents do, leaves few tiles: 12 heads of 4000 rows
+    // 25.9 us in two splits, 24.0 in one.)
     SPLIT = 1;
-    if (workgroup_splits() && wgs < 256) {
-      // enough workgroups for two per compute unit, at least two tiles each
-      int64_t want = (512 + wgs - 1) / wgs;
-      want = std::min<int64_t>(want, std::max<int64_t>(1, tiles / (2 * per)));
-      SPLIT = (int)std::min<int64_t>(want, 32);
+    if (workgroup_splits()) {
+      if (wgs < 256)
+        SPLIT = (int)std::min<int64_t>(std::min<int64_t>((512 + wgs - 1) / wgs, std::max<int64_t>(1, tiles / per)), 32);
+      else if (cond >= 0 && rvs.empty() && wgs <= 256 * OCC && nstr >= 2560)
+        SPLIT = 2;
     }
-    if (wgs > (int64_t)1 << 30) bad("too many workgroups");
-    (void)aw, (void)ow;
+    if (wgs * SPLIT > (int64_t)1 << 30) bad("too many workgroups");
+    TP = OTILES;
+    // positions repeat along the rows when the heads of a group share them
+    for (int v : ki.k.prims) {
+      const Node& n = nd(v);
+      if (n.op != KORCH_IOTA || numel(n.shape) != nown || !rows_owned) continue;
+      const int64_t period = n.shape[n.axis];
+      if (period < nown && nown % period == 0 && period % OT == 0) TP = period / OT;
+    }
   }
 
   GenKernel generate(int index) {
@@ -543,19 +641,20 @@ struct PlaneGen {
     ki.assign_args(gk, slot);
     const std::string T = ctype(dtype);
     const bool softmax = nm >= 0;
-    // functions on the plane (both variants allocate the vectors they read)
-    std::string fn[2];
-    for (int full = 0; full < 2; ++full) {
-      std::vector<std::pair<int, std::string>> want;
-      if (softmax) {
-        want.push_back({nsfinal, "v"});
-        if (cond >= 0 && !full) want.push_back({cond, "const float kc_"});
-      } else {
-        for (size_t i = 0; i < xnodes.size(); ++i) want.push_back({xnodes[i], "out[" + std::to_string(i) + "]"});
-      }
-      fn[full] = plane_body(want, full != 0);
-      if (softmax && cond >= 0 && !full) fn[full] += "    k = kc_ != 0.0f;\n";
-    }
+    // functions on the plane where the mask holds, and the mask
+    std::vector<std::pair<int, std::string>> want;
+    // Scores that are only a product with a constant > 0: the maximum is taken of
+    // the products as they are and the constant enters the exponent's.
+    double fold = 1.0;
+    if (softmax && nsfinal != scores[0] && nd(nsfinal).op == KORCH_MUL && nd(nsfinal).attrs.has_scalar && nd(nsfinal).in[0] == scores[0] &&
+        nd(nsfinal).attrs.scalar > 1e-3 && nd(nsfinal).attrs.scalar < 1e3)
+      fold = nd(nsfinal).attrs.scalar;
+    if (softmax)
+      want.push_back({fold != 1.0 ? scores[0] : nsfinal, "const float v_"});
+    else
+      for (size_t i = 0; i < xnodes.size(); ++i) want.push_back({xnodes[i], "out[" + std::to_string(i) + "]"});
+    const std::string fn = plane_body(want, true) + (softmax ? "    return v_;\n" : "");
+    const std::string keep_fn = cond >= 0 ? plane_body({{cond, "const float k_"}}, false) + "    return k_ != 0.0f;\n" : "    return true;\n";
     std::string bin_fn;
     if (bin_node >= 0) bin_fn = plane_body({{nd(bin_node).in[1], "const float id_"}}, false);
     std::string mask_expr = cond >= 0 ? range(cond) : "";
@@ -567,12 +666,13 @@ struct PlaneGen {
     p << "  static constexpr bool SOFTMAX = " << softmax << ", MASK = " << (cond >= 0) << ", WSPLIT = " << WSPLIT << ";\n";
     p << "  static constexpr i64 NOWN = " << nown << "LL, NSTR = " << nstr << "LL;\n";
     p << "  static constexpr int NW = " << NW << ", TS = " << TS << ", STAGES = " << STAGES << ", SPLIT = " << SPLIT << ", OTILES = " << OTILES
-      << ", NB = " << NB << ";\n";
+      << ", NB = " << NB << ", TP = " << TP << ", OCC = " << OCC << ";\n  static constexpr bool LAST_FIRST = " << rows_owned << ";\n";
     const int64_t nbin = bin_node >= 0 ? nd(bin_node).shape.back() : 0;
     p << "  static constexpr int NSP = " << scores.size() << ", NST = " << streamed.size() << ", NOP = " << outs_p.size() << ", NX = "
       << std::max<size_t>(1, xnodes.size()) << ", NBIN = " << nbin << ", XBIN = " << std::max(0, xbin) << ";\n";
     p << "  static constexpr int NTAB = " << tvs.size() << ", NOV = " << ovs.size() << ", NRV = " << rvs.size() << ";\n";
-    p << "  static constexpr float MINIT = " << flit(softmax && cond >= 0 ? low : -INFINITY) << ";\n";
+    p << "  static constexpr float MINIT = " << flit(softmax && cond >= 0 ? low / fold : -INFINITY)
+      << ", FOLD = " << flit(fold) << ";\n";
     auto table = [&](const char* name, const std::vector<int>& v) {
       p << "  static constexpr int " << name << "(int i) {\n    constexpr int t[] = {";
       for (int x : v) p << x << ", ";
@@ -581,6 +681,12 @@ struct PlaneGen {
     std::vector<int> sw;
     for (auto& w : streamed) sw.push_back((int)w.shape[0]);
     table("sw", sw);
+    std::vector<int> rs;
+    for (auto& w : streamed) {
+      if (w.stride * TS * dtype_bytes(dtype) >= (int64_t)1 << 30) bad("rows too far apart");
+      rs.push_back((int)w.stride);
+    }
+    table("srs", rs);
     table("sst", sst);
     table("ost", ost);
     table("ox", ox);
@@ -629,13 +735,51 @@ struct PlaneGen {
     vectors("rvec", rvs, false);
     p << "  static __device__ __forceinline__ Range mask_range(const KArgs& a, const B& b, const Range* ow, const Range* rv, float s0, float s1) {\n";
     p << "    return " << (cond >= 0 ? mask_expr : "r_pt(1.0f)") << ";\n  }\n";
-    const char* sig = softmax ? "logit(const KArgs& a, const B& b, const float* ov, const float* tv, i64 ro, i64 rs, const float* xs, float& v, bool& k)"
-                              : "plane(const KArgs& a, const B& b, const float* ov, const float* tv, i64 ro, i64 rs, const float* xs, float* out)";
-    p << "  template <bool CHECK> static __device__ __forceinline__ void " << sig << " {\n    if constexpr (CHECK) {\n" << fn[0]
-      << "    } else {\n" << fn[1] << "    }\n  }\n";
+    const std::string sig = "(const KArgs& a, const B& b, const float* ov, const float* tv, const float* lut, i64 ro, i64 rs";
+    p << "  static __device__ __forceinline__ " << (softmax ? "float logit" : "void plane") << sig << ", const float* xs" << (softmax ? "" : ", float* out")
+      << ") {\n" << fn << "  }\n";
+    p << "  static __device__ __forceinline__ bool keep" << sig << ") {\n    const float xs[2] = {};\n" << keep_fn << "  }\n";
     if (bin_node >= 0)
-      p << "  static __device__ __forceinline__ float bin(const KArgs& a, const B& b, const float* ov, const float* tv, i64 ro, i64 rs) {\n"
+      p << "  static __device__ __forceinline__ float bin" << sig << ") {\n"
         << "    const float xs[2] = {};\n" << bin_fn << "    return k_min(k_max(id_, 0.0f), " << flit((double)(nbin - 1)) << ");\n  }\n";
+    p << "  static constexpr int LUT = " << lut_size << ";\n  static __device__ __forceinline__ float lut_value(const KArgs& a, const B& b, int k) {\n";
+    for (auto& l : luts) {
+      auto e = emitter();
+      e->provide = [&](int node, const std::vector<Ix>&, std::string* out) { return node == l.index ? (*out = "kf", true) : false; };
+      std::vector<Ix> it = plane_index();
+      it[R - 2] = it[R - 1] = Ix::k(0);  // the tables do not vary along them
+      std::vector<Ix> idx(nd(l.node).shape.size());
+      for (size_t d = 0; d < idx.size(); ++d) idx[d] = nd(l.node).shape[d] == 1 ? Ix::k(0) : it[d + R - idx.size()];
+      const std::string x = e->value(l.node, idx);
+      p << "    if (k < " << l.at + l.size << ") {\n    const float kf = (float)(k - " << l.at << ");\n" << e->pre.str() << e->body.str() << "    return " << x
+        << ";\n    }\n";
+    }
+    p << "    return 0.0f;\n  }\n";
+    if (bin_node >= 0) {
+      // range of the index whose table gives the bins, and the bins at the table's ends
+      const int id = nd(bin_node).in[1];
+      const Lut* l = nullptr;
+      for (auto& x : luts)
+        if (x.node == id) l = &x;
+      std::string r = "r_all()", first = "0.0f", last = "0.0f";
+      if (l) {
+        const size_t nr = rvs.size(), no = ovs.size();
+        std::string e = range(l->index);
+        if (rvs.size() == nr && ovs.size() == no) {
+          r = e;
+          first = "lut[" + std::to_string(l->at) + "]";
+          last = "lut[" + std::to_string(l->at + l->size - 1) + "]";
+        } else {  // its range needs a vector that the kernel does not hold
+          rvs.resize(nr);
+          ovs.resize(no);
+        }
+      }
+      p << "  static constexpr int BIN_T = " << (l ? l->size : 1) << ";\n";
+      p << "  static __device__ __forceinline__ Range bin_range(const KArgs& a, const B& b, const Range* ow, float s0, float s1) {\n    return "
+        << r << ";\n  }\n";
+      p << "  static __device__ __forceinline__ float bin_end(const float* lut, bool high) { return k_min(k_max(high ? " << last << " : " << first
+        << ", 0.0f), " << flit((double)(nbin - 1)) << "); }\n";
+    }
     // results
     p << "  template <int o> static __device__ __forceinline__ void store(const KArgs& a, const B& b, i64 ro, int dim, float m, float l, f32x4 v) {\n";
     for (size_t i = 0; i < outs_p.size(); ++i) {
@@ -714,11 +858,10 @@ struct PlaneGen {
     p << "};\n";
     std::ostringstream src;
     src << source_header((int)gk.args.size()) << k_device_plane << "\n" << p.str();
-    src << "extern \"C\" __global__ void __launch_bounds__(" << NW * 64 << ") " << gk.name << "(KArgs a) {\n";
+    src << "extern \"C\" __global__ void __launch_bounds__(" << NW * 64 << ") __attribute__((amdgpu_waves_per_eu(" << WPE << ", " << WPE << "))) " << gk.name << "(KArgs a) {\n";
     src << "  __shared__ __attribute__((aligned(16))) char smem[Geo<Pol>::bytes];\n  Plane<Pol> k(a, smem);\n  k.run();\n}\n";
     gk.source = src.str();
-    gk.grid[0] = (int)(OTILES * NB);
-    gk.grid[1] = SPLIT;
+    gk.grid[0] = (int)(OTILES * NB * SPLIT);
     gk.block[0] = NW * 64;
     gk.lds_bytes = (int)lds_bytes();
     ki.fill_cost(gk);
