@@ -28,7 +28,7 @@ from . import primitives as prim
 ELEMENTWISE_UNARY = set(prim.UNARY)
 ELEMENTWISE_BINARY = set(prim.BINARY)
 REDUCE = {"reduce_sum", "reduce_mean", "reduce_max"}
-LAYOUT = {"transpose", "reshape", "slice", "pad", "concat"}
+LAYOUT = {"transpose", "reshape", "slice", "pad", "concat", "iota", "gather"}
 LINEAR = {"matmul", "conv2d"}
 
 
@@ -112,8 +112,13 @@ class Graph:
             return tuple(int(e) - int(b) for b, e in zip(a["begin"], a["end"]))
         if op == "pad":
             return tuple(s + int(l) + int(h) for s, l, h in zip(sh[0], a["lo"], a["hi"]))
-        if op == "fill":
+        if op in ("fill", "iota", "bin_sum"):
             return tuple(int(d) for d in a["shape"])
+        if op == "select":
+            out = _broadcast_shapes(sh[0], sh[1])
+            return out if len(sh) == 2 else _broadcast_shapes(out, sh[2])
+        if op == "gather":
+            return _broadcast_shapes(sh[0][:-1], sh[1])
         if op == "concat":
             ax = a["axis"]
             out = list(sh[0])
@@ -176,6 +181,14 @@ def evaluate_node(g: Graph, i: int, args):
         return prim.concat(args, a["axis"])
     if op == "fill":
         return prim.fill(a["shape"], a["value"])
+    if op == "iota":
+        return prim.iota(a["shape"], a["axis"])
+    if op == "select":
+        return prim.select(args[0], args[1], args[2] if len(args) == 3 else a["scalar"])
+    if op == "gather":
+        return prim.gather(args[0], args[1])
+    if op == "bin_sum":
+        return prim.bin_sum(args[0], args[1], a["shape"])
     if op == "matmul":
         return prim.matmul(args[0], args[1])
     if op == "conv2d":

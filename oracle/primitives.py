@@ -58,7 +58,17 @@ BINARY = {
     "div": np.divide,
     "max": np.maximum,
     "min": np.minimum,
+    "lt": lambda x, y: (x < y).astype(np.float64),
+    "le": lambda x, y: (x <= y).astype(np.float64),
+    "gt": lambda x, y: (x > y).astype(np.float64),
+    "ge": lambda x, y: (x >= y).astype(np.float64),
+    "eq": lambda x, y: (x == y).astype(np.float64),
 }
+
+
+def select(c, x, y):
+    """x where c is not 0, else y (each broadcast)."""
+    return np.array(np.where(np.asarray(c) != 0, np.asarray(x, dtype=np.float64), np.asarray(y, dtype=np.float64)))
 
 
 def elementwise(op: str, operands, scalar=None):
@@ -138,6 +148,38 @@ def fill(shape, value):
     """A constant tensor (no operands): the ones tensor of the transformation that
     writes a sum over an axis as a product (Section 3)."""
     return np.full(tuple(int(d) for d in shape), np.float64(value))
+
+
+def iota(shape, axis):
+    """Every element's index along ``axis`` (no operands)."""
+    shape = tuple(int(d) for d in shape)
+    axis %= len(shape)
+    return np.array(np.broadcast_to(np.arange(shape[axis], dtype=np.float64).reshape((-1,) + (1,) * (len(shape) - 1 - axis)), shape))
+
+
+def _whole(idx, size):
+    """Whole numbers clamped to a table of ``size`` (NaN: 0)."""
+    return np.clip(np.nan_to_num(np.asarray(idx, dtype=np.float64), nan=0.0, posinf=size - 1, neginf=0.0), 0, size - 1).astype(np.int64)
+
+
+def gather(table, idx):
+    """O[x] = table[x', idx[x]]: x' is x seen by the table's leading dims (broadcast)."""
+    table, idx = np.asarray(table, dtype=np.float64), np.asarray(idx)
+    shape = np.broadcast_shapes(table.shape[:-1], idx.shape)
+    rows = np.broadcast_to(table, shape + table.shape[-1:])
+    return np.take_along_axis(rows, _whole(np.broadcast_to(idx, shape), table.shape[-1])[..., None], -1)[..., 0]
+
+
+def bin_sum(x, idx, shape):
+    """The gather's adjoint: sums of x by idx, over every dim where ``shape`` is 1 (or missing)."""
+    x = np.asarray(x, dtype=np.float64)
+    lead, size = tuple(int(d) for d in shape[:-1]), int(shape[-1])
+    k = _whole(np.broadcast_to(np.asarray(idx), x.shape), size)
+    out = np.zeros((1,) * (x.ndim - len(lead)) + lead + (size,))
+    for at in np.ndindex(x.shape):
+        to = tuple(i if n != 1 else 0 for i, n in zip(at, out.shape[:-1]))
+        out[to + (k[at],)] += x[at]
+    return out.reshape(tuple(int(d) for d in shape))
 
 
 # ----------------------------------------------------------------------------

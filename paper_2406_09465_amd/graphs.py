@@ -391,20 +391,27 @@ class _Attention:
             b.inp("bucket", (2 * radius + 1,), "f32")
             b.inp("table", (self.heads, buckets))
         # positions of keys and queries (the last n positions in use)
-        self.op("key", "iota", [], shape=(1, self.m), axis=1)
-        self.op("row", "iota", [], shape=(self.group, self.n) if self.fold else (1, self.n), axis=1)
-        self.op("row_i", "reshape", ["row"], shape=(self.rows, 1))
+        if causal or slopes or buckets or lengths:
+            self.op("key", "iota", [], shape=(1, self.m), axis=1)
         if lengths:
             end = self.view("end", "lengths", (self.batch,) + ones + (1, 1), "f32")
-            self.op("first", "sub", [end], scalar=float(self.n))
-            self.op("pos", "add", ["row_i", "first"])
             # rows of K and V past a sequence's length are read as zeros
             self.op("key_r", "iota", [], shape=(self.m, 1), axis=0)
             self.op("used", "lt", ["key_r", end])
-        elif self.m != self.n:
-            self.op("pos", "add", ["row_i"], scalar=float(self.m - self.n))
-        else:
-            self.b.ids["pos"] = self.b.ids["row_i"]
+        if causal or slopes or buckets or documents:
+            pos = "row" if self.m == self.n and not lengths and not self.fold else "row_i"
+            if self.fold:
+                self.op("row", "iota", [], shape=(self.group, self.n), axis=1)
+                self.op("row_i", "reshape", ["row"], shape=(self.rows, 1))
+            else:
+                self.op(pos, "iota", [], shape=(self.n, 1), axis=0)
+            if lengths:
+                self.op("first", "sub", [end], scalar=float(self.n))
+                self.op("pos", "add", [pos, "first"])
+            elif self.m != self.n:
+                self.op("pos", "add", [pos], scalar=float(self.m - self.n))
+            else:
+                self.b.ids["pos"] = self.b.ids[pos]
         if slopes or buckets:
             self.op("rel", "sub", ["key", "pos"])
         mask = None
@@ -426,7 +433,7 @@ class _Attention:
             self.op("docq", "gather", [tab, "pos"])
             both(self.op("samedoc", "eq", ["docq", doc]))
         if lengths:
-            both(self.op("inuse", "lt", ["key", "end" if "end" in self.b.ids else "lengths"]))
+            both(self.op("inuse", "lt", ["key", end]))
         self.mask = mask
         self.lengths, self.slopes, self.buckets = lengths, slopes, buckets
 

@@ -144,3 +144,232 @@ def test_attention_gradient(case):
     _, s["O"] = ref.rounded(out["O"], sizes["dtype"])
     s["L"] = out["L"].astype(np.float32)
     _check(_run(graphs.build("mha_grad", **sizes), s), want, sizes["dtype"])
+
+
+@pytest.mark.parametrize("case", [c for c in GRAD if c["n"] * c.get("m", c["n"]) <= 70 * 300 and c.get("m", c["n"]) > 1],
+                         ids=lambda c: "-".join(f"{k}{v}" for k, v in c.items() if k != "lengths"))
+def test_one_kernel_per_primitive(case):
+    """The unfused plans store every tensor: sixteen-bit products and fp32 planes
+    as the graph says, so the same bounds hold."""
+    sizes, x, s, want = _unpack(case, grad=True)
+    out = _run(graphs.build("mha", **sizes), s, "unfused")
+    _check(out, want, sizes["dtype"], ("L",))
+    _, s["O"] = ref.rounded(out["O"], sizes["dtype"])
+    s["L"] = out["L"].astype(np.float32)
+    _check(_run(graphs.build("mha_grad", **sizes), s, "unfused"), want, sizes["dtype"])
+
+
+PRIMITIVES = [
+    ("lt", [(5, 1, 7), (6, 1)], {}), ("le", [(40, 3), (3,)], {}), ("gt", [(33,), (33,)], {}), ("ge", [(4, 9), (4, 1)], {}),
+    ("eq", [(5, 8), (5, 8)], {}), ("lt", [(9, 5)], dict(scalar=1.0)), ("select", [(4, 1, 6), (5, 6), (1, 1, 6)], {}),
+    ("select", [(3, 8), (3, 8)], dict(scalar=-2.5)), ("iota", [], dict(shape=(5, 7), axis=0)), ("iota", [], dict(shape=(3, 2, 9), axis=-1)),
+    ("gather", [(4, 1, 1, 6), (5, 7)], {}), ("gather", [(9,), (2, 3, 8)], {}), ("gather", [(2, 3, 1, 5), (2, 1, 4)], {}),
+    ("bin_sum", [(3, 4, 5, 7), (5, 7)], dict(shape=(4, 1, 1, 6))), ("bin_sum", [(6, 50), (6, 50)], dict(shape=(9,))),
+    ("bin_sum", [(2, 300, 40), (300, 1)], dict(shape=(2, 1, 1, 33))),
+]
+
+
+@pytest.mark.parametrize("op,shapes,attrs", PRIMITIVES, ids=str)
+def test_primitive_kernels(op, shapes, attrs):
+    """Every new primitive's own kernel against the oracle (NaN and values outside
+    a table among the indices)."""
+    from oracle import primitives as prim
+    rng = np.random.default_rng(5)
+    x = [rng.integers(-2, 8, s).astype(np.float64) for s in shapes]
+    for i in ([1] if op in ("gather", "bin_sum") else []):
+        x[i].reshape(-1)[0], x[i].reshape(-1)[-1] = np.nan, 1e30
+    if op in ("gather", "bin_sum"):
+        x[0] = ref.rounded(rng.normal(size=shapes[0]), "f32")[0]
+    w = graphs.layout_probe(op, "f32", shapes, **attrs)
+    got = _run(w, {f"in{i}": v.astype(np.float32) for i, v in enumerate(x)}, "unfused")["out"]
+    if op in ("lt", "le", "gt", "ge", "eq"):
+        want = prim.elementwise(op, x, attrs.get("scalar"))
+    elif op == "select":
+        want = prim.select(*x, *([attrs["scalar"]] if "scalar" in attrs else []))
+    elif op == "iota":
+        want = prim.iota(**attrs)
+    elif op == "gather":
+        want = prim.gather(*x)
+    else:
+        want = prim.bin_sum(*x, attrs["shape"])
+        # fp32 sums of at most x.size terms
+        assert np.max(np.abs(got - want)) <= x[0].size * 2.0 ** -24 * np.abs(x[0]).sum()
+        return
+    assert np.array_equal(got, want)
+
+
+def test_rows_that_the_mask_leaves_empty():
+    """Lengths of 0 and of fewer positions than queries: rows without a key are
+    zeros with zero gradients, the others are what they are alone."""
+    case = dict(dtype="f16", n=40, m=64, d=64, heads=4, kv_heads=2, lengths=(0, 7, 64), batch=3, causal=True)
+    sizes, x, s, want = _unpack(case, grad=True)
+    out = _run(graphs.build("mha", **sizes), s)
+    _check(out, want, "f16", ("L",))
+    assert np.all(out["O"][0] == 0) and np.all(out["L"][0] == 0) and np.all(out["O"][1, :, :33] == 0)
+    _, s["O"] = ref.rounded(out["O"], "f16")
+    s["L"] = out["L"].astype(np.float32)
+    out = _run(graphs.build("mha_grad", **sizes), s)
+    _check(out, want, "f16")
+    assert np.all(out["dQ"][0] == 0) and np.all(out["dK"][0] == 0) and np.all(out["dV"][1, :, 7:] == 0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 5, 70])
+def test_whatever_lies_behind_a_sequence(dtype, n):
+    """K and V past a sequence's length hold NaN, infinities and the type's lowest
+    values: the results are those of zeros there, and their gradients are zero."""
+    case = dict(dtype=dtype, n=n, m=150, d=64, heads=4, kv_heads=2, lengths=(70, 133), batch=2, causal=True, cap=8.0)
+    sizes, x, s, want = _unpack(case, grad=True)
+    bad = {"f32": np.array([np.nan, np.inf, -np.inf, np.finfo(np.float32).min], np.float32),
+           "bf16": np.array([0x7FC0, 0x7F80, 0xFF80, 0xFF7F], np.uint16)}[dtype]
+    for k in ("K", "V"):
+        for b, size in enumerate((70, 133)):
+            rows = s[k][b, :, size:]
+            rows[...] = np.resize(bad, rows.shape)
+    out = _run(graphs.build("mha", **sizes), s)
+    _check(out, want, dtype, ("L",))
+    _, s["O"] = ref.rounded(out["O"], dtype)
+    s["L"] = out["L"].astype(np.float32)
+    out = _run(graphs.build("mha_grad", **sizes), s)
+    _check(out, want, dtype)
+    assert np.all(out["dK"][0, :, 70:] == 0) and np.all(out["dV"][1, :, 133:] == 0)
+
+
+def test_large_scores():
+    """Scores in the hundreds, either sign, growing along the keys: the running
+    maximum moves in every tile."""
+    for dtype in ("f32", "f16"):
+        case = dict(dtype=dtype, n=64, m=400, d=64, heads=2)
+        sizes, x, s, _ = _unpack(case)
+        x["K"], s["K"] = ref.rounded(x["K"] * np.linspace(0.1, 40, 400)[None, None, :, None], dtype)
+        want = ref.attention(x, dtype, 2, 2)
+        _check(_run(graphs.build("mha", **sizes), s), want, dtype, ("L",))
+
+
+def _bits(t):
+    import torch
+    return t.view(torch.int32 if t.element_size() == 4 else torch.int16).cpu().numpy().copy()
+
+
+REPEAT = [
+    ("layernorm_grad", dict(m=700, d=768, dtype="f16")),
+    ("mha", dict(batch=2, heads=8, kv_heads=2, n=1, m=3000, d=64, dtype="bf16", lengths=True)),
+    ("mha", dict(heads=2, n=300, m=1500, d=128, dtype="f16", causal=True)),
+    ("mha_grad", dict(batch=2, heads=4, kv_heads=4, n=200, d=64, dtype="f16", radius=30, buckets=16)),
+]
+
+
+def _random_runner(name, sizes, seed=0, plan="fused"):
+    import torch
+    from paper_2406_09465_amd.runner import TORCH_DTYPE, PlanRunner
+    w = graphs.build(name, **sizes)
+    r = PlanRunner(w, plan)
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    for k, i in zip(w.input_names, w.graph.inputs()):
+        _, dt, shape = w.graph.node_info(i)
+        if k == "lengths":
+            t = torch.linspace(1, sizes["m"], sizes["batch"], device="cuda").round()
+        elif k == "bucket":
+            t = torch.from_numpy(ref.bucket_map(sizes["radius"], sizes["buckets"])).float().cuda()
+        else:
+            t = torch.randn(shape, generator=gen, device="cuda")
+        r.ins.append(t.to(TORCH_DTYPE[dt]).contiguous())
+    return r.bind()
+
+
+@pytest.mark.parametrize("name,sizes", REPEAT, ids=str)
+def test_same_bits_again_on_another_stream_and_replayed(name, sizes):
+    """Hand-overs between workgroups are in a fixed order: every execution gives
+    the same bits, on a stream of its own, allocation-free and as a replayed graph
+    with eager work between the replays."""
+    import torch
+    from paper_2406_09465_amd._abi import pointer_array
+    r = _random_runner(name, sizes)
+    r.launch_bound()
+    torch.cuda.synchronize()
+    first = [_bits(t) for t in r.outs]
+
+    def same(outs=None):
+        torch.cuda.synchronize()
+        for a, b in zip(first, outs or r.outs):
+            assert np.array_equal(a, _bits(b))
+        for t in outs or r.outs:
+            t.fill_(7)
+
+    same()
+    for _ in range(3):
+        r.launch_bound()
+        same()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    r.launch(s)
+    same()
+    other = [torch.empty_like(t) for t in r.outs]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        r.launch(torch.cuda.current_stream())
+    for _ in range(3):
+        g.replay()
+        same()
+        r.bind().launch_bound()
+        same()
+    if r.plan.workspace_bytes() < 30e6:
+        unsplit = r.plan
+        unsplit.execute_noalloc(pointer_array([t.data_ptr() for t in r.ins]), pointer_array([t.data_ptr() for t in other]),
+                                torch.cuda.current_stream().cuda_stream)
+        same(other)
+
+
+def test_a_cache_past_32_bits():
+    """Keys and values of 5.4 GB each: the last sequence lies behind 2^32 bytes."""
+    import torch
+    from paper_2406_09465_amd.runner import PlanRunner
+    batch, m, d = 5, 4194304 // 2, 256
+    w = graphs.build("mha", batch=batch, heads=2, kv_heads=1, n=1, m=m, d=d, dtype="f16", lengths=True)
+    r = PlanRunner(w, "fused")
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    kv = [torch.zeros(batch, 1, m, d, dtype=torch.float16, device="cuda") for _ in range(2)]
+    q = torch.randn(batch, 2, 1, d, generator=gen, device="cuda").half()
+    size = 900
+    for t in kv:
+        t[-1, 0, :size] = torch.randn(size, d, generator=gen, device="cuda").half()
+        t[-1, 0, size:] = float("nan")
+    lengths = torch.tensor([1.0, 1.0, 1.0, 1.0, float(size)], device="cuda")
+    r.ins = [q, kv[0], kv[1], lengths]
+    r.launch()
+    torch.cuda.synchronize()
+    x = dict(Q=q[-1:].double().cpu().numpy(), K=kv[0][-1:, :, :size].double().cpu().numpy(), V=kv[1][-1:, :, :size].double().cpu().numpy())
+    want = ref.attention(x, "f16", 2, 1)
+    for out, k in zip(r.outs, ("O", "L")):
+        assert ref.outside(out[-1:].double().cpu().numpy(), *want[k], "f32" if k == "L" else "f16") <= 1.0
+
+
+def test_a_layer_in_training():
+    """LayerNorm, attention over its result and both gradients, chained as a
+    training step runs them, in fp32 against float64 (the plans' fp32 tolerance)."""
+    from .helpers import TOL, close
+    rng = np.random.default_rng(9)
+    b, h, n, d = 2, 3, 90, 32
+    rows, width = b * n, h * d
+    X, sX = ref.rounded(rng.normal(0.2, 1.3, (rows, width)), "f32")
+    gamma, sg = ref.rounded(rng.normal(1, 0.1, width), "f32")
+    beta, sb = ref.rounded(rng.normal(0, 0.1, width), "f32")
+    dO, sdO = ref.rounded(rng.normal(0, 1, (b, h, n, d)), "f32")
+    heads = lambda y: np.ascontiguousarray(y.reshape(b, n, h, d).transpose(0, 2, 1, 3))  # noqa: E731
+    flat = lambda y: np.ascontiguousarray(y.transpose(0, 2, 1, 3)).reshape(rows, width)  # noqa: E731
+    f32 = lambda y: np.asarray(y, dtype=np.float32)  # noqa: E731
+    ln = _run(graphs.build("layernorm", m=rows, d=width, dtype="f32"), dict(X=sX, gamma=sg, beta=sb))
+    y = heads(f32(ln["Y"]))
+    sizes = dict(batch=b, heads=h, n=n, d=d, dtype="f32", causal=True)
+    at = _run(graphs.build("mha", **sizes), dict(Q=y, K=y, V=y))
+    gr = _run(graphs.build("mha_grad", **sizes), dict(Q=y, K=y, V=y, dO=sdO, O=f32(at["O"]), L=f32(at["L"])))
+    dY = f32(flat(gr["dQ"] + gr["dK"] + gr["dV"]))
+    back = _run(graphs.build("layernorm_grad", m=rows, d=width, dtype="f32"),
+                dict(X=sX, gamma=sg, mu=f32(ln["mu"]), r=f32(ln["r"]), dY=dY))
+    w = ref.layernorm(X, gamma, beta, np.zeros_like(X), 1e-5, "f32")
+    yw = heads(w["Y"][0])
+    a = ref.attention(dict(Q=yw, K=yw, V=yw, dO=dO), "f32", h, h, causal=True, grad=True)
+    w = ref.layernorm(X, gamma, beta, flat(a["dQ"][0] + a["dK"][0] + a["dV"][0]), 1e-5, "f32")
+    for k in ("dX", "dgamma", "dbeta"):
+        ok, mx, rel = close(back[k], w[k][0], TOL["f32"])
+        assert ok, (k, mx, rel)
