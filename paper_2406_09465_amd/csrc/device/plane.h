@@ -62,7 +62,7 @@ template <class P> struct Geo {
   static constexpr int GT = P::WSPLIT ? 64 : NT;        // threads that share a streamed tile
   static constexpr int NG = P::WSPLIT ? P::NW : 1;      // such groups
   static constexpr int OT = P::WSPLIT ? 32 : 32 * P::NW;  // owned indices of the workgroup
-  static constexpr bool DMA = !P::WSPLIT;               // tiles go straight to LDS
+  static constexpr bool DMA = P::DMA;                   // tiles go straight to LDS
   static constexpr int NSUB = P::TS / 32;
   static constexpr int width(int t) { return round_up(P::sw(t), 32); }
   // Rows lie back to back; a row's 16-byte chunk c is stored at chunk c ^ swz(row).
@@ -262,11 +262,13 @@ template <class P> struct Plane {
     }
     return in ? (unsigned)(row * P::srs(t) * (int)sizeof(T) + c * 16) : 0x80000000u;
   }
-  // DMA (the workgroup shares a tile): straight into the LDS of stage s, 64
+  // DMA: straight into the LDS of stage s, 64
   // consecutive chunks per instruction; a lane fetches the chunk that its place
-  // holds.  The workgroup waits for the loads before its next barrier (landed()).
+  // holds.  Its wave waits for the loads before the tile is shared (landed()).
   // Otherwise into registers, and from there to LDS when the tile before has been read.
   __device__ __forceinline__ void fetch(int s, i64 s0) {
+    // a wave alone has no barrier between its last reads of the stage and the loads that overwrite it
+    if constexpr (G::DMA && G::GT == 64) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     static_for<P::NST>([&](auto ti) {
       constexpr int t = decltype(ti)::value;
       const i32x4 rs = tile_rows<t>(s0);
@@ -274,12 +276,14 @@ template <class P> struct Plane {
         constexpr int CH = G::chunks(t), NI = P::TS * CH / 64;
         typedef __attribute__((address_space(3))) char lds_char;
         const unsigned to = (unsigned)(unsigned long long)(lds_char*)(stage(s) + G::tile_off(t));
+        constexpr int NWG = G::GT / 64;  // waves that share the tile
+        const int me = NWG > 1 ? wave : 0;
 #pragma unroll
-        for (int i = 0; i < NI; i += P::NW) {
-          if (NI % P::NW == 0 || i + wave < NI) {
-            const int u = (i + wave) * 64 + lane, row = u / CH, c = (u % CH) ^ G::template swz<t>(row);
+        for (int i = 0; i < NI; i += NWG) {
+          if (NI % NWG == 0 || i + me < NI) {
+            const int u = (i + me) * 64 + lane, row = u / CH, c = (u % CH) ^ G::template swz<t>(row);
             const unsigned off = tile_offset<t>(s0, row, c, c < P::sw(t) / VL);
-            const unsigned la = __builtin_amdgcn_readfirstlane(to + (i + wave) * 1024);
+            const unsigned la = __builtin_amdgcn_readfirstlane(to + (i + me) * 1024);
             // (the descriptor may come straight from vector instructions: five wait states)
             asm volatile("s_mov_b32 m0, %1\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %2, 0 offen lds" ::"v"(off), "s"(la), "s"(rs) : "memory", "m0");
           }

@@ -560,7 +560,7 @@ struct PlaneGen {
 
   // Splits of the streamed axis and geometry.
   int NW = 4, TS = 64, SPLIT = 1, STAGES = 2, WPE = 1, OCC = 1;
-  bool WSPLIT = false;
+  bool WSPLIT = false, DMA = true;
   int64_t OTILES = 1, NB = 1, TP = 1;
 
   size_t lds_bytes() const {
@@ -596,7 +596,14 @@ struct PlaneGen {
     // rows it loads alone: 62 us against 210 for 16 caches of up to 8192, width 128).
     TS = f32 || WSPLIT || (nm < 0 && WPE == 2) ? 32 : 64;
     NW = 4;
-    STAGES = WSPLIT ? 1 : 2;
+    // Tiles go straight to LDS, into a second stage while the first is read.  A
+    // wave's own tiles pass through its registers instead, as long as it has
+    // them: with one stage two workgroups fit a compute unit's LDS, and their
+    // loads keep twice the bytes in flight.
+    int staging = 0;
+    for (auto& w : streamed) staging += (int)(TS * w.shape[0] * dtype_bytes(dtype) / 256);
+    DMA = !WSPLIT || live + staging > 224;
+    STAGES = DMA ? 2 : 1;
     const size_t lds_most = 160 * 1024;
     while (lds_bytes() > lds_most && TS > 32) TS /= 2;
     while (lds_bytes() > lds_most && NW > 1) NW /= 2;
@@ -663,7 +670,7 @@ struct PlaneGen {
     std::ostringstream p;
     const int64_t nown = rows_owned ? N : M, nstr = rows_owned ? M : N;
     p << "struct Pol {\n  typedef " << T << " T;\n  struct B {\n    i64 c[" << std::max(1, R - 2) << "];\n  };\n";
-    p << "  static constexpr bool SOFTMAX = " << softmax << ", MASK = " << (cond >= 0) << ", WSPLIT = " << WSPLIT << ";\n";
+    p << "  static constexpr bool SOFTMAX = " << softmax << ", MASK = " << (cond >= 0) << ", WSPLIT = " << WSPLIT << ", DMA = " << DMA << ";\n";
     p << "  static constexpr i64 NOWN = " << nown << "LL, NSTR = " << nstr << "LL;\n";
     p << "  static constexpr int NW = " << NW << ", TS = " << TS << ", STAGES = " << STAGES << ", SPLIT = " << SPLIT << ", OTILES = " << OTILES
       << ", NB = " << NB << ", TP = " << TP << ", OCC = " << OCC << ";\n  static constexpr bool LAST_FIRST = " << rows_owned << ";\n";
