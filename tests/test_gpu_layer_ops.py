@@ -373,3 +373,25 @@ def test_a_layer_in_training():
     for k in ("dX", "dgamma", "dbeta"):
         ok, mx, rel = close(back[k], w[k][0], TOL["f32"])
         assert ok, (k, mx, rel)
+
+
+@pytest.mark.parametrize("workload,sizes", [
+    ("attention", dict(n=1024, d=64, dtype="f16")), ("attention", dict(n=300, d=40, nk=700, dtype="bf16")),
+    ("attention", dict(n=70, d=128, nk=256, dtype="f32")), ("attention", dict(n=1, d=64, nk=1000, dtype="f16")),
+    ("sra", dict(hh=136, ww=136, c=64, r=8, dtype="f16")), ("sra", dict(hh=160, ww=128, c=32, r=4, dtype="bf16")),
+], ids=str)
+def test_workloads_past_the_keys_that_fit_lds(workload, sizes):
+    """The workloads' fused plans with more keys than one workgroup's LDS holds."""
+    from oracle import configs as OC
+    from oracle.graph import run_unfused
+    from synthetic import storage_to_f64
+    from synthetic import workloads as W
+
+    from .helpers import TOL, close
+    w = graphs.build(workload, **sizes)
+    assert w.graph.family(*w.kernels("fused")[-1]) == "plane"
+    raw = W.inputs(workload, **sizes)
+    want = run_unfused(OC.build(workload, **{k: v for k, v in sizes.items()}), {k: storage_to_f64(v, sizes["dtype"]) for k, v in raw.items()})
+    got = _run(w, raw)
+    ok, mx, rel = close(got["O"], want["O"], TOL[sizes["dtype"]])
+    assert ok, (mx, rel)
