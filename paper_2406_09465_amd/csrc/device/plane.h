@@ -843,18 +843,29 @@ template <class P> struct Plane {
           }
           mtrue = m, lsum = l;
         }
+// up to 32 vectors of partial results in flight: a round trip to the
+        // device's point of coherence is 1 to 2 us
+        constexpr int ZB = share >= 32 ? 1 : P::SPLIT < 32 / share ? P::SPLIT : 32 / share;
 #pragma unroll
-        for (int g = 0; g < share; ++g) {
-          if (g0 + g >= NGRP) continue;
-          f32x4 s = {};
+        for (int g = 0; g < share; ++g) v[g] = f32x4{};
 #pragma unroll
-          for (int zz = 0; zz < P::SPLIT; ++zz) {
-            const float4 q = coherent_load4(rs, at(zz, g0 + g));
-            const f32x4 x = {q.x, q.y, q.z, q.w};
-            if constexpr (P::SOFTMAX) s += x * f[zz];
-            else s += x;
+        for (int z0 = 0; z0 < P::SPLIT; z0 += ZB) {
+          float4 q[ZB][share];
+#pragma unroll
+          for (int zz = 0; zz < ZB; ++zz)
+#pragma unroll
+            for (int g = 0; g < share; ++g)
+              q[zz][g] = coherent_load4(rs, at(z0 + zz < P::SPLIT ? z0 + zz : P::SPLIT - 1, g0 + g < NGRP ? g0 + g : NGRP - 1));
+#pragma unroll
+          for (int zz = 0; zz < ZB; ++zz) {
+            if (z0 + zz >= P::SPLIT) continue;
+#pragma unroll
+            for (int g = 0; g < share; ++g) {
+              const f32x4 x = {q[zz][g].x, q[zz][g].y, q[zz][g].z, q[zz][g].w};
+              if constexpr (P::SOFTMAX) v[g] += x * f[z0 + zz];
+              else v[g] += x;
+            }
           }
-          v[g] = s;
         }
       }
 #pragma unroll

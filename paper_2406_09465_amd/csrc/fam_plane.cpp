@@ -576,10 +576,16 @@ struct PlaneGen {
     return std::max(tiles, merge) + 4096 + (NW * ovs.size() * 2 + 8) * 4 + 80 + (lut_size + 3) / 4 * 16 + bins;
   }
 
-  void geometry() {
-    NB = 1;
-    for (int d = 0; d < R - 2; ++d) NB *= PS[d];
-    const int64_t nown = rows_owned ? N : M, nstr = rows_owned ? M : N;
+  // A vector that depends on a stored tensor (positions do not).
+  bool reads_data(int v) const {
+    if (!in(v)) return true;
+    for (int u : nd(v).in)
+      if (reads_data(u)) return true;
+    return false;
+  }
+
+  // Tiles, waves and LDS for workgroups whose waves share tiles or (ws) split the streamed axis.
+  void layout(bool ws) {
     const bool f32 = dtype == KORCH_F32;
     // Registers that live through the walk.  With up to 160 of them two waves fit
     // a SIMD; one computes while the other loads, reduces or waits (n = m = 4096,
@@ -589,11 +595,10 @@ struct PlaneGen {
     for (auto& w : out_w) live += (int)((w.shape[0] + 31) / 32 * 16);
     for (auto& o : sc_own) live += (int)((o.shape[0] + 31) / 32 * 32 * dtype_bytes(dtype) / 8);
     WPE = live > 160 || reg_relief() > 0 ? 1 : 2;
-    // Few owned indices: the waves share them and split the streamed axis.
-    WSPLIT = nown <= 32;
+    WSPLIT = ws;
     // Streamed rows of a tile: 64, or 32 where registers are short (two score
     // planes at two waves per SIMD: 406 us against 444; a wave's own tiles, whose
-    // rows it loads alone: 62 us against 210 for 16 caches of up to 8192, width 128).
+    // rows it loads alone: 62 us against 75 for 16 caches of up to 8192, width 128).
     TS = f32 || WSPLIT || (nm < 0 && WPE == 2) ? 32 : 64;
     NW = 4;
     // Tiles go straight to LDS, into a second stage while the first is read.  A
@@ -609,24 +614,55 @@ struct PlaneGen {
     while (lds_bytes() > lds_most && NW > 1) NW /= 2;
     while (lds_bytes() > lds_most && STAGES > 1) STAGES = 1;
     if (lds_bytes() > lds_most) bad("operands exceed the 160 KiB of LDS");
+    OCC = (int)std::max<int64_t>(1, std::min<int64_t>(WPE * 4 / NW, (int64_t)(lds_most / lds_bytes())));
+  }
+
+  void geometry() {
+    NB = 1;
+    for (int d = 0; d < R - 2; ++d) NB *= PS[d];
+    const int64_t nown = rows_owned ? N : M, nstr = rows_owned ? M : N;
+    // Few owned indices: the waves of a workgroup share 32 of them and split the
+    // streamed axis, joined through LDS (more waves at work, no barrier between
+    // tiles; every wave loads its own tiles).  Up to one and a half such
+    // workgroups for each that the chip holds: 4 heads of 2048 x 2048, width 64,
+    // fp16, half as many, forward 17 us, gradients 18 and 22 (shared tiles 21, 26
+    // and 32); 12 heads, one and a half times, 36, 41 and 48 (34, 43 and 57); 8
+    // heads of width 128, whose gradients take a compute unit each, twice as many
+    // 64 and 79 (51 and 73).
+    layout(true);
+    if ((nown + 31) / 32 * NB > 384 * OCC) layout(false);
     const int OT = WSPLIT ? 32 : 32 * NW;
     OTILES = (nown + OT - 1) / OT;
-    OCC = (int)std::max<int64_t>(1, std::min<int64_t>(WPE * 4 / NW, (int64_t)(lds_most / lds_bytes())));
     const int64_t wgs = OTILES * NB, tiles = (nstr + TS - 1) / TS, per = WSPLIT ? NW : 1;
-    // Fewer workgroups than compute units split the streamed axis, until there
-    // are two for each or every one has a tile.  A split costs its partial
-    // results (about 15 us per 512 workgroups of 128 rows of width 128), so
-    // workgroups that fill the chip once only split when a mask of positions makes
-    // them unequal and they are long: 16 heads of 4096 causal rows of width 128
-    // take 133 us in two splits, 167 in one; 32 of 2048 rows 84 and 83.  (A mask
-    // that reads data, as documents do, leaves few tiles: 12 heads of 4000 rows
-    // 25.9 us in two splits, 24.0 in one.)
+    // The streamed axis is split over workgroups where that shortens the walk by
+    // more than the hand-over takes: about 1.5 us, and the partial results, which
+    // pass the device's point of coherence at about 0.8 TB/s (written and read).
+    // A tile of 32 takes a wave about 0.3 us and 3.3 ns per column of all products
+    // (16-bit; 20 ns in fp32).  Splits beyond the workgroups that are resident at
+    // once gain nothing (2048 x 2048, one head of 128, fp16: 13.9 us in 4 splits,
+    // 22.6 in one, 19.4 in 8), unless a mask of positions makes them unequal: then
+    // up to twice as many (keys' gradient of 8 key heads of 2048 causal positions
+    // with four query heads each, width 128: 146 us in 4 splits, 203 in 2).
     SPLIT = 1;
+    bool uneven = cond >= 0;
+    for (int v : rvs) uneven = uneven && !reads_data(v);
+    int64_t pcols = 0, acols = 0;
+    for (auto& o : sc_own) pcols += o.shape[0];
+    for (auto& w : out_w) pcols += w.shape[0], acols += (w.shape[0] + 31) / 32 * 32;
+    const double t_tile = (0.3 + (dtype == KORCH_F32 ? 0.02 : 0.0033) * (double)pcols) * TS / 32;
+    const double t_part = (double)(wgs * OT * acols) * 4 / 0.8e6;
     if (workgroup_splits()) {
-      if (wgs < 256)
-        SPLIT = (int)std::min<int64_t>(std::min<int64_t>((512 + wgs - 1) / wgs, std::max<int64_t>(1, tiles / per)), 32);
-      else if (cond >= 0 && rvs.empty() && wgs <= 256 * OCC && nstr >= 2560)
-        SPLIT = 2;
+      const int64_t walk = (tiles + per - 1) / per, slots = 256 * OCC * (uneven && !WSPLIT ? 2 : 1);
+      double best = (double)walk * t_tile;
+      for (int64_t q = 2; q <= std::min<int64_t>({walk, 32, slots / std::max<int64_t>(1, wgs)}); ++q) {
+        const double t = (double)((walk + q - 1) / q) * t_tile + 1.5 + (double)q * t_part;
+        if (t < best) best = t, SPLIT = (int)q;
+      }
+      // Shared tiles that fill the chip once and are long: 16 heads of 4096 causal
+      // rows of width 128 take 124 us in two splits, 139 in one; 32 of 2048 rows
+      // 83 and 73.  (A mask that reads data, as documents do, leaves few tiles: 12
+      // heads of 4000 rows 27.5 us in two splits, 26.9 in one.)
+      if (!WSPLIT && uneven && wgs >= 256) SPLIT = wgs <= 256 * OCC && nstr >= 2560 ? 2 : 1;
     }
     if (wgs * SPLIT > (int64_t)1 << 30) bad("too many workgroups");
     TP = OTILES;
