@@ -140,17 +140,47 @@ template <int GT> __device__ __forceinline__ void group_sync() {
   }
 }
 
-__device__ __forceinline__ float wave_min(float v) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) v = k_min(v, __shfl_xor(v, m, 64));
+// Minima and maxima over 8 or 16 neighbouring lanes by data-parallel moves
+// (within quads, then mirrored halves and rows), over the wave by reading one
+// lane of each row, over a lane and its partner 32 further by a lane swap: none
+// waits for LDS as the general shuffle does.
+template <int CTRL> __device__ __forceinline__ float dpp(float v) {
+  const int i = __builtin_bit_cast(int, v);
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(i, i, CTRL, 0xf, 0xf, false));
+}
+template <int N> __device__ __forceinline__ float lanes_min(float v) {
+  v = k_min(v, dpp<0xB1>(v));
+  v = k_min(v, dpp<0x4E>(v));
+  v = k_min(v, dpp<0x141>(v));
+  if constexpr (N == 16) v = k_min(v, dpp<0x140>(v));
   return v;
+}
+template <int N> __device__ __forceinline__ float lanes_max(float v) {
+  v = k_max(v, dpp<0xB1>(v));
+  v = k_max(v, dpp<0x4E>(v));
+  v = k_max(v, dpp<0x141>(v));
+  if constexpr (N == 16) v = k_max(v, dpp<0x140>(v));
+  return v;
+}
+__device__ __forceinline__ float from_lane(float v, int l) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), l));
+}
+__device__ __forceinline__ float wave_min(float v) {
+  v = lanes_min<16>(v);
+  return k_min(k_min(from_lane(v, 0), from_lane(v, 16)), k_min(from_lane(v, 32), from_lane(v, 48)));
 }
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) v = k_max(v, __shfl_xor(v, m, 64));
-  return v;
+  v = lanes_max<16>(v);
+  return k_max(k_max(from_lane(v, 0), from_lane(v, 16)), k_max(from_lane(v, 32), from_lane(v, 48)));
 }
-
+struct Halves {
+  float a, b;  // of the lane in the lower half and of the one in the upper half
+};
+__device__ __forceinline__ Halves halves(float v) {
+  const unsigned i = __builtin_bit_cast(unsigned, v);
+  const auto r = __builtin_amdgcn_permlane32_swap(i, i, false, false);
+  return {__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1])};
+}
 __device__ __forceinline__ float uniform(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v)));
 }
@@ -448,7 +478,8 @@ template <class P> struct Plane {
       for (int sub = 0; sub < G::NSUB; ++sub)
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = k_max(top, x[sub][i]);
-      top = k_max(top, __shfl_xor(top, 32, 64));
+      const Halves th = halves(top);
+      top = k_max(th.a, th.b);
       mtrue = k_max(mtrue, top);
       if (__any(mtrue > mref + kLazy / P::FOLD)) {
         const float f = rare(mref) == mtrue ? 1.0f : __builtin_amdgcn_exp2f((mref - mtrue) * (P::FOLD * kLog2e));
@@ -625,33 +656,46 @@ template <class P> struct Plane {
         __syncthreads();  // the previous chunk's list is no longer read
         // state of each tile: 0 no pair, 1 some, 2 all; a group of TS / 4 lanes
         // reads the tile's vectors
-        constexpr int GL = P::TS / 4;
-        for (int t0 = 0; t0 < cn; t0 += P::NRV ? G::NT / GL : G::NT) {
-          const int t = t0 + (P::NRV ? tid / GL : tid);
-          const i64 s0 = (i64)(c0 + (t < cn ? t : cn - 1)) * P::TS;
-          Range rv[P::NRV > 0 ? P::NRV : 1];
-          if constexpr (P::NRV > 0) {
+        constexpr int GL = P::TS / 4, TPI = P::NRV ? G::NT / GL : G::NT;  // tiles of one step
+        constexpr int U = P::NRV ? 4 : 1;                                 // steps whose loads go out together
+        for (int t0 = 0; t0 < cn; t0 += U * TPI) {
+          float val[U][P::NRV > 0 ? P::NRV : 1][4];
+          auto first = [&](int u) {
+            const int t = t0 + u * TPI + (P::NRV ? tid / GL : tid);
+            return (i64)(c0 + (t < cn ? t : cn - 1)) * P::TS;
+          };
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int k = 0; k < P::NRV; ++k)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const i64 r = first(u) + (tid % GL) * 4 + j;
+                val[u][k][j] = P::rvec(a, b, k, r < P::NSTR ? r : P::NSTR - 1);
+              }
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            const int t = t0 + u * TPI + (P::NRV ? tid / GL : tid);
+            const i64 s0 = first(u);
+            Range rv[P::NRV > 0 ? P::NRV : 1];
 #pragma unroll
             for (int k = 0; k < P::NRV; ++k) {
               float lo = __builtin_huge_valf(), hi = -lo;
               bool bad = false;
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
-                const i64 r = s0 + (tid % GL) * 4 + j;
-                const float v = P::rvec(a, b, k, r < P::NSTR ? r : P::NSTR - 1);
+                const float v = val[u][k][j];
                 bad = bad || not_number(v);
                 lo = k_min(lo, v), hi = k_max(hi, v);
               }
               if (bad) lo = -__builtin_huge_valf(), hi = __builtin_huge_valf();
-#pragma unroll
-              for (int m = GL / 2; m >= 1; m >>= 1) lo = k_min(lo, __shfl_xor(lo, m, 64)), hi = k_max(hi, __shfl_xor(hi, m, 64));
-              rv[k] = {lo, hi};
+              rv[k] = {lanes_min<GL>(lo), lanes_max<GL>(hi)};
             }
+            const i64 s1 = s0 + P::TS - 1 < P::NSTR - 1 ? s0 + P::TS - 1 : P::NSTR - 1;
+            const Range c = P::mask_range(a, b, gr, rv, (float)s0, (float)s1);
+            const int state = c.hi == 0.0f ? 0 : (c.lo > 0.0f && s0 + P::TS <= P::NSTR ? 2 : 1);
+            if (t < cn && (!P::NRV || tid % GL == 0)) list[t] = (unsigned short)state;
           }
-          const i64 s1 = s0 + P::TS - 1 < P::NSTR - 1 ? s0 + P::TS - 1 : P::NSTR - 1;
-          const Range c = P::mask_range(a, b, gr, rv, (float)s0, (float)s1);
-          const int state = c.hi == 0.0f ? 0 : (c.lo > 0.0f && s0 + P::TS <= P::NSTR ? 2 : 1);
-          if (t < cn && (!P::NRV || tid % GL == 0)) list[t] = (unsigned short)state;
         }
         __syncthreads();
         // compaction by one wave, in order (entries move towards the front)
@@ -733,7 +777,8 @@ template <class P> struct Plane {
     constexpr int NGRP = NREG / 4;
     if constexpr (P::NBIN > 0) join_bins(bl, ot, z);
     if constexpr (P::SOFTMAX) {
-      lsum += __shfl_xor(lsum, 32, 64);
+      const Halves lh = halves(lsum);
+      lsum = lh.a + lh.b;
       // to the true maximum
       const float f = mref == mtrue ? 1.0f : __builtin_amdgcn_exp2f((mref - mtrue) * (P::FOLD * kLog2e));
       lsum *= f;
