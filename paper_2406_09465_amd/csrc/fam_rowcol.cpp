@@ -130,8 +130,12 @@ GenKernel gen_rowcol(const KInfo& ki, int index) {
   const int NT = std::max(rc.L > 4096 ? 1024 : 512, G);
   const int RPB = NT / G, WR = G > 64 ? G / 64 : 1;
   const int64_t blocks = (rc.R + RPB - 1) / RPB;
-  const int64_t NWG = std::min<int64_t>(blocks, 256);
   const int64_t NS = (int64_t)rc.cols.size(), LQ = (rc.L + 3) / 4 * 4, C = NS * LQ;  // partial sums, rows of whole 16-byte vectors
+  int64_t NWG = std::min<int64_t>(blocks, 256);
+  // allocation-free execution has little scratch: fewer workgroups hand over 16 MiB
+  const int64_t NWG_small = std::max<int64_t>(1, ((int64_t)16 << 20) / std::max<int64_t>(1, C * 4));
+  gk.wg_split = NWG > NWG_small;
+  if (!workgroup_splits()) NWG = std::min(NWG, NWG_small);
   const bool ragged = (rc.L / VEC) % G != 0;  // the last vector of some lanes is past the row
   auto guard = [&](int j) { return j == NC - 1 && ragged ? "c" + std::to_string(j) + "_ok" : std::string(); };
   // Row tensors are loaded one row ahead in their own type, into the registers
@@ -393,7 +397,6 @@ GenKernel gen_rowcol(const KInfo& ki, int index) {
   gk.source = s.str();
   gk.grid[0] = (int)NWG;
   gk.block[0] = NT;
-  gk.wg_split = false;
   ki.fill_cost(gk);
   return gk;
 }
