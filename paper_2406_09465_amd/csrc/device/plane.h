@@ -112,7 +112,8 @@ __device__ __forceinline__ float rare(float v) {
 
 // tanh with the fp32 accuracy that scores need (absolute: a few 2^-24), as one
 // exponential and one reciprocal: 1 - 2 / (e^{2x} + 1).
-// pl_ctanh: c tanh(a x) without the products by a and c.
+// pl_ctanh: c tanh(a x) without the products by a and c, for |c| up to 256: the
+// absolute error, a few 2^-24 of c, is then below what 16-bit operands give scores.
 __device__ __forceinline__ float pl_ctanh(float x, float a, float c) {
   return __builtin_fmaf(-2.0f * c, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * (a * 2.0f * kLog2e)) + 1.0f), c);
 }
@@ -186,34 +187,37 @@ __device__ __forceinline__ float uniform(float v) {
 }
 
 // Interval arithmetic on value ranges (rounding is monotone, so a range of
-// rounded operations holds the rounded values).
+// rounded operations holds the rounded values).  Values that may be anything,
+// NaN included, have NaN for both ends: so do vectors with a NaN or an infinity
+// (whose differences may be NaN), and what is computed from them; a comparison
+// with such a range may be false and may be true.
 struct Range {
   float lo, hi;
 };
+__device__ __forceinline__ bool finite(float v) { return v - v == 0.0f; }
 __device__ __forceinline__ Range r_pt(float v) { return {v, v}; }
-__device__ __forceinline__ Range r_all() { return {-__builtin_huge_valf(), __builtin_huge_valf()}; }
-__device__ __forceinline__ Range r_add(Range a, Range b) { return {a.lo + b.lo, a.hi + b.hi}; }
-__device__ __forceinline__ Range r_sub(Range a, Range b) { return {a.lo - b.hi, a.hi - b.lo}; }
+__device__ __forceinline__ Range r_all() { return {__builtin_nanf(""), __builtin_nanf("")}; }
+__device__ __forceinline__ Range r_if(bool known, Range a) { return known ? a : r_all(); }
+__device__ __forceinline__ Range r_sum(float lo, float hi) { return r_if(finite(lo) && finite(hi), {lo, hi}); }
+__device__ __forceinline__ Range r_add(Range a, Range b) { return r_sum(a.lo + b.lo, a.hi + b.hi); }
+__device__ __forceinline__ Range r_sub(Range a, Range b) { return r_sum(a.lo - b.hi, a.hi - b.lo); }
 __device__ __forceinline__ Range r_neg(Range a) { return {-a.hi, -a.lo}; }
-__device__ __forceinline__ Range r_max(Range a, Range b) { return {k_max(a.lo, b.lo), k_max(a.hi, b.hi)}; }
-__device__ __forceinline__ Range r_min(Range a, Range b) { return {k_min(a.lo, b.lo), k_min(a.hi, b.hi)}; }
+__device__ __forceinline__ bool r_known(Range a) { return a.lo == a.lo; }
+__device__ __forceinline__ Range r_max(Range a, Range b) { return r_if(r_known(a) && r_known(b), {k_max(a.lo, b.lo), k_max(a.hi, b.hi)}); }
+__device__ __forceinline__ Range r_min(Range a, Range b) { return r_if(r_known(a) && r_known(b), {k_min(a.lo, b.lo), k_min(a.hi, b.hi)}); }
 __device__ __forceinline__ Range r_mul(Range a, Range b) {
   const float p = a.lo * b.lo, q = a.lo * b.hi, r = a.hi * b.lo, s = a.hi * b.hi;
-  // an infinite end times zero says nothing
-  if (!(p - p == 0.0f && q - q == 0.0f && r - r == 0.0f && s - s == 0.0f)) return r_all();
-  return {k_min(k_min(p, q), k_min(r, s)), k_max(k_max(p, q), k_max(r, s))};
+  return r_if(finite(p) && finite(q) && finite(r) && finite(s), {k_min(k_min(p, q), k_min(r, s)), k_max(k_max(p, q), k_max(r, s))});
 }
 __device__ __forceinline__ Range r_abs(Range a) {
   const float p = __builtin_fabsf(a.lo), q = __builtin_fabsf(a.hi);
-  return {a.lo <= 0.0f && a.hi >= 0.0f ? 0.0f : k_min(p, q), k_max(p, q)};
+  return r_if(r_known(a), {a.lo <= 0.0f && a.hi >= 0.0f ? 0.0f : k_min(p, q), k_max(p, q)});
 }
-__device__ __forceinline__ Range r_lt(Range a, Range b) { return {a.hi < b.lo ? 1.0f : 0.0f, a.lo < b.hi ? 1.0f : 0.0f}; }
-__device__ __forceinline__ Range r_le(Range a, Range b) { return {a.hi <= b.lo ? 1.0f : 0.0f, a.lo <= b.hi ? 1.0f : 0.0f}; }
+__device__ __forceinline__ Range r_lt(Range a, Range b) { return {a.hi < b.lo ? 1.0f : 0.0f, a.lo >= b.hi ? 0.0f : 1.0f}; }
+__device__ __forceinline__ Range r_le(Range a, Range b) { return {a.hi <= b.lo ? 1.0f : 0.0f, a.lo > b.hi ? 0.0f : 1.0f}; }
 __device__ __forceinline__ Range r_eq(Range a, Range b) {
-  return {a.lo == a.hi && b.lo == b.hi && a.lo == b.lo ? 1.0f : 0.0f, a.lo <= b.hi && b.lo <= a.hi ? 1.0f : 0.0f};
+  return {a.lo == a.hi && b.lo == b.hi && a.lo == b.lo ? 1.0f : 0.0f, a.lo > b.hi || b.lo > a.hi ? 0.0f : 1.0f};
 }
-
-__device__ __forceinline__ bool not_number(float v) { return !(v == v); }
 
 template <class P> struct Plane {
   typedef typename P::T T;
@@ -632,7 +636,7 @@ template <class P> struct Plane {
     if constexpr (P::MASK || P::NBIN > 0) {
 #pragma unroll
       for (int k = 0; k < P::NOV; ++k) {
-        const bool bad = __any(not_number(ov[k]));
+        const bool bad = __any(!finite(ov[k]));
         wr[k] = bad ? r_all() : Range{uniform(wave_min(ov[k])), uniform(wave_max(ov[k]))};
         if (lane == 0) rng[(wave * P::NOV + k) * 2] = wr[k].lo, rng[(wave * P::NOV + k) * 2 + 1] = wr[k].hi;
       }
@@ -641,8 +645,8 @@ template <class P> struct Plane {
       for (int k = 0; k < P::NOV; ++k) {
         gr[k] = wr[k];
         for (int v = 0; v < P::NW; ++v) {
-          gr[k].lo = k_min(gr[k].lo, rng[(v * P::NOV + k) * 2]);
-          gr[k].hi = k_max(gr[k].hi, rng[(v * P::NOV + k) * 2 + 1]);
+          const Range o = {rng[(v * P::NOV + k) * 2], rng[(v * P::NOV + k) * 2 + 1]};
+          gr[k] = r_if(r_known(gr[k]) && r_known(o), {k_min(gr[k].lo, o.lo), k_max(gr[k].hi, o.hi)});
         }
       }
     }
@@ -685,11 +689,12 @@ template <class P> struct Plane {
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
                 const float v = val[u][k][j];
-                bad = bad || not_number(v);
+                bad = bad || !finite(v);
                 lo = k_min(lo, v), hi = k_max(hi, v);
               }
-              if (bad) lo = -__builtin_huge_valf(), hi = __builtin_huge_valf();
-              rv[k] = {lanes_min<GL>(lo), lanes_max<GL>(hi)};
+              // (an infinite end of the group marks it)
+              if (bad) lo = -__builtin_huge_valf(), hi = -lo;
+              rv[k] = r_sum(lanes_min<GL>(lo), lanes_max<GL>(hi));
             }
             const i64 s1 = s0 + P::TS - 1 < P::NSTR - 1 ? s0 + P::TS - 1 : P::NSTR - 1;
             const Range c = P::mask_range(a, b, gr, rv, (float)s0, (float)s1);
@@ -762,13 +767,15 @@ template <class P> struct Plane {
   }
 
   // ---- joining the waves and the splits, and the results -------------------------
+  // The row's maximum as the graph defines it (rows without a pair: the mask's own value).
+  __device__ __forceinline__ float top_score() const { return mtrue == P::MINIT ? P::LOW : mtrue * P::FOLD; }
   __device__ __forceinline__ void store_group(int at, f32x4 v) {  // register group `at` (4 registers) of the lane
     static_for<P::NOP>([&](auto oi) {
       constexpr int o = decltype(oi)::value;
       constexpr int lo = abase(o) * 4, hi = abase(o + 1) * 4;
       if (at >= lo && at < hi) {
         const int dim = ((at - lo) / 4) * 32 + 8 * ((at - lo) % 4) + 4 * h;
-        if (own_ok() && dim < P::sw(P::ost(o))) P::template store<o>(a, b, own(), dim, mtrue * P::FOLD, lsum, v);
+        if (own_ok() && dim < P::sw(P::ost(o))) P::template store<o>(a, b, own(), dim, top_score(), lsum, v);
       }
     });
   }
@@ -796,7 +803,7 @@ template <class P> struct Plane {
         store_group(g, v);
       }
       if constexpr (P::SOFTMAX)
-        if (own_ok() && h == 0) P::stats(a, b, own(), mtrue * P::FOLD, lsum);
+        if (own_ok() && h == 0) P::stats(a, b, own(), top_score(), lsum);
     } else {
       constexpr int NM = NGRP + 1;  // groups of four registers, then (m, l)
       float* lds = (float*)smem;
@@ -888,7 +895,7 @@ template <class P> struct Plane {
           }
           mtrue = m, lsum = l;
         }
-// up to 32 vectors of partial results in flight: a round trip to the
+        // up to 32 vectors of partial results in flight: a round trip to the
         // device's point of coherence is 1 to 2 us
         constexpr int ZB = share >= 32 ? 1 : P::SPLIT < 32 / share ? P::SPLIT : 32 / share;
 #pragma unroll
@@ -917,7 +924,7 @@ template <class P> struct Plane {
       for (int g = 0; g < share; ++g)
         if (g0 + g < NGRP) store_group(g0 + g, v[g]);
       if constexpr (P::SOFTMAX)
-        if (own_ok() && h == 0 && (!P::WSPLIT || wave == 0)) P::stats(a, b, own(), mtrue * P::FOLD, lsum);
+        if (own_ok() && h == 0 && (!P::WSPLIT || wave == 0)) P::stats(a, b, own(), top_score(), lsum);
     }
   }
 

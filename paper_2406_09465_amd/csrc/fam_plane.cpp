@@ -282,6 +282,8 @@ struct PlaneGen {
         if (!in(top) || t.op != KORCH_SELECT || !t.attrs.has_scalar || t.in[0] != c2 || t.in[1] != nsfinal)
           bad("the row maximum must be over select(mask, s, low)");
         low = t.attrs.scalar;
+        // rows' maxima start from it, masked pair or not: no score may lie below
+        if (low > (nd(nsfinal).dtype == KORCH_F16 ? -6e4 : -1e9)) bad("a masked score that others may lie below");
         cond = c2;
       } else if (top != nsfinal) {
         bad("the row maximum is not over the exponent's scores");
@@ -331,7 +333,7 @@ struct PlaneGen {
     int64_t regs = 0;
     for (auto& w : out_w) regs += (w.shape[0] + 31) / 32 * 16;
     for (auto& o : sc_own) regs += (o.shape[0] + 31) / 32 * 32 * dtype_bytes(dtype) / 8;
-    if (regs > 256) bad("owned operands and output products fill the registers");
+    if (regs > 384) bad("owned operands and output products fill the registers");
     // outputs
     for (int o : ki.k.outs) {
       if (below(o) == bin_node) {
@@ -457,7 +459,10 @@ struct PlaneGen {
       if (fast_math() && tanh_chain(node, &x0, &ca, &cc)) {
         const std::string x = e->value(x0, broadcast_index(nd(x0).shape, PS, it));
         *out = e->fresh("t");
-        e->body << "    const float " << *out << " = pl_ctanh(" << x << ", " << flit(ca) << ", " << flit(cc) << ");\n";
+        if (std::abs(cc) <= 256)
+          e->body << "    const float " << *out << " = pl_ctanh(" << x << ", " << flit(ca) << ", " << flit(cc) << ");\n";
+        else  // a wide cap leaves small arguments, whose relative error counts
+          e->body << "    const float " << *out << " = " << flit(cc) << " * tanhf(" << x << " * " << flit(ca) << ");\n";
         return true;
       }
       const PlaneCls c = cls(node);
@@ -715,7 +720,7 @@ struct PlaneGen {
       << std::max<size_t>(1, xnodes.size()) << ", NBIN = " << nbin << ", XBIN = " << std::max(0, xbin) << ";\n";
     p << "  static constexpr int NTAB = " << tvs.size() << ", NOV = " << ovs.size() << ", NRV = " << rvs.size() << ";\n";
     p << "  static constexpr float MINIT = " << flit(softmax && cond >= 0 ? low / fold : -INFINITY)
-      << ", FOLD = " << flit(fold) << ";\n";
+      << ", LOW = " << flit(softmax && cond >= 0 ? low : -INFINITY) << ", FOLD = " << flit(fold) << ";\n";
     auto table = [&](const char* name, const std::vector<int>& v) {
       p << "  static constexpr int " << name << "(int i) {\n    constexpr int t[] = {";
       for (int x : v) p << x << ", ";

@@ -336,8 +336,8 @@ class _Attention:
             raise ValueError("a prefix extends a causal mask: causal must be set")
         if bool(buckets) != bool(radius) or buckets < 0 or radius < 0:
             raise ValueError("radius and buckets go together")
-        if cap < 0:
-            raise ValueError("cap must not be negative (0: none)")
+        if not 0 <= cap < math.inf:
+            raise ValueError("cap must be finite and not negative (0: none)")
         self.b, self.sizes = b, dict(batch=batch, heads=heads, kv_heads=kv_heads, n=n, m=m, d=d, cap=cap, slopes=slopes,
                                      causal=causal, prefix=prefix, documents=documents, lengths=lengths, radius=radius,
                                      buckets=buckets)

@@ -395,3 +395,124 @@ def test_workloads_past_the_keys_that_fit_lds(workload, sizes):
     got = _run(w, raw)
     ok, mx, rel = close(got["O"], want["O"], TOL[sizes["dtype"]])
     assert ok, (mx, rel)
+
+
+WIDE = [
+    dict(dtype="f32", n=50, m=70, d=256, heads=2, kv_heads=1, causal=True),
+    dict(dtype="f32", n=40, d=192, heads=2, cap=4.0),
+    dict(dtype="f16", n=60, d=64, radius=3000, buckets=9, heads=3, batch=2),
+    dict(dtype="bf16", n=45, d=32, radius=30, buckets=300, heads=2, causal=True),
+]
+
+
+@pytest.mark.parametrize("case", WIDE, ids=lambda c: "-".join(f"{k}{v}" for k, v in c.items()))
+def test_gradient_at_the_ends_of_what_a_kernel_holds(case):
+    """The widest heads in fp32, a bucket map too long for LDS, many buckets."""
+    test_attention_gradient(case)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_a_cap_far_above_the_scores(dtype):
+    """cap tanh(s / cap) is s to 1e-9 then.  The tanh (two steps of fp32) and the two
+    products by constants add 6 half steps of |s| to the bound's 8, so its double holds."""
+    case = dict(dtype=dtype, n=70, m=130, d=64, heads=2)
+    sizes, x, s, want = _unpack(case, grad=True)
+    sizes["cap"] = 1e5
+    out = _run(graphs.build("mha", **sizes), s)
+    _check(out, {k: (v, 2 * b) for k, (v, b) in want.items()}, dtype, ("L",))
+    _, s["O"] = ref.rounded(out["O"], dtype)
+    s["L"] = out["L"].astype(np.float32)
+    _check(_run(graphs.build("mha_grad", **sizes), s), {k: (v, 2 * b) for k, (v, b) in want.items()}, dtype)
+
+
+def _masked_rows(mask, n, m, vectors, low, scale=0.1):
+    """Softmax attention with a mask made from two vectors u [n, 1] and v [1, m]: the
+    product, the row maxima and the sums as results."""
+    b = graphs._B("f32")
+    for k, sh in (("Q", (n, 16)), ("K", (m, 16)), ("V", (m, 16)), ("u", (n, 1)), ("v", (1, m))):
+        b.inp(k, sh)
+    b.op("KT", "transpose", ["K"], perm=(1, 0))
+    b.op("S0", "matmul", ["Q", "KT"])
+    b.op("S", "mul", ["S0"], scalar=scale)
+    prims = ["KT", "S0", "S"]
+    for name, op, ins, attrs in mask:
+        b.op(name, op, ins, **attrs)
+        prims.append(name)
+    c = mask[-1][0]
+    b.op("Sm", "select", [c, "S"], scalar=low)
+    b.op("m", "reduce_max", ["Sm"], axis=-1, keepdim=True)
+    b.op("Z", "sub", ["S", "m"])
+    b.op("Ex", "exp", ["Z"])
+    b.op("E", "select", [c, "Ex"], scalar=0.0)
+    b.op("l", "reduce_sum", ["E"], axis=-1, keepdim=True)
+    b.op("O", "matmul", ["E", "V"])
+    w = graphs._finish(b, "masked", ["O", "m", "l"], {})
+    w.plans["fused"] = [(prims + ["Sm", "m", "Z", "Ex", "E", "l", "O"], ["O", "m", "l"])]
+    return w
+
+
+MASKS = {
+    "abs": ([("a", "abs", ["v"], {}), ("c", "ge", ["a"], dict(scalar=0.0))], lambda u, v: np.broadcast_to(np.abs(v) >= 0, (u.size, v.size))),
+    "difference": ([("d", "sub", ["u", "v"], {}), ("c", "le", ["d"], dict(scalar=1e30))], lambda u, v: u - v <= 1e30),
+    "sum": ([("d", "add", ["v", "u"], {}), ("a", "abs", ["d"], {}), ("c", "ge", ["a"], dict(scalar=0.5))], lambda u, v: np.abs(u + v) >= 0.5),
+    "product": ([("d", "mul", ["v", "u"], {}), ("c", "lt", ["d"], dict(scalar=1e30))], lambda u, v: u * v < 1e30),
+    "equal": ([("c", "eq", ["u", "v"], {})], lambda u, v: u == v),
+    "either": ([("g", "gt", ["v", "u"], {}), ("h", "lt", ["v"], dict(scalar=-3.0)), ("c", "max", ["g", "h"], {})], lambda u, v: (v > u) | (v < -3)),
+}
+
+
+@pytest.mark.parametrize("name", MASKS)
+@pytest.mark.parametrize("low", [-1e30, -3.4e38, -np.inf])
+def test_masks_from_vectors_that_hold_anything(name, low):
+    """NaN and infinities among the values that a mask compares (a comparison with
+    NaN is false), tiles that are clean, mixed and all of a kind; the maximum of a
+    row that is left empty is the masked score itself."""
+    n, m = 150, 420
+    ops, truth = MASKS[name]
+    rng = np.random.default_rng(11)
+    x, s = {}, {}
+    for k, sh in (("Q", (n, 16)), ("K", (m, 16)), ("V", (m, 16))):
+        x[k], s[k] = ref.rounded(rng.normal(0, 1.5, sh), "f32")
+    u, v = rng.integers(-2, 3, (n, 1)).astype(np.float32), rng.integers(-2, 3, (1, m)).astype(np.float32)
+    v[0, 3], v[0, 40], v[0, 70] = np.nan, np.inf, -np.inf
+    v[0, 128:192], v[0, 192:256], v[0, 256:320] = np.nan, np.inf, -np.inf
+    u[5], u[40], u[77] = np.nan, np.inf, -np.inf
+    s["u"], s["v"] = u, v
+    with np.errstate(invalid="ignore"):
+        mask = truth(u.astype(np.float64), v.astype(np.float64))
+    sc = x["Q"] @ x["K"].T * 0.1
+    some = mask.any(1, keepdims=True)
+    mx = np.max(np.where(mask, sc, -np.inf), 1, keepdims=True)
+    e = np.where(mask, np.exp(sc - np.where(some, mx, 0)), 0)
+    w = _masked_rows(ops, n, m, (u, v), low)
+    assert w.graph.family(*w.kernels("fused")[0]) == "plane"
+    got = _run(w, s)
+    # 18 roundings of the product and the scale; an exponential's error is its argument's
+    e_s = 18 * ref.E * np.abs(x["Q"]) @ np.abs(x["K"]).T * 0.1
+    assert np.array_equal(got["m"][~some[:, 0]], np.full((int((~some).sum()), 1), low, np.float32).astype(np.float64))
+    assert np.all(np.abs(got["m"] - np.where(some, mx, 0))[some] <= e_s.max(1, keepdims=True)[some])
+    rel = 2 * e_s.max(1, keepdims=True) + ref.F + 4 * ref.E * np.abs(sc).max() * 2
+    assert np.all(np.abs(got["l"] - e.sum(1, keepdims=True)) <= (rel + m * ref.E) * e.sum(1, keepdims=True))
+    assert np.all(np.abs(got["O"] - e @ x["V"]) <= (rel + m * ref.E) * (e @ np.abs(x["V"])))
+
+
+def test_allocation_free_sums_of_long_rows():
+    """The column sums' hand-over of rows of 16384 exceeds the library's static
+    memory: without an allocation fewer workgroups hand over."""
+    import torch
+    from paper_2406_09465_amd._abi import pointer_array
+    m, d = 600, 16384
+    rng = np.random.default_rng(4)
+    x, s = {}, {}
+    for k, sh in (("X", (m, d)), ("gamma", (d,)), ("beta", (d,)), ("dY", (m, d))):
+        x[k], s[k] = ref.rounded(rng.normal(0.1, 1, sh), "f16")
+    want = ref.layernorm(x["X"], x["gamma"], x["beta"], x["dY"], 1e-5, "f16")
+    s["mu"], s["r"] = want["mu"][0].astype(np.float32), want["r"][0].astype(np.float32)
+    from paper_2406_09465_amd.runner import PlanRunner
+    r = PlanRunner(graphs.build("layernorm_grad", m=m, d=d, dtype="f16"), "fused")
+    r.set_inputs(s)
+    r.plan.execute_noalloc(pointer_array([t.data_ptr() for t in r.ins]), pointer_array([t.data_ptr() for t in r.outs]),
+                           torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    for k, t in zip(r.w.output_names, r.outs):
+        assert ref.outside(t.double().cpu().numpy(), *want[k], "f16") <= 1.0, k

@@ -243,3 +243,26 @@ def test_rewritten_graphs_keep_their_results():
         out = run_unfused(o, {str(i): x[k] for k, i in zip(w.input_names, g2.inputs())})
         for k, i in zip(w.output_names, g2.outputs()):
             assert np.allclose(out[str(i)], want[k][0], rtol=1e-9, atol=1e-11), (rules, k)
+
+
+@pytest.mark.parametrize("case", cases.WIDE, ids=str)
+def test_widest_gradients_compile(case):
+    sizes = cases._unpack(case)[0]
+    p = graphs.build("mha_grad", **sizes).plan("fused")
+    p.compile()
+    for k in range(p.num_kernels()):
+        for kernel, r in codeobj.kernel_resources(p.kernel_code(k)).items():
+            assert r["scratch"] == 0 and r["lds"] <= 160 * 1024, (kernel, r)
+
+
+def test_a_masked_score_that_scores_may_lie_below():
+    """The row maximum starts from the masked score: one of -100 is refused."""
+    for low, family in ((-1e30, "plane"), (-100.0, "none")):
+        w = cases._masked_rows(cases.MASKS["equal"][0], 60, 70, None, low)
+        assert w.graph.family(*w.kernels("fused")[0]) == family
+
+
+@pytest.mark.parametrize("cap", [float("inf"), float("nan")])
+def test_caps_that_are_no_numbers(cap):
+    with pytest.raises(ValueError):
+        graphs.build("mha", n=8, heads=2, d=16, cap=cap)
