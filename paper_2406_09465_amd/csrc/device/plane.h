@@ -364,9 +364,14 @@ template <class P> struct Plane {
       }
     }
   }
-  // This wave's direct loads have arrived.
-  __device__ __forceinline__ void landed() const {
-    if constexpr (G::DMA) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  // This wave's loads have arrived, the direct ones included.  As a builtin, so
+  // that the compiler knows it of its own loads: the owned operands' are done
+  // before the walk.  (Else it waits for them in every tile, with vmcnt(0), and
+  // so for the next tile's direct loads, which it cannot count.)
+  static __device__ __forceinline__ void landed() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+    asm volatile("" ::: "memory");
   }
   // Columns past a tensor's width take part in the score products: zeros
   // (direct loads write them with every tile).
@@ -739,8 +744,8 @@ template <class P> struct Plane {
         entry(e, s0, full);
         fetch(0, s0);
         put(0);
-        landed();
       }
+      landed();
       group_sync<G::GT>();
       int s = 0;
       for (; e < n; e += step) {
@@ -756,7 +761,7 @@ template <class P> struct Plane {
         if (more) {
           if constexpr (!ahead) fetch(0, sn);
           put(P::STAGES == 1 ? 0 : s ^ 1);
-          landed();
+          if constexpr (G::DMA) landed();
         }
         group_sync<G::GT>();
         if constexpr (P::STAGES == 2) s ^= 1;
