@@ -110,6 +110,15 @@ __device__ __forceinline__ float rare(float v) {
   return v;
 }
 
+// An address in LDS of which the compiler knows no part: small constant offsets
+// from it fit the loads (with a known part it adds that per load).
+typedef const __attribute__((address_space(3))) float* LdsFloat;
+__device__ __forceinline__ LdsFloat lds_base(const float* p) {
+  LdsFloat q = (LdsFloat)p;
+  asm("" : "+v"(q));
+  return q;
+}
+
 // tanh with the fp32 accuracy that scores need (absolute: a few 2^-24), as one
 // exponential and one reciprocal: 1 - 2 / (e^{2x} + 1).
 // pl_ctanh: c tanh(a x) without the products by a and c, for |c| up to 256: the
@@ -435,10 +444,13 @@ template <class P> struct Plane {
   // Streamed index (within its tile) of register i of subtile sub.
   __device__ __forceinline__ int sidx(int sub, int i) const { return sub * 32 + 8 * (i / 4) + 4 * h + i % 4; }
 
-  // f(i, values of the streamed vectors, streamed index (clamped), it exists) for the registers of a subtile.
+  // f(i, values of the streamed vectors, bases of the looked-up tables and offset
+  // from them, streamed index (clamped), it exists) for the registers of a subtile.
   template <class F> __device__ __forceinline__ void elements(const char* base, i64 s0, int sub, F&& f) {
     const float* tab = (const float*)(base + G::tab_off);
     const int rows = P::NSTR - s0 < P::TS ? (int)(P::NSTR - s0) : P::TS;
+    LdsFloat lb[P::NLUT > 0 ? P::NLUT : 1];
+    P::bases(ov, (const float*)(smem + G::lut_off), s0 + sub * 32 + 4 * h, lb);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       f32x4 tv4[P::NTAB > 0 ? P::NTAB : 1];
@@ -450,7 +462,7 @@ template <class P> struct Plane {
 #pragma unroll
         for (int k = 0; k < P::NTAB; ++k) tv[k] = tv4[k][r];
         const int s = sidx(sub, 4 * g + r);
-        f(4 * g + r, tv, s0 + (s < rows ? s : rows - 1), s < rows);
+        f(4 * g + r, tv, lb, 8 * g + r, s0 + (s < rows ? s : rows - 1), s < rows);
       }
     }
   }
@@ -467,9 +479,9 @@ template <class P> struct Plane {
       for (int sub = 0; sub < G::NSUB; ++sub) x[sub] = score<0>(base, sub);
 #pragma unroll
       for (int sub = 0; sub < G::NSUB; ++sub)
-        elements(base, s0, sub, [&](int i, const float* tv, i64 sc, bool) {
+        elements(base, s0, sub, [&](int i, const float* tv, const LdsFloat* lb, int kk, i64 sc, bool) {
           float xs[1] = {x[sub][i]};
-          x[sub][i] = P::logit(a, b, ov, tv, lut, own(), sc, xs);
+          x[sub][i] = P::logit(a, b, ov, tv, lut, lb, kk, own(), sc, xs);
         });
       if (!full) {
         float om[P::NOV > 0 ? P::NOV : 1];
@@ -478,8 +490,8 @@ template <class P> struct Plane {
         // a masked pair's score is -inf: its exponential is 0 whatever the maximum
 #pragma unroll
         for (int sub = 0; sub < G::NSUB; ++sub)
-          elements(base, s0, sub, [&](int i, const float* tv, i64 sc, bool ok) {
-            x[sub][i] = ok && P::keep(a, b, om, tv, lut, own(), sc) ? x[sub][i] : minus;
+          elements(base, s0, sub, [&](int i, const float* tv, const LdsFloat* lb, int kk, i64 sc, bool ok) {
+            x[sub][i] = ok && P::keep(a, b, om, tv, lut, lb, kk, own(), sc) ? x[sub][i] : minus;
           });
       }
       float top = x[0][0];
@@ -520,11 +532,11 @@ template <class P> struct Plane {
         f32x16 x[P::NSP];
         static_for<P::NSP>([&](auto pi) { x[decltype(pi)::value] = score<decltype(pi)::value>(base, sub); });
         float X[P::NX][16];
-        elements(base, s0, sub, [&](int i, const float* tv, i64 sc, bool) {
+        elements(base, s0, sub, [&](int i, const float* tv, const LdsFloat* lb, int kk, i64 sc, bool) {
           float xs[P::NSP], out[P::NX];
 #pragma unroll
           for (int p = 0; p < P::NSP; ++p) xs[p] = x[p][i];
-          P::plane(a, b, ov, tv, lut, own(), sc, xs, out);
+          P::plane(a, b, ov, tv, lut, lb, kk, own(), sc, xs, out);
 #pragma unroll
           for (int k = 0; k < P::NX; ++k) X[k][i] = out[k];
         });
@@ -532,8 +544,8 @@ template <class P> struct Plane {
           float om[P::NOV > 0 ? P::NOV : 1];
           for (int k = 0; k < P::NOV; ++k) om[k] = rare(ov[k]);
           const float zero = rare(0.0f);
-          elements(base, s0, sub, [&](int i, const float* tv, i64 sc, bool ok) {
-            const bool k1 = ok && P::keep(a, b, om, tv, lut, own(), sc);
+          elements(base, s0, sub, [&](int i, const float* tv, const LdsFloat* lb, int kk, i64 sc, bool ok) {
+            const bool k1 = ok && P::keep(a, b, om, tv, lut, lb, kk, own(), sc);
 #pragma unroll
             for (int k = 0; k < P::NX; ++k) X[k][i] = k1 ? X[k][i] : zero;
           });
@@ -567,7 +579,7 @@ template <class P> struct Plane {
       return;
     }
     int id[16];
-    elements(base, s0, sub, [&](int i, const float* tv, i64 sc, bool) { id[i] = (int)P::bin(a, b, ov, tv, lut, own(), sc) * 64; });
+    elements(base, s0, sub, [&](int i, const float* tv, const LdsFloat* lb, int kk, i64 sc, bool) { id[i] = (int)P::bin(a, b, ov, tv, lut, lb, kk, own(), sc) * 64; });
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       float old[4], add[4];

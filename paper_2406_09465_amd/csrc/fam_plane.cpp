@@ -69,6 +69,13 @@ struct PlaneGen {
     int node, index;  // gather, plane node that indexes (innermost)
     int64_t size;
     int at;           // first element
+    // Index = base + step * streamed index with whole numbers and step 1 or -1 (a
+    // distance): a lane's indices in a subtile are its first one's and its
+    // registers', so one clamped base and constant offsets address them all, with
+    // the ends repeated over `pad` more elements on both sides.
+    int step = 0;
+    int64_t pad = 0;
+    std::string base;
   };
   std::vector<Lut> luts;
   int64_t lut_size = 0;
@@ -415,6 +422,7 @@ struct PlaneGen {
   }
 
   static constexpr int64_t kLutMost = 4096;  // floats of all tables: 16 KiB of LDS
+  static constexpr int64_t kLutPad = 32;     // a subtile
 
   // The table for gather `node`, or null.
   const Lut* lut_for(int node) {
@@ -432,10 +440,38 @@ struct PlaneGen {
       size = ts.back();
       v = nd(v).in[1];
     }
-    if (v == node || cls(v) != FULLP || has_score(v) || lut_size + size > kLutMost) return nullptr;
-    luts.push_back({node, v, size, (int)lut_size});
-    lut_size += size;
+    if (v == node || cls(v) != FULLP || has_score(v) || lut_size + size + 2 * kLutPad > kLutMost) return nullptr;
+    Lut l{node, v, size, (int)lut_size};
+    const size_t no = ovs.size();
+    if (!stepped(v, &l.step, &l.base) || l.step * l.step != 1) {
+      ovs.resize(no);
+      l.step = 0;
+    }
+    l.pad = l.step ? kLutPad : 0;
+    lut_size += size + 2 * l.pad;
+    luts.push_back(l);
     return &luts.back();
+  }
+  // node = *expr (at streamed index rs) + *step * (streamed index - rs).
+  bool stepped(int v, int* step, std::string* expr) {
+    const Node& n = nd(v);
+    const PlaneCls c = cls(v);
+    *step = 0;
+    if (c != FULLP && is_owned(c)) return *expr = "ov[" + std::to_string(vec_id(ovs, v)) + "]", true;
+    if (!in(v)) return false;
+    if (n.op == KORCH_IOTA && is_streamed(c) && (int)n.shape.size() - n.axis == (rows_owned ? 1 : 2)) return *step = 1, *expr = "(float)(int)rs", true;
+    if (n.op == KORCH_IDENTITY) return stepped(n.in[0], step, expr);
+    if (n.op != KORCH_ADD && n.op != KORCH_SUB) return false;
+    int s2 = 0;
+    std::string x, y;
+    if (!stepped(n.in[0], step, &x)) return false;
+    if (n.attrs.has_scalar)
+      y = flit(n.attrs.scalar);
+    else if (!stepped(n.in[1], &s2, &y))
+      return false;
+    *step += n.op == KORCH_ADD ? s2 : -s2;
+    *expr = "(" + x + (n.op == KORCH_ADD ? " + " : " - ") + y + ")";
+    return true;
   }
 
   // Body of a function that evaluates plane nodes `want` into `dst`; `full`:
@@ -471,6 +507,10 @@ struct PlaneGen {
         if (Emitter::key(node, idx) != std_key(node, it)) return false;
         const Lut* l = lut_for(node);
         if (!l) return false;
+        if (l->step) {
+          *out = "lb[" + std::to_string(l - luts.data()) + (l->step > 0 ? "][kk]" : "][-kk]");
+          return true;
+        }
         const int at = l->at, index = l->index;
         const int64_t size = l->size;
         const std::string x = e->value(index, broadcast_index(nd(index).shape, PS, it));
@@ -783,13 +823,21 @@ struct PlaneGen {
     vectors("rvec", rvs, false);
     p << "  static __device__ __forceinline__ Range mask_range(const KArgs& a, const B& b, const Range* ow, const Range* rv, float s0, float s1) {\n";
     p << "    return " << (cond >= 0 ? mask_expr : "r_pt(1.0f)") << ";\n  }\n";
-    const std::string sig = "(const KArgs& a, const B& b, const float* ov, const float* tv, const float* lut, i64 ro, i64 rs";
+    const std::string sig = "(const KArgs& a, const B& b, const float* ov, const float* tv, const float* lut, const LdsFloat* lb, int kk, i64 ro, i64 rs";
     p << "  static __device__ __forceinline__ " << (softmax ? "float logit" : "void plane") << sig << ", const float* xs" << (softmax ? "" : ", float* out")
       << ") {\n" << fn << "  }\n";
     p << "  static __device__ __forceinline__ bool keep" << sig << ") {\n    const float xs[2] = {};\n" << keep_fn << "  }\n";
     if (bin_node >= 0)
       p << "  static __device__ __forceinline__ float bin" << sig << ") {\n"
         << "    const float xs[2] = {};\n" << bin_fn << "    return k_min(k_max(id_, 0.0f), " << flit((double)(nbin - 1)) << ");\n  }\n";
+    // where the tables of stepped indices are read from a subtile's first streamed index on
+    p << "  static constexpr int NLUT = " << luts.size() << ";\n";
+    p << "  static __device__ __forceinline__ void bases(const float* ov, const float* lut, i64 rs, LdsFloat* lb) {\n";
+    for (size_t i = 0; i < luts.size(); ++i)
+      if (luts[i].step)
+        p << "    lb[" << i << "] = lds_base(lut + " << luts[i].at + luts[i].pad << " + (int)floorf(k_min(k_max(" << luts[i].base << ", "
+          << flit(luts[i].step > 0 ? -(double)luts[i].pad : 0) << "), " << flit((double)(luts[i].size - 1 + (luts[i].step > 0 ? 0 : luts[i].pad))) << ")));\n";
+    p << "  }\n";
     p << "  static constexpr int LUT = " << lut_size << ";\n  static __device__ __forceinline__ float lut_value(const KArgs& a, const B& b, int k) {\n";
     for (auto& l : luts) {
       auto e = emitter();
@@ -799,7 +847,8 @@ struct PlaneGen {
       std::vector<Ix> idx(nd(l.node).shape.size());
       for (size_t d = 0; d < idx.size(); ++d) idx[d] = nd(l.node).shape[d] == 1 ? Ix::k(0) : it[d + R - idx.size()];
       const std::string x = e->value(l.node, idx);
-      p << "    if (k < " << l.at + l.size << ") {\n    const float kf = (float)(k - " << l.at << ");\n" << e->pre.str() << e->body.str() << "    return " << x
+      p << "    if (k < " << l.at + l.size + 2 * l.pad << ") {\n    const float kf = k_min(k_max((float)(k - " << l.at + l.pad << "), 0.0f), "
+        << flit((double)(l.size - 1)) << ");\n" << e->pre.str() << e->body.str() << "    return " << x
         << ";\n    }\n";
     }
     p << "    return 0.0f;\n  }\n";
@@ -815,8 +864,8 @@ struct PlaneGen {
         std::string e = range(l->index);
         if (rvs.size() == nr && ovs.size() == no) {
           r = e;
-          first = "lut[" + std::to_string(l->at) + "]";
-          last = "lut[" + std::to_string(l->at + l->size - 1) + "]";
+          first = "lut[" + std::to_string(l->at + l->pad) + "]";
+          last = "lut[" + std::to_string(l->at + l->pad + l->size - 1) + "]";
         } else {  // its range needs a vector that the kernel does not hold
           rvs.resize(nr);
           ovs.resize(no);
