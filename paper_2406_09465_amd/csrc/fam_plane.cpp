@@ -633,23 +633,24 @@ struct PlaneGen {
   void layout(bool ws) {
     const bool f32 = dtype == KORCH_F32;
     // Registers that live through the walk.  With up to 160 of them two waves fit
-    // a SIMD; one computes while the other loads, reduces or waits (n = m = 4096,
-    // head width 128, bf16: 363 us against 431 with one).  Gradients of the keys
-    // at width 128 hold 192: one wave per SIMD (730 us; two spill, 837).
+    // a SIMD; one computes while the other loads, reduces or waits (2x16 heads of
+    // 4096 x 4096, width 128, bf16: 275 us against 343 with one, the queries'
+    // gradients 374 against 511).  Gradients of the keys at width 128 hold 192:
+    // one wave per SIMD (two spill and gain nothing: 720 to 800 us either way).
     int live = 0;
     for (auto& w : out_w) live += (int)((w.shape[0] + 31) / 32 * 16);
     for (auto& o : sc_own) live += (int)((o.shape[0] + 31) / 32 * 32 * dtype_bytes(dtype) / 8);
     WPE = live > 160 || reg_relief() > 0 ? 1 : 2;
     WSPLIT = ws;
     // Streamed rows of a tile: 64, or 32 where registers are short (two score
-    // planes at two waves per SIMD: 406 us against 444; a wave's own tiles, whose
-    // rows it loads alone: 62 us against 75 for 16 caches of up to 8192, width 128).
+    // planes at two waves per SIMD: 372 us against 398; a wave's own tiles, whose
+    // rows it loads alone: 62 us against 64 for 16 caches of up to 8192, width 128).
     TS = f32 || WSPLIT || (nm < 0 && WPE == 2) ? 32 : 64;
     NW = 4;
     // Tiles go straight to LDS, into a second stage while the first is read.  A
     // wave's own tiles pass through its registers instead, as long as it has
     // them: with one stage two workgroups fit a compute unit's LDS, and their
-    // loads keep twice the bytes in flight.
+    // loads keep twice the bytes in flight (those caches: 62 us, straight to LDS 245).
     int staging = 0;
     for (auto& w : streamed) staging += (int)(TS * w.shape[0] * dtype_bytes(dtype) / 256);
     DMA = !WSPLIT || live + staging > 224;
@@ -670,10 +671,10 @@ struct PlaneGen {
     // streamed axis, joined through LDS (more waves at work, no barrier between
     // tiles; every wave loads its own tiles).  Up to one and a half such
     // workgroups for each that the chip holds: 4 heads of 2048 x 2048, width 64,
-    // fp16, half as many, forward 17 us, gradients 18 and 22 (shared tiles 21, 26
-    // and 32); 12 heads, one and a half times, 36, 41 and 48 (34, 43 and 57); 8
+    // fp16, half as many, forward 15 us, gradients 17 and 20 (shared tiles 20, 24
+    // and 33); 12 heads, one and a half times, 33, 38 and 45 (31, 40 and 57); 8
     // heads of width 128, whose gradients take a compute unit each, twice as many
-    // 64 and 79 (51 and 73).
+    // 63 and 67 (47 and 74).
     layout(true);
     if ((nown + 31) / 32 * NB > 384 * OCC) layout(false);
     const int OT = WSPLIT ? 32 : 32 * NW;
@@ -684,10 +685,10 @@ struct PlaneGen {
     // pass the device's point of coherence at about 0.8 TB/s (written and read).
     // A tile of 32 takes a wave about 0.3 us and 3.3 ns per column of all products
     // (16-bit; 20 ns in fp32).  Splits beyond the workgroups that are resident at
-    // once gain nothing (2048 x 2048, one head of 128, fp16: 13.9 us in 4 splits,
-    // 22.6 in one, 19.4 in 8), unless a mask of positions makes them unequal: then
+    // once gain nothing (2048 x 2048, one head of 128, fp16: 13.0 us in 4 splits,
+    // 19.5 in one, 18.7 in 8), unless a mask of positions makes them unequal: then
     // up to twice as many (keys' gradient of 8 key heads of 2048 causal positions
-    // with four query heads each, width 128: 146 us in 4 splits, 203 in 2).
+    // with four query heads each, width 128: 143 us in 4 splits, 192 in 2).
     SPLIT = 1;
     bool uneven = cond >= 0;
     for (int v : rvs) uneven = uneven && !reads_data(v);
@@ -704,9 +705,9 @@ struct PlaneGen {
         if (t < best) best = t, SPLIT = (int)q;
       }
       // Shared tiles that fill the chip once and are long: 16 heads of 4096 causal
-      // rows of width 128 take 124 us in two splits, 139 in one; 32 of 2048 rows
-      // 83 and 73.  (A mask that reads data, as documents do, leaves few tiles: 12
-      // heads of 4000 rows 27.5 us in two splits, 26.9 in one.)
+      // rows of width 128 take 116 us in two splits, 123 in one; 32 of 2048 rows
+      // 75 and 67.  (A mask that reads data, as documents do, leaves few tiles: 12
+      // heads of 4000 rows 33 us in two splits, 24.5 in one.)
       if (!WSPLIT && uneven && wgs >= 256) SPLIT = wgs <= 256 * OCC && nstr >= 2560 ? 2 : 1;
     }
     if (wgs * SPLIT > (int64_t)1 << 30) bad("too many workgroups");

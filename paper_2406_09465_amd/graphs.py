@@ -616,6 +616,9 @@ def mha_grad(batch=1, heads=8, kv_heads=None, n=1024, m=None, d=64, dtype="bf16"
     kout, vout = ko[-1:], vo[-1:]
     dk = rest + plane + ["XT"] + ko
     dv = rest + cols_p + vo
+    # dK and dV share their scores in one kernel as far as the registers go (2x16
+    # causal capped heads of 2048, width 128: 141 us, two kernels 206; 4096 without
+    # a mask 780 and 740)
     cols = [(sorted(set(dk + dv)), kout + vout)] if d <= 128 else [(dk, kout), (dv, vout)]
     w.plans["fused"] = [(["dOO", "delta"], ["delta"]), (rest + plane + rows, rows_out)] + cols + after
     return w
