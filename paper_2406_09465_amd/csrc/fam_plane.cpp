@@ -630,7 +630,7 @@ struct PlaneGen {
   }
 
   // Tiles, waves and LDS for workgroups whose waves share tiles or (ws) split the streamed axis.
-  void layout(bool ws) {
+  void layout(bool ws, int waves) {
     const bool f32 = dtype == KORCH_F32;
     // Registers that live through the walk.  With up to 160 of them two waves fit
     // a SIMD; one computes while the other loads, reduces or waits (2x16 heads of
@@ -646,7 +646,7 @@ struct PlaneGen {
     // planes at two waves per SIMD: 372 us against 398; a wave's own tiles, whose
     // rows it loads alone: 62 us against 64 for 16 caches of up to 8192, width 128).
     TS = f32 || WSPLIT || (nm < 0 && WPE == 2) ? 32 : 64;
-    NW = 4;
+    NW = waves;
     // Tiles go straight to LDS, into a second stage while the first is read.  A
     // wave's own tiles pass through its registers instead, as long as it has
     // them: with one stage two workgroups fit a compute unit's LDS, and their
@@ -675,8 +675,20 @@ struct PlaneGen {
     // and 33); 12 heads, one and a half times, 33, 38 and 45 (31, 40 and 57); 8
     // heads of width 128, whose gradients take a compute unit each, twice as many
     // 63 and 67 (47 and 74).
-    layout(true);
-    if ((nown + 31) / 32 * NB > 384 * OCC) layout(false);
+    const int64_t own32 = (nown + 31) / 32 * NB;
+    bool data = false;  // the mask reads data along the streamed axis: nobody knows which tiles have work
+    for (int v : rvs) data = data || (cond >= 0 && reads_data(v));
+    int64_t pcols = 0, acols = 0;
+    for (auto& o : sc_own) pcols += o.shape[0];
+    for (auto& w : out_w) pcols += w.shape[0], acols += (w.shape[0] + 31) / 32 * 32;
+    layout(true, 4);
+    // Gradients of packed documents: the longest walks decide, and two waves that
+    // split one halve it.  12 heads of 4000 rows, width 64, fp16 (rows / columns
+    // owned): 11 documents 25.6 / 34.7 us, shared tiles 30.5 / 39; 3 documents 44 /
+    // 55 (60 / 87); 200 documents 20 / 25 (18 / 23).  Width 128 loads too much that
+    // way (50 us, 40), and so do twice as many heads of 8000 (97, 83).
+    if (own32 > 384 * OCC && data && nm < 0 && pcols <= 256) layout(true, 2);
+    if (own32 > 384 * OCC) layout(false, 4);
     const int OT = WSPLIT ? 32 : 32 * NW;
     OTILES = (nown + OT - 1) / OT;
     const int64_t wgs = OTILES * NB, tiles = (nstr + TS - 1) / TS, per = WSPLIT ? NW : 1;
@@ -690,11 +702,7 @@ struct PlaneGen {
     // up to twice as many (keys' gradient of 8 key heads of 2048 causal positions
     // with four query heads each, width 128: 143 us in 4 splits, 192 in 2).
     SPLIT = 1;
-    bool uneven = cond >= 0;
-    for (int v : rvs) uneven = uneven && !reads_data(v);
-    int64_t pcols = 0, acols = 0;
-    for (auto& o : sc_own) pcols += o.shape[0];
-    for (auto& w : out_w) pcols += w.shape[0], acols += (w.shape[0] + 31) / 32 * 32;
+    const bool uneven = cond >= 0 && !data;
     const double t_tile = (0.3 + (dtype == KORCH_F32 ? 0.02 : 0.0033) * (double)pcols) * TS / 32;
     const double t_part = (double)(wgs * OT * acols) * 4 / 0.8e6;
     if (workgroup_splits()) {
