@@ -268,7 +268,7 @@ template <class P> struct Plane {
   typename P::B b;
   char* smem;
   int tid, wave, lane, l32, h, gt, gtid;
-  i64 own0;     // first owned index of the workgroup
+  i64 own0, own1;  // first owned index of the workgroup, end of its block (or axis)
   float ov[P::NOV > 0 ? P::NOV : 1];
   Frag bf[NF];
   f32x16 acc[NA > 0 ? NA : 1];
@@ -279,10 +279,10 @@ template <class P> struct Plane {
 
   __device__ __forceinline__ Plane(const KArgs& a_, char* s) : a(a_), smem(s) {}
 
-  // This lane's owned index (clamped to the axis), and whether it exists.
+  // This lane's owned index (clamped to the block), and whether it exists.
   __device__ __forceinline__ i64 own_raw() const { return own0 + (P::WSPLIT ? 0 : wave * 32) + l32; }
-  __device__ __forceinline__ i64 own() const { return own_raw() < P::NOWN ? own_raw() : P::NOWN - 1; }
-  __device__ __forceinline__ bool own_ok() const { return own_raw() < P::NOWN; }
+  __device__ __forceinline__ i64 own() const { return own_raw() < own1 ? own_raw() : own1 - 1; }
+  __device__ __forceinline__ bool own_ok() const { return own_raw() < own1; }
 
   __device__ __forceinline__ char* stage(int s) const { return smem + (P::WSPLIT ? wave * G::group_bytes : 0) + s * G::stage_bytes; }
 
@@ -612,8 +612,8 @@ template <class P> struct Plane {
   __device__ __forceinline__ void run() {
     tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, h = lane >> 5;
     gtid = P::WSPLIT ? lane : tid;
-    // Order of the work.  An owned axis is made of blocks of TP tiles (the
-    // positions of one head) along which a mask usually changes the work
+    // Order of the work.  An owned axis is made of blocks of SEG indices and TP
+    // tiles (the positions of one head) along which a mask usually changes the work
     // steadily.  The longest tiles of all blocks come first; of the workgroups
     // that are resident from the start (OCC per compute unit) every second round
     // over the compute units runs backwards, so that a long and a short one
@@ -630,7 +630,8 @@ template <class P> struct Plane {
     const int z = w % P::SPLIT, blk = x0 + w / P::SPLIT % NX, rank = w / P::SPLIT / NX;
     const int bl = blk / (P::OTILES / P::TP), ot = blk % (P::OTILES / P::TP) * P::TP + (P::LAST_FIRST ? P::TP - 1 - rank : rank);
     b = P::batch(bl);
-    own0 = (i64)ot * G::OT;
+    own0 = (i64)(ot / P::TP) * P::SEG + (i64)(ot % P::TP) * G::OT;
+    own1 = (i64)(ot / P::TP + 1) * P::SEG;
 #pragma unroll
     for (int k = 0; k < P::NOV; ++k) ov[k] = P::own(a, b, k, own());
     // owned fragments

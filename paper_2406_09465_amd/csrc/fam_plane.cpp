@@ -606,7 +606,7 @@ struct PlaneGen {
   // Splits of the streamed axis and geometry.
   int NW = 4, TS = 64, SPLIT = 1, STAGES = 2, WPE = 1, OCC = 1;
   bool WSPLIT = false, DMA = true;
-  int64_t OTILES = 1, NB = 1, TP = 1;
+  int64_t OTILES = 1, NB = 1, TP = 1, SEG = 1;
 
   size_t lds_bytes() const {
     const int es = dtype_bytes(dtype);
@@ -690,7 +690,19 @@ struct PlaneGen {
     if (own32 > 384 * OCC && data && nm < 0 && pcols <= 256) layout(true, 2);
     if (own32 > 384 * OCC) layout(false, 4);
     const int OT = WSPLIT ? 32 : 32 * NW;
-    OTILES = (nown + OT - 1) / OT;
+    // Positions repeat along the rows when the heads of a group share them.  With a
+    // mask no tile holds the end of one head and the start of the next (it would
+    // see every key): each head starts a tile, where that adds a quarter at most
+    // (16 heads on 4 of 4000 rows, eleven documents, width 64, fp16: 25 us, 130).
+    SEG = nown;
+    for (int v : ki.k.prims) {
+      const Node& n = nd(v);
+      if (n.op != KORCH_IOTA || numel(n.shape) != nown || !rows_owned || cond < 0) continue;
+      const int64_t period = n.shape[n.axis];
+      if (period < nown && nown % period == 0 && (period + OT - 1) / OT * OT * 4 <= period * 5) SEG = period;
+    }
+    TP = (SEG + OT - 1) / OT;
+    OTILES = nown / SEG * TP;
     const int64_t wgs = OTILES * NB, tiles = (nstr + TS - 1) / TS, per = WSPLIT ? NW : 1;
     // The streamed axis is split over workgroups where that shortens the walk by
     // more than the hand-over takes: about 1.5 us, and the partial results, which
@@ -719,14 +731,6 @@ struct PlaneGen {
       if (!WSPLIT && uneven && wgs >= 256) SPLIT = wgs <= 256 * OCC && nstr >= 2560 ? 2 : 1;
     }
     if (wgs * SPLIT > (int64_t)1 << 30) bad("too many workgroups");
-    TP = OTILES;
-    // positions repeat along the rows when the heads of a group share them
-    for (int v : ki.k.prims) {
-      const Node& n = nd(v);
-      if (n.op != KORCH_IOTA || numel(n.shape) != nown || !rows_owned) continue;
-      const int64_t period = n.shape[n.axis];
-      if (period < nown && nown % period == 0 && period % OT == 0) TP = period / OT;
-    }
   }
 
   GenKernel generate(int index) {
@@ -761,7 +765,7 @@ struct PlaneGen {
     const int64_t nown = rows_owned ? N : M, nstr = rows_owned ? M : N;
     p << "struct Pol {\n  typedef " << T << " T;\n  struct B {\n    i64 c[" << std::max(1, R - 2) << "];\n  };\n";
     p << "  static constexpr bool SOFTMAX = " << softmax << ", MASK = " << (cond >= 0) << ", WSPLIT = " << WSPLIT << ", DMA = " << DMA << ";\n";
-    p << "  static constexpr i64 NOWN = " << nown << "LL, NSTR = " << nstr << "LL;\n";
+    p << "  static constexpr i64 SEG = " << SEG << "LL, NSTR = " << nstr << "LL;\n";
     p << "  static constexpr int NW = " << NW << ", TS = " << TS << ", STAGES = " << STAGES << ", SPLIT = " << SPLIT << ", OTILES = " << OTILES
       << ", NB = " << NB << ", TP = " << TP << ", OCC = " << OCC << ";\n  static constexpr bool LAST_FIRST = " << rows_owned << ";\n";
     const int64_t nbin = bin_node >= 0 ? nd(bin_node).shape.back() : 0;

@@ -516,3 +516,17 @@ def test_allocation_free_sums_of_long_rows():
     torch.cuda.synchronize()
     for k, t in zip(r.w.output_names, r.outs):
         assert ref.outside(t.double().cpu().numpy(), *want[k], "f16") <= 1.0, k
+
+
+BLOCKS = [
+    dict(dtype="f16", n=150, d=64, heads=6, kv_heads=2, docs=3, causal=True, batch=2),
+    dict(dtype="f32", n=61, m=90, d=32, heads=4, kv_heads=1, causal=True, cap=4.0, slopes=True),
+    dict(dtype="bf16", n=250, m=260, d=128, heads=8, kv_heads=2, lengths=(251, 260), batch=2, causal=True),
+    dict(dtype="f16", n=120, d=64, heads=96, kv_heads=48, docs=2, batch=8),
+]
+
+
+@pytest.mark.parametrize("case", BLOCKS, ids=lambda c: "-".join(f"{k}{v}" for k, v in c.items() if k != "lengths"))
+def test_heads_of_a_group_that_end_inside_a_tile(case):
+    """Query heads that share a key head are rows of one axis: each starts a tile."""
+    test_attention_gradient(case)
