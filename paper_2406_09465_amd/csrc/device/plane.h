@@ -966,6 +966,7 @@ template <class P> struct Plane {
     const float* all = (const float*)(smem + G::bin_off);
     __syncthreads();
     // a wave per bin: the lanes' sums of every wave, then over the lanes
+#pragma unroll 4
     for (int k = wave; k < P::NBIN; k += P::NW) {
       float s = 0.0f;
       for (int v = 0; v < P::NW; ++v) s += all[(v * P::NBIN + k) * 64 + lane];
@@ -986,8 +987,15 @@ template <class P> struct Plane {
     float* red = (float*)smem;  // [groups][NBIN]
     constexpr int NG2 = P::NBIN < G::NT ? G::NT / P::NBIN : 1;
     for (int k = tid % (P::NBIN < G::NT ? P::NBIN : G::NT), g = P::NBIN < G::NT ? tid / P::NBIN : 0; k < P::NBIN && g < NG2; k += G::NT) {
+      // eight loads in flight: each is a round trip to the point of coherence
       float s = 0.0f;
-      for (int m = g; m < members; m += NG2) s += coherent_load(&part[(i64)m * P::NBIN + k]);
+      for (int m = g; m < members; m += 8 * NG2) {
+        float q[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) q[u] = coherent_load(&part[(i64)(m + u * NG2 < members ? m + u * NG2 : m) * P::NBIN + k]);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s += m + u * NG2 < members ? q[u] : 0.0f;
+      }
       red[g * P::NBIN + k] = s;
     }
     __syncthreads();
