@@ -195,6 +195,20 @@ __device__ __forceinline__ float uniform(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v)));
 }
 
+// Sum of x y over a row of D elements, by the two lanes that own the row.
+template <int D, typename T> __device__ __forceinline__ float row_dot(const T* x, const T* y) {
+  constexpr int VL = Mma<T>::VL;
+  float s = 0.0f;
+#pragma unroll 4
+  for (int c = ((threadIdx.x >> 5) & 1) * VL; c < D; c += 2 * VL) {
+    const vec_t<VL, T> u = *(const vec_t<VL, T>*)(x + c), v = *(const vec_t<VL, T>*)(y + c);
+#pragma unroll
+    for (int j = 0; j < VL; ++j) s = __builtin_fmaf(tof(u[j]), tof(v[j]), s);
+  }
+  const Halves r = halves(s);
+  return r.a + r.b;
+}
+
 // Interval arithmetic on value ranges (rounding is monotone, so a range of
 // rounded operations holds the rounded values).  Values that may be anything,
 // NaN included, have NaN for both ends: so do vectors with a NaN or an infinity
@@ -812,6 +826,8 @@ template <class P> struct Plane {
 
   __device__ __forceinline__ void finish(int bl, int ot, int z) {
     constexpr int NGRP = NREG / 4;
+    if constexpr (P::ROWOUT)
+      if (own_ok() && h == 0 && z == 0 && (!P::WSPLIT || wave == 0)) P::row_out(a, b, own(), ov);
     if constexpr (P::NBIN > 0) join_bins(bl, ot, z);
     if constexpr (P::SOFTMAX) {
       const Halves lh = halves(lsum);

@@ -14,8 +14,11 @@
 //     one kind, W stored like the scores' operands;
 //   * at most one softmax: m = max over a row, e = exp(s - m) (or 0 where a mask
 //     is false), l = sum of e; then P is e or e / l;
+//   * row vectors may be products of two stored tensors summed along their rows
+//     (the gradients' rowsum(dO O)), with rows owned;
 //   * every output is an elementwise function of one output product and of row
-//     statistics, a row statistic of the softmax, or a sum by bins of the plane.
+//     statistics, a row statistic of the softmax, such a sum, or a sum by bins of
+//     the plane.
 #include <algorithm>
 #include <cmath>
 #include <memory>
@@ -80,6 +83,7 @@ struct PlaneGen {
   std::vector<Lut> luts;
   int64_t lut_size = 0;
   std::map<int, int> prod_of;         // output -> output product index
+  std::vector<int> rowdots;           // sums of x y along the rows of stored tensors
   std::map<int, bool> has_score_memo;
 
   explicit PlaneGen(const KInfo& k) : ki(k), g(k.g) {}
@@ -266,10 +270,13 @@ struct PlaneGen {
       out_w.push_back(w);
       ost.push_back(add_streamed(w));
     }
+    std::vector<int> stats;
+    for (int r : ki.reduces) (is_rowdot(r) ? rowdots : stats).push_back(r);
+    if (!rowdots.empty() && !rows_owned) bad("a row sum where columns are owned");
     // softmax
-    if (!ki.reduces.empty()) {
-      if (ki.reduces.size() != 2 || !rows_owned || scores.size() != 1) bad("reductions other than one row softmax");
-      for (int r : ki.reduces) {
+    if (!stats.empty()) {
+      if (stats.size() != 2 || !rows_owned || scores.size() != 1) bad("reductions other than one row softmax");
+      for (int r : stats) {
         const Node& n = nd(r);
         if (n.axis != R - 1 || !n.attrs.keepdim || nd(n.in[0]).shape != PS) bad("a reduction is not along the plane's rows");
         if (n.op == KORCH_REDUCE_MAX) nm = r;
@@ -347,6 +354,7 @@ struct PlaneGen {
         bin_out = o;
         continue;
       }
+      if (std::find(rowdots.begin(), rowdots.end(), below(o)) != rowdots.end()) continue;
       int p = -1;
       for (size_t i = 0; i < outs_p.size(); ++i)
         if (depends(o, outs_p[i])) {
@@ -372,6 +380,34 @@ struct PlaneGen {
     }
   }
   bool divided = false;
+
+  // sum over the last axis of x y, stored, one row for each row of the plane
+  bool is_rowdot(int r) const {
+    const Node& n = nd(r);
+    const int x = n.in[0];
+    if (n.op != KORCH_REDUCE_SUM || !n.attrs.keepdim || !in(x) || nd(x).op != KORCH_MUL || nd(x).attrs.has_scalar) return false;
+    const Shape& s = nd(x).shape;
+    if (n.axis != (int)s.size() - 1 || numel(n.shape) * M != numel(PS)) return false;
+    for (int u : nd(x).in)
+      if (in(u) || nd(u).shape != s || nd(u).dtype != dtype || s.back() * dtype_bytes(dtype) % 16) return false;
+    return true;
+  }
+  // The rowdot that a vector is (its elements are in the plane's row order), or -1.
+  int rowdot_of(int v) const {
+    v = below(v);
+    return std::find(rowdots.begin(), rowdots.end(), v) != rowdots.end() ? v : -1;
+  }
+  int rowdot_slot(int rd) const {
+    for (size_t i = 0; i < ovs.size(); ++i)
+      if (rowdot_of(ovs[i]) == rd) return (int)i;
+    bad("a row sum that the plane does not read");
+  }
+  // Index of the plane's row `r`, over the whole batch.
+  std::string flat_row(const char* r) const {
+    std::string f = "(i64)0";
+    for (int d = 0; d < R - 2; ++d) f = "(" + f + " * " + std::to_string(PS[d]) + " + b.c[" + std::to_string(d) + "])";
+    return "(" + f + " * " + std::to_string(N) + "LL + " + r + ")";
+  }
 
   // Node below the reshapes that end an output (its elements are stored in the same order).
   int below(int o) const {
@@ -547,6 +583,14 @@ struct PlaneGen {
 
   // Value of a vector node at owned / streamed index variable `r`.
   std::string vector_value(int node, bool owned, std::string* stmts) {
+    const int rd = rowdot_of(node);
+    if (rd >= 0) {
+      const Node& x = nd(nd(rd).in[0]);
+      if (!owned) bad("a row sum that is streamed");
+      const std::string D = std::to_string(x.shape.back()), at = flat_row("r") + " * " + D;
+      auto p = [&](int u) { return "(const " + ctype(dtype) + "*)a.p[" + std::to_string(slot.at(u)) + "] + " + at; };
+      return "row_dot<" + D + ">(" + p(x.in[0]) + ", " + p(x.in[1]) + ")";
+    }
     std::vector<Ix> it(R);
     for (int d = 0; d < R - 2; ++d) it[d] = Ix::var("b.c[" + std::to_string(d) + "]");
     const bool rows = owned == rows_owned;
@@ -899,9 +943,14 @@ struct PlaneGen {
       p << "    }\n";
     }
     p << "  }\n";
+    p << "  static constexpr bool ROWOUT = " << !rowdots.empty() << ";\n  static __device__ __forceinline__ void row_out(const KArgs& a, const B& b, i64 ro, const float* ov) {\n";
+    for (int o : ki.k.outs)
+      if (rowdot_of(o) >= 0)
+        p << "    st1((" << ctype(nd(o).dtype) << "*)a.p[" << ki.out_slot(o) << "] + " << flat_row("ro") << ", ov[" << rowdot_slot(below(o)) << "]);\n";
+    p << "  }\n";
     p << "  static __device__ __forceinline__ void stats(const KArgs& a, const B& b, i64 ro, float m, float l) {\n";
     for (int o : ki.k.outs) {
-      if (o == bin_out || prod_of.count(o)) continue;
+      if (o == bin_out || prod_of.count(o) || rowdot_of(o) >= 0) continue;
       auto e = emitter();
       std::vector<Ix> it(R);
       for (int d = 0; d < R - 2; ++d) it[d] = Ix::var("b.c[" + std::to_string(d) + "]");

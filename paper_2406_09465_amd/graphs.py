@@ -558,7 +558,11 @@ def mha_grad(batch=1, heads=8, kv_heads=None, n=1024, m=None, d=64, dtype="bf16"
     a.operands()
     a.scores()
     lse = a.view("L4", "L", a.qlead + (a.rows, 1), "f32")
+    # delta as the kernel that sums it reads it, and as it is stored
     delta = a.view("delta4", "delta", a.qlead + (a.rows, 1), "f32")
+    head = ["dOO", "delta"] + (["delta4"] if delta != "delta" else [])
+    a.view("delta_s", "delta", (batch, heads, n), "f32")
+    a.view("delta_s4", "delta_s", a.qlead + (a.rows, 1), "f32")
     do = a.view("dO4", "dO", a.qlead + (a.rows, d))
     a.op("Z", "sub", [a.s, lse])
     a.op("Ex", "exp", ["Z"])
@@ -567,19 +571,28 @@ def mha_grad(batch=1, heads=8, kv_heads=None, n=1024, m=None, d=64, dtype="bf16"
     a.prims.clear()
     a.op("VT", "transpose", [a.v], dtype, perm=a.swap())
     a.op("dP", "matmul", [do, "VT"])
-    a.op("dD", "sub", ["dP", delta])
-    a.op("dS", "mul", [p, "dD"])
-    ds = a.masked("dSm", "dS")
-    dx = ds
-    if cap:
-        a.op("t2", "square", ["t"])
-        a.op("nt2", "neg", ["t2"])
-        a.op("dt", "add", ["nt2"], scalar=1.0)
-        a.op("dU", "mul", [ds, "dt"])
-        dx = a.masked("dX", "dU")
-    # P and dX are rounded to the operands' type for the products
-    xc = dx if dtype == "f32" else a.op("Xc", "identity", [dx], dtype)
-    plane = list(a.prims)
+    pre = list(a.prims)
+
+    def score_gradient(delta, c):
+        """dS and dX for one of the two kernels.  P and dX are rounded to the operands' type for
+        the products, half a step each, as every sum over them averages such errors out (two parts
+        of dX would keep it, for one product more in either kernel)."""
+        a.prims.clear()
+        a.op("dD" + c, "sub", ["dP", delta])
+        a.op("dS" + c, "mul", [p, "dD" + c])
+        ds = dx = a.masked("dSm" + c, "dS" + c)
+        if cap:
+            if not c:
+                b.op("t2", "square", ["t"], "f32")
+                b.op("nt2", "neg", ["t2"], "f32")
+                b.op("dt", "add", ["nt2"], "f32", scalar=1.0)
+            a.prims += ["t2", "nt2", "dt"]
+            a.op("dU" + c, "mul", [ds, "dt"])
+            dx = a.masked("dX" + c, "dU" + c)
+        xc = dx if dtype == "f32" else a.op("Xc" + c, "identity", [dx], dtype)
+        return ds, xc, pre + list(a.prims)
+
+    ds, xc, plane = score_gradient(delta, "")
     b.op("dQ0", "matmul", [xc, a.k], "f32")
     b.op("dQ1", "mul", ["dQ0"], scalar=a.scale)
     a.out("dQ", "dQ1", (batch, heads, n, d))
@@ -588,7 +601,8 @@ def mha_grad(batch=1, heads=8, kv_heads=None, n=1024, m=None, d=64, dtype="bf16"
         b.op("dT0", "bin_sum", [ds, "which"], shape=a.qlead[1:] + (1, 1, buckets))
         a.out("dT", "dT0", (heads, buckets))
         rows, rows_out = rows + ["dT0", "dT"], rows_out + ["dT"]
-    b.op("XT", "transpose", [xc], perm=a.swap())
+    _, xk, plane_k = score_gradient("delta_s4", "_k")
+    b.op("XT", "transpose", [xk], perm=a.swap())
     b.op("dK0", "matmul", ["XT", a.q], "f32")
     pc = p
     cols_p = []
@@ -614,13 +628,15 @@ def mha_grad(batch=1, heads=8, kv_heads=None, n=1024, m=None, d=64, dtype="bf16"
     outs = ["dQ", "dK", "dV"] + (["dT"] if buckets else [])
     w = _finish(b, "mha_grad", outs, a.sizes, extra_outputs)
     kout, vout = ko[-1:], vo[-1:]
-    dk = rest + plane + ["XT"] + ko
+    dk = rest + plane_k + ["XT"] + ko
     dv = rest + cols_p + vo
     # dK and dV share their scores in one kernel as far as the registers go (2x16
     # causal capped heads of 2048, width 128: 141 us, two kernels 206; 4096 without
     # a mask 780 and 740)
     cols = [(sorted(set(dk + dv)), kout + vout)] if d <= 128 else [(dk, kout), (dv, vout)]
-    w.plans["fused"] = [(["dOO", "delta"], ["delta"]), (rest + plane + rows, rows_out)] + cols + after
+    # the kernel that owns the queries also sums delta, which the keys' reads (as a
+    # node of its own: a kernel's output has a reader that is not in the kernel)
+    w.plans["fused"] = [(head + rest + plane + rows, ["delta"] + rows_out)] + cols + after
     return w
 
 
