@@ -677,22 +677,27 @@ template <class P> struct Plane {
     // ranges of the owned vectors, over the workgroup and over the wave
     float* rng = (float*)(smem + G::range_off);
     Range gr[P::NOV > 0 ? P::NOV : 1];
+    // (only of those that the mask or the bins compare: the others are still on their way)
     if constexpr (P::MASK || P::NBIN > 0) {
-#pragma unroll
-      for (int k = 0; k < P::NOV; ++k) {
-        const bool bad = __any(!finite(ov[k]));
-        wr[k] = bad ? r_all() : Range{uniform(wave_min(ov[k])), uniform(wave_max(ov[k]))};
-        if (lane == 0) rng[(wave * P::NOV + k) * 2] = wr[k].lo, rng[(wave * P::NOV + k) * 2 + 1] = wr[k].hi;
-      }
-      __syncthreads();
-#pragma unroll
-      for (int k = 0; k < P::NOV; ++k) {
-        gr[k] = wr[k];
-        for (int v = 0; v < P::NW; ++v) {
-          const Range o = {rng[(v * P::NOV + k) * 2], rng[(v * P::NOV + k) * 2 + 1]};
-          gr[k] = r_if(r_known(gr[k]) && r_known(o), {k_min(gr[k].lo, o.lo), k_max(gr[k].hi, o.hi)});
+      static_for<P::NOV>([&](auto ki) {
+        constexpr int k = decltype(ki)::value;
+        if constexpr (P::ranged(k)) {
+          const bool bad = __any(!finite(ov[k]));
+          wr[k] = bad ? r_all() : Range{uniform(wave_min(ov[k])), uniform(wave_max(ov[k]))};
+          if (lane == 0) rng[(wave * P::NOV + k) * 2] = wr[k].lo, rng[(wave * P::NOV + k) * 2 + 1] = wr[k].hi;
         }
-      }
+      });
+      __syncthreads();
+      static_for<P::NOV>([&](auto ki) {
+        constexpr int k = decltype(ki)::value;
+        if constexpr (P::ranged(k)) {
+          gr[k] = wr[k];
+          for (int v = 0; v < P::NW; ++v) {
+            const Range o = {rng[(v * P::NOV + k) * 2], rng[(v * P::NOV + k) * 2 + 1]};
+            gr[k] = r_if(r_known(gr[k]) && r_known(o), {k_min(gr[k].lo, o.lo), k_max(gr[k].hi, o.hi)});
+          }
+        }
+      });
     }
     unsigned short* list = (unsigned short*)(smem + G::list_off);
     int* misc = (int*)(smem + G::misc_off);

@@ -22,6 +22,7 @@
 #include <algorithm>
 #include <cmath>
 #include <memory>
+#include <set>
 
 #include "families.h"
 
@@ -83,6 +84,7 @@ struct PlaneGen {
   std::vector<Lut> luts;
   int64_t lut_size = 0;
   std::map<int, int> prod_of;         // output -> output product index
+  std::set<int> ranged;               // owned vectors whose range is read
   std::vector<int> rowdots;           // sums of x y along the rows of stored tensors
   std::map<int, bool> has_score_memo;
 
@@ -614,7 +616,11 @@ struct PlaneGen {
     const Node& n = nd(v);
     const PlaneCls c = cls(v);
     if (in(v) && n.op == KORCH_FILL) return "r_pt(" + flit(n.attrs.scalar) + ")";
-    if (c != FULLP && is_owned(c)) return "ow[" + std::to_string(vec_id(ovs, v)) + "]";
+    if (c != FULLP && is_owned(c)) {
+      const int k = vec_id(ovs, v);
+      ranged.insert(k);
+      return "ow[" + std::to_string(k) + "]";
+    }
     if (in(v)) {
       auto two = [&](const char* f) {
         return std::string(f) + "(" + range(n.in[0]) + ", " + (n.attrs.has_scalar ? "r_pt(" + flit(n.attrs.scalar) + ")" : range(n.in[1])) +
@@ -934,6 +940,9 @@ struct PlaneGen {
       p << "  static __device__ __forceinline__ float bin_end(const float* lut, bool high) { return k_min(k_max(high ? " << last << " : " << first
         << ", 0.0f), " << flit((double)(nbin - 1)) << "); }\n";
     }
+    p << "  static constexpr bool ranged(int k) {\n    constexpr bool t[] = {";
+    for (size_t k = 0; k < ovs.size(); ++k) p << (ranged.count((int)k) > 0) << ", ";
+    p << "0};\n    return t[k];\n  }\n";
     // results
     p << "  template <int o> static __device__ __forceinline__ void store(const KArgs& a, const B& b, i64 ro, int dim, float m, float l, f32x4 v) {\n";
     for (size_t i = 0; i < outs_p.size(); ++i) {
