@@ -734,7 +734,7 @@ struct PlaneGen {
     layout(true, 4);
     // Gradients of packed documents: the longest walks decide, and two waves that
     // split one halve it.  12 heads of 4000 rows, width 64, fp16 (rows / columns
-    // owned): 11 documents 25.6 / 34.7 us, shared tiles 30.5 / 39; 3 documents 44 /
+    // owned, without rowsum(dO O)): 11 documents 25.6 / 34.7 us, shared tiles 30.5 / 39; 3 documents 44 /
     // 55 (60 / 87); 200 documents 20 / 25 (18 / 23).  Width 128 loads too much that
     // way (50 us, 40), and so do twice as many heads of 8000 (97, 83).
     if (own32 > 384 * OCC && data && nm < 0 && pcols <= 256) layout(true, 2);
