@@ -530,3 +530,15 @@ BLOCKS = [
 def test_heads_of_a_group_that_end_inside_a_tile(case):
     """Query heads that share a key head are rows of one axis: each starts a tile."""
     test_attention_gradient(case)
+
+
+PAIRS = [
+    dict(dtype="f16", n=120, d=64, heads=32, docs=3, batch=8, causal=True),
+    dict(dtype="bf16", n=70, m=200, d=40, heads=64, kv_heads=32, docs=5, batch=6, causal=True, cap=6.0),
+]
+
+
+@pytest.mark.parametrize("case", PAIRS, ids=lambda c: "-".join(f"{k}{v}" for k, v in c.items()))
+def test_gradients_of_many_packed_heads(case):
+    """So many tiles of 32 that two waves, not four, share one."""
+    test_attention_gradient(case)
