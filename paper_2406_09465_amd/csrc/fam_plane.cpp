@@ -762,17 +762,20 @@ struct PlaneGen {
     // once gain nothing (2048 x 2048, one head of 128, fp16: 13.0 us in 4 splits,
     // 19.5 in one, 18.7 in 8), unless a mask of positions makes them unequal: then
     // up to twice as many (keys' gradient of 8 key heads of 2048 causal positions
-    // with four query heads each, width 128: 143 us in 4 splits, 192 in 2).
+    // with four query heads each, width 128: 143 us in 4 splits, 192 in 2).  Where
+    // waves split the axis too, for owned columns only, and where the model sees a
+    // clear gain (16 heads on 4 of 2800, width 40, fp16: 73 us in two splits, 116 in
+    // one; owned rows lose: one token over 16 x 8192 keys 80 us, 62).
     SPLIT = 1;
     const bool uneven = cond >= 0 && !data;
     const double t_tile = (0.3 + (dtype == KORCH_F32 ? 0.02 : 0.0033) * (double)pcols) * TS / 32;
     const double t_part = (double)(wgs * OT * acols) * 4 / 0.8e6;
     if (workgroup_splits()) {
-      const int64_t walk = (tiles + per - 1) / per, slots = 256 * OCC * (uneven && !WSPLIT ? 2 : 1);
+      const int64_t walk = (tiles + per - 1) / per, slots = 256 * OCC * (uneven && !(WSPLIT && rows_owned) ? 2 : 1);
       double best = (double)walk * t_tile;
       for (int64_t q = 2; q <= std::min<int64_t>({walk, 32, slots / std::max<int64_t>(1, wgs)}); ++q) {
         const double t = (double)((walk + q - 1) / q) * t_tile + 1.5 + (double)q * t_part;
-        if (t < best) best = t, SPLIT = (int)q;
+        if (t < best * (WSPLIT && wgs * q > 256 * OCC ? 0.85 : 1.0)) best = t, SPLIT = (int)q;
       }
       // Shared tiles that fill the chip once and are long: 16 heads of 4096 causal
       // rows of width 128 take 116 us in two splits, 123 in one; 32 of 2048 rows
