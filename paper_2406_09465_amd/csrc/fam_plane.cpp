@@ -738,7 +738,16 @@ struct PlaneGen {
     // 55 (60 / 87); 200 documents 20 / 25 (18 / 23).  Width 128 loads too much that
     // way (50 us, 40), and so do twice as many heads of 8000 (97, 83).
     if (own32 > 384 * OCC && data && nm < 0 && pcols <= 256) layout(true, 2);
-    if (own32 > 384 * OCC) layout(false, 4);
+    // Shared tiles: four waves, or two where a mask along the diagonal cuts short
+    // walks (64 owned rows see fewer masked pairs): causal 8x12 heads of 512 rows,
+    // width 64, fp16, forward 12.9 us, gradients 18.9 and 21.8 (four waves 15.1, 21.0
+    // and 24.3); 16x12 heads of 1000 60.7, 84 and 107 (61.6, 88 and 112).  Width 128
+    // (65 us, two waves 89) and masks without a diagonal (25, 26) keep four.
+    bool diagonal = false;
+    for (int k : ranged) diagonal = diagonal || cls(ovs[k]) != CONSTV;
+    int64_t widest = 0;
+    for (auto& w : streamed) widest = std::max(widest, w.shape[0]);
+    if (own32 > 384 * OCC) layout(false, diagonal && nstr <= 1024 && widest <= 64 ? 2 : 4);
     const int OT = WSPLIT ? 32 : 32 * NW;
     // Positions repeat along the rows when the heads of a group share them.  With a
     // mask no tile holds the end of one head and the start of the next (it would
