@@ -440,6 +440,10 @@ template <class P> struct Plane {
       typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 #pragma unroll
       for (int kk = 0; kk < 2; ++kk) {
+        // The plane's values are rounded to the operands' type: the matrix
+        // instructions take nothing else, two parts of a value would double this
+        // product, and in its sums such errors average out like the result's own
+        // rounding.  Statistics and sums keep the unrounded values.
         Frag x;
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = fromf<T>(X[8 * kk + j]);

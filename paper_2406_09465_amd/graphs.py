@@ -506,7 +506,8 @@ def mha(batch=1, heads=8, kv_heads=None, n=1024, m=None, d=64, dtype="bf16", cap
     prefix), ``documents`` [batch, m] (equal document numbers), ``lengths``
     [batch] (the first lengths[b] >= n of the m positions are in use, the
     queries are the last n of those; K and V past them are never used and may hold
-    anything).  Numbers are fp32 whole numbers below 2^24."""
+    anything).  Numbers are fp32 whole numbers below 2^24.  The fused plan takes
+    widths d of whole 16-byte vectors up to 256."""
     b = _B(dtype)
     a = _Attention(b, batch, heads, kv_heads, n, m, d, cap, slopes, causal, prefix, documents, lengths, radius, buckets)
     a.vectors(slopes, causal, prefix, documents, lengths, radius, buckets)
@@ -545,8 +546,9 @@ def mha_grad(batch=1, heads=8, kv_heads=None, n=1024, m=None, d=64, dtype="bf16"
       dT[h, k] = sum of dS over the batch and the pairs of bucket k.
 
     The scores are evaluated again by the kernel that owns the queries (dQ, dT)
-    and by the one that owns the keys (dK, dV): every sum is taken by one
-    workgroup in a fixed order."""
+    and by the one that owns the keys (dK, dV): every sum is taken in a fixed
+    order.  The fused plan takes as many buckets as their sums fit LDS beside the
+    tiles (about 400 for 16-bit heads of 64)."""
     b = _B(dtype)
     a = _Attention(b, batch, heads, kv_heads, n, m, d, cap, slopes, causal, prefix, documents, lengths, radius, buckets)
     b.inp("dO", (batch, heads, n, d))
