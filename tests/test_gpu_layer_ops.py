@@ -542,3 +542,22 @@ PAIRS = [
 def test_gradients_of_many_packed_heads(case):
     """So many tiles of 32 that two waves, not four, share one."""
     test_attention_gradient(case)
+
+
+@pytest.mark.parametrize("kind", ["runs", "apart", "past the last bucket", "one"])
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_bucket_maps(kind, dtype):
+    """Equal buckets that are neighbours, or apart by one or two distances, or equal
+    only once they are clamped to the table."""
+    case = dict(dtype=dtype, n=150, d=32, radius=40, buckets=6, heads=3, batch=2)
+    sizes, x, s, _ = _unpack(case)
+    t = np.arange(-40, 41)
+    maps = {"runs": np.minimum(np.abs(t) // 3, 5), "apart": (t * t) % 6, "past the last bucket": 4 + np.abs(t) % 3 * 2, "one": 0 * t + 3}
+    x["bucket"], s["bucket"] = ref.rounded(maps[kind], "f32")
+    x["bucket"] = np.clip(x["bucket"], 0, 5)
+    want = ref.attention(x, dtype, 3, 3, radius=40, grad=True)
+    out = _run(graphs.build("mha", **sizes), s)
+    _check(out, want, dtype, ("L",))
+    _, s["O"] = ref.rounded(out["O"], dtype)
+    s["L"] = out["L"].astype(np.float32)
+    _check(_run(graphs.build("mha_grad", **sizes), s), want, dtype)
