@@ -18,10 +18,10 @@
 // exponentials below 2^8 (half-precision products stay far from overflow);
 // the results are brought to the true maximum at the end.
 //
-// Tiles whose mask is false for every pair are never loaded: the mask's value
+// Tiles whose mask is 0 for every pair are never loaded: the mask's value
 // range over a tile follows from the ranges of its vectors (interval
 // arithmetic), and the tiles with work are listed first.  The same ranges tell
-// tiles without a masked pair, which skip the mask.
+// tiles whose mask is 0 for no pair, which skip it.
 //
 // P (generated) describes the kernel; see the constants and functions used.
 
@@ -751,7 +751,8 @@ template <class P> struct Plane {
             }
             const i64 s1 = s0 + P::TS - 1 < P::NSTR - 1 ? s0 + P::TS - 1 : P::NSTR - 1;
             const Range c = P::mask_range(a, b, gr, rv, (float)s0, (float)s1);
-            const int state = c.hi == 0.0f ? 0 : (c.lo > 0.0f && s0 + P::TS <= P::NSTR ? 2 : 1);
+            // (a select takes every value that is not 0 as true, negative ones too)
+            const int state = c.lo == 0.0f && c.hi == 0.0f ? 0 : ((c.lo > 0.0f || c.hi < 0.0f) && s0 + P::TS <= P::NSTR ? 2 : 1);
             if (t < cn && (!P::NRV || tid % GL == 0)) list[t] = (unsigned short)state;
           }
         }

@@ -1,0 +1,62 @@
+"""Masks of plane kernels as `select` takes them: every value that is not 0 is
+true (negative ones and NaN too)."""
+
+import numpy as np
+import pytest
+
+from paper_2406_09465_amd import graphs
+
+from . import layer_ref as ref
+from .test_gpu_layer_ops import _masked_rows, _run
+
+pytestmark = pytest.mark.gpu
+
+# primitives of the mask from u [n, 1] and v [1, m], and its value
+VALUES = {
+    "negated": ([("a", "le", ["v", "u"], {}), ("c", "neg", ["a"], {})], lambda u, v: -(v <= u).astype(float)),
+    "distance back": ([("a", "sub", ["v", "u"], {}), ("c", "min", ["a"], dict(scalar=0.0))], lambda u, v: np.fmin(v - u, 0)),  # (min drops a NaN)
+    "less one": ([("a", "lt", ["v", "u"], {}), ("c", "sub", ["a"], dict(scalar=1.0))], lambda u, v: (v < u) - 1.0),
+    "distance": ([("c", "sub", ["u", "v"], {})], lambda u, v: u - v),
+    "twice": ([("a", "le", ["v", "u"], {}), ("c", "mul", ["a"], dict(scalar=2.0))], lambda u, v: 2.0 * (v <= u)),
+    "plain": ([("c", "ge", ["u", "v"], {})], lambda u, v: 1.0 * (u >= v)),
+}
+
+
+def _inputs(n, m, u, v, dtype="f32"):
+    rng = np.random.default_rng(21)
+    x, s = {}, {}
+    for k, sh in (("Q", (n, 16)), ("K", (m, 16)), ("V", (m, 16))):
+        x[k], s[k] = ref.rounded(rng.normal(0, 1.5, sh), dtype)
+    s["u"], s["v"] = u.astype(np.float32), v.astype(np.float32)
+    return x, s
+
+
+def _softmax_check(got, x, mask, bias=0.0, e_bias=0.0):
+    sc = x["Q"] @ x["K"].T * 0.1 + bias
+    some = mask.any(1, keepdims=True)
+    mx = np.max(np.where(mask, sc, -np.inf), 1, keepdims=True)
+    e = np.where(mask, np.exp(sc - np.where(some, mx, 0)), 0)
+    m = mask.shape[1]
+    # 18 roundings of the product and the scale; an exponential's error is its argument's
+    e_s = 18 * ref.E * np.abs(x["Q"]) @ np.abs(x["K"]).T * 0.1 + e_bias
+    assert np.all(np.abs(got["m"] - np.where(some, mx, 0))[some] <= e_s.max(1, keepdims=True)[some])
+    rel = 2 * e_s.max(1, keepdims=True) + ref.F + 8 * ref.E * np.abs(sc).max()
+    assert np.all(np.abs(got["l"] - e.sum(1, keepdims=True)) <= (rel + m * ref.E) * e.sum(1, keepdims=True))
+    assert np.all(np.abs(got["O"] - e @ x["V"]) <= (rel + m * ref.E) * (e @ np.abs(x["V"])))
+
+
+@pytest.mark.parametrize("n,m", [(150, 420), (1, 300), (400, 150)])
+@pytest.mark.parametrize("name", VALUES)
+def test_masks_whose_truth_is_not_one(name, n, m):
+    """Positions (queries at the end), tiles without a pair, mixed and full, and
+    vectors that are NaN for some."""
+    ops, value = VALUES[name]
+    u, v = np.arange(n, dtype=np.float64)[:, None] + max(0, m - n), np.arange(m, dtype=np.float64)[None]
+    if n > 100:
+        u[70], u[3] = np.nan, np.inf
+    x, s = _inputs(n, m, u, v)
+    with np.errstate(invalid="ignore"):
+        mask = value(u, v) != 0
+    w = _masked_rows(ops, n, m, None, -1e30)
+    assert w.graph.family(*w.kernels("fused")[0]) == "plane"
+    _softmax_check(_run(w, s), x, mask)
