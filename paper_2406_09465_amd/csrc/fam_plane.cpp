@@ -512,8 +512,20 @@ struct PlaneGen {
     return true;
   }
 
+  // Whether a mask's values are 0 and 1 only: comparisons, and their products,
+  // maxima and minima.
+  bool truth(int v) const {
+    if (!in(v)) return false;
+    const Node& n = nd(v);
+    if (n.op >= KORCH_LT && n.op <= KORCH_EQ) return true;
+    if (n.op == KORCH_IDENTITY) return truth(n.in[0]);
+    if ((n.op == KORCH_MUL || n.op == KORCH_MAX || n.op == KORCH_MIN) && !n.attrs.has_scalar) return truth(n.in[0]) && truth(n.in[1]);
+    return false;
+  }
+
   // Body of a function that evaluates plane nodes `want` into `dst`; `full`:
-  // where the mask holds.
+  // where the mask holds (one of other values than 0 and 1 is evaluated, as its
+  // value may be read beside its truth).
   std::string plane_body(const std::vector<std::pair<int, std::string>>& want, bool full) {
     auto it = plane_index();
     auto e = emitter();
@@ -526,7 +538,7 @@ struct PlaneGen {
           *out = "xs[" + std::to_string(s) + "]";
           return true;
         }
-      if (full && node == cond) {
+      if (full && node == cond && truth(cond)) {
         *out = "(1.0f)";
         return true;
       }
