@@ -213,7 +213,8 @@ template <int D, typename T> __device__ __forceinline__ float row_dot(const T* x
 // rounded operations holds the rounded values).  Values that may be anything,
 // NaN included, have NaN for both ends: so do vectors with a NaN or an infinity
 // (whose differences may be NaN), and what is computed from them; a comparison
-// with such a range may be false and may be true.
+// with such a range may be false and may be true.  (No contraction: a fused
+// multiply-add would round otherwise than the primitives.)
 struct Range {
   float lo, hi;
 };
@@ -222,13 +223,20 @@ __device__ __forceinline__ Range r_pt(float v) { return {v, v}; }
 __device__ __forceinline__ Range r_all() { return {__builtin_nanf(""), __builtin_nanf("")}; }
 __device__ __forceinline__ Range r_if(bool known, Range a) { return known ? a : r_all(); }
 __device__ __forceinline__ Range r_sum(float lo, float hi) { return r_if(finite(lo) && finite(hi), {lo, hi}); }
-__device__ __forceinline__ Range r_add(Range a, Range b) { return r_sum(a.lo + b.lo, a.hi + b.hi); }
-__device__ __forceinline__ Range r_sub(Range a, Range b) { return r_sum(a.lo - b.hi, a.hi - b.lo); }
+__device__ __forceinline__ Range r_add(Range a, Range b) {
+#pragma clang fp contract(off)
+  return r_sum(a.lo + b.lo, a.hi + b.hi);
+}
+__device__ __forceinline__ Range r_sub(Range a, Range b) {
+#pragma clang fp contract(off)
+  return r_sum(a.lo - b.hi, a.hi - b.lo);
+}
 __device__ __forceinline__ Range r_neg(Range a) { return {-a.hi, -a.lo}; }
 __device__ __forceinline__ bool r_known(Range a) { return a.lo == a.lo; }
 __device__ __forceinline__ Range r_max(Range a, Range b) { return r_if(r_known(a) && r_known(b), {k_max(a.lo, b.lo), k_max(a.hi, b.hi)}); }
 __device__ __forceinline__ Range r_min(Range a, Range b) { return r_if(r_known(a) && r_known(b), {k_min(a.lo, b.lo), k_min(a.hi, b.hi)}); }
 __device__ __forceinline__ Range r_mul(Range a, Range b) {
+#pragma clang fp contract(off)
   const float p = a.lo * b.lo, q = a.lo * b.hi, r = a.hi * b.lo, s = a.hi * b.hi;
   return r_if(finite(p) && finite(q) && finite(r) && finite(s), {k_min(k_min(p, q), k_min(r, s)), k_max(k_max(p, q), k_max(r, s))});
 }

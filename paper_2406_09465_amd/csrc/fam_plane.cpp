@@ -816,6 +816,10 @@ struct PlaneGen {
     ki.assign_args(gk, slot);
     const std::string T = ctype(dtype);
     const bool softmax = nm >= 0;
+    // The mask, the bins and the vectors that they read round after every
+    // primitive: a fused multiply-add could lie outside the range that the same
+    // primitives give for a tile.
+    const std::string apart = "#pragma clang fp contract(off)\n";
     // functions on the plane where the mask holds, and the mask
     std::vector<std::pair<int, std::string>> want;
     // Scores that are only a product with a constant > 0: the maximum is taken of
@@ -885,7 +889,7 @@ struct PlaneGen {
       for (size_t i = 0; i < v.size(); ++i)
         p << "    if constexpr (t == " << i << ") return (const T*)a.p[" << slot.at(v[i].root) << "] + " << v[i].off << ";\n";
       p << "  }\n";
-      p << "  template <int t> static __device__ __forceinline__ bool " << okn << "(const KArgs& a, const B& b, i64 r) {\n";
+      p << "  template <int t> static __device__ __forceinline__ bool " << okn << "(const KArgs& a, const B& b, i64 r) {\n" << apart;
       for (size_t i = 0; i < v.size(); ++i) {
         if (v[i].mask < 0) continue;
         auto e = emitter();
@@ -897,7 +901,7 @@ struct PlaneGen {
     rows("srow", streamed, "srow_ok");
     rows("orow", sc_own, "orow_ok");
     auto vectors = [&](const char* name, const std::vector<int>& v, bool owned) {
-      p << "  static __device__ __forceinline__ float " << name << "(const KArgs& a, const B& b, int k, i64 r) {\n";
+      p << "  static __device__ __forceinline__ float " << name << "(const KArgs& a, const B& b, int k, i64 r) {\n" << apart;
       for (size_t i = 0; i < v.size(); ++i) {
         std::string st;
         const std::string x = vector_value(v[i], owned, &st);
@@ -908,24 +912,24 @@ struct PlaneGen {
     vectors("own", ovs, true);
     vectors("tab", tvs, false);
     vectors("rvec", rvs, false);
-    p << "  static __device__ __forceinline__ Range mask_range(const KArgs& a, const B& b, const Range* ow, const Range* rv, float s0, float s1) {\n";
+    p << "  static __device__ __forceinline__ Range mask_range(const KArgs& a, const B& b, const Range* ow, const Range* rv, float s0, float s1) {\n" << apart;
     p << "    return " << (cond >= 0 ? mask_expr : "r_pt(1.0f)") << ";\n  }\n";
     const std::string sig = "(const KArgs& a, const B& b, const float* ov, const float* tv, const float* lut, const LdsFloat* lb, int kk, i64 ro, i64 rs";
     p << "  static __device__ __forceinline__ " << (softmax ? "float logit" : "void plane") << sig << ", const float* xs" << (softmax ? "" : ", float* out")
       << ") {\n" << fn << "  }\n";
-    p << "  static __device__ __forceinline__ bool keep" << sig << ") {\n    const float xs[2] = {};\n" << keep_fn << "  }\n";
+    p << "  static __device__ __forceinline__ bool keep" << sig << ") {\n" << apart << "    const float xs[2] = {};\n" << keep_fn << "  }\n";
     if (bin_node >= 0)
-      p << "  static __device__ __forceinline__ float bin" << sig << ") {\n"
+      p << "  static __device__ __forceinline__ float bin" << sig << ") {\n" << apart
         << "    const float xs[2] = {};\n" << bin_fn << "    return k_min(k_max(id_, 0.0f), " << flit((double)(nbin - 1)) << ");\n  }\n";
     // where the tables of stepped indices are read from a subtile's first streamed index on
     p << "  static constexpr int NLUT = " << luts.size() << ";\n";
-    p << "  static __device__ __forceinline__ void bases(const float* ov, const float* lut, i64 rs, LdsFloat* lb) {\n";
+    p << "  static __device__ __forceinline__ void bases(const float* ov, const float* lut, i64 rs, LdsFloat* lb) {\n" << apart;
     for (size_t i = 0; i < luts.size(); ++i)
       if (luts[i].step)
         p << "    lb[" << i << "] = lds_base(lut + " << luts[i].at + luts[i].pad << " + (int)floorf(k_min(k_max(" << luts[i].base << ", "
           << flit(luts[i].step > 0 ? -(double)luts[i].pad : 0) << "), " << flit((double)(luts[i].size - 1 + (luts[i].step > 0 ? 0 : luts[i].pad))) << ")));\n";
     p << "  }\n";
-    p << "  static constexpr int LUT = " << lut_size << ";\n  static __device__ __forceinline__ float lut_value(const KArgs& a, const B& b, int k) {\n";
+    p << "  static constexpr int LUT = " << lut_size << ";\n  static __device__ __forceinline__ float lut_value(const KArgs& a, const B& b, int k) {\n" << apart;
     for (auto& l : luts) {
       auto e = emitter();
       e->provide = [&](int node, const std::vector<Ix>&, std::string* out) { return node == l.index ? (*out = "kf", true) : false; };
@@ -959,7 +963,7 @@ struct PlaneGen {
         }
       }
       p << "  static constexpr int BIN_T = " << (l ? l->size : 1) << ";\n";
-      p << "  static __device__ __forceinline__ Range bin_range(const KArgs& a, const B& b, const Range* ow, float s0, float s1) {\n    return "
+      p << "  static __device__ __forceinline__ Range bin_range(const KArgs& a, const B& b, const Range* ow, float s0, float s1) {\n" << apart << "    return "
         << r << ";\n  }\n";
       p << "  static __device__ __forceinline__ float bin_end(const float* lut, bool high) { return k_min(k_max(high ? " << last << " : " << first
         << ", 0.0f), " << flit((double)(nbin - 1)) << "); }\n";

@@ -1,6 +1,6 @@
 """Masks of plane kernels as `select` takes them: every value that is not 0 is
-true (negative ones and NaN too), and a mask that is read as a number keeps its
-value."""
+true (negative ones and NaN too), a mask that is read as a number keeps its
+value, and its roundings are those of the graph."""
 
 import numpy as np
 import pytest
@@ -139,3 +139,16 @@ def test_a_mask_that_is_also_a_factor(name, rows):
         k = np.clip(v - u + 8, 0, 16).astype(int) + 0 * X.astype(int)
         for i in range(17):
             assert abs(got["T"][0, 0, i] - X[k == i].sum()) <= (20 + n + m) * ref.E * A[k == i].sum() + 1e-30, i
+
+
+def test_a_mask_rounds_as_its_primitives_do():
+    """u v - 1 <= 0 with u v = 1 + 2^-36: the product rounds to 1, so every pair holds,
+    in full tiles, whose mask is known from ranges, and in the last one alike."""
+    n, m = 150, 420
+    u, v = np.full((n, 1), 1 + 2.0 ** -12), np.full((1, m), 1 - 2.0 ** -12 + 2.0 ** -24)
+    x, s = _inputs(n, m, u, v)
+    assert s["u"][0, 0] * s["v"][0, 0] == np.float32(1) and float(s["u"][0, 0]) * float(s["v"][0, 0]) > 1
+    ops = [("a", "mul", ["u", "v"], {}), ("b", "add", ["a"], dict(scalar=-1.0)), ("c", "le", ["b"], dict(scalar=0.0))]
+    w = _masked_rows(ops, n, m, None, -1e30)
+    assert w.graph.family(*w.kernels("fused")[0]) == "plane"
+    _softmax_check(_run(w, s), x, np.ones((n, m), bool))
