@@ -128,6 +128,8 @@ __device__ __forceinline__ float pl_ctanh(float x, float a, float c) {
 }
 __device__ __forceinline__ float pl_tanh(float x) { return pl_ctanh(x, 1.0f, 1.0f); }
 __device__ __forceinline__ float pl_exp(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+// exp(x) 2^sx
+__device__ __forceinline__ float pl_exp_by(float x, float sx) { return __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2e, sx)); }
 
 template <int V> struct ic {
   static constexpr int value = V;
@@ -286,6 +288,21 @@ template <class P> struct Plane {
   static constexpr int NA = abase(P::NOP);
   static constexpr int TABV = (P::NTAB * P::TS + G::GT - 1) / G::GT;
 
+  // P::SCALED (fp16 planes that are an exponential times what does not depend on
+  // it, as a gradient's P and dX): fp16 has ever fewer bits for values below
+  // 2^-14, which a gradient's are with many keys or a small dO, and no number past
+  // 65504.  So each output product's values carry a factor 2^n that its results lose
+  // in fp32: the first one's is added to the exponential's exponent (sx), the
+  // others' multiply their values once more (by[o]).  The factors are an owned
+  // index's own; like a softmax's reference they start where the first values put
+  // them and move only when values would pass kScaleMost, to where the largest
+  // is at most 2^kScaleAt.  (12 heads of 4000 rows, eleven packed documents, width
+  // 64: queries' gradients 27.2 us without, 28.1 with; keys' 32.6 and 34.5.  2x16
+  // causal heads of 2048: 50.1 and 53.1, 61 and 67; width 128, capped, 95 and 96,
+  // 132 and 140.)
+  static constexpr float kScaleMost = 65000.0f;
+  static constexpr int kScaleAt = 6, kScaleFirst = 40;
+
   const KArgs& a;
   typename P::B b;
   char* smem;
@@ -295,6 +312,7 @@ template <class P> struct Plane {
   Frag bf[NF];
   f32x16 acc[NA > 0 ? NA : 1];
   float mref, mtrue, lsum;
+  float sx, by[P::NOP > 0 ? P::NOP : 1];
   Range wr[P::NOV > 0 ? P::NOV : 1];  // ranges of the owned vectors over the wave
   V16 st[vtot()];
   float stab[TABV > 0 ? TABV : 1];
@@ -454,7 +472,7 @@ template <class P> struct Plane {
         // rounding.  Statistics and sums keep the unrounded values.
         Frag x;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = fromf<T>(X[8 * kk + j]);
+        for (int j = 0; j < 8; ++j) x[j] = fromf<T>(P::SCALED && o > 0 ? X[8 * kk + j] * by[o] : X[8 * kk + j]);
         // this lane's part of a read: row r (and r + 8), columns 8 c + 4 (lane & 1) .. + 3 of 32
         const int r = 4 * h + ((lane & 15) >> 2), c = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
         const T* r0 = w + (sub * 32 + kk * 16 + r) * G::pitch(t) + 4 * (lane & 1);
@@ -476,6 +494,58 @@ template <class P> struct Plane {
         for (int d = 0; d < ND; ++d)
           acc[abase(o) + d] = __builtin_amdgcn_mfma_f32_32x32x2f32(r0[((8 * d) ^ z) * VL], X[i], acc[abase(o) + d], 0, 0, 0);
       }
+    }
+  }
+
+  // With one wave per SIMD accumulators live in accumulation registers, which
+  // vector instructions do not reach.  A block that is rarely taken and multiplies
+  // them fetches and returns them itself with this at its ends (else they are
+  // copied with every subtile: keys' gradients of 2x16 causal heads of 2048, width
+  // 128, fp16, 15 us more).
+  __device__ __forceinline__ void home() {
+    if constexpr (P::WPE == 1)
+#pragma unroll
+      for (int d = 0; d < NA; ++d) asm volatile("" : "+a"(acc[d]));
+  }
+  // 2^-sx
+  __device__ __forceinline__ float unscaled() const { return __builtin_ldexpf(1.0f, -(int)sx); }
+  // Moves the scales where values of this subtile outgrow them.
+  __device__ __forceinline__ void rescale(float (*X)[16]) {
+    float top[P::NOP > 0 ? P::NOP : 1];
+    bool past = false;
+    static_for<P::NOP>([&](auto oi) {
+      constexpr int o = decltype(oi)::value, k = P::ox(o);
+      float t = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) t = k_max(t, __builtin_fabsf(X[k][i]));
+      const Halves th = halves(t);
+      top[o] = o ? k_max(th.a, th.b) * by[o] : k_max(th.a, th.b);
+      past = past || top[o] > kScaleMost;
+    });
+    if (__any(past)) {
+      home();
+      static_for<P::NOP>([&](auto oi) {
+        constexpr int o = decltype(oi)::value;
+        // (an infinity stays one whatever the scale)
+        const float t = rare(top[o]);
+        const int e = t > (float)(1 << kScaleAt) && finite(t) ? kScaleAt - __builtin_amdgcn_frexp_expf(t) : 0;
+        const float f = __builtin_ldexpf(1.0f, e);
+        if constexpr (o == 0) {
+          sx += (float)e;
+          for (int q = 1; q < P::NOP; ++q) by[q] *= __builtin_ldexpf(1.0f, -e);
+#pragma unroll
+          for (int k = 0; k < P::NX; ++k)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) X[k][i] *= f;
+        } else {
+          by[o] *= f;
+        }
+#pragma unroll
+        for (int d = abase(o); d < abase(o + 1); ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[d][i] *= f;
+      });
+      home();
     }
   }
 
@@ -574,7 +644,7 @@ template <class P> struct Plane {
           float xs[P::NSP], out[P::NX];
 #pragma unroll
           for (int p = 0; p < P::NSP; ++p) xs[p] = x[p][i];
-          P::plane(a, b, ov, tv, lut, lb, kk, own(), sc, xs, out);
+          P::plane(a, b, ov, tv, lut, lb, kk, own(), sc, xs, sx, out);
 #pragma unroll
           for (int k = 0; k < P::NX; ++k) X[k][i] = out[k];
         });
@@ -588,6 +658,7 @@ template <class P> struct Plane {
             for (int k = 0; k < P::NX; ++k) X[k][i] = k1 ? X[k][i] : zero;
           });
         }
+        if constexpr (P::SCALED) rescale(X);
         static_for<P::NOP>([&](auto oi) { output<decltype(oi)::value>(base, sub, X[P::ox(decltype(oi)::value)]); });
         if constexpr (P::NBIN > 0) bins(base, s0, sub, X[P::XBIN]);
       }
@@ -608,12 +679,13 @@ template <class P> struct Plane {
     const float* lut = (const float*)(smem + G::lut_off);
     const Range e = P::bin_range(a, b, wr, (float)(s0 + sub * 32), (float)(s0 + sub * 32 + 31));
     const bool live = own_ok();
+    const float back = P::SCALED ? unscaled() : 1.0f;
     if (e.lo >= (float)(P::BIN_T - 1) || e.hi <= 0.0f) {
       const int k = (int)P::bin_end(lut, e.hi > 0.0f);
       float sum = 0.0f;
 #pragma unroll
       for (int i = 0; i < 16; ++i) sum += X[i];  // zero past the axis
-      mine[k * 64] += live ? sum : 0.0f;
+      mine[k * 64] += live ? sum * back : 0.0f;
       return;
     }
     int id[16];
@@ -630,7 +702,7 @@ template <class P> struct Plane {
         for (int j = 0; j < 4; ++j) add[i] += id[4 * g + j] == id[4 * g + i] ? X[4 * g + j] : 0.0f;
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) mine[id[4 * g + i]] = old[i] + (live ? add[i] : 0.0f);
+      for (int i = 0; i < 4; ++i) mine[id[4 * g + i]] = old[i] + (live ? add[i] * back : 0.0f);
     }
   }
 
@@ -678,6 +750,9 @@ template <class P> struct Plane {
     for (int d = 0; d < NA; ++d) acc[d] = f32x16{};
     mref = mtrue = P::MINIT;
     lsum = 0.0f;
+    sx = (float)kScaleFirst;
+#pragma unroll
+    for (int o = 0; o < P::NOP; ++o) by[o] = 1.0f;
     if constexpr (P::NBIN > 0)
       for (int k = 0; k < P::NBIN; ++k) ((float*)(smem + G::bin_off))[(wave * P::NBIN + k) * 64 + lane] = 0.0f;
     clear_pads();
@@ -847,6 +922,17 @@ template <class P> struct Plane {
     if constexpr (P::ROWOUT)
       if (own_ok() && h == 0 && z == 0 && (!P::WSPLIT || wave == 0)) P::row_out(a, b, own(), ov);
     if constexpr (P::NBIN > 0) join_bins(bl, ot, z);
+    if constexpr (P::SCALED) {
+      const float back = unscaled();
+      static_for<P::NOP>([&](auto oi) {
+        constexpr int o = decltype(oi)::value;
+        const float f = o ? back / by[o] : back;
+#pragma unroll
+        for (int d = abase(o); d < abase(o + 1); ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[d][i] *= f;
+      });
+    }
     if constexpr (P::SOFTMAX) {
       const Halves lh = halves(lsum);
       lsum = lh.a + lh.b;

@@ -63,6 +63,7 @@ struct PlaneGen {
   std::vector<int> xnodes, ox;        // distinct plane operands of output products (and bins)
   int xbin = -1, bin_node = -1, bin_out = -1;
   int nm = -1, nl = -1, ne = -1, nexp = -1, nsfinal = -1;  // softmax
+  int nfactor = -1;                   // exponential that all plane operands are multiples of (fp16: it carries their scale)
   int cond = -1;                      // mask
   double low = -INFINITY;
   std::vector<int> ovs, tvs, rvs;     // owned vectors, streamed vectors, streamed vectors whose range is read
@@ -331,6 +332,13 @@ struct PlaneGen {
           xbin = k;
       }
       if (!same) cond = -1;
+      if (dtype == KORCH_F16 && !outs_p.empty())
+        for (int v : ki.k.prims)
+          if (nd(v).op == KORCH_EXP && nd(v).shape == PS && has_score(v)) {
+            bool all_by = true;
+            for (int x : xnodes) all_by = all_by && times(x, v);
+            if (all_by) nfactor = v;
+          }
     }
     if (bin_node >= 0) {
       if (!rows_owned && !outs_p.empty()) bad("a sum by bins goes with row-owned products");
@@ -382,6 +390,22 @@ struct PlaneGen {
     }
   }
   bool divided = false;
+
+  // v = f times what does not depend on f (sums of such values too).
+  bool times(int v, int f) const {
+    if (v == f) return true;
+    if (!in(v) || !depends(v, f) || nd(v).shape != PS) return false;
+    const Node& n = nd(v);
+    const bool one = n.in.size() == 1 || n.attrs.has_scalar;
+    switch (n.op) {
+      case KORCH_IDENTITY: case KORCH_NEG: return times(n.in[0], f);
+      case KORCH_MUL: return one ? times(n.in[0], f) : depends(n.in[0], f) ? times(n.in[0], f) && !depends(n.in[1], f) : times(n.in[1], f);
+      case KORCH_DIV: return times(n.in[0], f) && (one || !depends(n.in[1], f));
+      case KORCH_ADD: case KORCH_SUB: return !one && times(n.in[0], f) && times(n.in[1], f);
+      case KORCH_SELECT: return n.attrs.has_scalar && n.attrs.scalar == 0.0 && !depends(n.in[0], f) && times(n.in[1], f);
+      default: return false;
+    }
+  }
 
   // sum over the last axis of x y, stored, one row for each row of the plane
   bool is_rowdot(int r) const {
@@ -540,6 +564,13 @@ struct PlaneGen {
         }
       if (full && node == cond && truth(cond)) {
         *out = "(1.0f)";
+        return true;
+      }
+      if (node == nfactor) {
+        const int z = nd(node).in[0];
+        const std::string x = e->value(z, broadcast_index(nd(z).shape, PS, it));
+        *out = e->fresh("t");
+        e->body << "    const float " << *out << " = pl_exp_by(" << x << ", sx);\n";
         return true;
       }
       if (fast_math() && tanh_chain(node, &x0, &ca, &cc)) {
@@ -842,10 +873,11 @@ struct PlaneGen {
     std::ostringstream p;
     const int64_t nown = rows_owned ? N : M, nstr = rows_owned ? M : N;
     p << "struct Pol {\n  typedef " << T << " T;\n  struct B {\n    i64 c[" << std::max(1, R - 2) << "];\n  };\n";
-    p << "  static constexpr bool SOFTMAX = " << softmax << ", MASK = " << (cond >= 0) << ", WSPLIT = " << WSPLIT << ", DMA = " << DMA << ";\n";
+    p << "  static constexpr bool SOFTMAX = " << softmax << ", MASK = " << (cond >= 0) << ", WSPLIT = " << WSPLIT << ", DMA = " << DMA << ", SCALED = " << (nfactor >= 0)
+      << ";\n";
     p << "  static constexpr i64 SEG = " << SEG << "LL, NSTR = " << nstr << "LL;\n";
     p << "  static constexpr int NW = " << NW << ", TS = " << TS << ", STAGES = " << STAGES << ", SPLIT = " << SPLIT << ", OTILES = " << OTILES
-      << ", NB = " << NB << ", TP = " << TP << ", OCC = " << OCC << ";\n  static constexpr bool LAST_FIRST = " << rows_owned << ";\n";
+      << ", NB = " << NB << ", TP = " << TP << ", OCC = " << OCC << ", WPE = " << WPE << ";\n  static constexpr bool LAST_FIRST = " << rows_owned << ";\n";
     const int64_t nbin = bin_node >= 0 ? nd(bin_node).shape.back() : 0;
     p << "  static constexpr int NSP = " << scores.size() << ", NST = " << streamed.size() << ", NOP = " << outs_p.size() << ", NX = "
       << std::max<size_t>(1, xnodes.size()) << ", NBIN = " << nbin << ", XBIN = " << std::max(0, xbin) << ";\n";
@@ -915,7 +947,7 @@ struct PlaneGen {
     p << "  static __device__ __forceinline__ Range mask_range(const KArgs& a, const B& b, const Range* ow, const Range* rv, float s0, float s1) {\n" << apart;
     p << "    return " << (cond >= 0 ? mask_expr : "r_pt(1.0f)") << ";\n  }\n";
     const std::string sig = "(const KArgs& a, const B& b, const float* ov, const float* tv, const float* lut, const LdsFloat* lb, int kk, i64 ro, i64 rs";
-    p << "  static __device__ __forceinline__ " << (softmax ? "float logit" : "void plane") << sig << ", const float* xs" << (softmax ? "" : ", float* out")
+    p << "  static __device__ __forceinline__ " << (softmax ? "float logit" : "void plane") << sig << ", const float* xs" << (softmax ? "" : ", float sx, float* out")
       << ") {\n" << fn << "  }\n";
     p << "  static __device__ __forceinline__ bool keep" << sig << ") {\n" << apart << "    const float xs[2] = {};\n" << keep_fn << "  }\n";
     if (bin_node >= 0)

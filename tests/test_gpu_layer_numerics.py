@@ -1,0 +1,67 @@
+"""fp16 attention and its gradient where the plane's values lie below fp16's normal
+numbers, or past its largest: small and large gradients, long rows.  Limits are
+counted from the roundings (layer_rms)."""
+
+import numpy as np
+import pytest
+
+from paper_2406_09465_amd import graphs
+
+from . import layer_ref as ref
+from . import layer_rms as rms
+from .test_gpu_layer_ops import _run
+
+pytestmark = pytest.mark.gpu
+
+
+def _stored(x):
+    pairs = {k: ref.rounded(v, "f16") for k, v in x.items()}
+    return {k: v[0] for k, v in pairs.items()}, {k: v[1] for k, v in pairs.items()}
+
+
+def _train(sizes, s):
+    """Forward and gradient of one case: all results by name."""
+    out = _run(graphs.build("mha", **sizes), s)
+    s = dict(s, O=ref.rounded(out["O"], "f16")[1], L=out["L"].astype(np.float32))
+    return {**out, **_run(graphs.build("mha_grad", **sizes), s)}
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("std", [1e-4, 1e-3, 1.0, 300.0])
+def test_gradients_of_every_size(std, d, causal):
+    """dO from the smallest that a training step meets to loss-scaled ones."""
+    n = 1500
+    rng = np.random.default_rng(3)
+    x, s = _stored({k: rng.normal(0, f, (1, 1, n, d)) for k, f in (("Q", 1.5), ("K", 1.0), ("V", 1.0), ("dO", std))})
+    p, dx, want = rms.plane(x, causal)
+    lim = rms.limits(x, p, dx, want)
+    out = _train(dict(heads=1, n=n, d=d, dtype="f16", causal=causal), s)
+    off = {k: rms.rms(out[k], want[k]) / lim[k] for k in lim}
+    assert all(v <= 1.0 for v in off.values()), off
+
+
+@pytest.mark.parametrize("n,m", [(40, 50000), (7, 100000)])
+def test_gradients_of_long_rows(n, m):
+    """Weights of 2e-5 and 1e-5 each: below the normal numbers of fp16, all of them."""
+    d = 32
+    rng = np.random.default_rng(4)
+    x, s = _stored({k: rng.normal(0, f, (1, 1, r, d)) for k, f, r in (("Q", 0.5, n), ("K", 0.5, m), ("V", 1.0, m), ("dO", 100.0, n))})
+    p, dx, want = rms.plane(x, False)
+    lim = rms.limits(x, p, dx, want)
+    out = _train(dict(heads=1, n=n, m=m, d=d, dtype="f16"), s)
+    off = {k: rms.rms(out[k], want[k]) / lim[k] for k in lim}
+    assert all(v <= 1.0 for v in off.values()), off
+
+
+def test_gradients_past_the_range_of_fp16():
+    """P (dP - delta) up to 4e5, past what fp16 holds, where the results do not pass it."""
+    n, d = 200, 64
+    rng = np.random.default_rng(6)
+    x, s = _stored({k: rng.normal(0, f, (1, 1, n, d)) for k, f in (("Q", 0.002), ("K", 0.002), ("V", 1500.0), ("dO", 1500.0))})
+    p, dx, want = rms.plane(x, False)
+    assert np.abs(dx).max() > 65504 and all(np.abs(want[k]).max() < 65504 for k in want)
+    lim = rms.limits(x, p, dx, want)
+    out = _train(dict(heads=1, n=n, d=d, dtype="f16"), s)
+    off = {k: rms.rms(out[k], want[k]) / lim[k] for k in lim}
+    assert all(v <= 1.0 for v in off.values()), off
