@@ -15,7 +15,7 @@
 // With a softmax the row maximum and sum run along (one pass over the data);
 // the reference of the exponentials only moves when the maximum has grown by
 // more than kLazy, which keeps the rescaling of the accumulators rare and the
-// exponentials below 2^8 (half-precision products stay far from overflow);
+// exponentials below 2^8 (2^15 with fp16's factor: no overflow);
 // the results are brought to the true maximum at the end.
 //
 // Tiles whose mask is 0 for every pair are never loaded: the mask's value
@@ -30,6 +30,13 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 static constexpr float kLog2e = 1.4426950408889634f;
 static constexpr float kLazy = 5.5f;  // natural units: 2^8
 static constexpr int kListCap = 2048;
+
+template <typename T> struct is_f16 {
+  static constexpr bool value = false;
+};
+template <> struct is_f16<f16> {
+  static constexpr bool value = true;
+};
 
 template <typename T> struct Mma;
 template <> struct Mma<f16> {
@@ -302,6 +309,12 @@ template <class P> struct Plane {
   // 132 and 140.)
   static constexpr float kScaleMost = 65000.0f;
   static constexpr int kScaleAt = 6, kScaleFirst = 40;
+
+  // A softmax's exponentials in fp16 carry a factor 2^7 (at most 2^15 in all then):
+  // weights down to 2^-21 of a row's largest keep all bits of the type.  Without it
+  // those below 2^-14 lost them: where one key takes nearly all weight the others'
+  // share was off by up to 4 %.
+  static constexpr float kLift = is_f16<T>::value ? 7.0f : 0.0f;
 
   const KArgs& a;
   typename P::B b;
@@ -620,7 +633,7 @@ template <class P> struct Plane {
           for (int i = 0; i < 16; ++i) acc[d][i] *= f;
       }
       const float mz = mref == -__builtin_huge_valf() ? 0.0f : mref;
-      const float mc = -mz * (P::FOLD * kLog2e);
+      const float mc = kLift - mz * (P::FOLD * kLog2e);
 #pragma unroll
       for (int sub = 0; sub < G::NSUB; ++sub) {
         float X[16];
@@ -937,7 +950,7 @@ template <class P> struct Plane {
       const Halves lh = halves(lsum);
       lsum = lh.a + lh.b;
       // to the true maximum
-      const float f = mref == mtrue ? 1.0f : __builtin_amdgcn_exp2f((mref - mtrue) * (P::FOLD * kLog2e));
+      const float f = __builtin_amdgcn_exp2f((mref == mtrue ? 0.0f : (mref - mtrue) * (P::FOLD * kLog2e)) - kLift);
       lsum *= f;
 #pragma unroll
       for (int d = 0; d < NA; ++d)

@@ -1,6 +1,6 @@
-"""fp16 attention and its gradient where the plane's values lie below fp16's normal
-numbers, or past its largest: small and large gradients, long rows.  Limits are
-counted from the roundings (layer_rms)."""
+"""fp16 attention and its gradient where values below fp16's normal numbers meet
+others: small and large gradients, long rows, a key that takes nearly all of a
+row's weight.  Limits are counted from the roundings (layer_rms, layer_ref)."""
 
 import numpy as np
 import pytest
@@ -9,7 +9,7 @@ from paper_2406_09465_amd import graphs
 
 from . import layer_ref as ref
 from . import layer_rms as rms
-from .test_gpu_layer_ops import _run
+from .test_gpu_layer_ops import _check, _run
 
 pytestmark = pytest.mark.gpu
 
@@ -52,6 +52,23 @@ def test_gradients_of_long_rows(n, m):
     out = _train(dict(heads=1, n=n, m=m, d=d, dtype="f16"), s)
     off = {k: rms.rms(out[k], want[k]) / lim[k] for k in lim}
     assert all(v <= 1.0 for v in off.values()), off
+
+
+@pytest.mark.parametrize("at", [0, 1700])
+@pytest.mark.parametrize("n,m", [(1, 2000), (8, 4096), (200, 2000)])
+def test_a_key_that_takes_nearly_all_weight(n, m, at):
+    """One key scores 14 above the others, with zeros as its value: the result is
+    what the others' weights, 8e-7 each, leave, and so are their gradients."""
+    d, heads = 64, 2
+    rng = np.random.default_rng(5)
+    x = {"Q": rng.normal(0, 0.05, (1, heads, n, d)), "K": rng.normal(0, 0.05, (1, heads, m, d)), "V": 1 + rng.normal(0, 0.2, (1, heads, m, d)),
+         "dO": rng.normal(0, 100.0, (1, heads, n, d))}
+    x["Q"][..., 0], x["K"][..., 0] = 8.0, 0.0
+    x["K"][:, :, at, :], x["V"][:, :, at, :] = 0.0, 0.0
+    x["K"][:, :, at, 0] = 14.03125
+    x, s = _stored(x)
+    want = ref.attention(x, "f16", heads, heads, grad=True)
+    _check(_train(dict(heads=heads, n=n, m=m, d=d, dtype="f16"), s), want, "f16", ("L",))
 
 
 def test_gradients_past_the_range_of_fp16():
