@@ -957,7 +957,9 @@ template <class P> struct Plane {
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[d][i] *= f;
     }
-    if constexpr (!P::WSPLIT && P::SPLIT == 1) {
+    if constexpr (P::NOP == 0) {
+      // bins only: join_bins has joined the waves and the splits
+    } else if constexpr (!P::WSPLIT && P::SPLIT == 1) {
 #pragma unroll
       for (int g = 0; g < NGRP; ++g) {
         f32x4 v;

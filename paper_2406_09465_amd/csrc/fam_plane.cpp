@@ -1068,7 +1068,8 @@ struct PlaneGen {
       p << "  static constexpr int BCNT = " << gk.args.size() << ";\n";
       gk.args.push_back(cnt);
     }
-    if (SPLIT > 1) {
+    gk.wg_split = SPLIT > 1;
+    if (SPLIT > 1 && !outs_p.empty()) {
       int nreg = 0;
       for (auto& w : out_w) nreg += (int)((w.shape[0] + 31) / 32 * 32) / 2;
       ArgRef scr;
@@ -1081,7 +1082,6 @@ struct PlaneGen {
       cnt.bytes = (size_t)(NB * OTILES) * 128;
       p << "  static constexpr int CNT = " << gk.args.size() << ";\n";
       gk.args.push_back(cnt);
-      gk.wg_split = true;
     }
     p << "};\n";
     std::ostringstream src;
