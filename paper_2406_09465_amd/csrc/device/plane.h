@@ -1042,47 +1042,66 @@ template <class P> struct Plane {
         }
         __syncthreads();
         if (!misc[1]) return;
-        float f[P::SPLIT];
+        auto factor = [&](float mv) { return mv == mtrue ? 1.0f : __builtin_amdgcn_exp2f((mv - mtrue) * (P::FOLD * kLog2e)); };
+        // Rounds of up to 32 vectors of partial results: a round trip to the
+        // device's point of coherence is 1 to 2 us.  Unrolled, the compiler puts the
+        // loads of several rounds in flight (keys' gradients of 300 rows, 4 heads on
+        // 1, width 64, bf16: 8.6 us, 9.6 one round at a time), but past these vectors
+        // it spills them (width 224: 23 us, 15.5; one token, 4 fp32 heads of width
+        // 208 in 16 splits: 1140 registers, 133 us and 32).
+        constexpr int ZB = share >= 32 ? 1 : P::SPLIT < 32 / share ? P::SPLIT : 32 / share;
+        constexpr bool flat = P::SPLIT * share <= (P::WPE == 1 ? 112 : 48);
+        float ls[P::SPLIT], f[P::SPLIT];
         if constexpr (P::SOFTMAX) {
-          float mz[P::SPLIT], lz[P::SPLIT];
+          mtrue = P::MINIT, lsum = 0.0f;
 #pragma unroll
           for (int zz = 0; zz < P::SPLIT; ++zz) {
             const float4 q = coherent_load4(rs, at(zz, NGRP));
-            mz[zz] = q.x, lz[zz] = q.y;
+            f[zz] = q.x, ls[zz] = q.y;
           }
-          float m = P::MINIT, l = 0.0f;
 #pragma unroll
-          for (int zz = 0; zz < P::SPLIT; ++zz) m = k_max(m, mz[zz]);
+          for (int zz = 0; zz < P::SPLIT; ++zz) mtrue = k_max(mtrue, f[zz]);
+          if constexpr (flat)
 #pragma unroll
-          for (int zz = 0; zz < P::SPLIT; ++zz) {
-            f[zz] = mz[zz] == m ? 1.0f : __builtin_amdgcn_exp2f((mz[zz] - m) * (P::FOLD * kLog2e));
-            l += lz[zz] * f[zz];
-          }
-          mtrue = m, lsum = l;
+            for (int zz = 0; zz < P::SPLIT; ++zz) {
+              f[zz] = factor(f[zz]);
+              lsum += ls[zz] * f[zz];
+            }
         }
-        // up to 32 vectors of partial results in flight: a round trip to the
-        // device's point of coherence is 1 to 2 us
-        constexpr int ZB = share >= 32 ? 1 : P::SPLIT < 32 / share ? P::SPLIT : 32 / share;
 #pragma unroll
         for (int g = 0; g < share; ++g) v[g] = f32x4{};
+        auto round = [&](int z0) {
+          float4 q[ZB][share], mq[ZB];
 #pragma unroll
-        for (int z0 = 0; z0 < P::SPLIT; z0 += ZB) {
-          float4 q[ZB][share];
+          for (int zz = 0; zz < ZB; ++zz) {
+            const int zc = z0 + zz < P::SPLIT ? z0 + zz : P::SPLIT - 1;
+            if constexpr (P::SOFTMAX && !flat) mq[zz] = coherent_load4(rs, at(zc, NGRP));
 #pragma unroll
-          for (int zz = 0; zz < ZB; ++zz)
-#pragma unroll
-            for (int g = 0; g < share; ++g)
-              q[zz][g] = coherent_load4(rs, at(z0 + zz < P::SPLIT ? z0 + zz : P::SPLIT - 1, g0 + g < NGRP ? g0 + g : NGRP - 1));
+            for (int g = 0; g < share; ++g) q[zz][g] = coherent_load4(rs, at(zc, g0 + g < NGRP ? g0 + g : NGRP - 1));
+          }
 #pragma unroll
           for (int zz = 0; zz < ZB; ++zz) {
             if (z0 + zz >= P::SPLIT) continue;
+            float fz = 1.0f;
+            if constexpr (P::SOFTMAX && flat) fz = f[z0 + zz];
+            if constexpr (P::SOFTMAX && !flat) {
+              fz = factor(mq[zz].x);
+              lsum += mq[zz].y * fz;
+            }
 #pragma unroll
             for (int g = 0; g < share; ++g) {
               const f32x4 x = {q[zz][g].x, q[zz][g].y, q[zz][g].z, q[zz][g].w};
-              if constexpr (P::SOFTMAX) v[g] += x * f[z0 + zz];
+              if constexpr (P::SOFTMAX) v[g] += x * fz;
               else v[g] += x;
             }
           }
+        };
+        if constexpr (flat) {
+#pragma unroll
+          for (int z0 = 0; z0 < P::SPLIT; z0 += ZB) round(z0);
+        } else {
+#pragma unroll 1
+          for (int z0 = 0; z0 < P::SPLIT; z0 += ZB) round(z0);
         }
       }
 #pragma unroll
