@@ -261,6 +261,8 @@ def instnorm(hh=224, ww=224, c=32, dtype="f16", eps=1e-5, extra_outputs=()):
 def layernorm(m=4096, d=768, dtype="f16", eps=1e-5, extra_outputs=()):
     """LayerNorm of the rows of X that keeps what its gradient needs: the row
     means ``mu`` and reciprocal deviations ``r`` (fp32)."""
+    if not 0 <= eps < math.inf:
+        raise ValueError("eps must be finite and not negative")
     b = _B(dtype)
     b.inp("X", (m, d))
     b.inp("gamma", (d,))
@@ -336,8 +338,8 @@ class _Attention:
             raise ValueError("a prefix extends a causal mask: causal must be set")
         if bool(buckets) != bool(radius) or buckets < 0 or radius < 0:
             raise ValueError("radius and buckets go together")
-        if not 0 <= cap < math.inf:
-            raise ValueError("cap must be finite and not negative (0: none)")
+        if not (cap == 0 or 1e-30 <= cap < math.inf):  # (scores are divided by it in fp32)
+            raise ValueError("cap must be 0 (none) or finite and at least 1e-30")
         self.b, self.sizes = b, dict(batch=batch, heads=heads, kv_heads=kv_heads, n=n, m=m, d=d, cap=cap, slopes=slopes,
                                      causal=causal, prefix=prefix, documents=documents, lengths=lengths, radius=radius,
                                      buckets=buckets)
