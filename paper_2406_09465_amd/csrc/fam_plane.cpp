@@ -835,7 +835,7 @@ struct PlaneGen {
       // heads of 4000 rows 33 us in two splits, 24.5 in one.)
       if (!WSPLIT && uneven && wgs >= 256) SPLIT = wgs <= 256 * OCC && nstr >= 2560 ? 2 : 1;
     }
-    if (wgs * SPLIT > (int64_t)1 << 30) bad("too many workgroups");
+    if (wgs * SPLIT * NW * 64 >= (int64_t)1 << 32) bad("more threads than a launch holds");
   }
 
   GenKernel generate(int index) {

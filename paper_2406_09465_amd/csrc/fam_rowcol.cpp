@@ -420,6 +420,7 @@ bool match_binsum(const KInfo& ki, std::string* why) {
   if (b < 0 || ki.k.outs.size() != 1 || ki.k.outs[0] != b) return *why = "binsum: the only output must be the sum by bins", false;
   for (int v : ki.k.prims)
     if (v != b && !ki.ancestor(v, b)) return *why = "binsum: a node that the sum does not read", false;
+  if (numel(ki.g.nodes[b].shape) * 256 >= (int64_t)1 << 32) return *why = "binsum: more threads than a launch holds", false;
   return true;
 }
 
