@@ -27,4 +27,4 @@ def test_more_threads_than_a_launch_holds():
         assert w.graph.family(*w.kernels("fused")[0]) == family
     for rows, family in ((4095, "binsum"), (4096, "none")):
         w = graphs.layout_probe("bin_sum", "f32", [(rows, 8), (8,)], shape=(rows, 1, 4096))
-        assert w.graph.family(*w.kernels("unfused")[-1]) == family
+        assert w.graph.family([w.ids["out"]], [w.ids["out"]]) == family
