@@ -30,6 +30,21 @@ def to_f64(t: torch.Tensor) -> np.ndarray:
     return t.detach().float().cpu().numpy().astype(np.float64)
 
 
+def check_inputs(graph, names, tensors, device="cuda"):
+    """Kernels read the bytes behind a pointer: a tensor of another type, shape or
+    order than its graph input, or on another device, is an error here."""
+    if len(tensors) != len(names):
+        raise ValueError(f"{len(names)} inputs ({', '.join(names)}), got {len(tensors)} tensors")
+    for name, i, t in zip(names, graph.inputs(), tensors):
+        _, dt, shape = graph.node_info(i)
+        if t.dtype != TORCH_DTYPE[dt] or tuple(t.shape) != tuple(shape):
+            raise ValueError(f"input {name} is {dt} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+        if not t.is_contiguous():
+            raise ValueError(f"input {name} is not contiguous")
+        if t.device.type != torch.device(device).type:
+            raise ValueError(f"input {name} is on {t.device}")
+
+
 class PlanRunner:
     """A compiled plan plus device buffers for one workload instance."""
 
@@ -58,9 +73,10 @@ class PlanRunner:
     def _ptrs(self):
         """ctypes pointer arrays of the current input and output tensors (rebuilt
         only when a tensor changes, to keep the per-launch host cost low)."""
-        key = tuple(t.data_ptr() for t in self.ins) + (None,) + tuple(t.data_ptr() for t in self.outs)
+        key = tuple((id(t), t.data_ptr()) for t in self.ins) + (None,) + tuple(t.data_ptr() for t in self.outs)
         if getattr(self, "_ptr_key", None) != key:
-            self._ptr_key = key
+            check_inputs(self.w.graph, self.w.input_names, self.ins, self.device)
+            self._ptr_key, self._checked = key, list(self.ins)  # (held, so that no other tensor takes their ids)
             self._ptr_arrays = (pointer_array([t.data_ptr() for t in self.ins]),
                                 pointer_array([t.data_ptr() for t in self.outs]))
         return self._ptr_arrays

@@ -28,3 +28,20 @@ def test_more_threads_than_a_launch_holds():
     for rows, family in ((4095, "binsum"), (4096, "none")):
         w = graphs.layout_probe("bin_sum", "f32", [(rows, 8), (8,)], shape=(rows, 1, 4096))
         assert w.graph.family([w.ids["out"]], [w.ids["out"]]) == family
+
+
+def test_inputs_that_are_not_what_the_graph_says():
+    import torch
+
+    from paper_2406_09465_amd.runner import check_inputs
+    w = graphs.build("mha", batch=2, heads=4, kv_heads=2, n=3, m=8, d=16, dtype="f16")
+    make = lambda *s, dtype=torch.float16: torch.zeros(s, dtype=dtype)  # noqa: E731
+    q, kv = make(2, 4, 3, 16), make(2, 2, 8, 16)
+    ok = lambda *t: check_inputs(w.graph, w.input_names, t, "cpu")  # noqa: E731
+    ok(q, kv, kv)
+    for bad, what in (((q, kv), "3 inputs"), ((q, kv, make(2, 2, 7, 16)), "input V is f16"), ((q, make(2, 4, 8, 16), kv), "input K"),
+                      ((make(2, 4, 3, 16, dtype=torch.float32), kv, kv), "input Q"), ((q, make(2, 8, 2, 16).transpose(1, 2), kv), "contiguous")):
+        with pytest.raises(ValueError, match=what):
+            ok(*bad)
+    with pytest.raises(ValueError, match="on cpu"):
+        check_inputs(w.graph, w.input_names, (q, kv, kv), "cuda")
