@@ -9,7 +9,7 @@ from paper_2406_09465_amd import graphs
 
 from . import layer_ref as ref
 from . import layer_rms as rms
-from .test_gpu_layer_ops import _check, _run
+from .test_gpu_layer_ops import _check, _run, _unpack
 
 pytestmark = pytest.mark.gpu
 
@@ -82,3 +82,20 @@ def test_gradients_past_the_range_of_fp16():
     out = _train(dict(heads=1, n=n, d=d, dtype="f16"), s)
     off = {k: rms.rms(out[k], want[k]) / lim[k] for k in lim}
     assert all(v <= 1.0 for v in off.values()), off
+
+
+@pytest.mark.parametrize("n", [1, 70])
+def test_whatever_lies_behind_a_sequence_in_fp16(n):
+    """NaN, infinities and fp16's lowest number past a sequence's length move no scale:
+    results with dO of deviation 1e-3 are those of zeros there."""
+    case = dict(dtype="f16", n=n, m=150, d=64, heads=4, kv_heads=2, lengths=(70, 133), batch=2, causal=True)
+    sizes, x, s, _ = _unpack(case)
+    x["dO"], s["dO"] = ref.rounded(x["dO"] * 1e-3, "f16")
+    want = ref.attention(x, "f16", 4, 2, causal=True, grad=True)
+    for k in ("K", "V"):
+        for b, size in enumerate((70, 133)):
+            rows = s[k][b, :, size:]
+            rows[...] = np.resize(np.array([np.nan, np.inf, -np.inf, -65504], np.float16), rows.shape)
+    out = _train(sizes, s)
+    _check(out, want, "f16", ("L",))
+    assert np.all(out["dK"][0, :, 70:] == 0) and np.all(out["dV"][1, :, 133:] == 0)
