@@ -126,7 +126,9 @@ GenKernel gen_rowcol(const KInfo& ki, int index) {
   // Eight waves per workgroup and a workgroup per compute unit (16384 x 4096
   // bf16, three row tensors: 84 us, four waves and 512 workgroups 96; sixteen
   // waves 97).  Rows past 4096 take sixteen waves, whose hand-over of the sums
-  // is the wider one (500 x 8192 fp16: 32 us, with eight 55).
+  // is the wider one (500 x 8192 fp16: 32 us, with eight 55), although a lane then
+  // has 128 registers and the row loop spills some (28 to 38 at bf16 4608 to 12288,
+  // 43 to 52 at f32 7168 and 8192; 4096 x 5120 bf16: 57 us, its bytes 26).
   const int NT = std::max(rc.L > 4096 ? 1024 : 512, G);
   const int RPB = NT / G, WR = G > 64 ? G / 64 : 1;
   const int64_t blocks = (rc.R + RPB - 1) / RPB;
@@ -403,7 +405,8 @@ GenKernel gen_rowcol(const KInfo& ki, int index) {
 
 // ---------------------------------------------------------------------------
 // A sum by bins on its own (a plan that stores the summed tensor): a workgroup
-// per result element adds the matching values in a fixed order.
+// per result element adds the matching values in a fixed order, and so reads all
+// values once per bin (only plans of one kernel per primitive come here).
 // ---------------------------------------------------------------------------
 
 bool match_binsum(const KInfo& ki, std::string* why) {

@@ -521,8 +521,8 @@ def mha(batch=1, heads=8, kv_heads=None, n=1024, m=None, d=64, dtype="bf16", cap
     a.op("Ex", "exp", ["Z"])
     e = a.masked("E", "Ex")
     a.op("l", "reduce_sum", [e], axis=-1, keepdim=True)
-    # the exponentials are rounded to the operands' type for the product (at
-    # most 1, so a half step of that type each); their sum is fp32
+    # the exponentials are rounded to the operands' type for the product (half a
+    # step of that type each; the fused kernel's, in fp16, times 2^7); their sum is fp32
     ec = e if dtype == "f32" else a.op("Ec", "identity", [e], dtype)
     a.op("Ov", "matmul", [ec, a.v])
     a.op("lt", "max", ["l"], scalar=TINY)
@@ -550,7 +550,10 @@ def mha_grad(batch=1, heads=8, kv_heads=None, n=1024, m=None, d=64, dtype="bf16"
     The scores are evaluated again by the kernel that owns the queries (dQ, dT)
     and by the one that owns the keys (dK, dV): every sum is taken in a fixed
     order.  The fused plan takes as many buckets as their sums fit LDS beside the
-    tiles (about 400 for 16-bit heads of 64)."""
+    tiles (about 400 for 16-bit heads of 64); in fp16 it scales P and dX by powers of
+    two, so that a small dO keeps its bits and a large one stays finite (the
+    unfused plan stores both as they are).  Allocation-free execution has 32 MiB for
+    the buckets' partial sums."""
     b = _B(dtype)
     a = _Attention(b, batch, heads, kv_heads, n, m, d, cap, slopes, causal, prefix, documents, lengths, radius, buckets)
     b.inp("dO", (batch, heads, n, d))
@@ -580,7 +583,8 @@ def mha_grad(batch=1, heads=8, kv_heads=None, n=1024, m=None, d=64, dtype="bf16"
     def score_gradient(delta, c):
         """dS and dX for one of the two kernels.  P and dX are rounded to the operands' type for
         the products, half a step each, as every sum over them averages such errors out (two parts
-        of dX would keep it, for one product more in either kernel)."""
+        of dX would keep it, for one product more in either kernel).  In fp16 the fused kernels
+        round them times a power of two, which keeps them among its normal numbers."""
         a.prims.clear()
         a.op("dD" + c, "sub", ["dP", delta])
         a.op("dS" + c, "mul", [p, "dD" + c])
