@@ -41,7 +41,8 @@ def check_inputs(graph, names, tensors, device="cuda"):
             raise ValueError(f"input {name} is {dt} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
         if not t.is_contiguous():
             raise ValueError(f"input {name} is not contiguous")
-        if t.device.type != torch.device(device).type:
+        d = torch.device(device)
+        if t.device.type != d.type or (d.index is not None and t.device.index != d.index):
             raise ValueError(f"input {name} is on {t.device}")
 
 
@@ -75,7 +76,7 @@ class PlanRunner:
         only when a tensor changes, to keep the per-launch host cost low)."""
         key = tuple((id(t), t.data_ptr()) for t in self.ins) + (None,) + tuple(t.data_ptr() for t in self.outs)
         if getattr(self, "_ptr_key", None) != key:
-            check_inputs(self.w.graph, self.w.input_names, self.ins, self.device)
+            check_inputs(self.w.graph, self.w.input_names, self.ins, self.ws.device)
             self._ptr_key, self._checked = key, list(self.ins)  # (held, so that no other tensor takes their ids)
             self._ptr_arrays = (pointer_array([t.data_ptr() for t in self.ins]),
                                 pointer_array([t.data_ptr() for t in self.outs]))

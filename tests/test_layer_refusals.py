@@ -1,5 +1,7 @@
 """Arguments of the layer operators that no kernel can take."""
 
+import types
+
 import pytest
 
 from paper_2406_09465_amd import graphs
@@ -45,3 +47,6 @@ def test_inputs_that_are_not_what_the_graph_says():
             ok(*bad)
     with pytest.raises(ValueError, match="on cpu"):
         check_inputs(w.graph, w.input_names, (q, kv, kv), "cuda")
+    other = types.SimpleNamespace(dtype=q.dtype, shape=q.shape, is_contiguous=lambda: True, device=torch.device("cuda", 1))
+    with pytest.raises(ValueError, match="on cuda:1"):
+        check_inputs(w.graph, w.input_names, (other, kv, kv), "cuda:0")
