@@ -5,6 +5,7 @@ import pytest
 
 from .test_gpu_layer_ops import test_attention as attention
 from .test_gpu_layer_ops import test_attention_gradient as gradient
+from .test_gpu_layer_ops import test_same_bits_again_on_another_stream_and_replayed as same_bits
 
 FWD = [
     dict(dtype="f32", n=1, m=500, d=208, heads=4),
@@ -36,3 +37,14 @@ def test_attention_joined_in_rounds(case):
 @pytest.mark.parametrize("case", GRAD, ids=_id)
 def test_gradients_joined_in_rounds(case):
     gradient(case)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name,sizes", [
+    ("mha", dict(heads=4, n=1, m=500, d=208, dtype="f32")),
+    ("mha", dict(batch=2, heads=4, n=1, m=16305, d=128, dtype="bf16", slopes=True, lengths=True)),
+    ("mha_grad", dict(heads=4, kv_heads=1, n=300, d=128, dtype="f16", causal=True, cap=8.0)),
+    ("mha_grad", dict(heads=4, kv_heads=1, n=300, d=96, dtype="f32")),
+], ids=str)
+def test_joins_repeat_their_bits(name, sizes):
+    same_bits(name, sizes)
