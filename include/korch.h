@@ -77,6 +77,10 @@ typedef enum {
   KORCH_ADD = 32, KORCH_SUB, KORCH_MUL, KORCH_DIV, KORCH_MAX, KORCH_MIN,
   /* comparisons: 1 where I1[x] < (<=, >, >=, ==) I2[x], else 0 (NaN compares false) */
   KORCH_LT, KORCH_LE, KORCH_GT, KORCH_GE, KORCH_EQ,
+  /* O[x] = cos(I1[x] I2[x]) and sin(I1[x] I2[x]): a position times a frequency, in radians.  The
+     product is exact (never rounded to fp32) and reduced exactly while it is below 2^50, so
+     far positions keep their angles.  Two tensors, no scalar. */
+  KORCH_COS_MUL, KORCH_SIN_MUL,
   /* elementwise choice: O[x] = C[x] != 0 ? I1[x] : I2[x] (inputs C, I1, I2, broadcast like
      the binary ones), or I2 = scalar when attrs.has_scalar (inputs C, I1).  The value that is
      not chosen has no effect (it may be NaN). */
@@ -145,7 +149,12 @@ typedef enum {
   KORCH_FAM_PLANE = 8,       /* products that meet in a plane of scores kept in registers: attention of
                                 any length (softmax in one pass, masks, biases) and its gradients   */
   KORCH_FAM_ROWCOL = 9,      /* a row program with sums over the rows (LayerNorm's gradient)       */
-  KORCH_FAM_BINSUM = 10      /* a sum by bins on its own                                           */
+  KORCH_FAM_BINSUM = 10,     /* a sum by bins on its own                                           */
+  KORCH_FAM_GROUP = 11,      /* group norm, channels last: statistics of channel groups over the
+                                positions of an image, what normalizes by them, and its gradient   */
+  KORCH_FAM_ROTARY = 12,     /* pairs of a head's dims turned by angles that every head shares     */
+  KORCH_FAM_MULTI = 13       /* many tensors at once: the sum of their squares, or each of them
+                                times one number                                                    */
 } korch_family;
 
 const char* korch_last_error(void);

@@ -63,6 +63,8 @@ BINARY = {
     "gt": lambda x, y: (x > y).astype(np.float64),
     "ge": lambda x, y: (x >= y).astype(np.float64),
     "eq": lambda x, y: (x == y).astype(np.float64),
+    "cos_mul": lambda x, y: np.cos(x * y),
+    "sin_mul": lambda x, y: np.sin(x * y),
 }
 
 

@@ -42,7 +42,7 @@ OPS = {
     "neg": 1, "exp": 2, "log": 3, "tanh": 4, "sqrt": 5, "rsqrt": 6, "relu": 7, "square": 8, "recip": 9,
     "gelu_tanh": 10, "abs": 11, "identity": 12,
     "add": 32, "sub": 33, "mul": 34, "div": 35, "max": 36, "min": 37,
-    "lt": 38, "le": 39, "gt": 40, "ge": 41, "eq": 42, "select": 48,
+    "lt": 38, "le": 39, "gt": 40, "ge": 41, "eq": 42, "cos_mul": 43, "sin_mul": 44, "select": 48,
     "reduce_sum": 64, "reduce_mean": 65, "reduce_max": 66, "broadcast": 67,
     "transpose": 96, "reshape": 97, "slice": 98, "pad": 99, "concat": 100,
     "fill": 101, "iota": 102, "gather": 103, "bin_sum": 104,
@@ -53,7 +53,7 @@ OP_NAMES = {v: k for k, v in OPS.items()}
 RW_DEFER_DIV, RW_REDUCE_AS_PRODUCT, RW_MERGE_PRODUCTS, RW_FOLD_SCALE, RW_ALL = 1, 2, 4, 8, 47
 RW_LAYOUT_VARIANTS, RW_SPLIT_MOMENTS = 16, 32
 FAMILIES = {0: "none", 1: "pointwise", 2: "row", 3: "colreduce", 4: "gemm", 5: "conv", 6: "attention", 7: "splitk",
-            8: "plane", 9: "rowcol", 10: "binsum"}
+            8: "plane", 9: "rowcol", 10: "binsum", 11: "group", 12: "rotary", 13: "multi"}
 
 E_UNSUPPORTED = -20
 E_COMPILE = -23

@@ -205,6 +205,8 @@ std::string binary_expr(int op, const std::string& x, const std::string& y) {
     case KORCH_GT: return "(" + x + " > " + y + " ? 1.0f : 0.0f)";
     case KORCH_GE: return "(" + x + " >= " + y + " ? 1.0f : 0.0f)";
     case KORCH_EQ: return "(" + x + " == " + y + " ? 1.0f : 0.0f)";
+    case KORCH_COS_MUL: return "k_cos_mul(" + x + ", " + y + ")";
+    case KORCH_SIN_MUL: return "k_sin_mul(" + x + ", " + y + ")";
   }
   fail(KORCH_E_UNSUPPORTED, std::string("no binary expression for ") + op_name(op));
 }

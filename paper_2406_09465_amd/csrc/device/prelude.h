@@ -227,6 +227,35 @@ __device__ __forceinline__ float f_mish(float x) {
   return x * f_div(n, n + 2.0f);
 }
 
+// ---- cos and sin of a product of two fp32 numbers ---------------------------
+// The product a = x y has at most 48 bits: exact in fp64.  In turns it is
+// a / (2 pi), with 1 / (2 pi) as the sum of two doubles: p = a hi, whose
+// rounding error fma(a, hi, -p) is exact, plus a lo.  The whole turns leave p
+// exactly (p - rint(p)), so the angle inside the turn is good to 2^-50 turns as
+// long as a is below 2^50; the rest, at most an eighth of a turn beside a
+// quarter, goes on in fp32, where the Taylor sums below are off by less than
+// 2^-29 (x^11 / 11! and x^12 / 12! at x = pi / 4).
+struct SinCos {
+  float s, c;
+};
+__device__ __forceinline__ SinCos k_sincos_mul(float x, float y) {
+  const double a = (double)x * (double)y;
+  const double hi = 0x1.45f306dc9c883p-3, lo = -0x1.6b01ec5417056p-57;
+  const double p = a * hi;
+  double f = (p - __builtin_rint(p)) + __builtin_fma(a, lo, __builtin_fma(a, hi, -p));
+  f -= __builtin_rint(f);
+  const double q = __builtin_rint(f * 4.0);  // quarter turns, -2 .. 2
+  const float z = (float)((f - q * 0.25) * 6.283185307179586), z2 = z * z;
+  // the low bits of q (1.5 * 2^52 moves them to the end of the significand)
+  const int k = (int)__builtin_bit_cast(long long, q + 6755399441055744.0);
+  const float s = z + z * z2 * (-1.0f / 6 + z2 * (1.0f / 120 + z2 * (-1.0f / 5040 + z2 * (1.0f / 362880))));
+  const float c = 1.0f + z2 * (-0.5f + z2 * (1.0f / 24 + z2 * (-1.0f / 720 + z2 * (1.0f / 40320 - z2 * (1.0f / 3628800)))));
+  const float u = (k & 1) ? c : s, v = (k & 1) ? s : c;
+  return {(k & 2) ? -u : u, ((k + 1) & 2) ? -v : v};
+}
+__device__ __forceinline__ float k_cos_mul(float x, float y) { return k_sincos_mul(x, y).c; }
+__device__ __forceinline__ float k_sin_mul(float x, float y) { return k_sincos_mul(x, y).s; }
+
 // ---- fp32 partial results handed from workgroup to workgroup --------------
 // Device-scope (agent) atomic stores and loads are performed at the point of
 // coherence of the whole device, so a value one workgroup stores this way is

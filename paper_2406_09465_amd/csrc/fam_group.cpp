@@ -1,0 +1,932 @@
+// Group norm, channels last, and its gradient: kernels over a map
+// [B, P, G, K] (images, positions, groups, channels of a group; C = G K
+// channels are consecutive) whose nodes are
+//   * full: elementwise primitives on the map;
+//   * per channel, group or image: elementwise primitives on what does not
+//     vary along P ([B, 1, G, K], [B, 1, G, 1], [G, K] ..);
+//   * sums or means over P (full -> [B, 1, G, K]), over a group's channels
+//     ([B, 1, G, K] -> [B, 1, G, 1]) and over the images ([B, 1, G, K] -> [1, 1, G, K]);
+//   * reshapes that rename such tensors.
+//
+// HBM bound throughout (10 to 30 operations per element).  A thread keeps one
+// vector of channels for every row it visits, so what belongs to a channel or
+// its group is loaded and computed once per thread, and consecutive threads
+// read consecutive memory.  Kinds of kernels:
+//   * slab: a workgroup owns whole groups of one image, whose rows stay in its
+//     registers in their own type: every pass over the positions (mean, then
+//     variance, then the result) after the first reads registers, and the map
+//     is read once.  One launch;
+//   * sums: one pass over the positions, split over workgroups; the last
+//     workgroup of an image adds the partial sums in order and computes what
+//     follows from them;
+//   * moments: means and variances of groups in one pass (per thread, rows in
+//     batches of eight whose mean and centred squares merge into the running
+//     ones; then mean and M2 of threads and of workgroups merge likewise), so
+//     a mean far from zero costs the variance no bits;
+//   * apply: no sum over positions; rows are spread over the chip.
+// Every sum is fp32 in a fixed order (no floating-point atomics).
+#include <algorithm>
+#include <cmath>
+
+#include "families.h"
+
+namespace korch {
+
+namespace {
+
+int64_t pow2floor(int64_t x) {
+  int64_t p = 1;
+  while (2 * p <= x) p *= 2;
+  return p;
+}
+
+constexpr int kRowsInFlight = 8;     // rows that a thread loads together
+constexpr int64_t kHandOver = 16;    // partial results that one workgroup adds
+
+struct GroupGen {
+  const KInfo& ki;
+  const Graph& g;
+  int64_t B = 0, P = 0, G = 0, K = 0, C = 0;
+  Shape full;
+  enum Kind { Slab, Sums, Moments, Apply } kind = Apply;
+  std::map<int, int> root;           // reshape -> the node it renames
+  std::map<int, bool> is_full;       // nodes of the kernel (not reshapes)
+  std::map<int, int> gen;            // passes over the positions that a node needs
+  std::vector<int> r1, r3, r0;       // reductions over positions, a group's channels, images
+  std::vector<int> xfull;            // external maps
+  std::vector<int> full_outs, inv_outs;
+  int npass = 0;
+  int eb = 2;
+  // moments: the node of the mean, of the variance and the map
+  int mo_mu = -1, mo_var = -1, mo_x = -1;
+  std::set<int> mo_nodes;
+  // geometry
+  int VEC = 1, T = 256, NJ = 1, LY = 1, U = kRowsInFlight, NR = 1;
+  int64_t CT = 0, CVT = 0, tiles = 1, S = 1, chunk = 0;
+
+  GroupGen(const KInfo& k) : ki(k), g(k.g) {}
+
+  [[noreturn]] static void bad(const std::string& m) { fail(KORCH_E_UNSUPPORTED, "group: " + m); }
+  const Node& nd(int v) const { return g.nodes[v]; }
+  bool in(int v) const { return ki.in.count(v) > 0; }
+  int rt(int v) const {
+    auto f = root.find(v);
+    return f == root.end() ? v : f->second;
+  }
+
+  // Dims of a shape against the map's, right-aligned; false when it does not broadcast to it.
+  bool aligned(const Shape& s, Shape& d) const {
+    if (s.size() > 4) return false;
+    d.assign(4 - s.size(), 1);
+    d.insert(d.end(), s.begin(), s.end());
+    for (int i = 0; i < 4; ++i)
+      if (d[i] != 1 && d[i] != full[i]) return false;
+    return true;
+  }
+
+  void find_shape() {
+    for (int v : ki.reduces) {
+      const Shape& s = nd(nd(v).in[0]).shape;
+      if (nd(v).axis != 1 || s.size() != 4) continue;
+      if (!full.empty() && full != s) bad("sums over the positions of different maps");
+      full = s;
+    }
+    if (full.empty()) {
+      // no sum over positions: the map whose statistics [B, 1, G, 1] are read
+      int elementwise = 0;
+      for (int v : ki.k.prims) {
+        if (!is_elementwise(nd(v).op)) continue;
+        ++elementwise;
+        const Shape& s = nd(v).shape;
+        if (s.size() != 4 || (!full.empty() && numel(s) <= numel(full))) continue;
+        full = s;
+      }
+      if (full.empty() || elementwise < 2) bad("no map");
+      bool stat = false;
+      for (int u : ki.ext) stat = stat || (full[1] * full[3] > 1 && nd(u).shape == Shape{full[0], 1, full[2], 1});
+      if (!stat) bad("no statistics of groups are read");
+    }
+    B = full[0], P = full[1], G = full[2], K = full[3], C = G * K;
+    if (P >= ((int64_t)1 << 30) || C >= ((int64_t)1 << 20)) bad("more positions or channels than the kernels count");
+  }
+
+  void classify() {
+    std::set<int> outs(ki.k.outs.begin(), ki.k.outs.end());
+    for (int u : ki.ext) {
+      Shape d;
+      if (!aligned(nd(u).shape, d)) bad("an operand does not broadcast to the map");
+      if ((d[1] > 1 || P == 1) && nd(u).shape == full) {
+        // (with one position, a tensor that only sums over images read is theirs)
+        bool map = P > 1;
+        for (int c : g.consumers[u])
+          if (in(c) && !(op_kind(nd(c).op) == korch::Kind::Reduce && nd(c).axis == 0)) map = true;
+        if (map) {
+          xfull.push_back(u);
+          eb = std::max(eb, dtype_bytes(nd(u).dtype));
+        }
+      } else if (d[1] > 1) {
+        bad("an operand varies along the positions but is no map");
+      }
+    }
+    auto full_of = [&](int u) {
+      if (!in(u)) return std::find(xfull.begin(), xfull.end(), u) != xfull.end();
+      return (bool)is_full.at(rt(u));
+    };
+    auto gen_of = [&](int u) { return in(u) ? gen.at(rt(u)) : 0; };
+    for (int v : ki.k.prims) {
+      const Node& n = nd(v);
+      if (n.op == KORCH_RESHAPE) {
+        if (!in(n.in[0])) bad("a view of a stored tensor needs no kernel");
+        root[v] = rt(n.in[0]);
+        // an operand keeps the layout of what it renames
+        bool read = false;
+        for (int c : g.consumers[v]) read = read || (in(c) && nd(c).op != KORCH_RESHAPE);
+        if (read && n.shape != nd(root[v]).shape) bad("a reshaped operand");
+        if (dtype_bytes(n.dtype) < dtype_bytes(nd(root[v]).dtype) && !outs.count(v)) bad("a reshape that rounds");
+        continue;
+      }
+      Shape d;
+      if (op_kind(n.op) == korch::Kind::Reduce) {
+        if (n.op == KORCH_REDUCE_MAX || !n.attrs.keepdim || nd(n.in[0]).shape.size() != 4) bad("a reduction that is no sum or mean of the map with its axes kept");
+        const int u = n.in[0];
+        is_full[v] = false;
+        if (n.axis == 1) {
+          if (!full_of(u)) bad("a sum over positions of something that has none");
+          r1.push_back(v);
+          gen[v] = gen_of(u) + 1;
+          npass = std::max(npass, gen[v]);
+        } else if (n.axis == 3) {
+          if (full_of(u) || nd(u).shape != Shape{B, 1, G, K}) bad("a sum over a group's channels of something else than sums over positions");
+          if (!in(u)) bad("a sum over a group's channels of a stored tensor");
+          r3.push_back(v);
+          gen[v] = gen_of(u);
+        } else if (n.axis == 0) {
+          if (nd(u).shape != Shape{B, 1, G, K} || full_of(u)) bad("a sum over images of something else than per-channel values");
+          for (int c : g.consumers[v])
+            if (in(c) && nd(c).op != KORCH_RESHAPE) bad("a sum over images is read in the kernel");
+          r0.push_back(v);
+          gen[v] = gen_of(u);
+        } else {
+          bad("a sum over groups");
+        }
+        continue;
+      }
+      if (!is_elementwise(n.op)) bad(std::string("unsupported primitive ") + op_name(n.op));
+      if (!aligned(n.shape, d)) bad("a node does not broadcast to the map");
+      bool f = false;
+      int gn = 0;
+      for (int u : n.in) {
+        if (in(u) && std::find(r0.begin(), r0.end(), rt(u)) != r0.end()) bad("a sum over images is read in the kernel");
+        f = f || full_of(u), gn = std::max(gn, gen_of(u));
+      }
+      if (f && n.shape != full) bad("a node of the map in another shape");
+      if (!f && d[1] > 1) bad("a node varies along the positions without a map");
+      is_full[v] = f;
+      gen[v] = gn;
+    }
+    for (int o : ki.k.outs) {
+      const int v = rt(o);
+      if (std::find(r0.begin(), r0.end(), v) != r0.end()) continue;
+      if (is_full.at(v)) {
+        full_outs.push_back(o);
+        eb = std::max(eb, dtype_bytes(nd(o).dtype));
+      } else {
+        // one value per channel or per group of an image
+        const Shape& s = nd(v).shape;
+        if (s != Shape{B, 1, G, K} && s != Shape{B, 1, G, 1}) bad("an output that is neither a map nor per channel or group");
+        inv_outs.push_back(o);
+      }
+    }
+    for (int v : r0) {
+      bool out = false;
+      for (int o : ki.k.outs) out = out || rt(o) == v;
+      if (!out) bad("a sum over images that is not an output");
+    }
+    for (int v : r1) {
+      const Node& n = nd(v);
+      (void)n;
+      if (nd(v).shape != Shape{B, 1, G, K}) bad("sum over positions");
+    }
+  }
+
+  // mean over the positions (and the group), then the mean of the centred squares
+  bool find_moments() {
+    if (r1.size() != 2 || npass != 2 || xfull.size() != 1 || !full_outs.empty() || !r0.empty()) return false;
+    mo_x = xfull[0];
+    auto group = [&](int v) -> int {
+      if (K == 1) return v;
+      for (int r : r3)
+        if (nd(r).in[0] == v && nd(r).op == KORCH_REDUCE_MEAN) return r;
+      return -1;
+    };
+    const int a = r1[0], b = r1[1];
+    if (nd(a).op != KORCH_REDUCE_MEAN || nd(b).op != KORCH_REDUCE_MEAN || nd(a).in[0] != mo_x) return false;
+    mo_mu = group(a), mo_var = group(b);
+    if (mo_mu < 0 || mo_var < 0 || (K > 1 && r3.size() != 2)) return false;
+    const int q = nd(b).in[0];
+    if (!in(q) || !(nd(q).op == KORCH_SQUARE || (nd(q).op == KORCH_MUL && !nd(q).attrs.has_scalar && nd(q).in[0] == nd(q).in[1]))) return false;
+    const int d = nd(q).in[0];
+    if (!in(d) || nd(d).op != KORCH_SUB || nd(d).attrs.has_scalar || nd(d).in[0] != mo_x || nd(d).in[1] != mo_mu) return false;
+    mo_nodes = {a, b, mo_mu, mo_var, q, d};
+    for (int v : mo_nodes) {
+      if (v == mo_mu || v == mo_var) continue;
+      for (int c : g.consumers[v])
+        if (in(c) && !mo_nodes.count(c)) return false;
+      for (int o : ki.k.outs)
+        if (rt(o) == v) return false;
+    }
+    return true;
+  }
+
+  // Threads over a tile of CT channels.
+  void lanes(int threads) {
+    T = threads;
+    CVT = CT / VEC;
+    NJ = (int)((CVT + T - 1) / T);
+    LY = NJ == 1 ? (int)(T / CVT) : 1;
+  }
+
+  // Whether `nr` rows of `words` maps stay in a thread's registers beside the
+  // fp32 values of a row and the channels' own (256 registers; 1024 threads have 128 each).
+  bool slab_fits(int threads, int64_t nr, int vec, int words) const {
+    const int64_t raw = nr * std::max(1, vec * eb / 4) * words, own = (int64_t)vec * (words > 1 ? 8 : 5);
+    return threads == 256 ? raw <= 24 && nr <= 24 : threads == 512 ? raw <= 48 && nr <= 48 : raw + own <= 64 && nr <= 24;
+  }
+
+  // A slab of whole groups in a workgroup's registers: the fewest groups whose
+  // channels make runs of 64 bytes, so that half of each line a load touches
+  // is used; where those do not fit, the most that do.
+  bool slab_geometry() {
+    if (P > 65536 || xfull.empty()) return false;
+    const int words = std::max<int>(1, (int)xfull.size());
+    bool found = false;
+    int64_t best = 0;
+    for (int64_t gt = 1; gt <= G; ++gt) {
+      if (G % gt) continue;
+      int vec = 16 / eb;
+      while ((gt * K) % vec) vec /= 2;
+      const int64_t ct = gt * K;
+      bool fits = false;
+      for (int t : {256, 512, 1024}) {
+        if (ct / vec > t) continue;
+        const int64_t ly = t / (ct / vec), nr = (P + ly - 1) / ly;
+        if (slab_fits(t, nr, vec, words)) {
+          fits = true;
+          break;
+        }
+      }
+      if (!fits) continue;
+      found = true;
+      best = gt;
+      if (ct * eb >= 64) break;
+    }
+    if (!found) return false;
+    CT = best * K;
+    tiles = G / best;
+    VEC = 16 / eb;
+    while (CT % VEC) VEC /= 2;
+    for (int t : {256, 512, 1024}) {
+      if (CT / VEC > t) continue;
+      lanes(t);
+      NR = (int)((P + LY - 1) / LY);
+      if (slab_fits(t, NR, VEC, words)) break;
+    }
+    U = NR;
+    if (!r0.empty()) {
+      // the sums over images are handed over
+      if (B > kHandOver * 32 || B * tiles * ((int64_t)r0.size() * ((CT + 3) / 4 * 4)) * 4 * 17 / 16 > ((int64_t)16 << 20)) return false;
+    }
+    return B * tiles * T < ((int64_t)1 << 32);
+  }
+
+  void stream_geometry(int threads) {
+    CT = C;
+    VEC = 16 / eb;
+    while (CT % VEC) VEC /= 2;
+    while (threads < 1024 && CT / VEC > threads) threads *= 2;
+    lanes(threads);
+    if ((int64_t)NJ * VEC > 16 || CT > 8192) bad("more channels than a workgroup keeps");
+  }
+
+  void analyze() {
+    if (!ki.linear.empty()) bad("has linear primitives");
+    for (int v : ki.k.prims)
+      if (nd(v).op == KORCH_BIN_SUM || nd(v).op == KORCH_FILL || nd(v).op == KORCH_IOTA) bad("constants or bins");
+    find_shape();
+    classify();
+    for (int v : r0)
+      if (npass == 0 ? in(nd(v).in[0]) : !in(nd(v).in[0])) bad("a sum over images beside other sums");
+    if (npass == 0 && !inv_outs.empty()) bad("an output per channel without a sum");
+    if (npass == 0 && full_outs.empty()) bad("no map among the outputs");
+    if (npass == 0 && !r3.empty()) bad("a sum over a group's channels of a stored tensor");
+    for (int v : r0)
+      if (npass > 0 && std::find(r1.begin(), r1.end(), nd(v).in[0]) == r1.end()) bad("a sum over images of computed values");
+    if (npass == 0) {
+      kind = Apply;
+      stream_geometry(256);
+      // about eight workgroups to a compute unit, a thread's rows in whole
+      // batches, so that the channels' values are loaded for several rows
+      const int64_t want = std::max<int64_t>(1, 2048 / B);
+      chunk = std::max<int64_t>((P + want - 1) / want, 1);
+      U = (int)std::min<int64_t>(4, (chunk + LY - 1) / LY);
+      chunk = (chunk + (int64_t)LY * U - 1) / ((int64_t)LY * U) * ((int64_t)LY * U);
+      S = (P + chunk - 1) / chunk;
+      if (B * S * T + ((int64_t)C * 1024) >= ((int64_t)1 << 32) || S >= ((int64_t)1 << 31)) bad("more threads than a launch holds");
+      return;
+    }
+    if (slab_geometry()) {
+      kind = Slab;
+      return;
+    }
+    if (!full_outs.empty() || !r0.empty()) bad("a map and sums over it that do not fit the registers of a workgroup");
+    if (find_moments())
+      kind = Moments;
+    else if (npass == 1)
+      kind = Sums;
+    else
+      bad("sums that depend on sums over the same positions");
+    stream_geometry(512);
+    // a workgroup of eight waves per compute unit, each thread with two batches of rows at least
+    U = kind == Moments ? kRowsInFlight : 4;
+    S = std::max<int64_t>(1, std::min<int64_t>((256 + B - 1) / B, P / ((int64_t)LY * U * 2)));
+    chunk = (P + S - 1) / S;
+    chunk = (chunk + LY - 1) / LY * LY;
+    S = (P + chunk - 1) / chunk;
+    if (B * S * T >= ((int64_t)1 << 32)) bad("more threads than a launch holds");
+  }
+
+  // ---- code ------------------------------------------------------------------
+
+  GenKernel gk;
+  std::map<int, int> slot;
+  std::ostringstream s;
+  std::set<int> inv_done;      // per-channel nodes and operands already in registers
+
+  std::string ptr(int u) const { return "((const " + ctype(nd(u).dtype) + "*)a.p[" + std::to_string(slot.at(u)) + "])"; }
+  std::string outp(int o) const { return "((" + ctype(nd(o).dtype) + "*)a.p[" + std::to_string(ki.out_slot(o)) + "])"; }
+  static std::string id(int v) { return std::to_string(v); }
+  std::string jdecl(const std::string& name) const {
+    return "  float " + name + "[" + std::to_string(NJ) + "][" + std::to_string(VEC) + "];\n";
+  }
+  // `stmt` for every channel of the thread: j (vector), e (element), ch(j) + e the channel
+  std::string each(const std::string& stmt) const {
+    return "#pragma unroll\n  for (int j = 0; j < " + std::to_string(NJ) + "; ++j)\n#pragma unroll\n    for (int e = 0; e < " + std::to_string(VEC) + "; ++e) { " +
+           stmt + " }\n";
+  }
+
+  std::string elem_expr(int v, const std::function<std::string(int)>& operand) const {
+    const Node& n = nd(v);
+    switch (op_kind(n.op)) {
+      case korch::Kind::Unary: return unary_expr(n.op, operand(n.in[0]));
+      case korch::Kind::Binary: return binary_expr(n.op, operand(n.in[0]), n.attrs.has_scalar ? flit(n.attrs.scalar) : operand(n.in[1]));
+      default:
+        return "(" + operand(n.in[0]) + " != 0.0f ? " + operand(n.in[1]) + " : " + (n.attrs.has_scalar ? flit(n.attrs.scalar) : operand(n.in[2])) + ")";
+    }
+  }
+
+  // A per-channel value (the thread's channels in registers); emits it and what it needs.
+  std::string inv(int v) {
+    if (in(v)) v = rt(v);
+    const std::string name = "n" + id(v);
+    if (inv_done.count(v)) return name + "[j][e]";
+    if (!in(v)) {
+      Shape d;
+      aligned(nd(v).shape, d);
+      const int64_t sk = d[3] > 1 ? 1 : 0, sg = d[2] > 1 ? d[3] : 0, sb = d[0] > 1 ? d[2] * d[3] : 0;
+      s << jdecl(name);
+      const bool run = (sk || K == 1) && (sg == K || G == 1);  // consecutive over the channels
+      const std::string base = ptr(v) + (sb ? " + (i64)b * " + std::to_string(sb) : "");
+      if (run)
+        s << "#pragma unroll\n  for (int j = 0; j < " << NJ << "; ++j) ldv<" << VEC << ">(" << name << "[j], " << base << " + c0[j]);\n";
+      else if (!sk && !sg)
+        s << "  {\n    const float x_ = ld1(" << base << ");\n  " << each(name + "[j][e] = x_;") << "  }\n";
+      else
+        s << each("const int c_ = c0[j] + e; " + name + "[j][e] = ld1(" + base + " + (c_ / " + std::to_string(K) + ") * " + std::to_string(sg) +
+                  (sk ? " + c_ % " + std::to_string(K) : std::string()) + ");");
+      inv_done.insert(v);
+      return name + "[j][e]";
+    }
+    if (op_kind(nd(v).op) == korch::Kind::Reduce) bad("internal: a sum that is not there yet");
+    const std::string ex = elem_expr(v, [&](int u) { return inv(u); });
+    s << jdecl(name) << each(name + "[j][e] = " + ex + ";");
+    inv_done.insert(v);
+    return name + "[j][e]";
+  }
+
+  // Statements for one element of the map; per-channel operands must be in registers.
+  struct Body {
+    std::ostringstream o;
+    std::set<int> done;
+  };
+  std::string full_value(int v, Body& b) {
+    if (in(v)) v = rt(v);
+    if (!in(v) && std::find(xfull.begin(), xfull.end(), v) != xfull.end()) {
+      if (b.done.insert(v).second) b.o << "        const float f" << id(v) << " = tof(x" << id(v) << "[i][j]" << (VEC > 1 ? "[e]" : "") << ");\n";
+      return "f" + id(v);
+    }
+    if (!in(v) || !is_full.at(v)) return inv(v);
+    if (b.done.insert(v).second) {
+      const std::string ex = elem_expr(v, [&](int u) { return full_value(u, b); });
+      b.o << "        const float f" << id(v) << " = " << ex << ";\n";
+    }
+    return "f" + id(v);
+  }
+  bool fast_full() const { return eb == 2; }
+
+  std::string raw_decl() const {
+    std::ostringstream o;
+    for (int u : xfull) o << "  vec_t<" << VEC << ", " << ctype(nd(u).dtype) << "> x" << id(u) << "[" << U << "][" << NJ << "];\n";
+    return o.str();
+  }
+  // Loads rows row0 + i LY (i < U), clamped to the last row `end` - 1.
+  std::string raw_load(const std::string& row0, const std::string& end) const {
+    std::ostringstream o;
+    o << "#pragma unroll\n    for (int i = 0; i < " << U << "; ++i) {\n      const int r_ = " << row0 << " + i * " << LY << ", row = r_ < " << end << " ? r_ : "
+      << end << " - 1;\n";
+    // within an image of less than 2 GiB, a 32-bit offset from a base that is the same for all lanes
+    const bool narrow = (double)P * C * 4 < 2147483648.0;
+    o << "      const " << (narrow ? "unsigned" : "i64") << " at = " << (narrow ? "(unsigned)" : "(i64)") << "row * " << C << ";\n";
+    for (int u : xfull)
+      o << "#pragma unroll\n      for (int j = 0; j < " << NJ << "; ++j) x" << id(u) << "[i][j] = *(const vec_t<" << VEC << ", " << ctype(nd(u).dtype) << ">*)(" << ptr(u)
+        << " + (i64)b * " << P * C << "LL + (at + c0[j]));\n";
+    o << "    }\n";
+    return o.str();
+  }
+  // The raw rows pass through an empty statement: a pass converts them anew, and
+  // the compiler does not keep the fp32 values of one pass for the next one
+  // (which took twice the registers, and spilled).
+  std::string raw_again() const {
+    const int words = VEC * 2 / 4;  // (of 16-bit rows; fp32 rows need no conversion)
+    std::ostringstream o;
+    for (int u : xfull)
+      if (dtype_bytes(nd(u).dtype) == 2 && words >= 1) {
+        const std::string w = words == 1 ? "unsigned" : "u32_" + std::to_string(words);
+        o << "  {\n";
+        if (words > 1) o << "    typedef unsigned " << w << " __attribute__((ext_vector_type(" << words << ")));\n";
+        o << "#pragma unroll\n    for (int i = 0; i < " << U << "; ++i)\n#pragma unroll\n      for (int j = 0; j < " << NJ << "; ++j) {\n        " << w << " w_ = __builtin_bit_cast(" << w
+          << ", x" << id(u) << "[i][j]);\n        asm volatile(\"\" : \"+v\"(w_));\n        x" << id(u) << "[i][j] = __builtin_bit_cast(vec_t<" << VEC << ", " << ctype(nd(u).dtype)
+          << ">, w_);\n      }\n  }\n";
+      }
+    return o.str();
+  }
+  // The loop over the rows in registers.
+  std::string row_loop(const std::string& row0, const std::string& end, const std::string& elem, const std::string& after_j) const {
+    std::ostringstream o;
+    o << "#pragma unroll\n    for (int i = 0; i < " << U << "; ++i) {\n      const int row = " << row0 << " + i * " << LY << ";\n      const bool live = row < " << end
+      << ";\n#pragma unroll\n      for (int j = 0; j < " << NJ << "; ++j) {\n";
+    for (int v : full_outs) o << "        float o" << id(v) << "[" << VEC << "];\n";
+    o << "#pragma unroll\n        for (int e = 0; e < " << VEC << "; ++e) {\n" << elem << "        }\n" << after_j << "      }\n    }\n";
+    return o.str();
+  }
+  std::string store_rows() const {
+    std::ostringstream o;
+    for (int v : full_outs)
+      o << "        if (live && act" << (NJ > 1 ? "[j]" : "") << ") " << out_store(g, v, outp(v), "((i64)b * " + std::to_string(P) + " + row) * " + std::to_string(C) + " + c0[j]", VEC, "o" + id(v))
+        << ";\n";
+    return o.str();
+  }
+
+  // Per-channel sums of the threads' values acc (nodes `vs`), into chan[i][CT4].
+  int64_t CT4() const { return (CT + 3) / 4 * 4; }
+  void channel_sums(const std::vector<std::string>& acc) {
+    const int n = (int)acc.size();
+    const std::string A = NJ > 1 ? "act[j]" : "act";
+    if (LY == 1) {
+      for (int i = 0; i < n; ++i) s << each("if (" + A + ") chan[" + std::to_string(i * CT4()) + " + c0[j] - ct0 + e] = " + acc[i] + "[j][e];");
+      s << "  __syncthreads();\n";
+      return;
+    }
+    const int64_t slab = (int64_t)LY * CT;
+    for (int i = 0; i < n; ++i) s << each("if (act) red[" + std::to_string(i * slab) + " + ly * " + std::to_string(CT) + " + c0[j] - ct0 + e] = " + acc[i] + "[j][e];");
+    s << "  __syncthreads();\n";
+    int64_t L = 1;
+    if (CT < T) L = std::min<int64_t>(std::min<int64_t>(16, pow2floor(T / CT)), pow2floor(LY));
+    if (L > 1) {
+      // a thread per channel and slice of the rows of lanes; then the slices
+      s << "  if (tid < " << L * CT << ") {\n    const int c = tid % " << CT << ", l = tid / " << CT << ";\n";
+      for (int i = 0; i < n; ++i)
+        s << "    float t" << i << "_ = 0.0f;\n";
+      s << "#pragma unroll 8\n    for (int y = l; y < " << LY << "; y += " << L << ") {\n";
+      for (int i = 0; i < n; ++i) s << "      t" << i << "_ += red[" << i * slab << " + y * " << CT << " + c];\n";
+      s << "    }\n";
+      for (int i = 0; i < n; ++i) s << "    part[" << i * L * CT << " + tid] = t" << i << "_;\n";
+      s << "  }\n  __syncthreads();\n  if (tid < " << CT << ") {\n";
+      for (int i = 0; i < n; ++i) {
+        s << "    float t" << i << "_ = part[" << i * L * CT << " + tid];\n#pragma unroll\n    for (int l = 1; l < " << L << "; ++l) t" << i << "_ += part[" << i * L * CT
+          << " + l * " << CT << " + tid];\n    chan[" << i * CT4() << " + tid] = t" << i << "_;\n";
+      }
+      s << "  }\n  __syncthreads();\n";
+      return;
+    }
+    s << "  for (int c = tid; c < " << CT << "; c += " << T << ") {\n";
+    for (int i = 0; i < n; ++i) s << "    float t" << i << "_ = 0.0f;\n";
+    s << "#pragma unroll 8\n    for (int y = 0; y < " << LY << "; ++y) {\n";
+    for (int i = 0; i < n; ++i) s << "      t" << i << "_ += red[" << i * slab << " + y * " << CT << " + c];\n";
+    s << "    }\n";
+    for (int i = 0; i < n; ++i) s << "    chan[" << i * CT4() << " + c] = t" << i << "_;\n";
+    s << "  }\n  __syncthreads();\n";
+  }
+  // Sums over a group's channels of chan[base ..]: grp[g - g0].
+  void group_sums(int64_t base) {
+    const int64_t gt = CT / K;
+    const int64_t L = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(64, pow2floor(K)), pow2floor(std::max<int64_t>(1, T / gt))));
+    s << "  for (int q = tid; q < " << (gt * L + T - 1) / T * T << "; q += " << T << ") {\n    const int gr = q / " << L << ", l = q % " << L << ";\n    float t_ = 0.0f;\n";
+    s << "    if (gr < " << gt << ")\n#pragma unroll 4\n      for (int k = l; k < " << K << "; k += " << L << ") t_ += chan[" << base << " + gr * " << K << " + k];\n";
+    if (L > 1) s << "    t_ = group_sum<" << L << ">(t_);\n";
+    s << "    if (l == 0 && gr < " << gt << ") grp[gr] = t_;\n  }\n  __syncthreads();\n";
+  }
+  // Sums over positions of pass `k` are in chan: they and what follows from
+  // them become per-channel values.
+  void after_pass(int k, const std::vector<int>& sums) {
+    for (size_t i = 0; i < sums.size(); ++i) {
+      const int v = sums[i];
+      s << jdecl("n" + id(v)) << each("n" + id(v) + "[j][e] = chan[" + std::to_string(i * CT4()) + " + c0[j] - ct0 + e]" +
+                                      (nd(v).op == KORCH_REDUCE_MEAN ? " / " + flit((double)P) : std::string()) + ";");
+      inv_done.insert(v);
+    }
+    for (int v : ki.k.prims)
+      if (std::find(r3.begin(), r3.end(), v) != r3.end() && gen.at(v) == k) {
+        const std::string x = inv(nd(v).in[0]);
+        s << "  __syncthreads();\n" << each("if (" + std::string(NJ > 1 ? "act[j]" : "act") + " && ly == 0) chan[c0[j] - ct0 + e] = " + x + ";") << "  __syncthreads();\n";
+        group_sums(0);
+        s << jdecl("n" + id(v)) << each("n" + id(v) + "[j][e] = grp[(c0[j] - ct0 + e) / " + std::to_string(K) + "]" +
+                                        (nd(v).op == KORCH_REDUCE_MEAN ? " / " + flit((double)K) : std::string()) + ";");
+        inv_done.insert(v);
+      }
+    s << "  __syncthreads();\n";
+  }
+  // Per-channel and per-group outputs, by the first row of lanes.
+  void store_inv(bool whole_rounds) {
+    (void)whole_rounds;
+    for (int o : inv_outs) {
+      const int v = rt(o);
+      const std::string x = inv(v), A = NJ > 1 ? "act[j]" : "act";
+      const bool chan = nd(v).shape[3] == K;
+      const std::string at = chan ? "(i64)b * " + std::to_string(C) + " + c0[j] + e" : "(i64)b * " + std::to_string(G) + " + (c0[j] + e) / " + std::to_string(K);
+      s << each("if (" + A + " && ly == 0" + (chan ? "" : " && (c0[j] + e) % " + std::to_string(K) + " == 0") + ") " + out_store(g, o, outp(o), at, 0, x) + ";");
+    }
+  }
+
+  // Hands `rowf` floats of chan (a multiple of four) from workgroup to
+  // workgroup: `units` of them make a set; the last to arrive has their sum in
+  // chan and goes on, the others end.  Past 32 units in two levels, groups of
+  // 16 first.  `merge` joins partial rows m of the array at row `from` instead
+  // of adding them.
+  void hand_over(int64_t sets, const std::string& set, int64_t units, const std::string& unit, int64_t rowf,
+                 const std::function<void(const std::string& from, const std::string& m, int64_t maxm, int level)>& merge) {
+    const int64_t GS = units <= 32 ? units : kHandOver, NG = (units + GS - 1) / GS;
+    const int64_t rows = units + (NG > 1 ? NG : 0);
+    ArgRef a;
+    a.kind = ArgRef::Scratch;
+    a.bytes = (size_t)(sets * rows * rowf) * 4;
+    const int scr = (int)gk.args.size();
+    gk.args.push_back(a);
+    a.kind = ArgRef::Counter;
+    a.bytes = (size_t)(sets * (NG > 1 ? NG + 1 : 1)) * 128;
+    const int cnt = (int)gk.args.size();
+    gk.args.push_back(a);
+    s << "  __shared__ int last_;\n  float* const hand = (float*)a.p[" << scr << "] + (i64)(" << set << ") * " << rows * rowf << ";\n";
+    s << "  int* const cnt = (int*)a.p[" << cnt << "] + (" << set << ") * " << (NG > 1 ? NG + 1 : 1) * 32 << ";\n";
+    auto put = [&](const std::string& row) {
+      s << "  {\n    const __amdgpu_buffer_rsrc_t r_ = __builtin_amdgcn_make_buffer_rsrc(hand + (i64)(" << row << ") * " << rowf << ", 0, 0x7fffffff, 0x00020000);\n";
+      s << "    for (int q = tid; q < " << rowf / 4 << "; q += " << T << ") coherent_store4(r_, (unsigned)q * 16, *(const float4*)(chan + q * 4));\n  }\n";
+      s << "  __builtin_amdgcn_s_waitcnt(0);  // this wave's partial stores are performed\n  __syncthreads();\n";
+    };
+    auto arrive = [&](const std::string& c, const std::string& n) {
+      s << "  if (tid == 0) {\n    int* c_ = cnt + (" << c << ") * 32;\n";
+      s << "    last_ = __hip_atomic_fetch_add(c_, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (" << n << ") - 1;\n";
+      s << "    if (last_) __hip_atomic_store(c_, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);\n  }\n  __syncthreads();\n  if (!last_) return;\n";
+    };
+    put(unit);
+    if (NG > 1) {
+      s << "  const int grp_ = (" << unit << ") / " << GS << ", gsz_ = " << units << " - grp_ * " << GS << " < " << GS << " ? " << units << " - grp_ * " << GS << " : " << GS
+        << ";\n";
+      arrive("1 + grp_", "gsz_");
+      merge("grp_ * " + std::to_string(GS), "gsz_", GS, 1);
+      s << "  __syncthreads();\n";
+      put(std::to_string(units) + " + grp_");
+      arrive("0", std::to_string(NG));
+      merge(std::to_string(units), std::to_string(NG), NG, 2);
+    } else {
+      arrive("0", std::to_string(units));
+      merge("0", std::to_string(units), units, 0);
+    }
+    s << "  __syncthreads();\n";
+  }
+  int64_t slices(int64_t rowf, int64_t maxm) const {
+    int64_t z = 1;
+    while (z < 8 && z * 2 <= maxm && 2 * z * (rowf / 4) <= T) z *= 2;
+    return z;
+  }
+  // LDS that adding the partial rows of `units` workgroups takes (floats).
+  int64_t slice_floats(int64_t rowf, int64_t units) const {
+    int64_t most = 0;
+    for (int64_t m : {units <= 32 ? units : kHandOver, units <= 32 ? (int64_t)1 : (units + kHandOver - 1) / kHandOver}) {
+      const int64_t z = slices(rowf, m);
+      if (z > 1) most = std::max(most, z * rowf);
+    }
+    return most;
+  }
+  // Adds partial rows in order: a thread per 16-byte vector and slice of the
+  // rows, all loads of a thread in flight together, then the slices.
+  void add_rows(int64_t rowf, const std::string& from, const std::string& m, int64_t maxm) {
+    const int64_t CQ = rowf / 4, ZS = slices(rowf, maxm);
+    const int64_t per = (maxm + ZS - 1) / ZS, step = std::min<int64_t>(CQ, T / ZS);
+    s << "  {\n    const __amdgpu_buffer_rsrc_t r_ = __builtin_amdgcn_make_buffer_rsrc(hand + (i64)(" << from << ") * " << rowf << ", 0, 0x7fffffff, 0x00020000);\n"
+      << "    const int m_ = " << m << ", zs = tid / " << step << ";\n";
+    s << "    if (zs < " << ZS << ")\n      for (int v = tid % " << step << "; v < " << CQ << "; v += " << step << ") {\n        float4 q_[" << per
+      << "];\n#pragma unroll\n        for (int z = 0; z < " << per << "; ++z) {\n          const int zz = zs * " << per << " + z;\n          q_[z] = coherent_load4(r_, (unsigned)((zz < m_ ? zz : m_ - 1) * "
+      << rowf * 4 << " + v * 16));\n        }\n        f32x4 t_ = {};\n#pragma unroll\n        for (int z = 0; z < " << per << "; ++z)\n          if (zs * " << per
+      << " + z < m_) t_ += f32x4{q_[z].x, q_[z].y, q_[z].z, q_[z].w};\n";
+    if (ZS == 1) {
+      s << "        *(f32x4*)(chan + v * 4) = t_;\n      }\n  }\n";
+      return;
+    }
+    s << "        *(f32x4*)(red + (zs * " << CQ << " + v) * 4) = t_;\n      }\n    __syncthreads();\n    for (int v = tid; v < " << CQ << "; v += " << T
+      << ") {\n      f32x4 t_ = *(const f32x4*)(red + v * 4);\n#pragma unroll\n      for (int z = 1; z < " << ZS << "; ++z) t_ += *(const f32x4*)(red + (z * " << CQ
+      << " + v) * 4);\n      *(f32x4*)(chan + v * 4) = t_;\n    }\n  }\n";
+  }
+
+  void head(int64_t lds_red, int64_t lds_part, int64_t lds_chan) {
+    if (lds_red) s << "  __shared__ __attribute__((aligned(16))) float red[" << lds_red << "];\n";
+    if (lds_part) s << "  __shared__ float part[" << lds_part << "];\n";
+    if (lds_chan) s << "  __shared__ __attribute__((aligned(16))) float chan[" << lds_chan << "];\n  __shared__ float grp[" << CT / K << "];\n";
+    s << "  const int tid = threadIdx.x;\n";
+    if (NJ == 1) {
+      s << "  const int ly = tid / " << CVT << ";\n  const bool act = ly < " << LY << ";\n";
+      s << "  const int c0[1] = {ct0 + (tid - ly * " << CVT << ") * " << VEC << "};\n";
+    } else {
+      s << "  const int ly = 0;\n  int c0[" << NJ << "];\n  bool act[" << NJ << "];\n#pragma unroll\n  for (int j = 0; j < " << NJ << "; ++j) {\n    const int v = tid + j * " << T
+        << ";\n    act[j] = v < " << CVT << ";\n    c0[j] = ct0 + (act[j] ? v : 0) * " << VEC << ";\n  }\n";
+    }
+  }
+  // Lanes past the last whole row of lanes do no work of their own; they take part in the barriers.
+  std::string first_row() const { return NJ == 1 ? "(act ? ly : " + std::to_string(LY - 1) + ")" : "0"; }
+
+  int64_t red_floats(int n) const { return LY > 1 ? (int64_t)n * LY * CT : 0; }
+  int64_t part_floats(int n) const {
+    if (LY == 1 || CT >= T) return 0;
+    const int64_t L = std::min<int64_t>(std::min<int64_t>(16, pow2floor(T / CT)), pow2floor(LY));
+    return L > 1 ? n * L * CT : 0;
+  }
+
+  void load_invariants(const std::vector<int>& targets) {
+    // per-channel operands of the nodes that the targets need, before the row loops
+    std::set<int> seen;
+    std::function<void(int)> walk = [&](int v) {
+      if (in(v)) v = rt(v);
+      if (!seen.insert(v).second) return;
+      if (!in(v)) {
+        if (std::find(xfull.begin(), xfull.end(), v) == xfull.end()) inv(v);
+        return;
+      }
+      if (!is_full.at(v)) {
+        inv(v);
+        return;
+      }
+      for (int u : nd(v).in) walk(u);
+    };
+    for (int v : targets) walk(v);
+  }
+
+  // One pass's accumulation: `sums` over the rows in registers.
+  std::string accumulate(const std::vector<int>& sums) {
+    Body b;
+    std::ostringstream acc;
+    for (int v : sums) {
+      const std::string x = full_value(nd(v).in[0], b);
+      acc << "        a" << id(v) << "[j][e] += live ? " << x << " : 0.0f;\n";
+    }
+    return b.o.str() + acc.str();
+  }
+  std::string results() {
+    Body b;
+    std::ostringstream st;
+    for (int o : full_outs) {
+      const std::string x = full_value(o, b);
+      st << "        o" << id(o) << "[e] = " << x << ";\n";
+    }
+    return b.o.str() + st.str();
+  }
+
+  void gen_slab() {
+    std::vector<std::vector<int>> pass(npass);
+    size_t widest = 1;
+    for (int v : r1) pass[gen.at(v) - 1].push_back(v);
+    for (auto& p : pass) widest = std::max(widest, p.size());
+    const int64_t rowf = (int64_t)r0.size() * CT4();
+    const int64_t red = std::max(red_floats((int)widest), r0.empty() || B == 1 ? 0 : slice_floats(rowf, B));
+    s << "  const int b = blockIdx.x / " << tiles << ", ct0 = (int)(blockIdx.x % " << tiles << ") * " << CT << ";\n";
+    head(red, part_floats((int)widest), std::max<int64_t>(widest, r0.size()) * CT4());
+    s << raw_decl() << "  const int row0 = " << first_row() << ";\n  {\n" << raw_load("row0", std::to_string(P)) << "  }\n";
+    const std::string end = NJ == 1 ? "(act ? " + std::to_string(P) + " : 0)" : std::to_string(P);
+    for (int k = 0; k < npass; ++k) {
+      std::vector<int> targets;
+      for (int v : pass[k]) targets.push_back(nd(v).in[0]);
+      set_fast_math(false);
+      load_invariants(targets);
+      set_fast_math(fast_full());
+      const std::string body = accumulate(pass[k]);
+      std::vector<std::string> acc;
+      for (int v : pass[k]) {
+        s << "  float a" << id(v) << "[" << NJ << "][" << VEC << "] = {};\n";
+        acc.push_back("a" + id(v));
+      }
+      s << "  {\n" << row_loop("row0", end, body, "") << "  }\n";
+      set_fast_math(false);
+      channel_sums(acc);
+      after_pass(k + 1, pass[k]);
+      s << raw_again();
+    }
+    if (!full_outs.empty()) {
+      set_fast_math(false);
+      load_invariants(full_outs);
+      set_fast_math(fast_full());
+      const std::string body = results();
+      s << "  {\n" << row_loop("row0", end, body, store_rows()) << "  }\n";
+    }
+    set_fast_math(false);
+    store_inv(true);
+    if (!r0.empty()) {
+      // sums over the images, image by image
+      s << "  __syncthreads();\n";
+      for (size_t i = 0; i < r0.size(); ++i) {
+        const std::string x = inv(nd(r0[i]).in[0]);
+        s << each("if (" + std::string(NJ > 1 ? "act[j]" : "act") + " && ly == 0) chan[" + std::to_string(i * CT4()) + " + c0[j] - ct0 + e] = " + x + ";");
+        if (CT4() > CT) s << "  if (tid < " << CT4() - CT << ") chan[" << i * CT4() + CT << " + tid] = 0.0f;\n";
+      }
+      s << "  __syncthreads();\n";
+      if (B > 1)
+        hand_over(tiles, "blockIdx.x % " + std::to_string(tiles), B, "b", rowf,
+                  [&](const std::string& from, const std::string& m, int64_t maxm, int) { add_rows(rowf, from, m, maxm); });
+      store_r0("chan", "ct0");
+    }
+    gk.grid[0] = (int)(B * tiles);
+  }
+  // The sums over images in chan[i][..], channels c0 .. c0 + CT - 1.
+  void store_r0(const std::string& arr, const std::string& first) {
+    for (size_t i = 0; i < r0.size(); ++i)
+      for (int o : ki.k.outs)
+        if (rt(o) == r0[i]) {
+          std::string x = arr + "[" + std::to_string(i * CT4()) + " + c]";
+          if (nd(r0[i]).op == KORCH_REDUCE_MEAN) x += " / " + flit((double)B);
+          s << "  for (int c = tid; c < " << CT << "; c += " << T << ") " << out_store(g, o, outp(o), "(" + first + " + c)", 0, x) << ";\n";
+        }
+  }
+
+  void gen_sums() {
+    const int64_t rowf = (int64_t)r1.size() * CT4();
+    s << "  const int b = blockIdx.x / " << S << ", sp = blockIdx.x % " << S << ", ct0 = 0;\n";
+    head(std::max(red_floats((int)r1.size()), S > 1 ? slice_floats(rowf, S) : 0), part_floats((int)r1.size()), rowf);
+    std::vector<int> targets;
+    for (int v : r1) targets.push_back(nd(v).in[0]);
+    load_invariants(targets);
+    set_fast_math(fast_full());
+    const std::string body = accumulate(r1);
+    set_fast_math(false);
+    std::vector<std::string> acc;
+    for (int v : r1) {
+      s << "  float a" << id(v) << "[" << NJ << "][" << VEC << "] = {};\n";
+      acc.push_back("a" + id(v));
+    }
+    s << raw_decl() << "  const int p1 = (sp + 1) * " << chunk << " < " << P << " ? (sp + 1) * " << chunk << " : " << P << ", lim = " << (NJ == 1 ? "act ? p1 : 0" : "p1") << ";\n";
+    s << "  for (int row0 = sp * " << chunk << " + " << first_row() << "; row0 < p1; row0 += " << (int64_t)U * LY << ") {\n" << raw_load("row0", "p1")
+      << row_loop("row0", "lim", body, "") << "  }\n";
+    channel_sums(acc);
+    if (CT4() > CT) {
+      for (size_t i = 0; i < r1.size(); ++i) s << "  if (tid < " << CT4() - CT << ") chan[" << i * CT4() + CT << " + tid] = 0.0f;\n";
+      s << "  __syncthreads();\n";
+    }
+    if (S > 1)
+      hand_over(B, "b", S, "sp", rowf, [&](const std::string& from, const std::string& m, int64_t maxm, int) { add_rows(rowf, from, m, maxm); });
+    after_pass(1, r1);
+    store_inv(true);
+    gk.grid[0] = (int)(B * S);
+  }
+
+  void gen_moments() {
+    const int64_t G4 = (G + 3) / 4 * 4, rowf = 2 * G4;
+    s << "  const int b = blockIdx.x / " << S << ", sp = blockIdx.x % " << S << ", ct0 = 0;\n";
+    head(red_floats(1), part_floats(1), std::max(CT4(), rowf));
+    s << "  __shared__ float gmean[" << G << "];\n";
+    s << raw_decl() << "  const int p1 = (sp + 1) * " << chunk << " < " << P << " ? (sp + 1) * " << chunk << " : " << P << ";\n";
+    s << "  float mean[" << NJ << "][" << VEC << "] = {}, m2[" << NJ << "][" << VEC << "] = {}, cnt_ = 0.0f;\n";
+    const std::string x = "tof(x" + id(mo_x) + "[i][j]" + (VEC > 1 ? "[e]" : "") + ")";
+    s << "  for (int row0 = sp * " << chunk << " + " << first_row() << "; row0 < " << (NJ == 1 ? "(act ? p1 : 0)" : "p1") << "; row0 += " << (int64_t)U * LY << ") {\n"
+      << raw_load("row0", "p1");
+    s << "    const int left = (p1 - row0 + " << LY - 1 << ") / " << LY << ";\n    const float n = (float)(left < " << U << " ? left : " << U
+      << "), nn = cnt_ + n, w = n / nn, w2 = cnt_ * w, ni = 1.0f / n;\n    cnt_ = nn;\n";
+    s << "#pragma unroll\n    for (int j = 0; j < " << NJ << "; ++j)\n#pragma unroll\n      for (int e = 0; e < " << VEC << "; ++e) {\n        float t = 0.0f, q = 0.0f;\n";
+    s << "        if (left >= " << U << ") {\n#pragma unroll\n          for (int i = 0; i < " << U << "; ++i) t += " << x << ";\n          t *= " << flit(1.0 / U)
+      << ";\n#pragma unroll\n          for (int i = 0; i < " << U << "; ++i) { const float d = " << x << " - t; q = __builtin_fmaf(d, d, q); }\n        } else {\n";
+    s << "#pragma unroll\n          for (int i = 0; i < " << U << "; ++i) t += i < left ? " << x << " : 0.0f;\n          t *= ni;\n#pragma unroll\n          for (int i = 0; i < " << U
+      << "; ++i) { const float d = i < left ? " << x << " - t : 0.0f; q = __builtin_fmaf(d, d, q); }\n        }\n";
+    s << "        const float d = t - mean[j][e];\n        mean[j][e] = __builtin_fmaf(d, w, mean[j][e]);\n        m2[j][e] += __builtin_fmaf(d * w2, d, q);\n      }\n  }\n";
+    // the workgroup's group means, then its sums of centred squares about them
+    s << "  float nm[" << NJ << "][" << VEC << "];\n" << each("nm[j][e] = cnt_ * mean[j][e];");
+    channel_sums({"nm"});
+    group_sums(0);
+    s << "  const float rows_ = (float)(p1 - sp * " << chunk << ");\n  for (int q = tid; q < " << G << "; q += " << T << ") gmean[q] = grp[q] / (rows_ * " << flit((double)K)
+      << ");\n  __syncthreads();\n";
+    s << each("const float d = mean[j][e] - gmean[(c0[j] + e) / " + std::to_string(K) + "]; nm[j][e] = __builtin_fmaf(cnt_ * d, d, m2[j][e]);");
+    channel_sums({"nm"});
+    group_sums(0);
+    s << "  for (int q = tid; q < " << G4 << "; q += " << T << ") {\n    chan[q] = q < " << G << " ? gmean[q] : 0.0f;\n    chan[" << G4 << " + q] = q < " << G
+      << " ? grp[q] : 0.0f;\n  }\n  __syncthreads();\n";
+    if (S > 1) {
+      const int64_t GS = S <= 32 ? S : kHandOver;
+      hand_over(B, "b", S, "sp", rowf, [&](const std::string& from, const std::string& m, int64_t maxm, int level) {
+        // rows (positions) of partial z: a split's, or those of a whole group of splits
+        const int64_t per = level == 2 ? chunk * GS : chunk;
+        const std::string first = level == 1 ? "(" + from + " + z)" : "z";
+        const int64_t L = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(16, pow2floor(maxm)), pow2floor(std::max<int64_t>(1, T / G))));
+        const int64_t nz = (maxm + L - 1) / L;
+        s << "  for (int q = tid; q < " << (G * L + T - 1) / T * T << "; q += " << T << ") {\n    const int gr_ = q / " << L << ", gr = gr_ < " << G << " ? gr_ : " << G - 1
+          << ", l = q % " << L << ", m_ = " << m << ";\n    float a_[" << nz << "], b_[" << nz << "], n_[" << nz << "], t = 0.0f, n = 0.0f, v = 0.0f;\n";
+        s << "    float* const p_ = hand + (i64)(" << from << ") * " << rowf << " + gr;\n";
+        s << "#pragma unroll\n    for (int i = 0; i < " << nz << "; ++i) {\n      const int z_ = l + i * " << L << ", z = z_ < m_ ? z_ : m_ - 1;\n      a_[i] = coherent_load(p_ + (i64)z * " << rowf
+          << ");\n      b_[i] = coherent_load(p_ + (i64)z * " << rowf << " + " << G4 << ");\n      const int lo = " << first << " * " << per << ", hi = lo + " << per << " < " << P
+          << " ? lo + " << per << " : " << P << ";\n      n_[i] = z_ < m_ ? (float)(hi - lo) : 0.0f;\n    }\n";
+        s << "#pragma unroll\n    for (int i = 0; i < " << nz << "; ++i) { t = __builtin_fmaf(n_[i], a_[i], t); n += n_[i]; }\n";
+        if (L > 1) s << "    t = group_sum<" << L << ">(t);\n    n = group_sum<" << L << ">(n);\n";
+        s << "    t /= n;\n#pragma unroll\n    for (int i = 0; i < " << nz << "; ++i) {\n      const float d = a_[i] - t;\n      v += n_[i] > 0.0f ? __builtin_fmaf(n_[i] * " << flit((double)K)
+          << " * d, d, b_[i]) : 0.0f;\n    }\n";
+        if (L > 1) s << "    v = group_sum<" << L << ">(v);\n";
+        s << "    if (l == 0 && gr_ < " << G << ") { chan[gr] = t; chan[" << G4 << " + gr] = v; }\n  }\n";
+        if (G4 > G) s << "  if (tid < " << G4 - G << ") { chan[" << G << " + tid] = 0.0f; chan[" << G4 + G << " + tid] = 0.0f; }\n";
+      });
+    }
+    for (int v : {mo_mu, mo_var}) {
+      s << jdecl("n" + id(v)) << each("n" + id(v) + "[j][e] = chan[" + (v == mo_var ? std::to_string(G4) + " + " : std::string()) + "(c0[j] + e) / " + std::to_string(K) + "]" +
+                                      (v == mo_var ? " / " + flit((double)P * (double)K) : std::string()) + ";");
+      inv_done.insert(v);
+    }
+    store_inv(true);
+    gk.grid[0] = (int)(B * S);
+  }
+
+  void gen_apply() {
+    const int64_t nblk = r0.empty() ? 0 : (C + 63) / 64;
+    if (nblk) {
+      // sums over the images: 64 channels to a workgroup, the images over its waves
+      s << "  if (blockIdx.x >= " << B * S << ") {\n    __shared__ float sum_[" << T << "];\n    const int t_ = threadIdx.x, c = (int)(blockIdx.x - " << B * S
+        << ") * 64 + (t_ & 63);\n";
+      for (int v : r0) {
+        const int u = nd(v).in[0];
+        s << "    {\n      float x_ = 0.0f;\n      if (c < " << C << ")\n#pragma unroll 8\n        for (int i = t_ >> 6; i < " << B << "; i += " << T / 64 << ") x_ += ld1(" << ptr(u)
+          << " + (i64)i * " << C << " + c);\n      sum_[t_] = x_;\n      __syncthreads();\n      if (t_ < 64 && c < " << C << ") {\n#pragma unroll\n        for (int w = 1; w < " << T / 64
+          << "; ++w) x_ += sum_[w * 64 + t_];\n";
+        for (int o : ki.k.outs)
+          if (rt(o) == v) s << "        " << out_store(g, o, outp(o), "c", 0, nd(v).op == KORCH_REDUCE_MEAN ? "x_ / " + flit((double)B) : "x_") << ";\n";
+        s << "      }\n      __syncthreads();\n    }\n";
+      }
+      s << "    return;\n  }\n";
+    }
+    s << "  const int b = blockIdx.x / " << S << ", sp = blockIdx.x % " << S << ", ct0 = 0;\n";
+    head(0, 0, 0);
+    set_fast_math(false);
+    load_invariants(full_outs);
+    set_fast_math(fast_full());
+    const std::string body = results();
+    s << raw_decl() << "  const int p1 = (sp + 1) * " << chunk << " < " << P << " ? (sp + 1) * " << chunk << " : " << P << ";\n";
+    s << "  for (int row0 = sp * " << chunk << " + " << (NJ == 1 ? "ly" : "0") << "; row0 < " << (NJ == 1 ? "(act ? p1 : 0)" : "p1") << "; row0 += " << (int64_t)U * LY << ") {\n"
+      << raw_load("row0", "p1") << row_loop("row0", "p1", body, store_rows()) << "  }\n";
+    gk.grid[0] = (int)(B * S + nblk);
+  }
+
+  GenKernel generate(int index) {
+    analyze();
+    gk.family = KORCH_FAM_GROUP;
+    gk.name = kernel_name(index, "group");
+    ki.assign_args(gk, slot);
+    const bool was = fast_math();
+    set_fast_math(false);
+    switch (kind) {
+      case Slab: gen_slab(); break;
+      case Sums: gen_sums(); break;
+      case Moments: gen_moments(); break;
+      case Apply: gen_apply(); break;
+    }
+    set_fast_math(was);
+    gk.block[0] = T;
+    gk.source = source_header((int)gk.args.size()) + "extern \"C\" __global__ void __launch_bounds__(" + std::to_string(T) + ") " + gk.name + "(KArgs a) {\n" + s.str() + "}\n";
+    ki.fill_cost(gk);
+    return gk;
+  }
+};
+
+}  // namespace
+
+bool match_group(const KInfo& ki, std::string* why) {
+  try {
+    GroupGen(ki).analyze();
+  } catch (Error& e) {
+    *why = e.what();
+    return false;
+  }
+  return true;
+}
+
+GenKernel gen_group(const KInfo& ki, int index) { return GroupGen(ki).generate(index); }
+
+}  // namespace korch

@@ -1213,6 +1213,7 @@ static int match_family_canonical(const Graph& g, const KernelDesc& k, std::stri
       return KORCH_FAM_NONE;
     }
     if (!ki.reduces.empty()) {
+      if (ki.k.prims.size() > 2 && match_multi(ki, why)) return KORCH_FAM_MULTI;
       if (has_fill) {
         *why = "row programs do not evaluate constant tensors";
         return KORCH_FAM_NONE;
@@ -1220,8 +1221,14 @@ static int match_family_canonical(const Graph& g, const KernelDesc& k, std::stri
       if (match_row(ki, why)) return KORCH_FAM_ROW;
       if (match_colreduce(ki, why)) return KORCH_FAM_COLREDUCE;
       if (match_rowcol(ki, why)) return KORCH_FAM_ROWCOL;
+      if (match_group(ki, why)) return KORCH_FAM_GROUP;
       return KORCH_FAM_NONE;
     }
+    // (a map normalized by statistics of its groups: the pointwise family would load those per element)
+    if (match_group(ki, why)) return KORCH_FAM_GROUP;
+    // (heads that turn share their angles; the pointwise family would evaluate those per element)
+    if (match_rotary(ki, why)) return KORCH_FAM_ROTARY;
+    if (match_multi(ki, why)) return KORCH_FAM_MULTI;
     if (match_pointwise(ki, why)) return KORCH_FAM_POINTWISE;
   } catch (Error& e) {
     *why = e.what();
@@ -1257,6 +1264,9 @@ static GenKernel generate_canonical(const Graph& g, const KernelDesc& k, int ind
     case KORCH_FAM_PLANE: return gen_plane(ki, index);
     case KORCH_FAM_ROWCOL: return gen_rowcol(ki, index);
     case KORCH_FAM_BINSUM: return gen_binsum(ki, index);
+    case KORCH_FAM_GROUP: return gen_group(ki, index);
+    case KORCH_FAM_ROTARY: return gen_rotary(ki, index);
+    case KORCH_FAM_MULTI: return gen_multi(ki, index);
   }
   fail(KORCH_E_UNSUPPORTED, "kernel " + std::to_string(index) + ": no family implements it (" + why + ")");
 }

@@ -40,6 +40,9 @@ bool match_attention(const KInfo& ki, std::string* why);
 bool match_plane(const KInfo& ki, std::string* why);
 bool match_rowcol(const KInfo& ki, std::string* why);
 bool match_binsum(const KInfo& ki, std::string* why);
+bool match_group(const KInfo& ki, std::string* why);
+bool match_rotary(const KInfo& ki, std::string* why);
+bool match_multi(const KInfo& ki, std::string* why);
 
 GenKernel gen_pointwise(const KInfo& ki, int index);
 GenKernel gen_row(const KInfo& ki, int index);
@@ -50,5 +53,8 @@ GenKernel gen_attention(const KInfo& ki, int index);
 GenKernel gen_plane(const KInfo& ki, int index);
 GenKernel gen_rowcol(const KInfo& ki, int index);
 GenKernel gen_binsum(const KInfo& ki, int index);
+GenKernel gen_group(const KInfo& ki, int index);
+GenKernel gen_rotary(const KInfo& ki, int index);
+GenKernel gen_multi(const KInfo& ki, int index);
 
 }  // namespace korch

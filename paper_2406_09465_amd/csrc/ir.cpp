@@ -36,7 +36,7 @@ const char* dtype_name(int dtype) {
 Kind op_kind(int op) {
   if (op == KORCH_INPUT) return Kind::Input;
   if (op >= KORCH_NEG && op <= KORCH_IDENTITY) return Kind::Unary;
-  if (op >= KORCH_ADD && op <= KORCH_EQ) return Kind::Binary;
+  if (op >= KORCH_ADD && op <= KORCH_SIN_MUL) return Kind::Binary;
   if (op == KORCH_SELECT) return Kind::Select;
   if (op >= KORCH_REDUCE_SUM && op <= KORCH_REDUCE_MAX) return Kind::Reduce;
   if (op == KORCH_BROADCAST) return Kind::Broadcast;
@@ -78,6 +78,8 @@ const char* op_name(int op) {
     case KORCH_GT: return "gt";
     case KORCH_GE: return "ge";
     case KORCH_EQ: return "eq";
+    case KORCH_COS_MUL: return "cos_mul";
+    case KORCH_SIN_MUL: return "sin_mul";
     case KORCH_SELECT: return "select";
     case KORCH_REDUCE_SUM: return "reduce_sum";
     case KORCH_REDUCE_MEAN: return "reduce_mean";
@@ -152,6 +154,7 @@ int Graph::add_op(int op, const std::vector<int>& in, const korch_attrs* attrs, 
       break;
     case Kind::Binary:
       if (a.has_scalar) {
+        if (op == KORCH_COS_MUL || op == KORCH_SIN_MUL) fail(KORCH_E_ARG, std::string(op_name(op)) + " takes two tensors, no scalar");
         need(1);
         n.shape = sh(0);
       } else {

@@ -648,6 +648,396 @@ def mha_grad(batch=1, heads=8, kv_heads=None, n=1024, m=None, d=64, dtype="bf16"
     return w
 
 
+# Activations after a group norm.
+ACTIVATIONS = ("none", "relu", "silu")
+
+
+class _GroupNorm:
+    """The sizes and views that group norm and its gradient share: a map
+    [batch, hh, ww, c] is read as [batch, positions, groups, channels of a group]."""
+
+    def __init__(self, b, batch, hh, ww, c, groups, eps, act):
+        if min(batch, hh, ww, c, groups) < 1 or c % groups:
+            raise ValueError("c must be a positive multiple of groups, and every size positive")
+        if hh * ww * (c // groups) < 2:
+            raise ValueError("a group needs two elements")
+        if not 0 <= eps < math.inf:
+            raise ValueError("eps must be finite and not negative")
+        if act not in ACTIVATIONS:
+            raise ValueError(f"act must be one of {', '.join(ACTIVATIONS)}")
+        self.b, self.act, self.eps = b, act, eps
+        self.batch, self.groups, self.per, self.positions = batch, groups, c // groups, hh * ww
+        self.map, self.sizes = (batch, hh, ww, c), dict(batch=batch, hh=hh, ww=ww, c=c, groups=groups, act=act)
+        self.full = (batch, self.positions, groups, self.per)
+        self.stat = (batch, 1, groups, 1)
+        self.prims = []
+
+    def view(self, name, src, shape, dtype=None):
+        """A view of a stored tensor (no kernel computes it)."""
+        self.b.op(name, "reshape", [src], dtype, shape=shape)
+        return name
+
+    def op(self, name, op, ins, dtype="f32", **attrs):
+        """A primitive that kernels compute."""
+        self.b.op(name, op, ins, dtype, **attrs)
+        self.prims.append(name)
+        return name
+
+    def over_group(self, name, op, src):
+        """A reduction over the positions and the channels of a group."""
+        src = self.op(name + "_p" if self.per > 1 else name, op, [src], axis=1, keepdim=True)
+        return self.op(name, op, [src], axis=3, keepdim=True) if self.per > 1 else src
+
+
+def groupnorm(batch=1, hh=64, ww=64, c=320, groups=32, dtype="f16", eps=1e-5, act="silu", extra_outputs=()):
+    """Group norm of a map X [batch, hh, ww, c] (channels last) with an activation,
+    that keeps what its gradient needs: per image and group of c / groups
+    channels the mean ``mu`` and the reciprocal deviation ``r`` over all
+    positions and the group's channels (fp32 [batch, groups]).
+
+      Xh = (X - mu) r,  Z = Xh gamma + beta,  Y = Z, relu(Z) or silu(Z) = Z / (1 + exp(-Z))
+
+    The "fused" plan is one kernel where an image's group fits the registers of
+    a workgroup, else the statistics and the rest ("layered")."""
+    b = _B(dtype)
+    m = _GroupNorm(b, batch, hh, ww, c, groups, eps, act)
+    b.inp("X", m.map)
+    b.inp("gamma", (c,))
+    b.inp("beta", (c,))
+    m.view("X4", "X", m.full)
+    m.view("gamma4", "gamma", m.full[2:])
+    m.view("beta4", "beta", m.full[2:])
+    mu = m.over_group("mu4", "reduce_mean", "X4")
+    m.op("mu", "reshape", [mu], shape=(batch, groups))
+    m.op("D", "sub", ["X4", mu])
+    m.op("D2", "square", ["D"])
+    var = m.over_group("var", "reduce_mean", "D2")
+    m.op("ve", "add", [var], scalar=eps)
+    m.op("r4", "rsqrt", ["ve"])
+    m.op("r", "reshape", ["r4"], shape=(batch, groups))
+    stats = list(m.prims)
+    # the statistics as what comes after them reads them, stored or not
+    m.op("mu_s", "reshape", ["mu"], shape=m.stat)
+    m.op("r_s", "reshape", ["r"], shape=m.stat)
+    views = m.prims[len(stats):]
+    m.op("Dn", "sub", ["X4", "mu_s"])
+    m.op("Xh", "mul", ["Dn", "r_s"])
+    m.op("Yg", "mul", ["Xh", "gamma4"])
+    if act == "none":
+        last = m.op("Z", "add", ["Yg", "beta4"], dtype)
+    else:
+        m.op("Z", "add", ["Yg", "beta4"])
+        if act == "relu":
+            last = m.op("Ya", "relu", ["Z"], dtype)
+        else:
+            m.op("nZ", "neg", ["Z"])
+            m.op("eZ", "exp", ["nZ"])
+            m.op("eZ1", "add", ["eZ"], scalar=1.0)
+            last = m.op("Ya", "div", ["Z", "eZ1"], dtype)
+    m.op("Y", "reshape", [last], dtype, shape=m.map)
+    w = _finish(b, "groupnorm", ["Y", "mu", "r"], m.sizes, extra_outputs)
+    rest = [p for p in m.prims if p not in stats and p not in views]
+    whole = (list(m.prims), ["Y", "mu", "r"])
+    w.plans["layered"] = [(stats, ["mu", "r"]), (rest, ["Y"])]
+    w.plans["fused"] = [whole] if _one_kernel(w, whole) else w.plans["layered"]
+    return w
+
+
+def _one_kernel(w, kernel):
+    """Whether a family takes the kernel (names) as one."""
+    prims, outs = kernel
+    return w.graph.family([w.ids[p] for p in prims], [w.ids[o] for o in outs]) != "none"
+
+
+def groupnorm_grad(batch=1, hh=64, ww=64, c=320, groups=32, dtype="f16", eps=1e-5, act="silu", extra_outputs=()):
+    """The gradient of ``groupnorm`` (same arguments) from dY and the saved
+    statistics: dX, dgamma and dbeta.  The activation's input is evaluated again
+    (so ``beta`` is an input where there is an activation).
+
+      dZ = dY act'(Z),  dbeta = sum dZ,  dgamma = sum dZ Xh  over images and positions,
+      g = dZ gamma,  dX = r (g - mean(g) - Xh mean(g Xh))   means over a group's positions and channels,
+
+    with relu'(Z) = [Z > 0] and silu'(Z) = s (1 + Z (1 - s)), s = 1 / (1 + exp(-Z)).
+    The means come from the sums over the positions that dgamma and dbeta need
+    anyway.  (``eps`` is in the saved r.)"""
+    b = _B(dtype)
+    m = _GroupNorm(b, batch, hh, ww, c, groups, eps, act)
+    b.inp("X", m.map)
+    b.inp("gamma", (c,))
+    if act != "none":
+        b.inp("beta", (c,))
+    b.inp("mu", (batch, groups), "f32")
+    b.inp("r", (batch, groups), "f32")
+    b.inp("dY", m.map)
+    m.view("X4", "X", m.full)
+    m.view("dY4", "dY", m.full)
+    m.view("gamma4", "gamma", m.full[2:])
+    m.view("mu4", "mu", m.stat, "f32")
+    m.view("r4", "r", m.stat, "f32")
+    if act != "none":
+        m.view("beta4", "beta", m.full[2:])
+
+    def plane(c):
+        """Xh and dZ (the kernel of the sums and the one of dX evaluate them each)."""
+        m.prims.clear()
+        m.op("D" + c, "sub", ["X4", "mu4"])
+        m.op("Xh" + c, "mul", ["D" + c, "r4"])
+        if act == "none":
+            return "dY4"
+        m.op("Yg" + c, "mul", ["Xh" + c, "gamma4"])
+        m.op("Z" + c, "add", ["Yg" + c, "beta4"])
+        if act == "relu":
+            m.op("on" + c, "gt", ["Z" + c], scalar=0.0)
+            return m.op("dZ" + c, "select", ["on" + c, "dY4"], scalar=0.0)
+        m.op("nZ" + c, "neg", ["Z" + c])
+        m.op("eZ" + c, "exp", ["nZ" + c])
+        m.op("eZ1" + c, "add", ["eZ" + c], scalar=1.0)
+        m.op("s" + c, "recip", ["eZ1" + c])
+        m.op("ns" + c, "neg", ["s" + c])
+        m.op("s1" + c, "add", ["ns" + c], scalar=1.0)
+        m.op("Zs" + c, "mul", ["Z" + c, "s1" + c])
+        m.op("Zs1" + c, "add", ["Zs" + c], scalar=1.0)
+        m.op("slope" + c, "mul", ["s" + c, "Zs1" + c])
+        return m.op("dZ" + c, "mul", ["dY4", "slope" + c])
+
+    dz = plane("")
+    m.op("dZx", "mul", [dz, "Xh"])
+    m.op("sb", "reduce_sum", [dz], axis=1, keepdim=True)
+    m.op("sg", "reduce_sum", ["dZx"], axis=1, keepdim=True)
+
+    def mean(name, src):
+        m.op(name + "_g", "mul", [src, "gamma4"])
+        if m.per > 1:
+            m.op(name + "_s", "reduce_sum", [name + "_g"], axis=3, keepdim=True)
+        return m.op(name, "mul", [name + ("_s" if m.per > 1 else "_g")], scalar=1.0 / (m.positions * m.per))
+
+    mean("c1", "sb")
+    mean("c2", "sg")
+    sums = list(m.prims)
+    dz = plane("_x")
+    m.op("g", "mul", [dz, "gamma4"])
+    m.op("G1", "sub", ["g", "c1"])
+    m.op("Xc", "mul", ["Xh_x", "c2"])
+    m.op("G2", "sub", ["G1", "Xc"])
+    m.op("dX4", "mul", ["G2", "r4"], dtype)
+    m.op("dX", "reshape", ["dX4"], dtype, shape=m.map)
+    m.op("dgamma4", "reduce_sum", ["sg"], dtype, axis=0, keepdim=True)
+    m.op("dgamma", "reshape", ["dgamma4"], dtype, shape=(c,))
+    m.op("dbeta4", "reduce_sum", ["sb"], dtype, axis=0, keepdim=True)
+    m.op("dbeta", "reshape", ["dbeta4"], dtype, shape=(c,))
+    outs = ["dX", "dgamma", "dbeta"]
+    w = _finish(b, "groupnorm_grad", outs, m.sizes, extra_outputs)
+    whole = (sums + m.prims, outs)
+    w.plans["layered"] = [(sums, ["sb", "sg", "c1", "c2"]), (list(m.prims), outs)]
+    w.plans["fused"] = [whole] if _one_kernel(w, whole) else w.plans["layered"]
+    return w
+
+
+class _Rotary:
+    """The angles and the turn that ``rotary`` and its gradient share."""
+
+    def __init__(self, b, batch, heads, kv_heads, n, d, rot, axes, interleaved, packed):
+        kv_heads = heads if kv_heads is None else kv_heads
+        rot = d if rot is None else rot
+        if min(batch, heads, kv_heads, n, d, axes) < 1 or heads % kv_heads:
+            raise ValueError("heads must be a positive multiple of kv_heads, and every size positive")
+        if rot < 2 or rot % 2 or rot > d:
+            raise ValueError("rot must be even, at least 2 and at most d")
+        self.b, self.batch, self.heads, self.kv, self.n, self.d, self.rot = b, batch, heads, kv_heads, n, d, rot
+        self.pairs, self.axes, self.interleaved, self.packed = rot // 2, axes, interleaved, packed
+        self.sizes = dict(batch=batch, heads=heads, kv_heads=kv_heads, n=n, d=d, rot=rot, axes=axes, interleaved=interleaved, packed=packed)
+        self.prims = []
+
+    def op(self, name, op, ins, dtype="f32", **attrs):
+        self.b.op(name, op, ins, dtype, **attrs)
+        self.prims.append(name)
+        return name
+
+    def angles(self):
+        b = self.b
+        b.inp("positions", (self.batch, self.n, self.axes), "f32")
+        if self.axes > 1:
+            b.inp("axis", (self.pairs,), "f32")
+        b.inp("freq", (self.pairs,), "f32")
+        if self.axes > 1:
+            b.op("places", "reshape", ["positions"], "f32", shape=(self.batch, 1, self.n, 1, self.axes))
+            at = self.op("place", "gather", ["places", "axis"])
+        else:
+            at = "place"
+            b.op(at, "reshape", ["positions"], "f32", shape=(self.batch, 1, self.n, 1))
+        self.op("co", "cos_mul", [at, "freq"])
+        self.op("si", "sin_mul", [at, "freq"])
+        if self.interleaved:
+            for x in ("co", "si"):
+                self.op(x + "_i", "reshape", [x], shape=(self.batch, 1, self.n, self.pairs, 1))
+
+    def _part(self, name, src, first, last):
+        """[.., first:last] of the last axis."""
+        shape = self.b.g.node_info(self.b.ids[src])[2]
+        if (first, last) == (0, shape[-1]):
+            return src
+        return self.op(name, "slice", [src], self.b.dtype, begin=(0,) * (len(shape) - 1) + (first,), end=shape[:-1] + (last,))
+
+    def turn(self, name, src, heads, back):
+        """``name`` = src [batch, heads, n, d] turned by the angles, or by their negatives."""
+        p, t = self.pairs, self.b.dtype
+        if self.interleaved:
+            x = self._part(name + "_t", src, 0, 2 * p)
+            x = self.op(name + "_x", "reshape", [x], t, shape=(self.batch, heads, self.n, p, 2))
+            one, two, co, si = self._part(name + "_1", x, 0, 1), self._part(name + "_2", x, 1, 2), "co_i", "si_i"
+        else:
+            one, two, co, si = self._part(name + "_1", src, 0, p), self._part(name + "_2", src, p, 2 * p), "co", "si"
+        self.op(name + "_1c", "mul", [one, co])
+        self.op(name + "_2s", "mul", [two, si])
+        self.op(name + "_a", "add" if back else "sub", [name + "_1c", name + "_2s"], t)
+        self.op(name + "_2c", "mul", [two, co])
+        self.op(name + "_1s", "mul", [one, si])
+        self.op(name + "_b", "sub" if back else "add", [name + "_2c", name + "_1s"], t)
+        rest = [self._part(name + "_r", src, 2 * p, self.d)] if self.rot < self.d else []
+        ab = [name + "_a", name + "_b"]
+        if not self.interleaved:
+            return self.op(name, "concat", ab + rest, t, axis=-1)
+        both = self.op(name + "_ab", "concat", ab, t, axis=-1)
+        flat = self.op(name + "_f" if rest else name, "reshape", [both], t, shape=(self.batch, heads, self.n, 2 * p))
+        return self.op(name, "concat", [flat] + rest, t, axis=-1) if rest else flat
+
+
+def rotary(batch=1, heads=8, kv_heads=None, n=1024, d=64, rot=None, axes=1, interleaved=False, packed=False, dtype="bf16", extra_outputs=()):
+    """Rotary positions of queries and keys along one or several axes (time,
+    height, width), in one kernel.  Pair p of a token's head turns by the angle
+    a = positions[b, i, axis[p]] freq[p]:
+
+      (x1, x2) -> (x1 cos a - x2 sin a, x2 cos a + x1 sin a)
+
+    The first ``rot`` (default d) of a head's d dims turn, in rot / 2 pairs:
+    dims p and p + rot / 2, or with ``interleaved`` dims 2 p and 2 p + 1; the
+    rest stays.  Inputs ``positions`` [batch, n, axes] (any fp32 numbers),
+    ``axis`` [rot / 2] (fp32 whole numbers; left out where there is one axis)
+    and ``freq`` [rot / 2], radians per position (fp32).  The angle is the exact
+    product of its two fp32 factors, so far positions keep theirs.
+
+    Q [batch, heads, n, d] and K [batch, kv_heads, n, d] give ``Qr`` and ``Kr``;
+    ``packed`` takes QKV [batch, n, heads + 2 kv_heads, d] as a projection's
+    product leaves it and gives Qr, Kr and V in the layout that ``mha`` reads
+    (heads before tokens).  n = 1 is the next token of each sequence."""
+    b = _B(dtype)
+    a = _Rotary(b, batch, heads, kv_heads, n, d, rot, axes, interleaved, packed)
+    if packed:
+        b.inp("QKV", (batch, n, a.heads + 2 * a.kv, d))
+    else:
+        b.inp("Q", (batch, a.heads, n, d))
+        b.inp("K", (batch, a.kv, n, d))
+    a.angles()
+    src, outs = ("Q", "K"), ["Qr", "Kr"]
+    if packed:
+        first = 0
+        for x, h in (("Q", a.heads), ("K", a.kv), ("V", a.kv)):
+            a.op(x + "p", "slice", ["QKV"], dtype, begin=(0, 0, first, 0), end=(batch, n, first + h, d))
+            a.op(x + "t" if x != "V" else "V", "transpose", [x + "p"], dtype, perm=(0, 2, 1, 3))
+            first += h
+        src, outs = ("Qt", "Kt"), ["Qr", "Kr", "V"]
+    a.turn("Qr", src[0], a.heads, False)
+    a.turn("Kr", src[1], a.kv, False)
+    w = _finish(b, "rotary", outs, a.sizes, extra_outputs)
+    w.plans["fused"] = [(list(a.prims), outs)]
+    return w
+
+
+def rotary_grad(batch=1, heads=8, kv_heads=None, n=1024, d=64, rot=None, axes=1, interleaved=False, packed=False, dtype="bf16", extra_outputs=()):
+    """The gradient of ``rotary`` (same arguments): dQr and dKr turned back by the
+    same angles, dQ and dK; ``packed`` takes dV too and gives dQKV in the
+    projection's layout.  (The turn is orthogonal: its transpose is the turn back.)"""
+    b = _B(dtype)
+    a = _Rotary(b, batch, heads, kv_heads, n, d, rot, axes, interleaved, packed)
+    b.inp("dQr", (batch, a.heads, n, d))
+    b.inp("dKr", (batch, a.kv, n, d))
+    if packed:
+        b.inp("dV", (batch, a.kv, n, d))
+    a.angles()
+    a.turn("dQ", "dQr", a.heads, True)
+    a.turn("dK", "dKr", a.kv, True)
+    outs = ["dQ", "dK"]
+    if packed:
+        for x in ("dQ", "dK", "dV"):
+            a.op(x + "t", "transpose", [x], dtype, perm=(0, 2, 1, 3))
+        a.op("dQKV", "concat", ["dQt", "dKt", "dVt"], dtype, axis=2)
+        outs = ["dQKV"]
+    w = _finish(b, "rotary_grad", outs, a.sizes, extra_outputs)
+    w.plans["fused"] = [(list(a.prims), outs)]
+    return w
+
+
+# Tensors that one kernel of grad_clip takes: their addresses are kernel
+# arguments (8 bytes each, in and out, of the 4 KiB that a launch passes safely).
+CLIP_TENSORS = 200
+
+
+def grad_clip(shapes=((768,), (768, 768)), dtype="bf16", dtypes=None, max_norm=1.0, eps=1e-6, extra_outputs=()):
+    """The global norm of many gradients and the gradients clipped by it:
+
+      norm = sqrt(sum over all tensors and elements of G^2),   C_i = G_i min(1, max_norm / (norm + eps))
+
+    Inputs G0, G1, .. of ``shapes`` (and ``dtypes``, default ``dtype`` for all);
+    outputs ``norm`` [1] (fp32) and C0, C1, .. of the inputs' shapes and types,
+    which may share their gradients' memory (every kernel reads an element
+    before it writes it).  The sum of squares is held in 64 bits by the fused
+    plan, so neither 1e30 nor 1e-30 leaves its range, and taken in a fixed order.
+    A norm that is not a number leaves none in any gradient; an infinite one
+    leaves zeros, and NaN where the gradient itself is infinite."""
+    shapes = [tuple(int(x) for x in s) for s in shapes]
+    dtypes = [dtype] * len(shapes) if dtypes is None else list(dtypes)
+    if not shapes or len(dtypes) != len(shapes):
+        raise ValueError("one shape at least, and a type for each")
+    if not (0 < max_norm < math.inf and 0 <= eps < math.inf):
+        raise ValueError("max_norm must be positive and finite, eps finite and not negative")
+    b = _B(dtype)
+    k = len(shapes)
+    for i, (s, t) in enumerate(zip(shapes, dtypes)):
+        if not s or min(s) < 1 or len(s) > 8:
+            raise ValueError(f"shape {s} of gradient {i}: one to eight positive sizes")
+        b.inp(f"G{i}", s, t)
+    parts = [list(range(i, min(i + CLIP_TENSORS, k))) for i in range(0, k, CLIP_TENSORS)]
+
+    def root_of_squares(name, tensors, c):
+        """``name`` [1] = the root of the sum of the squares of tensors (name, type, elements); the kernel's primitives."""
+        prims = []
+        for x, t, count in tensors:
+            b.op(f"{x}_f{c}", "reshape", [x], t, shape=(count, 1))
+            b.op(f"{x}_q{c}", "square", [f"{x}_f{c}"], "f32")
+            b.op(f"{x}_s{c}", "reduce_sum", [f"{x}_q{c}"], "f32", axis=0, keepdim=False)
+            prims += [f"{x}_q{c}", f"{x}_s{c}"]
+        total = prims[-1]
+        if len(tensors) > 1:
+            b.op(name + "_c", "concat", prims[1::2], "f32", axis=0)
+            b.op(name + "_r", "reshape", [name + "_c"], "f32", shape=(len(tensors), 1))
+            b.op(name + "_t", "reduce_sum", [name + "_r"], "f32", axis=0, keepdim=False)
+            prims += [name + "_c", name + "_r", name + "_t"]
+            total = name + "_t"
+        b.op(name, "sqrt", [total], "f32")
+        return prims + [name]
+
+    tensors = [(f"G{i}", t, math.prod(s)) for i, (s, t) in enumerate(zip(shapes, dtypes))]
+    kernels = []
+    if len(parts) > 1:  # norms of parts, whose norm is the whole one
+        for j, part in enumerate(parts):
+            kernels.append((root_of_squares(f"norm{j}", [tensors[i] for i in part], ""), [f"norm{j}"]))
+        tensors = [(f"norm{j}", "f32", 1) for j in range(len(parts))]
+    tail = root_of_squares("norm", tensors, "")
+    b.op("norm_e", "add", ["norm"], "f32", scalar=eps)
+    b.op("limit", "fill", [], "f32", shape=(1,), scalar=max_norm)
+    b.op("ratio", "div", ["limit", "norm_e"], "f32")
+    b.op("below", "gt", ["ratio"], "f32", scalar=1.0)
+    b.op("one", "fill", [], "f32", shape=(1,), scalar=1.0)
+    b.op("factor", "select", ["below", "one", "ratio"], "f32")
+    tail += ["norm_e", "limit", "ratio", "below", "one", "factor"]
+    for i in range(k):
+        b.op(f"C{i}", "mul", [f"G{i}", "factor"], dtypes[i])
+    w = _finish(b, "grad_clip", ["norm"] + [f"C{i}" for i in range(k)], dict(shapes=shapes, dtypes=dtypes, max_norm=max_norm), extra_outputs)
+    kernels.append((tail, ["norm", "factor"]))
+    w.plans["fused"] = kernels + [([f"C{i}" for i in part], [f"C{i}" for i in part]) for part in parts]
+    return w
+
+
 def layout_probe(op, dtype, shapes, **attrs):
     """A graph of one layout primitive (transpose, slice, pad or concat) on
     graph inputs of the given shapes; a concat whose ``fill`` attribute is set
@@ -673,7 +1063,8 @@ def layout_probe(op, dtype, shapes, **attrs):
 
 BUILDERS = {"attention": attention, "mlp": mlp, "sra": sra, "conv": conv, "linattn": linattn, "instnorm": instnorm}
 # Operators of a transformer layer's training and serving, built by name like the workloads.
-OPERATORS = {"layernorm": layernorm, "layernorm_grad": layernorm_grad, "mha": mha, "mha_grad": mha_grad}
+OPERATORS = {"layernorm": layernorm, "layernorm_grad": layernorm_grad, "mha": mha, "mha_grad": mha_grad, "groupnorm": groupnorm,
+             "groupnorm_grad": groupnorm_grad, "rotary": rotary, "rotary_grad": rotary_grad, "grad_clip": grad_clip}
 
 
 def rewritten(w: Workload, rules=None):
