@@ -239,6 +239,8 @@ struct SinCos {
   float s, c;
 };
 __device__ __forceinline__ SinCos k_sincos_mul(float x, float y) {
+// (p - rint(p) as one fused operation on a hi would hold p's rounding error already)
+#pragma clang fp contract(off)
   const double a = (double)x * (double)y;
   const double hi = 0x1.45f306dc9c883p-3, lo = -0x1.6b01ec5417056p-57;
   const double p = a * hi;

@@ -1,0 +1,528 @@
+"""Group norm with an activation, rotary positions with several axes, gradient
+clipping, and their gradients on the GPU, against plain float64 forms with bounds
+counted from the definitions."""
+
+from fractions import Fraction
+
+import numpy as np
+import pytest
+
+from paper_2406_09465_amd import graphs
+
+from . import vision_ref as ref
+from .test_gpu_layer_ops import _bits
+
+pytestmark = pytest.mark.gpu
+
+
+def _run(w, x, plan="fused"):
+    from paper_2406_09465_amd.runner import PlanRunner
+    return PlanRunner(w, plan).run(x)
+
+
+def _check(out, want, dtype, f32=()):
+    for k, (v, b) in want.items():
+        if k in out:
+            worst = ref.outside(out[k], v, b, "f32" if k in f32 else dtype)
+            assert worst <= 1.0, (k, worst)
+
+
+# ---- group norm ------------------------------------------------------------------
+
+# (dtype, batch, hh, ww, c, groups, act)
+GN = [
+    ("f16", 1, 16, 16, 320, 32, "silu"),      # whole groups in registers, ten channels to a group
+    ("f32", 2, 5, 7, 30, 5, "relu"),          # six channels: vectors of two
+    ("bf16", 3, 9, 11, 21, 7, "silu"),        # no vector divides the channels
+    ("f16", 2, 1, 1, 64, 8, "silu"),          # one position
+    ("f32", 3, 4, 4, 12, 12, "none"),         # one channel to a group
+    ("bf16", 2, 13, 6, 40, 1, "relu"),        # one group
+    ("f16", 40, 3, 5, 48, 4, "silu"),         # images handed over in two levels
+    ("f32", 1, 63, 65, 33, 3, "silu"),        # 4095 positions, eleven channels
+    ("f16", 1, 200, 301, 32, 4, "none"),      # positions split over more than 32 workgroups
+    ("bf16", 2, 151, 149, 64, 32, "silu"),    # two channels to a group: vectors over four groups
+    ("f32", 2, 97, 101, 260, 2, "relu"),      # 130 channels to a group
+    ("f16", 3, 70, 71, 96, 8, "silu"),
+    ("f32", 1, 30, 41, 2050, 5, "silu"),      # more vectors than threads
+    ("bf16", 1, 24, 24, 4096, 32, "silu"),
+    ("f16", 1, 2, 1, 8192, 32, "relu"),
+    ("f32", 5, 1, 2, 1, 1, "none"),           # one channel, two positions
+    ("bf16", 1, 300, 300, 7, 7, "silu"),      # odd channels, split
+]
+
+
+def _gn_inputs(dtype, batch, hh, ww, c, seed=0, mean=0.3, std=1.5):
+    rng = np.random.default_rng(seed)
+    x, s = {}, {}
+    at = rng.normal(0, 0.5, c)
+    for k, v in (("X", rng.normal(mean, std, (batch, hh, ww, c)) + at), ("gamma", rng.normal(1, 0.2, c)), ("beta", rng.normal(0, 0.2, c)),
+                 ("dY", rng.normal(0, 1, (batch, hh, ww, c)))):
+        x[k], s[k] = ref.rounded(v, dtype)
+    return x, s
+
+
+def _gn_sizes(case):
+    return dict(zip(("dtype", "batch", "hh", "ww", "c", "groups", "act"), case))
+
+
+@pytest.mark.parametrize("case", GN, ids=str)
+def test_groupnorm_and_gradient(case):
+    z = _gn_sizes(case)
+    x, s = _gn_inputs(*case[:5])
+    want = ref.groupnorm(x["X"], x["gamma"], x["beta"], z["groups"], 1e-5, z["act"], z["dtype"], x["dY"])
+    for plan in ("layered", "fused"):
+        out = _run(graphs.build("groupnorm", **z), s, plan)
+        _check(out, want, z["dtype"], ("mu", "r"))
+        g = {**s, "mu": out["mu"].astype(np.float32), "r": out["r"].astype(np.float32)}
+        _check(_run(graphs.build("groupnorm_grad", **z), g, plan), want, z["dtype"])
+
+
+@pytest.mark.parametrize("case", [("f32", 2, 3, 5, 12, 4, "silu"), ("f32", 2, 4, 4, 6, 6, "relu")], ids=str)
+def test_groupnorm_one_kernel_per_primitive(case):
+    z = _gn_sizes(case)
+    x, s = _gn_inputs(*case[:5])
+    want = ref.groupnorm(x["X"], x["gamma"], x["beta"], z["groups"], 1e-5, z["act"], z["dtype"], x["dY"])
+    out = _run(graphs.build("groupnorm", **z), s, "unfused")
+    _check(out, want, z["dtype"], ("mu", "r"))
+    s.update(mu=out["mu"].astype(np.float32), r=out["r"].astype(np.float32))
+    _check(_run(graphs.build("groupnorm_grad", **z), s, "unfused"), want, z["dtype"])
+
+
+@pytest.mark.parametrize("hh", [8, 128])
+def test_groupnorm_far_from_zero(hh):
+    """A mean of a thousand deviations costs the variance no more than the mean's own rounding."""
+    z = dict(dtype="f32", batch=2, hh=hh, ww=hh, c=32, groups=4, act="none")
+    x, s = _gn_inputs("f32", 2, hh, hh, 32, mean=1000.0, std=1.0)
+    want = ref.groupnorm(x["X"], x["gamma"], x["beta"], 4, 1e-5, "none", "f32")
+    out = _run(graphs.build("groupnorm", **z), s)
+    _check(out, want, "f32", ("mu", "r"))
+    # far inside the bound: the variance by centred squares, not by E[x^2] - mu^2 (off by 6 % here)
+    assert np.max(np.abs(out["r"] / want["r"][0] - 1)) < 1e-4
+
+
+@pytest.mark.parametrize("hh", [6, 100])
+def test_groupnorm_a_group_that_is_no_number(hh):
+    """NaN and infinities of one group of one image stay in it, forward and back (the sums of its channels excepted)."""
+    z = dict(dtype="f16", batch=3, hh=hh, ww=hh, c=48, groups=4, act="silu")
+    x, s = _gn_inputs("f16", 3, hh, hh, 48)
+    want = ref.groupnorm(x["X"], x["gamma"], x["beta"], 4, 1e-5, "silu", "f16", x["dY"])
+    s["X"] = s["X"].copy()
+    s["X"][1, hh // 2, 3, 14] = np.nan
+    s["X"][1, 0, 0, 30] = np.inf
+    out = _run(graphs.build("groupnorm", **z), s)
+    s.update(mu=out["mu"].astype(np.float32), r=out["r"].astype(np.float32))
+    out.update(_run(graphs.build("groupnorm_grad", **z), s))
+    hit = np.zeros((3, 4), bool)
+    hit[1, 1] = hit[1, 2] = True
+    full = np.broadcast_to(np.repeat(hit, 12, axis=1)[:, None, None], x["X"].shape)
+    chan = np.repeat(hit.any(0), 12)
+    for k, bad in (("Y", full), ("dX", full), ("mu", hit), ("r", hit), ("dgamma", chan), ("dbeta", chan)):
+        v, b = want[k]
+        assert np.all(np.isnan(out[k][bad])) or k in ("mu", "r"), k
+        assert ref.outside(out[k][~bad], v[~bad], b[~bad], "f32" if k in ("mu", "r") else "f16") <= 1.0, k
+
+
+def test_groupnorm_constant_groups():
+    """A group of equal numbers: its variance is zero, its deviation eps' root."""
+    z = dict(dtype="f32", batch=2, hh=9, ww=9, c=16, groups=4, act="none")
+    x, s = _gn_inputs("f32", 2, 9, 9, 16)
+    s["X"] = np.full_like(s["X"], 3.0)
+    out = _run(graphs.build("groupnorm", **z), s)
+    assert np.allclose(out["r"], 1e-5 ** -0.5, rtol=1e-6) and np.all(out["mu"] == 3.0)
+    assert np.array_equal(out["Y"], np.broadcast_to(x["beta"], out["Y"].shape))
+
+
+# ---- rotary positions --------------------------------------------------------------
+
+ROT = [
+    dict(dtype="f16", batch=2, heads=4, kv_heads=2, n=37, d=64, axes=2),
+    dict(dtype="bf16", batch=3, heads=8, kv_heads=2, n=1, d=128, axes=3, packed=True, first=5000),
+    dict(dtype="f32", batch=2, heads=3, kv_heads=3, n=101, d=40, rot=24, interleaved=True, first=900000, step=0.25),
+    dict(dtype="f32", batch=1, heads=1, kv_heads=1, n=5, d=8, first=16000000),
+    dict(dtype="f16", batch=2, heads=6, kv_heads=3, n=50, d=48, rot=24, axes=3, packed=True),
+    dict(dtype="bf16", batch=2, heads=2, kv_heads=1, n=33, d=10, rot=6, axes=2),
+    dict(dtype="f16", batch=2, heads=2, kv_heads=2, n=7, d=18, rot=18, interleaved=True, packed=True),
+    dict(dtype="f32", batch=1, heads=2, kv_heads=1, n=3, d=7, rot=2),
+    dict(dtype="f32", batch=1, heads=2, kv_heads=1, n=3, d=9, rot=4, interleaved=True),
+    dict(dtype="bf16", batch=5, heads=12, kv_heads=12, n=700, d=64, axes=2, interleaved=True),
+    dict(dtype="f16", batch=1, heads=2, kv_heads=2, n=2, d=256, packed=True),
+    dict(dtype="f32", batch=2, heads=4, kv_heads=4, n=4, d=16, packed=True, axes=2),  # as many heads as tokens
+    dict(dtype="f16", batch=1, heads=1, kv_heads=1, n=3, d=1024),                      # more pairs than threads
+]
+
+
+def _rot_case(c, seed=0):
+    c = dict(c)
+    first, step = c.pop("first", 0), c.pop("step", 1.0)
+    rng = np.random.default_rng(seed)
+    rot = c.get("rot", c["d"])
+    P, A = rot // 2, c.get("axes", 1)
+    x, s = {}, {}
+    b, h, hk, n, d = (c[k] for k in ("batch", "heads", "kv_heads", "n", "d"))
+    shapes = {"QKV": (b, n, h + 2 * hk, d)} if c.get("packed") else {"Q": (b, h, n, d), "K": (b, hk, n, d)}
+    shapes.update(dQr=(b, h, n, d), dKr=(b, hk, n, d), dV=(b, hk, n, d))
+    for k, sh in shapes.items():
+        x[k], s[k] = ref.rounded(rng.normal(0, 1, sh), c["dtype"])
+    pos = first + step * rng.integers(0, 4 * n, (b, n, A))
+    x["positions"], s["positions"] = ref.rounded(pos, "f32")
+    x["freq"], s["freq"] = ref.rounded(10000.0 ** (-np.arange(P) / P), "f32")
+    x["axis"], s["axis"] = ref.rounded(rng.integers(0, A, P), "f32")
+    return c, x, s
+
+
+def _rot_want(c, x):
+    axis = x["axis"] if c.get("axes", 1) > 1 else None
+    t = lambda v, back: ref.turn(v, x["positions"], axis, x["freq"], c.get("interleaved", False), back, c["dtype"])  # noqa: E731
+    h, hk = c["heads"], c["kv_heads"]
+    if not c.get("packed"):
+        return {"Qr": t(x["Q"], False), "Kr": t(x["K"], False)}, {"dQ": t(x["dQr"], True), "dK": t(x["dKr"], True)}
+    m = x["QKV"].transpose(0, 2, 1, 3)
+    v = m[:, h + hk:]
+    back = [t(x["dQr"], True), t(x["dKr"], True), (x["dV"], np.zeros_like(x["dV"]))]
+    grad = tuple(np.concatenate([p[i] for p in back], 1).transpose(0, 2, 1, 3) for i in (0, 1))
+    return {"Qr": t(m[:, :h], False), "Kr": t(m[:, h:h + hk], False), "V": (v, np.zeros_like(v))}, {"dQKV": grad}
+
+
+@pytest.mark.parametrize("case", ROT, ids=str)
+def test_rotary_and_gradient(case):
+    c, x, s = _rot_case(case)
+    fwd, back = _rot_want(c, x)
+    for plan in ("fused", "unfused") if c["n"] < 40 else ("fused",):
+        _check(_run(graphs.build("rotary", **c), s, plan), fwd, c["dtype"])
+        _check(_run(graphs.build("rotary_grad", **c), s, plan), back, c["dtype"])
+
+
+def test_angles_of_far_positions():
+    """cos_mul and sin_mul: products up to 2^50, signs, zero, and what is no number."""
+    from paper_2406_09465_amd._abi import Graph
+    from paper_2406_09465_amd.graphs import Workload
+    rng = np.random.default_rng(3)
+    a = np.concatenate([rng.normal(0, 1, 3000), rng.uniform(-1, 1, 3000) * 2.0 ** rng.uniform(0, 24, 3000), [0.0, -0.0, 1e-40, 16777216.0]])
+    f = np.concatenate([rng.normal(0, 3, 3000), rng.uniform(0, 1, 3000) * 2.0 ** rng.uniform(-20, 25, 3000), [1.0, 1.0, 1.0, 33554432.0]])
+    a, sa = ref.rounded(a, "f32")
+    f, sf = ref.rounded(f, "f32")
+    # the rest of each angle beyond its whole turns, in exact fractions (2 pi to 60 digits)
+    turn = 2 * Fraction("3.14159265358979323846264338327950288419716939937510582097494")
+    angle = [Fraction(p) * Fraction(q) for p, q in zip(a.tolist(), f.tolist())]
+    left = np.array([float(t - round(t / turn) * turn) for t in angle])
+    g = Graph()
+    ia, jf = g.input("f32", (len(a),)), g.input("f32", (len(a),))
+    outs = [g.op(op, [ia, jf], "f32") for op in ("cos_mul", "sin_mul")]
+    for o in outs:
+        g.output(o)
+    g.finalize()
+    w = Workload("angles", "f32", g, dict(a=ia, f=jf, c=outs[0], s=outs[1]), ["a", "f"], ["c", "s"])
+    w.plans["fused"] = [(["c"], ["c"]), (["s"], ["s"])]
+    out = _run(w, dict(a=sa, f=sf))
+    assert np.max(np.abs(a * f)) == 2.0 ** 49
+    for k, v in (("c", np.cos(left)), ("s", np.sin(left))):
+        assert np.all(np.abs(out[k] - v) <= 3 * ref.E), k
+    assert np.all(np.abs(out["c"] ** 2 + out["s"] ** 2 - 1) < 8 * ref.E)
+    odd, so = ref.rounded(np.array([np.inf, -np.inf, np.nan, 3e38, 1.0]), "f32")
+    g = Graph()
+    ia, jf = g.input("f32", (5,)), g.input("f32", (5,))
+    o = g.op("sin_mul", [ia, jf], "f32")
+    g.output(o)
+    g.finalize()
+    w = Workload("odd", "f32", g, dict(a=ia, f=jf, s=o), ["a", "f"], ["s"], {"fused": [(["s"], ["s"])]})
+    got = _run(w, dict(a=so, f=np.array([1, 1, 1, 3e38, np.inf], np.float32)))["s"]
+    assert np.all(np.isnan(got[[0, 1, 2, 4]])) and (np.isnan(got[3]) or abs(got[3]) <= 1)
+
+
+# ---- gradient clipping -----------------------------------------------------------------
+
+CLIP = [
+    dict(shapes=[(5,)], dtype="f32"),
+    dict(shapes=[(1,), (1,)], dtype="bf16"),
+    dict(shapes=[(768,), (768, 40), (77,), (3, 5, 7), (1,), (333, 41)], dtype="f16"),
+    dict(shapes=[(100, 100), (768,), (1001,), (64, 64)], dtypes=["bf16", "f32", "f16", "f32"]),
+    dict(shapes=[(2000, 3001), (50,)], dtype="bf16"),
+    dict(shapes=[(16384,), (16385,), (8192,), (2048,), (2049,)], dtype="f16"),  # whole chunks, and one element more
+    dict(shapes=[(1 + i % 37, 11) for i in range(450)], dtype="f32"),           # more tensors than a kernel takes
+]
+
+
+def _clip_case(c, scale=1.0, seed=0):
+    rng = np.random.default_rng(seed)
+    dt = c.get("dtypes") or [c["dtype"]] * len(c["shapes"])
+    x, s = {}, {}
+    for i, (sh, t) in enumerate(zip(c["shapes"], dt)):
+        x[f"G{i}"], s[f"G{i}"] = ref.rounded(rng.normal(0, scale * (1 + i % 3), sh), t)
+    return dt, x, s
+
+
+@pytest.mark.parametrize("max_norm", [0.5, 1e6])
+@pytest.mark.parametrize("case", CLIP, ids=lambda c: f"{len(c['shapes'])}x{c['shapes'][0]}")
+def test_clipped_gradients(case, max_norm):
+    dt, x, s = _clip_case(case)
+    want = ref.clipped(list(x.values()), dt, max_norm, 1e-6)
+    out = _run(graphs.build("grad_clip", **case, max_norm=max_norm), s)
+    for i, t in enumerate(dt):
+        assert ref.outside(out[f"C{i}"], *want[f"C{i}"], t) <= 1.0, i
+    assert ref.outside(out["norm"], *want["norm"], "f32") <= (1.0 if len(dt) < 200 else 2.0)  # (norms of parts are rounded too)
+
+
+@pytest.mark.parametrize("scale", [1e25, 1e-25])
+def test_norms_whose_squares_leave_fp32(scale):
+    case = dict(shapes=[(100, 30), (77,)], dtype="f32")
+    dt, x, s = _clip_case(case, scale)
+    want = ref.clipped(list(x.values()), dt, 2 * scale, 0.0)
+    out = _run(graphs.build("grad_clip", **case, max_norm=2 * scale, eps=0.0), s)
+    _check(out, want, "f32")
+
+
+def test_norms_that_are_no_numbers():
+    case = dict(shapes=[(300,), (4, 5)], dtype="f32")
+    for bad in (np.nan, np.inf, -np.inf):
+        _, x, s = _clip_case(case)
+        s["G0"] = s["G0"].copy()
+        s["G0"][17] = bad
+        out = _run(graphs.build("grad_clip", **case), s)
+        if np.isnan(bad):
+            assert np.isnan(out["norm"][0]) and all(np.all(np.isnan(out[f"C{i}"])) for i in (0, 1))
+        else:
+            assert out["norm"][0] == np.inf and np.isnan(out["C0"][17])
+            assert np.all(np.delete(out["C0"], 17) == 0) and np.all(out["C1"] == 0)
+    zero = {k: np.zeros_like(v) for k, v in s.items()}
+    out = _run(graphs.build("grad_clip", **case), zero)
+    assert out["norm"][0] == 0 and np.all(out["C0"] == 0)
+
+
+def test_clipping_in_place():
+    import torch
+    from paper_2406_09465_amd.runner import PlanRunner
+    case = CLIP[3]
+    dt, x, s = _clip_case(case)
+    r = PlanRunner(graphs.build("grad_clip", **case, max_norm=0.5), "fused")
+    r.set_inputs(s)
+    r.launch()
+    want = [t.clone() for t in r.outs]
+    r.outs[1:] = r.ins
+    r.launch()
+    torch.cuda.synchronize()
+    for a, b in zip(want, r.outs):
+        assert torch.equal(a, b)
+
+
+def test_clipping_one_kernel_per_primitive():
+    dt, x, s = _clip_case(dict(shapes=[(30, 7), (11,)], dtype="f32"))
+    want = ref.clipped(list(x.values()), dt, 0.5, 1e-6)
+    out = _run(graphs.build("grad_clip", shapes=[(30, 7), (11,)], dtype="f32", max_norm=0.5), s, "unfused")
+    n = 30 * 7 + 11  # squares added in fp32
+    assert abs(out["norm"][0] - want["norm"][0][0]) <= (n + 4) * ref.E * want["norm"][0][0]
+    for i in (0, 1):
+        v, b = want[f"C{i}"]
+        assert np.all(np.abs(out[f"C{i}"] - v) <= b + (n + 4) * ref.E * np.abs(v))
+
+
+# ---- executions ----------------------------------------------------------------------------
+
+REPEAT = [
+    ("groupnorm", dict(batch=1, hh=16, ww=16, c=320, groups=32, dtype="f16")),
+    ("groupnorm", dict(batch=2, hh=150, ww=150, c=64, groups=8, dtype="bf16")),
+    ("groupnorm", dict(batch=1, hh=300, ww=200, c=96, groups=8, dtype="f32")),
+    ("groupnorm_grad", dict(batch=40, hh=4, ww=4, c=64, groups=8, dtype="f16")),
+    ("groupnorm_grad", dict(batch=1, hh=300, ww=200, c=96, groups=8, dtype="f16")),
+    ("rotary", dict(batch=2, heads=8, kv_heads=2, n=70, d=64, axes=2, packed=True, dtype="bf16")),
+    ("rotary_grad", dict(batch=2, heads=8, kv_heads=2, n=70, d=64, axes=2, packed=True, dtype="bf16")),
+    ("grad_clip", dict(shapes=[(1000, 1000), (77,), (500, 900)], dtype="bf16", max_norm=0.5)),
+    ("grad_clip", dict(shapes=[(4000, 5000)], dtype="f32", max_norm=0.5)),
+]
+
+
+def _random_runner(name, sizes, seed=0, device="cuda"):
+    import torch
+    from paper_2406_09465_amd.runner import TORCH_DTYPE, PlanRunner
+    w = graphs.build(name, **sizes)
+    r = PlanRunner(w, "fused", device=device)
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    for k, i in zip(w.input_names, w.graph.inputs()):
+        _, dt, shape = w.graph.node_info(i)
+        t = torch.randn(shape, generator=gen, device="cuda")
+        r.ins.append((t.abs() + 0.5 if k == "r" else t).to(TORCH_DTYPE[dt]).contiguous())
+    return r.bind()
+
+
+@pytest.mark.parametrize("name,sizes", REPEAT, ids=str)
+def test_same_bits_again_on_another_stream_and_replayed(name, sizes):
+    """Every execution gives the same bits, on a stream of its own, allocation-free
+    and as a replayed graph with eager work between the replays."""
+    import torch
+    from paper_2406_09465_amd._abi import pointer_array
+    r = _random_runner(name, sizes)
+    r.launch_bound()
+    torch.cuda.synchronize()
+    first = [_bits(t) for t in r.outs]
+
+    def same(outs=None):
+        torch.cuda.synchronize()
+        for a, b in zip(first, outs or r.outs):
+            assert np.array_equal(a, _bits(b))
+        for t in outs or r.outs:
+            t.fill_(7)
+
+    same()
+    for _ in range(3):
+        r.launch_bound()
+        same()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    r.launch(s)
+    same()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        r.launch(torch.cuda.current_stream())
+    for _ in range(3):
+        g.replay()
+        same()
+        r.bind().launch_bound()
+        same()
+    other = [torch.empty_like(t) for t in r.outs]
+    r.plan.execute_noalloc(pointer_array([t.data_ptr() for t in r.ins]), pointer_array([t.data_ptr() for t in other]),
+                           torch.cuda.current_stream().cuda_stream)
+    same(other)
+
+
+@pytest.mark.parametrize("name,sizes", [REPEAT[2], REPEAT[4], REPEAT[8]], ids=str)
+def test_two_plans_at_once(name, sizes):
+    """Two plans of the same graph on two streams, each with its own workspace and counters."""
+    import torch
+    a, b = _random_runner(name, sizes, 0), _random_runner(name, sizes, 1)
+    want = []
+    for r in (a, b):
+        r.launch_bound()
+        torch.cuda.synchronize()
+        want.append([_bits(t) for t in r.outs])
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(5):
+        for r, s in zip((a, b), streams):
+            r.launch(s)
+    torch.cuda.synchronize()
+    for r, w in zip((a, b), want):
+        for x, y in zip(w, r.outs):
+            assert np.array_equal(x, _bits(y))
+
+
+def test_outputs_past_their_end_are_left():
+    """Buffers around the results keep what they hold (odd sizes, last tiles)."""
+    import torch
+    from paper_2406_09465_amd.runner import TORCH_DTYPE
+    for name, sizes in (("groupnorm", dict(batch=3, hh=7, ww=5, c=21, groups=3, dtype="f16")), ("groupnorm", dict(batch=1, hh=211, ww=97, c=22, groups=2, dtype="f16")),
+                        ("groupnorm_grad", dict(batch=3, hh=67, ww=41, c=22, groups=2, dtype="bf16")),
+                        ("rotary", dict(batch=1, heads=3, kv_heads=1, n=13, d=24, rot=8, packed=True, dtype="f16")),
+                        ("grad_clip", dict(shapes=[(77,), (5,), (4099,)], dtype="f16"))):
+        r = _random_runner(name, sizes)
+        r.launch_bound()
+        torch.cuda.synchronize()
+        want = [_bits(t) for t in r.outs]
+        big = []
+        for i, o in enumerate(r.w.graph.outputs()):
+            _, dt, shape = r.w.graph.node_info(o)
+            n = int(np.prod(shape))
+            big.append(torch.full((n + 64,), 5.0, dtype=TORCH_DTYPE[dt], device="cuda"))
+            r.outs[i] = big[-1][:n].view(shape)
+        r.launch()
+        torch.cuda.synchronize()
+        for t, b, v in zip(r.outs, want, big):
+            assert np.array_equal(_bits(t), b) and bool((v[t.numel():] == 5.0).all())
+
+
+def test_a_map_past_32_bits():
+    """Maps of 4.8 GB: the last image lies behind 2^32 bytes, one image alone past 2 GiB."""
+    import torch
+    from paper_2406_09465_amd.runner import PlanRunner
+    z = dict(batch=2, hh=3000, ww=3125, c=128, groups=8, dtype="f16", act="relu")
+    r = PlanRunner(graphs.build("groupnorm", **z), "fused")
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    X = torch.randn((2, 3000, 3125, 128), generator=gen, device="cuda", dtype=torch.float16)
+    gamma, beta = torch.rand(128, generator=gen, device="cuda").half() + 0.5, torch.randn(128, generator=gen, device="cuda").half()
+    r.ins = [X, gamma, beta]
+    r.launch()
+    torch.cuda.synchronize()
+    part = X[1].reshape(-1, 8, 16)
+    total = torch.zeros(8, dtype=torch.float64, device="cuda")
+    sq = torch.zeros_like(total)
+    for rows in part.split(1 << 20):
+        d = rows.double()
+        total += d.sum((0, 2))
+        sq += (d * d).sum((0, 2))
+    n = part.shape[0] * 16
+    mu = total / n
+    rs = (sq / n - mu * mu + 1e-5) ** -0.5
+    assert torch.allclose(r.outs[1][1].double(), mu, rtol=0, atol=(ref.depth(n) + 2) * ref.E) and torch.allclose(r.outs[2][1].double(), rs, rtol=ref.depth(n) * ref.E)
+    x = X[1, -1].double().reshape(-1, 8, 16)
+    y = torch.relu((x - mu[:, None]) * rs[:, None] * gamma.double().reshape(8, 16) + beta.double().reshape(8, 16))
+    # the statistics' bound and half a step
+    assert torch.all((r.outs[0][1, -1].double().reshape(-1, 8, 16) - y).abs() <= 2.0 ** -11 * y + 8 * ref.depth(n) * ref.E)
+
+
+# ---- together --------------------------------------------------------------------------------
+
+
+def test_a_training_step_of_an_image_transformer():
+    """Group norm, a projection, rotary positions of two axes, attention, their
+    gradients back to the map, and the clipping of all of them: against float64 autograd."""
+    import torch
+    from paper_2406_09465_amd.runner import PlanRunner
+    B, S, C, H, D = 2, 6, 32, 2, 16
+    N = S * S
+    gen = torch.Generator().manual_seed(0)
+    randn = lambda *s: torch.randn(s, generator=gen).double()  # noqa: E731
+    X, gamma, beta = randn(B, S, S, C), 1 + 0.2 * randn(C), 0.2 * randn(C)
+    Wp, dO = randn(C, 3 * H * D) / C ** 0.5, randn(B, H, N, D)
+    pos = torch.stack(torch.meshgrid(torch.arange(S), torch.arange(S), indexing="ij"), -1).reshape(N, 2).double().expand(B, N, 2)
+    axis = (torch.arange(D // 2) >= D // 4).double()
+    freq = 100.0 ** (-(torch.arange(D // 2) % (D // 4)).double() / (D // 4))
+    gpu = lambda t: t.float().contiguous().cuda()  # noqa: E731
+
+    def plan(name, ins, **sizes):
+        w = graphs.build(name, dtype="f32", **sizes)
+        r = PlanRunner(w, "fused")
+        r.ins = [ins[k] for k in w.input_names]
+        r.launch()
+        return dict(zip(w.output_names, r.outs))
+
+    gn = dict(batch=B, hh=S, ww=S, c=C, groups=4, act="silu")
+    ro = dict(batch=B, heads=H, kv_heads=H, n=N, d=D, axes=2, packed=True)
+    x = dict(X=gpu(X), gamma=gpu(gamma), beta=gpu(beta), positions=gpu(pos), axis=gpu(axis), freq=gpu(freq), dO=gpu(dO))
+    x.update(plan("groupnorm", x, **gn))
+    flat = x["Y"].reshape(B * N, C)
+    x["QKV"] = (flat @ gpu(Wp)).reshape(B, N, 3 * H, D)
+    x.update(plan("rotary", x, **ro))
+    at = dict(batch=B, heads=H, n=N, d=D)
+    att = {"Q": x["Qr"], "K": x["Kr"], "V": x["V"], "dO": x["dO"]}
+    att.update(plan("mha", att, **at))
+    att.update(plan("mha_grad", att, **at))
+    x.update(dQr=att["dQ"], dKr=att["dK"], dV=att["dV"])
+    x.update(plan("rotary_grad", x, **ro))
+    dq = x["dQKV"].reshape(B * N, -1)
+    x["dY"] = (dq @ gpu(Wp).t().contiguous()).reshape(B, S, S, C)
+    dW = flat.t().contiguous() @ dq
+    x.update(plan("groupnorm_grad", x, **gn))
+    grads = [x["dX"], x["dgamma"], x["dbeta"], dW]
+    clip = plan("grad_clip", {f"G{i}": g for i, g in enumerate(grads)}, shapes=[tuple(g.shape) for g in grads], max_norm=0.5)
+    # float64 autograd
+    leaves = [t.clone().requires_grad_() for t in (X, gamma, beta, Wp)]
+    Xl, ga, be, Wl = leaves
+    m = Xl.reshape(B, N, 4, C // 4)
+    mu = m.mean((1, 3), keepdim=True)
+    z = (m - mu) / torch.sqrt(((m - mu) ** 2).mean((1, 3), keepdim=True) + 1e-5) * ga.reshape(4, -1) + be.reshape(4, -1)
+    y = (z * torch.sigmoid(z)).reshape(B, N, C)
+    qkv = (y @ Wl).reshape(B, N, 3 * H, D).transpose(1, 2)
+    ang = (pos[..., axis.long()] * freq)[:, None]
+
+    def turned(t):
+        a, b = t[..., : D // 2], t[..., D // 2:]
+        return torch.cat((a * ang.cos() - b * ang.sin(), b * ang.cos() + a * ang.sin()), -1)
+
+    q, k, v = turned(qkv[:, :H]), turned(qkv[:, H:2 * H]), qkv[:, 2 * H:]
+    o = torch.softmax(q @ k.transpose(2, 3) / D ** 0.5, -1) @ v
+    (o * dO).sum().backward()
+    want = [t.grad for t in leaves]
+    norm = torch.sqrt(sum((w * w).sum() for w in want))
+    f = min(1.0, 0.5 / (float(norm) + 1e-6))
+    # every sum here is of at most 2048 terms in fp32, seven in a row along the step
+    tol = 7 * 2048 * ref.E
+    assert abs(clip["norm"].item() - float(norm)) <= tol * float(norm)
+    for i, w in enumerate(want):
+        assert float((clip[f"C{i}"].double().cpu() - w * f).norm()) <= tol * float((w * f).norm()), i
