@@ -41,7 +41,8 @@ int64_t pow2floor(int64_t x) {
 }
 
 constexpr int kRowsInFlight = 8;     // rows that a thread loads together
-constexpr int64_t kHandOver = 16;    // partial results that one workgroup adds
+constexpr int64_t kHandOver = 16;    // partial results that one workgroup adds where there are two levels
+constexpr int64_t kOneLevel = 64;    // and at most with one
 
 struct GroupGen {
   const KInfo& ki;
@@ -203,9 +204,9 @@ struct GroupGen {
       if (!out) bad("a sum over images that is not an output");
     }
     for (int v : r1) {
-      const Node& n = nd(v);
-      (void)n;
       if (nd(v).shape != Shape{B, 1, G, K}) bad("sum over positions");
+      for (int w : r1)
+        if (gen[w] == gen[v] && nd(w).op != nd(v).op) bad("sums and means of one pass");
     }
   }
 
@@ -254,8 +255,10 @@ struct GroupGen {
   }
 
   // A slab of whole groups in a workgroup's registers: the fewest groups whose
-  // channels make runs of 64 bytes, so that half of each line a load touches
-  // is used; where those do not fit, the most that do.
+  // channels make runs of 64 bytes, so that half of each line a load touches is
+  // used; where all groups of all images are 64 at most, of 16 bytes (few
+  // workgroups wait for few loads: 1x16x16x320 f16 with runs of 20 bytes 4.2 us, of
+  // 80 bytes 6.6).  Where those do not fit, the most groups that do.
   bool slab_geometry() {
     if (P > 65536 || xfull.empty()) return false;
     const int words = std::max<int>(1, (int)xfull.size());
@@ -278,9 +281,15 @@ struct GroupGen {
       if (!fits) continue;
       found = true;
       best = gt;
-      if (ct * eb >= 64) break;
+      if (ct * eb >= (B * G <= 64 ? 16 : 64)) break;
     }
     if (!found) return false;
+    // Past about a thousand cache lines of a map (64 bytes; runs that are no whole
+    // part of a line touch one more), one compute unit's loads take longer than a second launch: forward
+    // 2x32x32x512 f16 (1024 lines) 6.2 us, 10.0 in two kernels; 1x64x64x128 f16 (4096) 12.2 and 9.6;
+    // 8x32x32x640 bf16 (runs of 80 bytes, 2304) 12.9 and 11.8.
+    const int64_t run = best * K * eb;
+    if ((double)P * (run % 64 == 0 ? run / 64.0 : 64 % run == 0 ? 1.0 : run / 64.0 + 1.0) > 1024.0) return false;
     CT = best * K;
     tiles = G / best;
     VEC = 16 / eb;
@@ -326,7 +335,7 @@ struct GroupGen {
       stream_geometry(256);
       // about eight workgroups to a compute unit, a thread's rows in whole
       // batches, so that the channels' values are loaded for several rows
-      const int64_t want = std::max<int64_t>(1, 2048 / B);
+      const int64_t want = std::max<int64_t>(1, ((double)B * P * C * eb >= 67108864.0 ? 4096 : 2048) / B);
       chunk = std::max<int64_t>((P + want - 1) / want, 1);
       U = (int)std::min<int64_t>(4, (chunk + LY - 1) / LY);
       chunk = (chunk + (int64_t)LY * U - 1) / ((int64_t)LY * U) * ((int64_t)LY * U);
@@ -346,9 +355,15 @@ struct GroupGen {
     else
       bad("sums that depend on sums over the same positions");
     stream_geometry(512);
-    // a workgroup of eight waves per compute unit, each thread with two batches of rows at least
-    U = kind == Moments ? kRowsInFlight : 4;
-    S = std::max<int64_t>(1, std::min<int64_t>((256 + B - 1) / B, P / ((int64_t)LY * U * 2)));
+    // A workgroup of eight waves to a compute unit, each thread with a batch of
+    // rows at least; batches of few rows, as a workgroup of few rows runs its code
+    // once and waits for its instructions (batches of 8 and 4, one set loading
+    // while the other is summed: 13.9 us instead of 11.0 for the gradient's sums of
+    // 8x32x32x640 bf16, 41.6 instead of 34.7 at 4x416x416x64 f16).
+    U = kind == Moments ? P * B >= (int64_t)256 * LY * 32 ? 8 : 4 : 2;
+    S = std::max<int64_t>(1, std::min<int64_t>((256 + B - 1) / B, P / ((int64_t)LY * U)));
+    // one level of hand-over as long as a thread's rows stay few
+    if (S > kOneLevel && P <= kOneLevel * LY * 16) S = kOneLevel;
     chunk = (P + S - 1) / S;
     chunk = (chunk + LY - 1) / LY * LY;
     S = (P + chunk - 1) / chunk;
@@ -433,6 +448,7 @@ struct GroupGen {
   }
   bool fast_full() const { return eb == 2; }
 
+  // Rows in registers in their own type.
   std::string raw_decl() const {
     std::ostringstream o;
     for (int u : xfull) o << "  vec_t<" << VEC << ", " << ctype(nd(u).dtype) << "> x" << id(u) << "[" << U << "][" << NJ << "];\n";
@@ -497,7 +513,14 @@ struct GroupGen {
       return;
     }
     const int64_t slab = (int64_t)LY * CT;
-    for (int i = 0; i < n; ++i) s << each("if (act) red[" + std::to_string(i * slab) + " + ly * " + std::to_string(CT) + " + c0[j] - ct0 + e] = " + acc[i] + "[j][e];");
+    // (whole vectors: element by element, lanes VEC floats apart would share LDS banks)
+    for (int i = 0; i < n; ++i) {
+      if (VEC >= 4)
+        s << "  if (act) {\n#pragma unroll\n    for (int e = 0; e < " << VEC << "; e += 4) *(f32x4*)(red + " << i * slab << " + ly * " << CT << " + c0[0] - ct0 + e) = f32x4{" << acc[i] << "[0][e], "
+          << acc[i] << "[0][e + 1], " << acc[i] << "[0][e + 2], " << acc[i] << "[0][e + 3]};\n  }\n";
+      else
+        s << each("if (act) red[" + std::to_string(i * slab) + " + ly * " + std::to_string(CT) + " + c0[j] - ct0 + e] = " + acc[i] + "[j][e];");
+    }
     s << "  __syncthreads();\n";
     int64_t L = 1;
     if (CT < T) L = std::min<int64_t>(std::min<int64_t>(16, pow2floor(T / CT)), pow2floor(LY));
@@ -526,33 +549,66 @@ struct GroupGen {
     for (int i = 0; i < n; ++i) s << "    chan[" << i * CT4() << " + c] = t" << i << "_;\n";
     s << "  }\n  __syncthreads();\n";
   }
-  // Sums over a group's channels of chan[base ..]: grp[g - g0].
-  void group_sums(int64_t base) {
+  // Sums over a group's channels of chan[base ..]: grp[at + g - g0].  (The caller waits for the others.)
+  void group_sums(int64_t base, int64_t at = 0) {
     const int64_t gt = CT / K;
     const int64_t L = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(64, pow2floor(K)), pow2floor(std::max<int64_t>(1, T / gt))));
     s << "  for (int q = tid; q < " << (gt * L + T - 1) / T * T << "; q += " << T << ") {\n    const int gr = q / " << L << ", l = q % " << L << ";\n    float t_ = 0.0f;\n";
     s << "    if (gr < " << gt << ")\n#pragma unroll 4\n      for (int k = l; k < " << K << "; k += " << L << ") t_ += chan[" << base << " + gr * " << K << " + k];\n";
     if (L > 1) s << "    t_ = group_sum<" << L << ">(t_);\n";
-    s << "    if (l == 0 && gr < " << gt << ") grp[gr] = t_;\n  }\n  __syncthreads();\n";
+    s << "    if (l == 0 && gr < " << gt << ") grp[" << at << " + gr] = t_;\n  }\n";
   }
   // Sums over positions of pass `k` are in chan: they and what follows from
   // them become per-channel values.
   void after_pass(int k, const std::vector<int>& sums) {
+    const int64_t gt = CT / K;
+    std::vector<int> left, direct;
+    for (int v : ki.k.prims)
+      if (std::find(r3.begin(), r3.end(), v) != r3.end() && gen.at(v) == k)
+        (std::find(sums.begin(), sums.end(), nd(v).in[0]) != sums.end() ? direct : left).push_back(v);
+    auto take = [&](const std::vector<int>& vs, const std::string& scale) {
+      s << "  __syncthreads();\n";
+      for (size_t i = 0; i < vs.size(); ++i) {
+        const int v = vs[i];
+        s << jdecl("n" + id(v)) << each("n" + id(v) + "[j][e] = grp[" + std::to_string(i * gt) + " + (c0[j] - ct0 + e) / " + std::to_string(K) + "]" +
+                                        (nd(v).op == KORCH_REDUCE_MEAN ? " / " + flit((double)K) : std::string()) + scale + ";");
+        inv_done.insert(v);
+      }
+    };
+    // sums over groups of the sums themselves, as they lie
+    for (size_t i = 0; i < direct.size(); ++i)
+      group_sums((std::find(sums.begin(), sums.end(), nd(direct[i]).in[0]) - sums.begin()) * CT4(), i * gt);
     for (size_t i = 0; i < sums.size(); ++i) {
       const int v = sums[i];
       s << jdecl("n" + id(v)) << each("n" + id(v) + "[j][e] = chan[" + std::to_string(i * CT4()) + " + c0[j] - ct0 + e]" +
                                       (nd(v).op == KORCH_REDUCE_MEAN ? " / " + flit((double)P) : std::string()) + ";");
       inv_done.insert(v);
     }
-    for (int v : ki.k.prims)
-      if (std::find(r3.begin(), r3.end(), v) != r3.end() && gen.at(v) == k) {
-        const std::string x = inv(nd(v).in[0]);
-        s << "  __syncthreads();\n" << each("if (" + std::string(NJ > 1 ? "act[j]" : "act") + " && ly == 0) chan[c0[j] - ct0 + e] = " + x + ";") << "  __syncthreads();\n";
-        group_sums(0);
-        s << jdecl("n" + id(v)) << each("n" + id(v) + "[j][e] = grp[(c0[j] - ct0 + e) / " + std::to_string(K) + "]" +
-                                        (nd(v).op == KORCH_REDUCE_MEAN ? " / " + flit((double)K) : std::string()) + ";");
-        inv_done.insert(v);
-      }
+    if (!direct.empty()) take(direct, nd(nd(direct[0]).in[0]).op == KORCH_REDUCE_MEAN ? " / " + flit((double)P) : std::string());
+    // of values that follow from them, as many together as do not wait for each other
+    std::function<bool(int)> ready = [&](int v) {
+      if (!in(v)) return true;
+      v = rt(v);
+      if (inv_done.count(v)) return true;
+      if (op_kind(nd(v).op) == korch::Kind::Reduce) return false;
+      for (int u : nd(v).in)
+        if (!ready(u)) return false;
+      return true;
+    };
+    while (!left.empty()) {
+      std::vector<int> now, later;
+      for (int v : left) (ready(nd(v).in[0]) ? now : later).push_back(v);
+      if (now.empty()) bad("sums over groups that wait for each other");
+      std::vector<std::string> x;
+      for (int v : now) x.push_back(inv(nd(v).in[0]));
+      s << "  __syncthreads();\n";
+      for (size_t i = 0; i < now.size(); ++i)
+        s << each("if (" + std::string(NJ > 1 ? "act[j]" : "act") + " && ly == 0) chan[" + std::to_string(i * CT4()) + " + c0[j] - ct0 + e] = " + x[i] + ";");
+      s << "  __syncthreads();\n";
+      for (size_t i = 0; i < now.size(); ++i) group_sums(i * CT4(), i * gt);
+      take(now, "");
+      left = later;
+    }
     s << "  __syncthreads();\n";
   }
   // Per-channel and per-group outputs, by the first row of lanes.
@@ -569,12 +625,12 @@ struct GroupGen {
 
   // Hands `rowf` floats of chan (a multiple of four) from workgroup to
   // workgroup: `units` of them make a set; the last to arrive has their sum in
-  // chan and goes on, the others end.  Past 32 units in two levels, groups of
+  // chan and goes on, the others end.  Past 64 units in two levels, groups of
   // 16 first.  `merge` joins partial rows m of the array at row `from` instead
   // of adding them.
-  void hand_over(int64_t sets, const std::string& set, int64_t units, const std::string& unit, int64_t rowf,
+  void hand_over(int64_t sets, const std::string& set, int64_t units, const std::string& unit, int64_t rowf, int64_t one,
                  const std::function<void(const std::string& from, const std::string& m, int64_t maxm, int level)>& merge) {
-    const int64_t GS = units <= 32 ? units : kHandOver, NG = (units + GS - 1) / GS;
+    const int64_t GS = units <= one ? units : kHandOver, NG = (units + GS - 1) / GS;
     const int64_t rows = units + (NG > 1 ? NG : 0);
     ArgRef a;
     a.kind = ArgRef::Scratch;
@@ -621,23 +677,25 @@ struct GroupGen {
   // LDS that adding the partial rows of `units` workgroups takes (floats).
   int64_t slice_floats(int64_t rowf, int64_t units) const {
     int64_t most = 0;
-    for (int64_t m : {units <= 32 ? units : kHandOver, units <= 32 ? (int64_t)1 : (units + kHandOver - 1) / kHandOver}) {
+    for (int64_t m : {units <= kOneLevel ? units : kHandOver, units <= kOneLevel ? (int64_t)1 : (units + kHandOver - 1) / kHandOver}) {
       const int64_t z = slices(rowf, m);
       if (z > 1) most = std::max(most, z * rowf);
     }
     return most;
   }
   // Adds partial rows in order: a thread per 16-byte vector and slice of the
-  // rows, all loads of a thread in flight together, then the slices.
+  // rows, up to sixteen loads of a thread in flight together, then the slices.
   void add_rows(int64_t rowf, const std::string& from, const std::string& m, int64_t maxm) {
     const int64_t CQ = rowf / 4, ZS = slices(rowf, maxm);
     const int64_t per = (maxm + ZS - 1) / ZS, step = std::min<int64_t>(CQ, T / ZS);
     s << "  {\n    const __amdgpu_buffer_rsrc_t r_ = __builtin_amdgcn_make_buffer_rsrc(hand + (i64)(" << from << ") * " << rowf << ", 0, 0x7fffffff, 0x00020000);\n"
       << "    const int m_ = " << m << ", zs = tid / " << step << ";\n";
-    s << "    if (zs < " << ZS << ")\n      for (int v = tid % " << step << "; v < " << CQ << "; v += " << step << ") {\n        float4 q_[" << per
-      << "];\n#pragma unroll\n        for (int z = 0; z < " << per << "; ++z) {\n          const int zz = zs * " << per << " + z;\n          q_[z] = coherent_load4(r_, (unsigned)((zz < m_ ? zz : m_ - 1) * "
-      << rowf * 4 << " + v * 16));\n        }\n        f32x4 t_ = {};\n#pragma unroll\n        for (int z = 0; z < " << per << "; ++z)\n          if (zs * " << per
-      << " + z < m_) t_ += f32x4{q_[z].x, q_[z].y, q_[z].z, q_[z].w};\n";
+    const int64_t RD = std::min<int64_t>(per, 16);
+    s << "    if (zs < " << ZS << ")\n      for (int v = tid % " << step << "; v < " << CQ << "; v += " << step << ") {\n        f32x4 t_ = {};\n";
+    s << (per > RD ? "#pragma unroll 1\n" : "") << "        for (int z0 = 0; z0 < " << per << "; z0 += " << RD << ") {\n          float4 q_[" << RD << "];\n#pragma unroll\n          for (int z = 0; z < " << RD
+      << "; ++z) {\n            const int zz = zs * " << per << " + z0 + z;\n            q_[z] = coherent_load4(r_, (unsigned)((zz < m_ ? zz : m_ - 1) * " << rowf * 4
+      << " + v * 16));\n          }\n#pragma unroll\n          for (int z = 0; z < " << RD << "; ++z)\n            if (zs * " << per << " + z0 + z < m_" << (per % RD ? " && z0 + z < " + std::to_string(per) : std::string())
+      << ") t_ += f32x4{q_[z].x, q_[z].y, q_[z].z, q_[z].w};\n        }\n";
     if (ZS == 1) {
       s << "        *(f32x4*)(chan + v * 4) = t_;\n      }\n  }\n";
       return;
@@ -650,7 +708,7 @@ struct GroupGen {
   void head(int64_t lds_red, int64_t lds_part, int64_t lds_chan) {
     if (lds_red) s << "  __shared__ __attribute__((aligned(16))) float red[" << lds_red << "];\n";
     if (lds_part) s << "  __shared__ float part[" << lds_part << "];\n";
-    if (lds_chan) s << "  __shared__ __attribute__((aligned(16))) float chan[" << lds_chan << "];\n  __shared__ float grp[" << CT / K << "];\n";
+    if (lds_chan) s << "  __shared__ __attribute__((aligned(16))) float chan[" << lds_chan << "];\n  __shared__ float grp[" << std::max<int64_t>(1, r3.size()) * (CT / K) << "];\n";
     s << "  const int tid = threadIdx.x;\n";
     if (NJ == 1) {
       s << "  const int ly = tid / " << CVT << ";\n  const bool act = ly < " << LY << ";\n";
@@ -689,6 +747,13 @@ struct GroupGen {
     for (int v : targets) walk(v);
   }
 
+  // A thread's rows of its workgroup's part in batches, the first of which is loaded already.
+  std::string stream(const std::string& work) const {
+    std::ostringstream o;
+    o << "  while (row0 < lim) {\n" << work << "    row0 += " << (int64_t)U * LY << ";\n    if (row0 >= lim) break;\n" << raw_load("row0", "p1") << "  }\n";
+    return o.str();
+  }
+
   // One pass's accumulation: `sums` over the rows in registers.
   std::string accumulate(const std::vector<int>& sums) {
     Body b;
@@ -717,7 +782,7 @@ struct GroupGen {
     const int64_t rowf = (int64_t)r0.size() * CT4();
     const int64_t red = std::max(red_floats((int)widest), r0.empty() || B == 1 ? 0 : slice_floats(rowf, B));
     s << "  const int b = blockIdx.x / " << tiles << ", ct0 = (int)(blockIdx.x % " << tiles << ") * " << CT << ";\n";
-    head(red, part_floats((int)widest), std::max<int64_t>(widest, r0.size()) * CT4());
+    head(red, part_floats((int)widest), std::max<int64_t>({(int64_t)widest, (int64_t)r0.size(), (int64_t)r3.size()}) * CT4());
     s << raw_decl() << "  const int row0 = " << first_row() << ";\n  {\n" << raw_load("row0", std::to_string(P)) << "  }\n";
     const std::string end = NJ == 1 ? "(act ? " + std::to_string(P) + " : 0)" : std::to_string(P);
     for (int k = 0; k < npass; ++k) {
@@ -757,7 +822,7 @@ struct GroupGen {
       }
       s << "  __syncthreads();\n";
       if (B > 1)
-        hand_over(tiles, "blockIdx.x % " + std::to_string(tiles), B, "b", rowf,
+        hand_over(tiles, "blockIdx.x % " + std::to_string(tiles), B, "b", rowf, kOneLevel,
                   [&](const std::string& from, const std::string& m, int64_t maxm, int) { add_rows(rowf, from, m, maxm); });
       store_r0("chan", "ct0");
     }
@@ -777,9 +842,11 @@ struct GroupGen {
   void gen_sums() {
     const int64_t rowf = (int64_t)r1.size() * CT4();
     s << "  const int b = blockIdx.x / " << S << ", sp = blockIdx.x % " << S << ", ct0 = 0;\n";
-    head(std::max(red_floats((int)r1.size()), S > 1 ? slice_floats(rowf, S) : 0), part_floats((int)r1.size()), rowf);
+    head(std::max(red_floats((int)r1.size()), S > 1 ? slice_floats(rowf, S) : 0), part_floats((int)r1.size()), std::max<int64_t>(rowf, r3.size() * CT4()));
     std::vector<int> targets;
     for (int v : r1) targets.push_back(nd(v).in[0]);
+    s << raw_decl() << "  const int p1 = (sp + 1) * " << chunk << " < " << P << " ? (sp + 1) * " << chunk << " : " << P << ", lim = " << (NJ == 1 ? "act ? p1 : 0" : "p1") << ";\n";
+    s << "  int row0 = sp * " << chunk << " + " << first_row() << ";\n" << raw_load("row0", "p1");
     load_invariants(targets);
     set_fast_math(fast_full());
     const std::string body = accumulate(r1);
@@ -789,16 +856,14 @@ struct GroupGen {
       s << "  float a" << id(v) << "[" << NJ << "][" << VEC << "] = {};\n";
       acc.push_back("a" + id(v));
     }
-    s << raw_decl() << "  const int p1 = (sp + 1) * " << chunk << " < " << P << " ? (sp + 1) * " << chunk << " : " << P << ", lim = " << (NJ == 1 ? "act ? p1 : 0" : "p1") << ";\n";
-    s << "  for (int row0 = sp * " << chunk << " + " << first_row() << "; row0 < p1; row0 += " << (int64_t)U * LY << ") {\n" << raw_load("row0", "p1")
-      << row_loop("row0", "lim", body, "") << "  }\n";
+    s << stream(row_loop("row0", "lim", body, ""));
     channel_sums(acc);
     if (CT4() > CT) {
       for (size_t i = 0; i < r1.size(); ++i) s << "  if (tid < " << CT4() - CT << ") chan[" << i * CT4() + CT << " + tid] = 0.0f;\n";
       s << "  __syncthreads();\n";
     }
     if (S > 1)
-      hand_over(B, "b", S, "sp", rowf, [&](const std::string& from, const std::string& m, int64_t maxm, int) { add_rows(rowf, from, m, maxm); });
+      hand_over(B, "b", S, "sp", rowf, kOneLevel, [&](const std::string& from, const std::string& m, int64_t maxm, int) { add_rows(rowf, from, m, maxm); });
     after_pass(1, r1);
     store_inv(true);
     gk.grid[0] = (int)(B * S);
@@ -809,33 +874,38 @@ struct GroupGen {
     s << "  const int b = blockIdx.x / " << S << ", sp = blockIdx.x % " << S << ", ct0 = 0;\n";
     head(red_floats(1), part_floats(1), std::max(CT4(), rowf));
     s << "  __shared__ float gmean[" << G << "];\n";
-    s << raw_decl() << "  const int p1 = (sp + 1) * " << chunk << " < " << P << " ? (sp + 1) * " << chunk << " : " << P << ";\n";
+    s << raw_decl() << "  const int p1 = (sp + 1) * " << chunk << " < " << P << " ? (sp + 1) * " << chunk << " : " << P << ", lim = " << (NJ == 1 ? "act ? p1 : 0" : "p1") << ";\n";
+    s << "  int row0 = sp * " << chunk << " + " << first_row() << ";\n" << raw_load("row0", "p1");
     s << "  float mean[" << NJ << "][" << VEC << "] = {}, m2[" << NJ << "][" << VEC << "] = {}, cnt_ = 0.0f;\n";
     const std::string x = "tof(x" + id(mo_x) + "[i][j]" + (VEC > 1 ? "[e]" : "") + ")";
-    s << "  for (int row0 = sp * " << chunk << " + " << first_row() << "; row0 < " << (NJ == 1 ? "(act ? p1 : 0)" : "p1") << "; row0 += " << (int64_t)U * LY << ") {\n"
-      << raw_load("row0", "p1");
-    s << "    const int left = (p1 - row0 + " << LY - 1 << ") / " << LY << ";\n    const float n = (float)(left < " << U << " ? left : " << U
+    std::ostringstream o;
+    o << "    const int left = (p1 - row0 + " << LY - 1 << ") / " << LY << ";\n    const float n = (float)(left < " << U << " ? left : " << U
       << "), nn = cnt_ + n, w = n / nn, w2 = cnt_ * w, ni = 1.0f / n;\n    cnt_ = nn;\n";
-    s << "#pragma unroll\n    for (int j = 0; j < " << NJ << "; ++j)\n#pragma unroll\n      for (int e = 0; e < " << VEC << "; ++e) {\n        float t = 0.0f, q = 0.0f;\n";
-    s << "        if (left >= " << U << ") {\n#pragma unroll\n          for (int i = 0; i < " << U << "; ++i) t += " << x << ";\n          t *= " << flit(1.0 / U)
-      << ";\n#pragma unroll\n          for (int i = 0; i < " << U << "; ++i) { const float d = " << x << " - t; q = __builtin_fmaf(d, d, q); }\n        } else {\n";
-    s << "#pragma unroll\n          for (int i = 0; i < " << U << "; ++i) t += i < left ? " << x << " : 0.0f;\n          t *= ni;\n#pragma unroll\n          for (int i = 0; i < " << U
-      << "; ++i) { const float d = i < left ? " << x << " - t : 0.0f; q = __builtin_fmaf(d, d, q); }\n        }\n";
-    s << "        const float d = t - mean[j][e];\n        mean[j][e] = __builtin_fmaf(d, w, mean[j][e]);\n        m2[j][e] += __builtin_fmaf(d * w2, d, q);\n      }\n  }\n";
+    o << "#pragma unroll\n    for (int j = 0; j < " << NJ << "; ++j)\n#pragma unroll\n      for (int e = 0; e < " << VEC << "; ++e) {\n        float t = 0.0f, q = 0.0f;\n";
+    // (whole batches without the selects where there are many: 22.4 us with them at 4x416x416x64 f16)
+    if (U == 8)
+      o << "        if (left >= " << U << ") {\n#pragma unroll\n          for (int i = 0; i < " << U << "; ++i) t += " << x << ";\n          t *= " << flit(1.0 / U) << ";\n#pragma unroll\n          for (int i = 0; i < "
+        << U << "; ++i) { const float d = " << x << " - t; q = __builtin_fmaf(d, d, q); }\n        } else {\n";
+    o << "#pragma unroll\n        for (int i = 0; i < " << U << "; ++i) t += i < left ? " << x << " : 0.0f;\n        t *= ni;\n#pragma unroll\n        for (int i = 0; i < " << U
+      << "; ++i) { const float d = i < left ? " << x << " - t : 0.0f; q = __builtin_fmaf(d, d, q); }\n" << (U == 8 ? "        }\n" : "");
+    o << "        const float d = t - mean[j][e];\n        mean[j][e] = __builtin_fmaf(d, w, mean[j][e]);\n        m2[j][e] += __builtin_fmaf(d * w2, d, q);\n      }\n";
+    s << stream(o.str());
     // the workgroup's group means, then its sums of centred squares about them
     s << "  float nm[" << NJ << "][" << VEC << "];\n" << each("nm[j][e] = cnt_ * mean[j][e];");
     channel_sums({"nm"});
     group_sums(0);
-    s << "  const float rows_ = (float)(p1 - sp * " << chunk << ");\n  for (int q = tid; q < " << G << "; q += " << T << ") gmean[q] = grp[q] / (rows_ * " << flit((double)K)
+    s << "  __syncthreads();\n  const float rows_ = (float)(p1 - sp * " << chunk << ");\n  for (int q = tid; q < " << G << "; q += " << T << ") gmean[q] = grp[q] / (rows_ * " << flit((double)K)
       << ");\n  __syncthreads();\n";
     s << each("const float d = mean[j][e] - gmean[(c0[j] + e) / " + std::to_string(K) + "]; nm[j][e] = __builtin_fmaf(cnt_ * d, d, m2[j][e]);");
     channel_sums({"nm"});
     group_sums(0);
-    s << "  for (int q = tid; q < " << G4 << "; q += " << T << ") {\n    chan[q] = q < " << G << " ? gmean[q] : 0.0f;\n    chan[" << G4 << " + q] = q < " << G
+    s << "  __syncthreads();\n  for (int q = tid; q < " << G4 << "; q += " << T << ") {\n    chan[q] = q < " << G << " ? gmean[q] : 0.0f;\n    chan[" << G4 << " + q] = q < " << G
       << " ? grp[q] : 0.0f;\n  }\n  __syncthreads();\n";
     if (S > 1) {
-      const int64_t GS = S <= 32 ? S : kHandOver;
-      hand_over(B, "b", S, "sp", rowf, [&](const std::string& from, const std::string& m, int64_t maxm, int level) {
+      // (sixteen means and squares of a lane in flight, 32 where a lane has a group to itself)
+      const int64_t one = std::max<int64_t>(32, std::min(kOneLevel, 16 * std::min<int64_t>(16, pow2floor(std::max<int64_t>(1, T / G)))));
+      const int64_t GS = S <= one ? S : kHandOver;
+      hand_over(B, "b", S, "sp", rowf, one, [&](const std::string& from, const std::string& m, int64_t maxm, int level) {
         // rows (positions) of partial z: a split's, or those of a whole group of splits
         const int64_t per = level == 2 ? chunk * GS : chunk;
         const std::string first = level == 1 ? "(" + from + " + z)" : "z";
