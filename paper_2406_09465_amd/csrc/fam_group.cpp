@@ -308,8 +308,9 @@ struct GroupGen {
     return B * tiles * T < ((int64_t)1 << 32);
   }
 
-  void stream_geometry(int threads) {
-    CT = C;
+  void stream_geometry(int threads, int64_t channels) {
+    CT = channels;
+    tiles = C / CT;
     VEC = 16 / eb;
     while (CT % VEC) VEC /= 2;
     while (threads < 1024 && CT / VEC > threads) threads *= 2;
@@ -332,7 +333,7 @@ struct GroupGen {
       if (npass > 0 && std::find(r1.begin(), r1.end(), nd(v).in[0]) == r1.end()) bad("a sum over images of computed values");
     if (npass == 0) {
       kind = Apply;
-      stream_geometry(256);
+      stream_geometry(256, C);
       // about eight workgroups to a compute unit, a thread's rows in whole
       // batches, so that the channels' values are loaded for several rows
       const int64_t want = std::max<int64_t>(1, ((double)B * P * C * eb >= 67108864.0 ? 4096 : 2048) / B);
@@ -354,20 +355,31 @@ struct GroupGen {
       kind = Sums;
     else
       bad("sums that depend on sums over the same positions");
-    stream_geometry(512);
+    // The sums of few wide maps are split into tiles of whole groups (runs of two
+    // cache lines or more) as well: a tile's partial sums are a fraction of the channels', and
+    // the tiles' last workgroups add theirs side by side.  It pays past 128 KiB of
+    // partial sums per image (1x64x64x320 bf16, the gradient's sums: 9.1 us, 10.4 without;
+    // 4x32x32x320, 107 KiB: 8.7 and 7.6).
+    stream_geometry(512, C);
+    int64_t tile = C;
+    if (kind == Sums && (double)B * P * C * eb * xfull.size() <= 16777216.0 &&
+        std::min<int64_t>(kOneLevel, P / ((int64_t)LY * 2)) * (int64_t)r1.size() * C * 4 > 131072)
+      for (int64_t gt = G; gt >= 1; --gt)
+        if (G % gt == 0 && gt * K * eb >= 128 && B * (G / gt) <= 32) tile = gt * K;
+    stream_geometry(512, tile);
     // A workgroup of eight waves to a compute unit, each thread with a batch of
     // rows at least; batches of few rows, as a workgroup of few rows runs its code
     // once and waits for its instructions (batches of 8 and 4, one set loading
     // while the other is summed: 13.9 us instead of 11.0 for the gradient's sums of
     // 8x32x32x640 bf16, 41.6 instead of 34.7 at 4x416x416x64 f16).
     U = kind == Moments ? P * B >= (int64_t)256 * LY * 32 ? 8 : 4 : 2;
-    S = std::max<int64_t>(1, std::min<int64_t>((256 + B - 1) / B, P / ((int64_t)LY * U)));
+    S = std::max<int64_t>(1, std::min<int64_t>((256 + B * tiles - 1) / (B * tiles), P / ((int64_t)LY * U * (tiles > 1 ? 2 : 1))));
     // one level of hand-over as long as a thread's rows stay few
     if (S > kOneLevel && P <= kOneLevel * LY * 16) S = kOneLevel;
     chunk = (P + S - 1) / S;
     chunk = (chunk + LY - 1) / LY * LY;
     S = (P + chunk - 1) / chunk;
-    if (B * S * T >= ((int64_t)1 << 32)) bad("more threads than a launch holds");
+    if (B * tiles * S * T >= ((int64_t)1 << 32)) bad("more threads than a launch holds");
   }
 
   // ---- code ------------------------------------------------------------------
@@ -494,11 +506,21 @@ struct GroupGen {
     o << "#pragma unroll\n        for (int e = 0; e < " << VEC << "; ++e) {\n" << elem << "        }\n" << after_j << "      }\n    }\n";
     return o.str();
   }
+  // Maps past half of the 256 MiB that the device's last cache holds go by it:
+  // their reader would not find them there, and what the next kernel reads again
+  // stays (32x128x128x256 bf16 trained 366 us, 405 through the cache; 8x64x64x320 44.5 and 43.9).
+  bool stream_out() const {
+    double bytes = 0;
+    for (int v : full_outs) bytes += (double)numel(nd(v).shape) * dtype_bytes(nd(v).dtype);
+    return bytes >= 134217728.0;
+  }
   std::string store_rows() const {
     std::ostringstream o;
-    for (int v : full_outs)
-      o << "        if (live && act" << (NJ > 1 ? "[j]" : "") << ") " << out_store(g, v, outp(v), "((i64)b * " + std::to_string(P) + " + row) * " + std::to_string(C) + " + c0[j]", VEC, "o" + id(v))
-        << ";\n";
+    for (int v : full_outs) {
+      const std::string at = "((i64)b * " + std::to_string(P) + " + row) * " + std::to_string(C) + " + c0[j]";
+      o << "        if (live && act" << (NJ > 1 ? "[j]" : "") << ") "
+        << (stream_out() ? "st_stream<" + std::to_string(VEC) + ">(" + outp(v) + " + " + at + ", o" + id(v) + ")" : out_store(g, v, outp(v), at, VEC, "o" + id(v))) << ";\n";
+    }
     return o.str();
   }
 
@@ -841,7 +863,7 @@ struct GroupGen {
 
   void gen_sums() {
     const int64_t rowf = (int64_t)r1.size() * CT4();
-    s << "  const int b = blockIdx.x / " << S << ", sp = blockIdx.x % " << S << ", ct0 = 0;\n";
+    s << "  const int set = blockIdx.x / " << S << ", sp = blockIdx.x % " << S << ", b = set / " << tiles << ", ct0 = (set % " << tiles << ") * " << CT << ";\n";
     head(std::max(red_floats((int)r1.size()), S > 1 ? slice_floats(rowf, S) : 0), part_floats((int)r1.size()), std::max<int64_t>(rowf, r3.size() * CT4()));
     std::vector<int> targets;
     for (int v : r1) targets.push_back(nd(v).in[0]);
@@ -863,15 +885,15 @@ struct GroupGen {
       s << "  __syncthreads();\n";
     }
     if (S > 1)
-      hand_over(B, "b", S, "sp", rowf, kOneLevel, [&](const std::string& from, const std::string& m, int64_t maxm, int) { add_rows(rowf, from, m, maxm); });
+      hand_over(B * tiles, "set", S, "sp", rowf, kOneLevel, [&](const std::string& from, const std::string& m, int64_t maxm, int) { add_rows(rowf, from, m, maxm); });
     after_pass(1, r1);
     store_inv(true);
-    gk.grid[0] = (int)(B * S);
+    gk.grid[0] = (int)(B * tiles * S);
   }
 
   void gen_moments() {
-    const int64_t G4 = (G + 3) / 4 * 4, rowf = 2 * G4;
-    s << "  const int b = blockIdx.x / " << S << ", sp = blockIdx.x % " << S << ", ct0 = 0;\n";
+    const int64_t G = CT / K, G4 = (G + 3) / 4 * 4, rowf = 2 * G4;  // of the tile
+    s << "  const int set = blockIdx.x / " << S << ", sp = blockIdx.x % " << S << ", b = set / " << tiles << ", ct0 = (set % " << tiles << ") * " << CT << ";\n";
     head(red_floats(1), part_floats(1), std::max(CT4(), rowf));
     s << "  __shared__ float gmean[" << G << "];\n";
     s << raw_decl() << "  const int p1 = (sp + 1) * " << chunk << " < " << P << " ? (sp + 1) * " << chunk << " : " << P << ", lim = " << (NJ == 1 ? "act ? p1 : 0" : "p1") << ";\n";
@@ -896,7 +918,7 @@ struct GroupGen {
     group_sums(0);
     s << "  __syncthreads();\n  const float rows_ = (float)(p1 - sp * " << chunk << ");\n  for (int q = tid; q < " << G << "; q += " << T << ") gmean[q] = grp[q] / (rows_ * " << flit((double)K)
       << ");\n  __syncthreads();\n";
-    s << each("const float d = mean[j][e] - gmean[(c0[j] + e) / " + std::to_string(K) + "]; nm[j][e] = __builtin_fmaf(cnt_ * d, d, m2[j][e]);");
+    s << each("const float d = mean[j][e] - gmean[(c0[j] - ct0 + e) / " + std::to_string(K) + "]; nm[j][e] = __builtin_fmaf(cnt_ * d, d, m2[j][e]);");
     channel_sums({"nm"});
     group_sums(0);
     s << "  __syncthreads();\n  for (int q = tid; q < " << G4 << "; q += " << T << ") {\n    chan[q] = q < " << G << " ? gmean[q] : 0.0f;\n    chan[" << G4 << " + q] = q < " << G
@@ -905,7 +927,7 @@ struct GroupGen {
       // (sixteen means and squares of a lane in flight, 32 where a lane has a group to itself)
       const int64_t one = std::max<int64_t>(32, std::min(kOneLevel, 16 * std::min<int64_t>(16, pow2floor(std::max<int64_t>(1, T / G)))));
       const int64_t GS = S <= one ? S : kHandOver;
-      hand_over(B, "b", S, "sp", rowf, one, [&](const std::string& from, const std::string& m, int64_t maxm, int level) {
+      hand_over(B * tiles, "set", S, "sp", rowf, one, [&](const std::string& from, const std::string& m, int64_t maxm, int level) {
         // rows (positions) of partial z: a split's, or those of a whole group of splits
         const int64_t per = level == 2 ? chunk * GS : chunk;
         const std::string first = level == 1 ? "(" + from + " + z)" : "z";
@@ -927,12 +949,12 @@ struct GroupGen {
       });
     }
     for (int v : {mo_mu, mo_var}) {
-      s << jdecl("n" + id(v)) << each("n" + id(v) + "[j][e] = chan[" + (v == mo_var ? std::to_string(G4) + " + " : std::string()) + "(c0[j] + e) / " + std::to_string(K) + "]" +
+      s << jdecl("n" + id(v)) << each("n" + id(v) + "[j][e] = chan[" + (v == mo_var ? std::to_string(G4) + " + " : std::string()) + "(c0[j] - ct0 + e) / " + std::to_string(K) + "]" +
                                       (v == mo_var ? " / " + flit((double)P * (double)K) : std::string()) + ";");
       inv_done.insert(v);
     }
     store_inv(true);
-    gk.grid[0] = (int)(B * S);
+    gk.grid[0] = (int)(B * tiles * S);
   }
 
   void gen_apply() {
@@ -979,7 +1001,10 @@ struct GroupGen {
     }
     set_fast_math(was);
     gk.block[0] = T;
-    gk.source = source_header((int)gk.args.size()) + "extern \"C\" __global__ void __launch_bounds__(" + std::to_string(T) + ") " + gk.name + "(KArgs a) {\n" + s.str() + "}\n";
+    const char* const streamed =
+        "template <int V, typename T> __device__ __forceinline__ void st_stream(T* p, const float* s) {\n  vec_t<V, T> v;\n  if constexpr (V == 1) {\n    v = fromf<T>(s[0]);\n  } else {\n"
+        "#pragma unroll\n    for (int i = 0; i < V; ++i) v[i] = fromf<T>(s[i]);\n  }\n  __builtin_nontemporal_store(v, (vec_t<V, T>*)p);\n}\n";
+    gk.source = source_header((int)gk.args.size()) + (stream_out() ? streamed : "") + "extern \"C\" __global__ void __launch_bounds__(" + std::to_string(T) + ") " + gk.name + "(KArgs a) {\n" + s.str() + "}\n";
     ki.fill_cost(gk);
     return gk;
   }

@@ -189,8 +189,14 @@ struct MultiGen {
     s << "template <typename T> __device__ __forceinline__ void chunk_" << (scale ? "(const T* x, T* y, i64 left, float f)" : "(const T* x, i64 left, double& sum)")
       << " {\n  constexpr int V = 16 / (int)sizeof(T);\n  typedef vec_t<V, T> VT;\n  const int tid = threadIdx.x;\n";
     s << "  if (left >= " << kT * kV << " * V) {\n    VT q[" << kV << "];\n#pragma unroll\n    for (int i = 0; i < " << kV << "; ++i) q[i] = *(const VT*)(x + ((i * " << kT << " + tid) * V));\n";
+    // Results past half of the 256 MiB that the device's last cache holds go by it:
+    // their reader would not find them there, and the gradients that the norm's
+    // kernel has just read stay (204 M bf16 gradients: norm and product 208 us, 233 through the cache).
+    double written = 0;
+    for (int o : out_) written += (double)numel(nd(o).shape) * dtype_bytes(nd(o).dtype);
+    const bool stream = written > 134217728.0;
     auto one = [&](const std::string& q, const std::string& at) {
-      if (scale) return "VT r_;\n#pragma unroll\n      for (int e = 0; e < V; ++e) r_[e] = fromf<T>(tof(" + q + "[e]) * f);\n      *(VT*)(y + " + at + ") = r_;\n";
+      if (scale) return "VT r_;\n#pragma unroll\n      for (int e = 0; e < V; ++e) r_[e] = fromf<T>(tof(" + q + "[e]) * f);\n      " + (stream ? "__builtin_nontemporal_store(r_, (VT*)(y + " + at + "));\n" : "*(VT*)(y + " + at + ") = r_;\n");
       return "#pragma unroll\n      for (int e = 0; e < V; ++e) { const double d = (double)tof(" + q + "[e]); sum = __builtin_fma(d, d, sum); }\n";
     };
     s << "#pragma unroll\n    for (int i = 0; i < " << kV << "; ++i) {\n      " << one("q[i]", "((i * " + id(kT) + " + tid) * V)") << "    }\n    return;\n  }\n";
