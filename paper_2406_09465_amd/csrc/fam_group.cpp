@@ -158,7 +158,7 @@ struct GroupGen {
           npass = std::max(npass, gen[v]);
         } else if (n.axis == 3) {
           if (full_of(u) || nd(u).shape != Shape{B, 1, G, K}) bad("a sum over a group's channels of something else than sums over positions");
-          if (!in(u)) bad("a sum over a group's channels of a stored tensor");
+          if (gen_of(u) == 0) bad("a sum over a group's channels of stored values");
           r3.push_back(v);
           gen[v] = gen_of(u);
         } else if (n.axis == 0) {
@@ -303,7 +303,8 @@ struct GroupGen {
     U = NR;
     if (!r0.empty()) {
       // the sums over images are handed over
-      if (B > kHandOver * 32 || B * tiles * ((int64_t)r0.size() * ((CT + 3) / 4 * 4)) * 4 * 17 / 16 > ((int64_t)16 << 20)) return false;
+      const int64_t lines = B <= kOneLevel ? 1 : (B + kHandOver - 1) / kHandOver + 1;  // counters of a tile (allocation-free execution has 64 KiB of them)
+      if (B > kHandOver * 32 || tiles * lines > 256 || B * tiles * ((int64_t)r0.size() * ((CT + 3) / 4 * 4)) * 4 * 17 / 16 > ((int64_t)16 << 20)) return false;
     }
     return B * tiles * T < ((int64_t)1 << 32);
   }
@@ -328,7 +329,6 @@ struct GroupGen {
       if (npass == 0 ? in(nd(v).in[0]) : !in(nd(v).in[0])) bad("a sum over images beside other sums");
     if (npass == 0 && !inv_outs.empty()) bad("an output per channel without a sum");
     if (npass == 0 && full_outs.empty()) bad("no map among the outputs");
-    if (npass == 0 && !r3.empty()) bad("a sum over a group's channels of a stored tensor");
     for (int v : r0)
       if (npass > 0 && std::find(r1.begin(), r1.end(), nd(v).in[0]) == r1.end()) bad("a sum over images of computed values");
     if (npass == 0) {
@@ -958,16 +958,18 @@ struct GroupGen {
   }
 
   void gen_apply() {
-    const int64_t nblk = r0.empty() ? 0 : (C + 63) / 64;
+    const int64_t nblk = r0.empty() ? 0 : (C + 15) / 16;
     if (nblk) {
-      // sums over the images: 64 channels to a workgroup, the images over its waves
+      // sums over the images: 16 channels to a workgroup (a cache line of an
+      // image's), the images over its groups of 16 lanes, sixteen in flight
+      const int GR = T / 16;
       s << "  if (blockIdx.x >= " << B * S << ") {\n    __shared__ float sum_[" << T << "];\n    const int t_ = threadIdx.x, c = (int)(blockIdx.x - " << B * S
-        << ") * 64 + (t_ & 63);\n";
+        << ") * 16 + (t_ & 15);\n";
       for (int v : r0) {
         const int u = nd(v).in[0];
-        s << "    {\n      float x_ = 0.0f;\n      if (c < " << C << ")\n#pragma unroll 8\n        for (int i = t_ >> 6; i < " << B << "; i += " << T / 64 << ") x_ += ld1(" << ptr(u)
-          << " + (i64)i * " << C << " + c);\n      sum_[t_] = x_;\n      __syncthreads();\n      if (t_ < 64 && c < " << C << ") {\n#pragma unroll\n        for (int w = 1; w < " << T / 64
-          << "; ++w) x_ += sum_[w * 64 + t_];\n";
+        s << "    {\n      float x_ = 0.0f;\n      if (c < " << C << ")\n#pragma unroll 16\n        for (int i = t_ >> 4; i < " << B << "; i += " << GR << ") x_ += ld1(" << ptr(u)
+          << " + (i64)i * " << C << " + c);\n      sum_[t_] = x_;\n      __syncthreads();\n      if (t_ < 16 && c < " << C << ") {\n#pragma unroll\n        for (int w = 1; w < " << GR
+          << "; ++w) x_ += sum_[w * 16 + t_];\n";
         for (int o : ki.k.outs)
           if (rt(o) == v) s << "        " << out_store(g, o, outp(o), "c", 0, nd(v).op == KORCH_REDUCE_MEAN ? "x_ / " + flit((double)B) : "x_") << ";\n";
         s << "      }\n      __syncthreads();\n    }\n";

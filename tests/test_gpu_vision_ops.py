@@ -48,6 +48,11 @@ GN = [
     ("f16", 1, 2, 1, 8192, 32, "relu"),
     ("f32", 5, 1, 2, 1, 1, "none"),           # one channel, two positions
     ("bf16", 1, 300, 300, 7, 7, "silu"),      # odd channels, split
+    ("bf16", 1, 40, 41, 8192, 64, "silu"),    # the widest
+    ("f32", 1, 70, 3, 8191, 1, "relu"),       # and with no vector
+    ("f16", 700, 3, 3, 32, 4, "silu"),        # more images than slabs hand over
+    ("f16", 300, 2, 2, 2048, 64, "none"),     # more tiles and images than counters
+    ("bf16", 2, 64, 64, 320, 32, "relu"),     # sums by tiles of groups
 ]
 
 
@@ -130,6 +135,46 @@ def test_groupnorm_constant_groups():
     out = _run(graphs.build("groupnorm", **z), s)
     assert np.allclose(out["r"], 1e-5 ** -0.5, rtol=1e-6) and np.all(out["mu"] == 3.0)
     assert np.array_equal(out["Y"], np.broadcast_to(x["beta"], out["Y"].shape))
+
+
+SAMPLED = [("groupnorm", ("f32", 2, 3, 5, 12, 4, "silu"), 3), ("groupnorm", ("f32", 3, 70, 40, 12, 3, "relu"), 3), ("groupnorm", ("f32", 2, 4, 4, 6, 6, "silu"), 2),
+           ("groupnorm_grad", ("f32", 3, 70, 40, 12, 3, "none"), 2), ("groupnorm_grad", ("f32", 2, 3, 5, 12, 4, "none"), 2)]
+
+
+def sampled(name, case, count):
+    """Random valid plans of the graph whose kernels are the new families' and single primitives."""
+    import random
+
+    from paper_2406_09465_amd import search
+    w = graphs.build(name, **_gn_sizes(case))
+    cands = [c for c in w.graph.candidates(max_prims=14, max_outs=2, only_supported=True) if len(c[0]) == 1 or w.graph.family(*c) not in ("pointwise", "none")]
+    view, rng = search.GraphView(w.graph), random.Random(5)
+    # wide kernels first, so that plans are not of single primitives alone
+    wide = [c for c in cands if len(c[0]) > 4]
+    plans = []
+    for _ in range(count):
+        plan = search.random_plan(view, rng.sample(wide, min(len(wide), 60)) + [c for c in cands if len(c[0]) <= 2], rng)
+        made = {o for _, outs in plan for o in outs}
+        plans.append(plan + [([o], [o]) for o in w.graph.outputs() if o not in made])  # (views that are outputs)
+    return w, plans
+
+
+@pytest.mark.parametrize("name,case,count", SAMPLED, ids=str)
+def test_groupnorm_by_sampled_plans(name, case, count):
+    from paper_2406_09465_amd.runner import PlanRunner
+    z = _gn_sizes(case)
+    x, s = _gn_inputs(*case[:5])
+    want = ref.groupnorm(x["X"], x["gamma"], x["beta"], z["groups"], 1e-5, z["act"], z["dtype"], x["dY"])
+    if name == "groupnorm_grad":
+        s.update({k: want[k][0].astype(np.float32) for k in ("mu", "r")})
+    w, plans = sampled(name, case, count)
+    fams = set()
+    for i, ks in enumerate(plans):
+        print(f"\n[case] {name} {case} plan {i}: {len(ks)} kernels", flush=True)
+        r = PlanRunner(w, kernels=ks)
+        fams |= {r.plan.kernel_info(k)[0] for k in range(r.plan.num_kernels())}
+        _check(r.run(s), want, z["dtype"], ("mu", "r"))
+    assert "group" in fams
 
 
 # ---- rotary positions --------------------------------------------------------------

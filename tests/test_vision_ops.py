@@ -179,6 +179,29 @@ def test_look_alikes_are_not_taken():
     assert w.graph.family([w.ids["G0_q"], first], [first]) in ("colreduce", "row", "rowcol")
 
 
+@pytest.mark.parametrize("name,sizes", [
+    ("groupnorm", dict(batch=2, hh=3, ww=5, c=12, groups=4, act="silu")),
+    ("groupnorm", dict(batch=2, hh=1, ww=1, c=12, groups=4, act="none")),
+    ("groupnorm", dict(batch=2, hh=300, ww=5, c=6, groups=6, act="relu")),
+    ("groupnorm_grad", dict(batch=3, hh=3, ww=5, c=12, groups=4, act="none")),
+    ("groupnorm_grad", dict(batch=3, hh=700, ww=9, c=12, groups=4, act="none")),
+    ("grad_clip", dict(shapes=[(5,), (3, 4)])),
+], ids=str)
+def test_every_kernel_that_a_family_takes_is_generated(name, sizes):
+    """What the matchers accept, the generators write, for all convex parts of the graphs."""
+    w = graphs.build(name, dtype="f32", **sizes)
+    taken = 0
+    for prims, outs in w.graph.candidates(max_prims=7, max_outs=2, only_supported=True):
+        if w.graph.family(prims, outs) in ("group", "multi"):
+            assert len(w.graph.kernel_source(prims, outs)) > 1000
+            taken += 1
+    assert taken > 20
+    # a sum over a group's channels of stored sums belongs to no kernel of other sums
+    if name == "groupnorm_grad":
+        ids = [w.ids[k] for k in ("dZx", "sg", "c1_g", "c1_s", "c1")]
+        assert w.graph.family(ids, [w.ids["sg"], w.ids["c1"]]) == "none"
+
+
 # ---- kernels --------------------------------------------------------------------------
 
 
