@@ -580,13 +580,64 @@ struct GroupGen {
     if (L > 1) s << "    t_ = group_sum<" << L << ">(t_);\n";
     s << "    if (l == 0 && gr < " << gt << ") grp[" << at << " + gr] = t_;\n  }\n";
   }
+  // Sums over a tile's groups of the threads' values acc, straight into grp[i * groups ..]:
+  // a thread adds what of a vector lies in one group, a group's lanes the rest.
+  // (The caller waits before and after; by way of the channels' sums it takes
+  // twice the barriers.)
+  int group_piece() const {
+    int sv = VEC;
+    while (K % sv) sv /= 2;
+    return sv;
+  }
+  int64_t direct_floats(int n) const { return (int64_t)n * LY * (CT / group_piece()); }
+  void group_sums_of(const std::vector<std::string>& acc) {
+    const int SV = group_piece();
+    const int64_t gt = CT / K, row = CT / SV, KS = K / SV;
+    for (size_t i = 0; i < acc.size(); ++i) {
+      s << "#pragma unroll\n  for (int j = 0; j < " << NJ << "; ++j)\n    if (" << (NJ > 1 ? "act[j]" : "act") << ")\n#pragma unroll\n      for (int q = 0; q < " << VEC / SV
+        << "; ++q) {\n        float t_ = " << acc[i] << "[j][q * " << SV << "];\n#pragma unroll\n        for (int e = 1; e < " << SV << "; ++e) t_ += " << acc[i] << "[j][q * " << SV
+        << " + e];\n        red[" << i * LY * row << " + ly * " << row << " + (c0[j] - ct0) / " << SV << " + q] = t_;\n      }\n";
+    }
+    s << "  __syncthreads();\n";
+    const int64_t L = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(64, pow2floor(LY * KS)), pow2floor(std::max<int64_t>(1, T / gt))));
+    for (size_t i = 0; i < acc.size(); ++i) {
+      s << "  for (int q = tid; q < " << (gt * L + T - 1) / T * T << "; q += " << T << ") {\n    const int gr = q / " << L << ", l = q % " << L << ";\n    float t_ = 0.0f;\n    if (gr < " << gt
+        << ")\n#pragma unroll 4\n      for (int k = l; k < " << LY * KS << "; k += " << L << ") t_ += red[" << i * LY * row << " + k / " << KS << " * " << row << " + gr * " << KS << " + k % " << KS << "];\n";
+      if (L > 1) s << "    t_ = group_sum<" << L << ">(t_);\n";
+      s << "    if (l == 0 && gr < " << gt << ") grp[" << i * gt << " + gr] = t_;\n  }\n";
+    }
+  }
+  // Sums of pass `k` that only sums over groups read.
+  bool only_groups(const std::vector<int>& sums) const {
+    if (K == 1) return false;
+    for (int v : sums) {
+      for (int c : g.consumers[v])
+        if (in(c) && std::find(r3.begin(), r3.end(), c) == r3.end()) return false;
+      for (int o : ki.k.outs)
+        if (rt(o) == v) return false;
+    }
+    return true;
+  }
+  void after_group_pass(const std::vector<int>& sums) {
+    s << "  __syncthreads();\n";
+    for (size_t i = 0; i < sums.size(); ++i)
+      for (int v : r3)
+        if (nd(v).in[0] == sums[i]) {
+          s << jdecl("n" + id(v)) << each("n" + id(v) + "[j][e] = grp[" + std::to_string(i * (CT / K)) + " + (c0[j] - ct0 + e) / " + std::to_string(K) + "]" +
+                                          (nd(v).op == KORCH_REDUCE_MEAN ? " / " + flit((double)K) : std::string()) +
+                                          (nd(sums[i]).op == KORCH_REDUCE_MEAN ? " / " + flit((double)P) : std::string()) + ";");
+          inv_done.insert(v);
+        }
+    s << "  __syncthreads();\n";
+  }
+
   // Sums over positions of pass `k` are in chan: they and what follows from
   // them become per-channel values.
   void after_pass(int k, const std::vector<int>& sums) {
     const int64_t gt = CT / K;
     std::vector<int> left, direct;
     for (int v : ki.k.prims)
-      if (std::find(r3.begin(), r3.end(), v) != r3.end() && gen.at(v) == k)
+      if (std::find(r3.begin(), r3.end(), v) != r3.end() && gen.at(v) == k && !inv_done.count(v))
         (std::find(sums.begin(), sums.end(), nd(v).in[0]) != sums.end() ? direct : left).push_back(v);
     auto take = [&](const std::vector<int>& vs, const std::string& scale) {
       s << "  __syncthreads();\n";
@@ -606,6 +657,7 @@ struct GroupGen {
                                       (nd(v).op == KORCH_REDUCE_MEAN ? " / " + flit((double)P) : std::string()) + ";");
       inv_done.insert(v);
     }
+    if (sums.empty() && left.empty()) return;
     if (!direct.empty()) take(direct, nd(nd(direct[0]).in[0]).op == KORCH_REDUCE_MEAN ? " / " + flit((double)P) : std::string());
     // of values that follow from them, as many together as do not wait for each other
     std::function<bool(int)> ready = [&](int v) {
@@ -802,7 +854,10 @@ struct GroupGen {
     for (int v : r1) pass[gen.at(v) - 1].push_back(v);
     for (auto& p : pass) widest = std::max(widest, p.size());
     const int64_t rowf = (int64_t)r0.size() * CT4();
-    const int64_t red = std::max(red_floats((int)widest), r0.empty() || B == 1 ? 0 : slice_floats(rowf, B));
+    int64_t red = red_floats((int)widest);
+    for (auto& p : pass)
+      if (only_groups(p)) red = std::max(red, direct_floats((int)p.size()));
+    red = std::max(red, r0.empty() || B == 1 ? 0 : slice_floats(rowf, B));
     s << "  const int b = blockIdx.x / " << tiles << ", ct0 = (int)(blockIdx.x % " << tiles << ") * " << CT << ";\n";
     head(red, part_floats((int)widest), std::max<int64_t>({(int64_t)widest, (int64_t)r0.size(), (int64_t)r3.size()}) * CT4());
     s << raw_decl() << "  const int row0 = " << first_row() << ";\n  {\n" << raw_load("row0", std::to_string(P)) << "  }\n";
@@ -821,8 +876,14 @@ struct GroupGen {
       }
       s << "  {\n" << row_loop("row0", end, body, "") << "  }\n";
       set_fast_math(false);
-      channel_sums(acc);
-      after_pass(k + 1, pass[k]);
+      if (only_groups(pass[k])) {
+        group_sums_of(acc);
+        after_group_pass(pass[k]);
+        after_pass(k + 1, {});
+      } else {
+        channel_sums(acc);
+        after_pass(k + 1, pass[k]);
+      }
       s << raw_again();
     }
     if (!full_outs.empty()) {
@@ -894,7 +955,7 @@ struct GroupGen {
   void gen_moments() {
     const int64_t G = CT / K, G4 = (G + 3) / 4 * 4, rowf = 2 * G4;  // of the tile
     s << "  const int set = blockIdx.x / " << S << ", sp = blockIdx.x % " << S << ", b = set / " << tiles << ", ct0 = (set % " << tiles << ") * " << CT << ";\n";
-    head(red_floats(1), part_floats(1), std::max(CT4(), rowf));
+    head(direct_floats(1), 0, rowf);
     s << "  __shared__ float gmean[" << G << "];\n";
     s << raw_decl() << "  const int p1 = (sp + 1) * " << chunk << " < " << P << " ? (sp + 1) * " << chunk << " : " << P << ", lim = " << (NJ == 1 ? "act ? p1 : 0" : "p1") << ";\n";
     s << "  int row0 = sp * " << chunk << " + " << first_row() << ";\n" << raw_load("row0", "p1");
@@ -914,13 +975,11 @@ struct GroupGen {
     s << stream(o.str());
     // the workgroup's group means, then its sums of centred squares about them
     s << "  float nm[" << NJ << "][" << VEC << "];\n" << each("nm[j][e] = cnt_ * mean[j][e];");
-    channel_sums({"nm"});
-    group_sums(0);
+    group_sums_of({"nm"});
     s << "  __syncthreads();\n  const float rows_ = (float)(p1 - sp * " << chunk << ");\n  for (int q = tid; q < " << G << "; q += " << T << ") gmean[q] = grp[q] / (rows_ * " << flit((double)K)
       << ");\n  __syncthreads();\n";
     s << each("const float d = mean[j][e] - gmean[(c0[j] - ct0 + e) / " + std::to_string(K) + "]; nm[j][e] = __builtin_fmaf(cnt_ * d, d, m2[j][e]);");
-    channel_sums({"nm"});
-    group_sums(0);
+    group_sums_of({"nm"});
     s << "  __syncthreads();\n  for (int q = tid; q < " << G4 << "; q += " << T << ") {\n    chan[q] = q < " << G << " ? gmean[q] : 0.0f;\n    chan[" << G4 << " + q] = q < " << G
       << " ? grp[q] : 0.0f;\n  }\n  __syncthreads();\n";
     if (S > 1) {
