@@ -379,6 +379,9 @@ struct GroupGen {
     chunk = (P + S - 1) / S;
     chunk = (chunk + LY - 1) / LY * LY;
     S = (P + chunk - 1) / chunk;
+    // few rows: in as few batches as hold them evenly, one where it can be
+    const int64_t rows = chunk / LY, most = kind == Moments ? 8 : 4;
+    if (rows <= 2 * most) U = (int)((rows + (rows + most - 1) / most - 1) / ((rows + most - 1) / most));
     if (B * tiles * S * T >= ((int64_t)1 << 32)) bad("more threads than a launch holds");
   }
 
