@@ -251,7 +251,8 @@ struct GroupGen {
   // fp32 values of a row and the channels' own (256 registers; 1024 threads have 128 each).
   bool slab_fits(int threads, int64_t nr, int vec, int words) const {
     const int64_t raw = nr * std::max(1, vec * eb / 4) * words, own = (int64_t)vec * (words > 1 ? 8 : 5);
-    return threads == 256 ? raw <= 24 && nr <= 24 : threads == 512 ? raw <= 48 && nr <= 48 : raw + own <= 64 && nr <= 24;
+    if (threads < 256) return nr == 1;  // (maps of a few positions: no more threads than vectors)
+    return threads <= 256 ? raw <= 24 && nr <= 24 : threads == 512 ? raw <= 48 && nr <= 48 : raw + own <= 64 && nr <= 24;
   }
 
   // A slab of whole groups in a workgroup's registers: the fewest groups whose
@@ -270,7 +271,7 @@ struct GroupGen {
       while ((gt * K) % vec) vec /= 2;
       const int64_t ct = gt * K;
       bool fits = false;
-      for (int t : {256, 512, 1024}) {
+      for (int t : {64, 128, 256, 512, 1024}) {
         if (ct / vec > t) continue;
         const int64_t ly = t / (ct / vec), nr = (P + ly - 1) / ly;
         if (slab_fits(t, nr, vec, words)) {
@@ -294,7 +295,7 @@ struct GroupGen {
     tiles = G / best;
     VEC = 16 / eb;
     while (CT % VEC) VEC /= 2;
-    for (int t : {256, 512, 1024}) {
+    for (int t : {64, 128, 256, 512, 1024}) {
       if (CT / VEC > t) continue;
       lanes(t);
       NR = (int)((P + LY - 1) / LY);
@@ -315,6 +316,7 @@ struct GroupGen {
     VEC = 16 / eb;
     while (CT % VEC) VEC /= 2;
     while (threads < 1024 && CT / VEC > threads) threads *= 2;
+    while (threads > 64 && threads / 2 >= P * (CT / VEC)) threads /= 2;  // (maps of a few positions)
     lanes(threads);
     if ((int64_t)NJ * VEC > 16 || CT > 8192) bad("more channels than a workgroup keeps");
   }
@@ -341,7 +343,7 @@ struct GroupGen {
       U = (int)std::min<int64_t>(4, (chunk + LY - 1) / LY);
       chunk = (chunk + (int64_t)LY * U - 1) / ((int64_t)LY * U) * ((int64_t)LY * U);
       S = (P + chunk - 1) / chunk;
-      if (B * S * T + ((int64_t)C * 1024) >= ((int64_t)1 << 32) || S >= ((int64_t)1 << 31)) bad("more threads than a launch holds");
+      if (B * S * T + (((int64_t)C + 16) * 4 * T) >= ((int64_t)1 << 32) || S >= ((int64_t)1 << 31)) bad("more threads than a launch holds");
       return;
     }
     if (slab_geometry()) {
@@ -381,7 +383,10 @@ struct GroupGen {
     S = (P + chunk - 1) / chunk;
     // few rows: in as few batches as hold them evenly, one where it can be
     const int64_t rows = chunk / LY, most = kind == Moments ? 8 : 4;
-    if (rows <= 2 * most) U = (int)((rows + (rows + most - 1) / most - 1) / ((rows + most - 1) / most));
+    // (as far as they fit registers beside the sums)
+    const int64_t room = std::max<int64_t>(1, 32 / std::max<int64_t>(1, (int64_t)NJ * VEC * eb / 4 * (int64_t)xfull.size()));
+    U = (int)std::min<int64_t>(U, room);
+    if (rows <= 2 * most && most <= room) U = (int)((rows + (rows + most - 1) / most - 1) / ((rows + most - 1) / most));
     if (B * tiles * S * T >= ((int64_t)1 << 32)) bad("more threads than a launch holds");
   }
 
@@ -1021,21 +1026,31 @@ struct GroupGen {
 
   void gen_apply() {
     const int64_t nblk = r0.empty() ? 0 : (C + 15) / 16;
+    int64_t rblk = 0;
     if (nblk) {
       // sums over the images: 16 channels to a workgroup (a cache line of an
-      // image's), the images over its groups of 16 lanes, sixteen in flight
+      // image's), the images over its groups of 16 lanes, sixteen in flight, and
+      // many images over up to 64 workgroups (100000 images of 64 channels in one: 1.2 ms)
       const int GR = T / 16;
-      s << "  if (blockIdx.x >= " << B * S << ") {\n    __shared__ float sum_[" << T << "];\n    const int t_ = threadIdx.x, c = (int)(blockIdx.x - " << B * S
-        << ") * 16 + (t_ & 15);\n";
-      for (int v : r0) {
-        const int u = nd(v).in[0];
-        s << "    {\n      float x_ = 0.0f;\n      if (c < " << C << ")\n#pragma unroll 16\n        for (int i = t_ >> 4; i < " << B << "; i += " << GR << ") x_ += ld1(" << ptr(u)
-          << " + (i64)i * " << C << " + c);\n      sum_[t_] = x_;\n      __syncthreads();\n      if (t_ < 16 && c < " << C << ") {\n#pragma unroll\n        for (int w = 1; w < " << GR
-          << "; ++w) x_ += sum_[w * 16 + t_];\n";
-        for (int o : ki.k.outs)
-          if (rt(o) == v) s << "        " << out_store(g, o, outp(o), "c", 0, nd(v).op == KORCH_REDUCE_MEAN ? "x_ / " + flit((double)B) : "x_") << ";\n";
-        s << "      }\n      __syncthreads();\n    }\n";
+      const int64_t RS = nblk > 256 ? 1 : std::max<int64_t>(1, std::min<int64_t>(kOneLevel, B / (GR * 32))), per = (B + RS - 1) / RS, rowf = (int64_t)r0.size() * 16;
+      rblk = nblk * RS;
+      const int64_t red = RS > 1 ? slice_floats(rowf, RS) : 0;
+      s << "  if (blockIdx.x >= " << B * S << ") {\n    __shared__ __attribute__((aligned(16))) float sum_[" << T << "], chan[" << rowf << "]";
+      if (red) s << ", red[" << red << "]";
+      s << ";\n    const int tid = threadIdx.x, k_ = (int)(blockIdx.x - " << B * S << "), set = k_ / " << RS << ", rs = k_ % " << RS << ", c = set * 16 + (tid & 15);\n    const int i1 = (rs + 1) * " << per
+        << " < " << B << " ? (rs + 1) * " << per << " : " << B << ";\n";
+      for (size_t k = 0; k < r0.size(); ++k) {
+        s << "    {\n      float x_ = 0.0f;\n      if (c < " << C << ")\n#pragma unroll 16\n        for (int i = rs * " << per << " + (tid >> 4); i < i1; i += " << GR << ") x_ += ld1(" << ptr(nd(r0[k]).in[0])
+          << " + (i64)i * " << C << " + c);\n      sum_[tid] = x_;\n      __syncthreads();\n      if (tid < 16) {\n#pragma unroll\n        for (int w = 1; w < " << GR
+          << "; ++w) x_ += sum_[w * 16 + tid];\n        chan[" << k * 16 << " + tid] = x_;\n      }\n      __syncthreads();\n    }\n";
       }
+      if (RS > 1)
+        hand_over(nblk, "set", RS, "rs", rowf, kOneLevel, [&](const std::string& from, const std::string& m, int64_t maxm, int) { add_rows(rowf, from, m, maxm); });
+      for (size_t k = 0; k < r0.size(); ++k)
+        for (int o : ki.k.outs)
+          if (rt(o) == r0[k])
+            s << "    if (tid < 16 && c < " << C << ") " << out_store(g, o, outp(o), "c", 0, "chan[" + std::to_string(k * 16) + " + tid]" + (nd(r0[k]).op == KORCH_REDUCE_MEAN ? " / " + flit((double)B) : std::string()))
+              << ";\n";
       s << "    return;\n  }\n";
     }
     s << "  const int b = blockIdx.x / " << S << ", sp = blockIdx.x % " << S << ", ct0 = 0;\n";
@@ -1047,7 +1062,7 @@ struct GroupGen {
     s << raw_decl() << "  const int p1 = (sp + 1) * " << chunk << " < " << P << " ? (sp + 1) * " << chunk << " : " << P << ";\n";
     s << "  for (int row0 = sp * " << chunk << " + " << (NJ == 1 ? "ly" : "0") << "; row0 < " << (NJ == 1 ? "(act ? p1 : 0)" : "p1") << "; row0 += " << (int64_t)U * LY << ") {\n"
       << raw_load("row0", "p1") << row_loop("row0", "p1", body, store_rows()) << "  }\n";
-    gk.grid[0] = (int)(B * S + nblk);
+    gk.grid[0] = (int)(B * S + rblk);
   }
 
   GenKernel generate(int index) {

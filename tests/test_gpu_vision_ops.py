@@ -53,6 +53,8 @@ GN = [
     ("f16", 700, 3, 3, 32, 4, "silu"),        # more images than slabs hand over
     ("f16", 300, 2, 2, 2048, 64, "none"),     # more tiles and images than counters
     ("bf16", 2, 64, 64, 320, 32, "relu"),     # sums by tiles of groups
+    ("f16", 5000, 2, 3, 24, 4, "silu"),       # images summed by several workgroups, a few positions each
+    ("f32", 20000, 1, 2, 3, 1, "none"),
 ]
 
 
