@@ -1029,21 +1029,24 @@ struct GroupGen {
     int64_t rblk = 0;
     if (nblk) {
       // sums over the images: 16 channels to a workgroup (a cache line of an
-      // image's), the images over its groups of 16 lanes, sixteen in flight, and
+      // image's), the images over its groups of 16 lanes, sixteen loads in flight, and
       // many images over up to 64 workgroups (100000 images of 64 channels in one: 1.2 ms)
       const int GR = T / 16;
-      const int64_t RS = nblk > 256 ? 1 : std::max<int64_t>(1, std::min<int64_t>(kOneLevel, B / (GR * 32))), per = (B + RS - 1) / RS, rowf = (int64_t)r0.size() * 16;
+      const int64_t RS = nblk > 256 ? 1 : std::max<int64_t>(1, std::min<int64_t>(kOneLevel, B / (GR * 16))), per = (B + RS - 1) / RS, rowf = (int64_t)r0.size() * 16;
       rblk = nblk * RS;
       const int64_t red = RS > 1 ? slice_floats(rowf, RS) : 0;
       s << "  if (blockIdx.x >= " << B * S << ") {\n    __shared__ __attribute__((aligned(16))) float sum_[" << T << "], chan[" << rowf << "]";
       if (red) s << ", red[" << red << "]";
       s << ";\n    const int tid = threadIdx.x, k_ = (int)(blockIdx.x - " << B * S << "), set = k_ / " << RS << ", rs = k_ % " << RS << ", c = set * 16 + (tid & 15);\n    const int i1 = (rs + 1) * " << per
         << " < " << B << " ? (rs + 1) * " << per << " : " << B << ";\n";
-      for (size_t k = 0; k < r0.size(); ++k) {
-        s << "    {\n      float x_ = 0.0f;\n      if (c < " << C << ")\n#pragma unroll 16\n        for (int i = rs * " << per << " + (tid >> 4); i < i1; i += " << GR << ") x_ += ld1(" << ptr(nd(r0[k]).in[0])
-          << " + (i64)i * " << C << " + c);\n      sum_[tid] = x_;\n      __syncthreads();\n      if (tid < 16) {\n#pragma unroll\n        for (int w = 1; w < " << GR
-          << "; ++w) x_ += sum_[w * 16 + tid];\n        chan[" << k * 16 << " + tid] = x_;\n      }\n      __syncthreads();\n    }\n";
-      }
+      for (size_t k = 0; k < r0.size(); ++k) s << "    float x" << k << "_ = 0.0f;\n";
+      s << "    if (c < " << C << ")\n#pragma unroll " << (r0.size() > 1 ? 8 : 16) << "\n      for (int i = rs * " << per << " + (tid >> 4); i < i1; i += " << GR << ") {\n";
+      for (size_t k = 0; k < r0.size(); ++k) s << "        x" << k << "_ += ld1(" << ptr(nd(r0[k]).in[0]) << " + (i64)i * " << C << " + c);\n";
+      s << "      }\n";
+      for (size_t k = 0; k < r0.size(); ++k)
+        s << "    " << (k ? "__syncthreads();\n    " : "") << "sum_[tid] = x" << k << "_;\n    __syncthreads();\n    if (tid < 16) {\n#pragma unroll\n      for (int w = 1; w < " << GR << "; ++w) x" << k
+          << "_ += sum_[w * 16 + tid];\n      chan[" << k * 16 << " + tid] = x" << k << "_;\n    }\n";
+      s << "    __syncthreads();\n";
       if (RS > 1)
         hand_over(nblk, "set", RS, "rs", rowf, kOneLevel, [&](const std::string& from, const std::string& m, int64_t maxm, int) { add_rows(rowf, from, m, maxm); });
       for (size_t k = 0; k < r0.size(); ++k)
