@@ -602,9 +602,16 @@ struct GroupGen {
     const int SV = group_piece();
     const int64_t gt = CT / K, row = CT / SV, KS = K / SV;
     for (size_t i = 0; i < acc.size(); ++i) {
-      s << "#pragma unroll\n  for (int j = 0; j < " << NJ << "; ++j)\n    if (" << (NJ > 1 ? "act[j]" : "act") << ")\n#pragma unroll\n      for (int q = 0; q < " << VEC / SV
-        << "; ++q) {\n        float t_ = " << acc[i] << "[j][q * " << SV << "];\n#pragma unroll\n        for (int e = 1; e < " << SV << "; ++e) t_ += " << acc[i] << "[j][q * " << SV
-        << " + e];\n        red[" << i * LY * row << " + ly * " << row << " + (c0[j] - ct0) / " << SV << " + q] = t_;\n      }\n";
+      // (consecutive pieces as vectors: one by one, the lanes' pieces would share LDS banks)
+      const int NQ = VEC / SV, W = NQ % 4 == 0 ? 4 : NQ % 2 == 0 ? 2 : 1;
+      s << "#pragma unroll\n  for (int j = 0; j < " << NJ << "; ++j)\n    if (" << (NJ > 1 ? "act[j]" : "act") << ") {\n      float t_[" << NQ << "];\n#pragma unroll\n      for (int q = 0; q < " << NQ
+        << "; ++q) {\n        t_[q] = " << acc[i] << "[j][q * " << SV << "];\n#pragma unroll\n        for (int e = 1; e < " << SV << "; ++e) t_[q] += " << acc[i] << "[j][q * " << SV
+        << " + e];\n      }\n#pragma unroll\n      for (int q = 0; q < " << NQ << "; q += " << W << ") {\n        vec_t<" << W << ", float> w_;\n";
+      if (W == 1)
+        s << "        w_ = t_[q];\n";
+      else
+        for (int k = 0; k < W; ++k) s << "        w_[" << k << "] = t_[q + " << k << "];\n";
+      s << "        *(vec_t<" << W << ", float>*)(red + " << i * LY * row << " + ly * " << row << " + (c0[j] - ct0) / " << SV << " + q) = w_;\n      }\n    }\n";
     }
     s << "  __syncthreads();\n";
     const int64_t L = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(64, pow2floor(LY * KS)), pow2floor(std::max<int64_t>(1, T / gt))));
@@ -693,16 +700,77 @@ struct GroupGen {
     }
     s << "  __syncthreads();\n";
   }
-  // Per-channel and per-group outputs, by the first row of lanes.
-  void store_inv(bool whole_rounds) {
-    (void)whole_rounds;
+  // Per-channel outputs by the first row of lanes, as vectors; per-group outputs by
+  // the threads whose vectors begin a group, or, where a vector may begin many, by a
+  // thread each, by way of chan.
+  void store_inv() {
+    const std::string A = NJ > 1 ? "act[j]" : "act";
+    std::vector<int> of_group;
     for (int o : inv_outs) {
       const int v = rt(o);
-      const std::string x = inv(v), A = NJ > 1 ? "act[j]" : "act";
-      const bool chan = nd(v).shape[3] == K;
-      const std::string at = chan ? "(i64)b * " + std::to_string(C) + " + c0[j] + e" : "(i64)b * " + std::to_string(G) + " + (c0[j] + e) / " + std::to_string(K);
-      s << each("if (" + A + " && ly == 0" + (chan ? "" : " && (c0[j] + e) % " + std::to_string(K) + " == 0") + ") " + out_store(g, o, outp(o), at, 0, x) + ";");
+      if (nd(v).shape[3] != K || K == 1) {
+        of_group.push_back(o);
+        continue;
+      }
+      const std::string x = inv(v);
+      s << "#pragma unroll\n  for (int j = 0; j < " << NJ << "; ++j)\n    if (" << A << " && ly == 0) {\n      float o_[" << VEC << "];\n#pragma unroll\n      for (int e = 0; e < " << VEC
+        << "; ++e) o_[e] = " << x << ";\n      " << out_store(g, o, outp(o), "(i64)b * " + std::to_string(C) + " + c0[j]", VEC, "o_") << ";\n    }\n";
     }
+    for (int o : of_group) {
+      const std::string x = inv(rt(o));
+      if (VEC / group_piece() <= 2) {
+        const std::string SV = std::to_string(group_piece());
+        s << "#pragma unroll\n  for (int j = 0; j < " << NJ << "; ++j)\n#pragma unroll\n    for (int e = 0; e < " << VEC << "; e += " << SV << ")\n      if (" << A << " && ly == 0 && (c0[j] + e) % " << K
+          << " == 0) " << out_store(g, o, outp(o), "(i64)b * " + std::to_string(G) + " + (c0[j] + e) / " + std::to_string(K), 0, x) << ";\n";
+        continue;
+      }
+      s << "  __syncthreads();\n" << each("if (" + A + " && ly == 0) chan[c0[j] - ct0 + e] = " + x + ";") << "  __syncthreads();\n  for (int q = tid; q < " << CT / K << "; q += " << T << ") "
+        << out_store(g, o, outp(o), "(i64)b * " + std::to_string(G) + " + ct0 / " + std::to_string(K) + " + q", 0, "chan[q * " + std::to_string(K) + "]") << ";\n";
+    }
+  }
+
+  // Outputs that depend on the groups' means and variances alone: a thread per
+  // group evaluates and stores them (eight channels to a thread, each of which may
+  // begin a group, took 2 us).  False where a node varies along a group's channels.
+  bool store_groups(int64_t G4) {
+    std::function<bool(int)> per_group = [&](int v) {
+      if (in(v)) v = rt(v);
+      if (v == mo_mu || v == mo_var) return true;
+      Shape d;
+      if (!aligned(nd(v).shape, d) || (d[3] > 1 && K > 1) || d[1] > 1) return false;
+      if (!in(v)) return true;
+      for (int u : nd(v).in)
+        if (!per_group(u)) return false;
+      return true;
+    };
+    for (int o : inv_outs)
+      if (!per_group(o)) return false;
+    std::set<int> done;
+    std::function<std::string(int)> value = [&](int v) -> std::string {
+      if (in(v)) v = rt(v);
+      const std::string name = "h" + id(v);
+      if (!done.insert(v).second) return name;
+      if (v == mo_mu) {
+        s << "    const float " << name << " = chan[q];\n";
+      } else if (v == mo_var) {
+        s << "    const float " << name << " = chan[" << G4 << " + q] / " << flit((double)P * (double)K) << ";\n";
+      } else if (!in(v)) {
+        Shape d;
+        aligned(nd(v).shape, d);
+        s << "    const float " << name << " = ld1(" << ptr(v) << (d[0] > 1 ? " + (i64)b * " + std::to_string(d[2]) : std::string()) << (d[2] > 1 ? " + gr" : "") << ");\n";
+      } else {
+        const std::string ex = elem_expr(v, value);
+        s << "    const float " << name << " = " << ex << ";\n";
+      }
+      return name;
+    };
+    s << "  for (int q = tid; q < " << CT / K << "; q += " << T << ") {\n    const int gr = ct0 / " << K << " + q;\n";
+    for (int o : inv_outs) {
+      const std::string x = value(o);
+      s << "    " << out_store(g, o, outp(o), "(i64)b * " + std::to_string(G) + " + gr", 0, x) << ";\n";
+    }
+    s << "  }\n";
+    return true;
   }
 
   // Hands `rowf` floats of chan (a multiple of four) from workgroup to
@@ -902,7 +970,7 @@ struct GroupGen {
       s << "  {\n" << row_loop("row0", end, body, store_rows()) << "  }\n";
     }
     set_fast_math(false);
-    store_inv(true);
+    store_inv();
     if (!r0.empty()) {
       // sums over the images, image by image
       s << "  __syncthreads();\n";
@@ -956,14 +1024,14 @@ struct GroupGen {
     if (S > 1)
       hand_over(B * tiles, "set", S, "sp", rowf, kOneLevel, [&](const std::string& from, const std::string& m, int64_t maxm, int) { add_rows(rowf, from, m, maxm); });
     after_pass(1, r1);
-    store_inv(true);
+    store_inv();
     gk.grid[0] = (int)(B * tiles * S);
   }
 
   void gen_moments() {
     const int64_t G = CT / K, G4 = (G + 3) / 4 * 4, rowf = 2 * G4;  // of the tile
     s << "  const int set = blockIdx.x / " << S << ", sp = blockIdx.x % " << S << ", b = set / " << tiles << ", ct0 = (set % " << tiles << ") * " << CT << ";\n";
-    head(direct_floats(1), 0, rowf);
+    head(direct_floats(1), 0, std::max(CT4(), rowf));
     s << "  __shared__ float gmean[" << G << "];\n";
     s << raw_decl() << "  const int p1 = (sp + 1) * " << chunk << " < " << P << " ? (sp + 1) * " << chunk << " : " << P << ", lim = " << (NJ == 1 ? "act ? p1 : 0" : "p1") << ";\n";
     s << "  int row0 = sp * " << chunk << " + " << first_row() << ";\n" << raw_load("row0", "p1");
@@ -1015,13 +1083,14 @@ struct GroupGen {
         if (G4 > G) s << "  if (tid < " << G4 - G << ") { chan[" << G << " + tid] = 0.0f; chan[" << G4 + G << " + tid] = 0.0f; }\n";
       });
     }
+    gk.grid[0] = (int)(B * tiles * S);
+    if (store_groups(G4)) return;
     for (int v : {mo_mu, mo_var}) {
       s << jdecl("n" + id(v)) << each("n" + id(v) + "[j][e] = chan[" + (v == mo_var ? std::to_string(G4) + " + " : std::string()) + "(c0[j] - ct0 + e) / " + std::to_string(K) + "]" +
                                       (v == mo_var ? " / " + flit((double)P * (double)K) : std::string()) + ";");
       inv_done.insert(v);
     }
-    store_inv(true);
-    gk.grid[0] = (int)(B * tiles * S);
+    store_inv();
   }
 
   void gen_apply() {
