@@ -648,6 +648,9 @@ def mha_grad(batch=1, heads=8, kv_heads=None, n=1024, m=None, d=64, dtype="bf16"
     return w
 
 
+# The least normal and the largest fp32 number (eps and limits of a norm are fp32 in the kernels).
+_F32_MIN, _F32_MAX = 2.0 ** -126, (2.0 - 2.0 ** -23) * 2.0 ** 127
+
 # Activations after a group norm.
 ACTIVATIONS = ("none", "relu", "silu")
 
@@ -661,8 +664,8 @@ class _GroupNorm:
             raise ValueError("c must be a positive multiple of groups, and every size positive")
         if hh * ww * (c // groups) < 2:
             raise ValueError("a group needs two elements")
-        if not 0 <= eps < math.inf:
-            raise ValueError("eps must be finite and not negative")
+        if not 0 <= eps <= _F32_MAX:
+            raise ValueError("eps must be finite in fp32 and not negative")
         if act not in ACTIVATIONS:
             raise ValueError(f"act must be one of {', '.join(ACTIVATIONS)}")
         self.b, self.act, self.eps = b, act, eps
@@ -698,7 +701,8 @@ def groupnorm(batch=1, hh=64, ww=64, c=320, groups=32, dtype="f16", eps=1e-5, ac
       Xh = (X - mu) r,  Z = Xh gamma + beta,  Y = Z, relu(Z) or silu(Z) = Z / (1 + exp(-Z))
 
     The "fused" plan is one kernel where an image's group fits the registers of
-    a workgroup, else the statistics and the rest ("layered")."""
+    a workgroup, else the statistics and the rest ("layered"), which take up to
+    8192 channels."""
     b = _B(dtype)
     m = _GroupNorm(b, batch, hh, ww, c, groups, eps, act)
     b.inp("X", m.map)
@@ -914,7 +918,7 @@ def rotary(batch=1, heads=8, kv_heads=None, n=1024, d=64, rot=None, axes=1, inte
     rest stays.  Inputs ``positions`` [batch, n, axes] (any fp32 numbers),
     ``axis`` [rot / 2] (fp32 whole numbers; left out where there is one axis)
     and ``freq`` [rot / 2], radians per position (fp32).  The angle is the exact
-    product of its two fp32 factors, so far positions keep theirs.
+    product of its two fp32 factors (up to 2^50), so far positions keep theirs.
 
     Q [batch, heads, n, d] and K [batch, kv_heads, n, d] give ``Qr`` and ``Kr``;
     ``packed`` takes QKV [batch, n, heads + 2 kv_heads, d] as a projection's
@@ -978,18 +982,19 @@ def grad_clip(shapes=((768,), (768, 768)), dtype="bf16", dtypes=None, max_norm=1
       norm = sqrt(sum over all tensors and elements of G^2),   C_i = G_i min(1, max_norm / (norm + eps))
 
     Inputs G0, G1, .. of ``shapes`` (and ``dtypes``, default ``dtype`` for all);
-    outputs ``norm`` [1] (fp32) and C0, C1, .. of the inputs' shapes and types,
-    which may share their gradients' memory (every kernel reads an element
-    before it writes it).  The sum of squares is held in 64 bits by the fused
-    plan, so neither 1e30 nor 1e-30 leaves its range, and taken in a fixed order.
+    outputs ``norm`` [1] (fp32) and C0, C1, .. of the inputs' shapes and types.
+    C_i may share the memory of its own G_i (every kernel reads an element before
+    it writes it), as long as no two gradients lie in one memory.  The sum of
+    squares is held in 64 bits by the fused plan, so neither 1e30 nor 1e-30
+    leaves its range, and taken in a fixed order.
     A norm that is not a number leaves none in any gradient; an infinite one
     leaves zeros, and NaN where the gradient itself is infinite."""
     shapes = [tuple(int(x) for x in s) for s in shapes]
     dtypes = [dtype] * len(shapes) if dtypes is None else list(dtypes)
     if not shapes or len(dtypes) != len(shapes):
         raise ValueError("one shape at least, and a type for each")
-    if not (0 < max_norm < math.inf and 0 <= eps < math.inf):
-        raise ValueError("max_norm must be positive and finite, eps finite and not negative")
+    if not (_F32_MIN <= max_norm <= _F32_MAX and 0 <= eps <= _F32_MAX):
+        raise ValueError("max_norm must be a positive normal fp32 number, eps finite in fp32 and not negative")
     b = _B(dtype)
     k = len(shapes)
     for i, (s, t) in enumerate(zip(shapes, dtypes)):

@@ -374,6 +374,8 @@ REPEAT = [
     ("rotary_grad", dict(batch=2, heads=8, kv_heads=2, n=70, d=64, axes=2, packed=True, dtype="bf16")),
     ("grad_clip", dict(shapes=[(1000, 1000), (77,), (500, 900)], dtype="bf16", max_norm=0.5)),
     ("grad_clip", dict(shapes=[(4000, 5000)], dtype="f32", max_norm=0.5)),
+    ("groupnorm_grad", dict(batch=20000, hh=1, ww=2, c=40, groups=4, dtype="bf16")),  # images summed by several workgroups
+    ("groupnorm_grad", dict(batch=1, hh=64, ww=64, c=320, groups=32, dtype="bf16")),  # channels in tiles
 ]
 
 

@@ -125,6 +125,19 @@ def test_arguments_refused(name, sizes, what):
         graphs.build(name, **sizes)
 
 
+@pytest.mark.parametrize("name,sizes,what", [
+    ("groupnorm", dict(eps=1e39), "eps"),
+    ("groupnorm_grad", dict(eps=float("inf")), "eps"),
+    ("grad_clip", dict(max_norm=1e39), "max_norm"),
+    ("grad_clip", dict(max_norm=1e-50), "max_norm"),
+    ("grad_clip", dict(max_norm=float("nan")), "max_norm"),
+    ("grad_clip", dict(eps=1e39), "eps"),
+], ids=str)
+def test_numbers_that_fp32_does_not_hold_refused(name, sizes, what):
+    with pytest.raises(ValueError, match=what):
+        graphs.build(name, **sizes)
+
+
 def test_inputs_refused():
     import torch
 
