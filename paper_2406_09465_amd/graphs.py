@@ -686,6 +686,12 @@ class _GroupNorm:
         self.prims.append(name)
         return name
 
+    def relu(self, name, z, dtype="f32"):
+        """max(z, 0), and NaN where z is (the relu primitive is a maximum instruction, which drops it)."""
+        self.op(name + "_off", "le", [z], scalar=0.0)
+        self.op(name + "_on", "eq", [name + "_off"], scalar=0.0)
+        return self.op(name, "select", [name + "_on", z], dtype, scalar=0.0)
+
     def over_group(self, name, op, src):
         """A reduction over the positions and the channels of a group."""
         src = self.op(name + "_p" if self.per > 1 else name, op, [src], axis=1, keepdim=True)
@@ -732,7 +738,7 @@ def groupnorm(batch=1, hh=64, ww=64, c=320, groups=32, dtype="f16", eps=1e-5, ac
     else:
         m.op("Z", "add", ["Yg", "beta4"])
         if act == "relu":
-            last = m.op("Ya", "relu", ["Z"], dtype)
+            last = m.relu("Ya", "Z", dtype)
         else:
             m.op("nZ", "neg", ["Z"])
             m.op("eZ", "exp", ["nZ"])
@@ -761,7 +767,7 @@ def groupnorm_grad(batch=1, hh=64, ww=64, c=320, groups=32, dtype="f16", eps=1e-
       dZ = dY act'(Z),  dbeta = sum dZ,  dgamma = sum dZ Xh  over images and positions,
       g = dZ gamma,  dX = r (g - mean(g) - Xh mean(g Xh))   means over a group's positions and channels,
 
-    with relu'(Z) = [Z > 0] and silu'(Z) = s (1 + Z (1 - s)), s = 1 / (1 + exp(-Z)).
+    with relu'(Z) = [Z > 0] (NaN where Z is) and silu'(Z) = s (1 + Z (1 - s)), s = 1 / (1 + exp(-Z)).
     The means come from the sums over the positions that dgamma and dbeta need
     anyway.  (``eps`` is in the saved r.)"""
     b = _B(dtype)
@@ -792,7 +798,7 @@ def groupnorm_grad(batch=1, hh=64, ww=64, c=320, groups=32, dtype="f16", eps=1e-
         m.op("Z" + c, "add", ["Yg" + c, "beta4"])
         if act == "relu":
             m.op("on" + c, "gt", ["Z" + c], scalar=0.0)
-            return m.op("dZ" + c, "select", ["on" + c, "dY4"], scalar=0.0)
+            return m.op("dZ" + c, "select", ["on" + c, "dY4", m.relu("Zp" + c, "Z" + c)])
         m.op("nZ" + c, "neg", ["Z" + c])
         m.op("eZ" + c, "exp", ["nZ" + c])
         m.op("eZ1" + c, "add", ["eZ" + c], scalar=1.0)

@@ -1,0 +1,70 @@
+"""Group norm, rotary positions and gradient clipping at the edges of what they
+take, without a GPU: what is no number, sizes that a kernel just takes or just
+does not, and what the generated code needs."""
+
+import numpy as np
+import pytest
+
+from oracle.graph import run_unfused
+from paper_2406_09465_amd import graphs
+from tests import test_gpu_vision_ops as cases
+from tests import vision_ref as ref
+from tests.test_layer_ops import _oracle_copy
+
+
+def _oracle(name, x, **sizes):
+    w = graphs.build(name, **sizes)
+    return run_unfused(_oracle_copy(w), {k: x[k] for k in w.input_names})
+
+
+# ---- what is no number ------------------------------------------------------------
+
+
+def poisoned(dtype, hh, act):
+    """Three images with a NaN in group 1 and an infinity in group 2 of the second; the
+    plain results of what is not hit, and which elements of each result are."""
+    x, s = cases._gn_inputs(dtype, 3, hh, hh, 48)
+    want = ref.groupnorm(x["X"], x["gamma"], x["beta"], 4, 1e-5, act, dtype, x["dY"])
+    s["X"] = s["X"].copy()
+    x["X"] = x["X"].copy()
+    for v, at in ((np.nan, (1, hh // 2, 3, 14)), (np.inf, (1, 0, 0, 30))):
+        x["X"][at] = v
+        s["X"][at] = ref.rounded(np.array([v]), dtype)[1][0]
+    hit = np.zeros((3, 4), bool)
+    hit[1, 1] = hit[1, 2] = True
+    full = np.broadcast_to(np.repeat(hit, 12, axis=1)[:, None, None], x["X"].shape)
+    chan = np.repeat(hit.any(0), 12)
+    # without an activation dbeta is a sum of dY alone
+    return x, s, want, dict(Y=full, dX=full, mu=hit, r=hit, dgamma=chan, dbeta=chan if act != "none" else np.zeros_like(chan))
+
+
+def check_poisoned(out, want, hit, dtype):
+    for k, bad in hit.items():
+        v, b = want[k]
+        if k == "mu":  # (a group with an infinity: its mean is infinite, or none where parts of it merge)
+            assert np.isnan(out[k][1, 1]) and not np.isfinite(out[k][1, 2])
+        else:
+            assert np.all(np.isnan(out[k][bad])), k
+        if not bad.all():
+            assert ref.outside(out[k][~bad], v[~bad], b[~bad], "f32" if k in ("mu", "r") else dtype) <= 1.0, k
+
+
+@pytest.mark.parametrize("act", graphs.ACTIVATIONS)
+def test_a_group_that_is_no_number_stays_none(act):
+    """Every result of such a group is NaN, the sums over its channels too, whatever the activation."""
+    x, _, want, hit = poisoned("f32", 6, act)
+    z = dict(batch=3, hh=6, ww=6, c=48, groups=4, act=act, dtype="f32")
+    with np.errstate(invalid="ignore"):
+        x.update(_oracle("groupnorm", x, **z))
+        x.update(_oracle("groupnorm_grad", x, **z))
+    check_poisoned(x, want, hit, "f32")
+
+
+def test_relu_keeps_what_is_no_number_in_the_kernels():
+    """The maximum instruction drops a NaN: the kernels compare and select."""
+    for name in ("groupnorm", "groupnorm_grad"):
+        w = graphs.build(name, batch=3, hh=6, ww=6, c=48, groups=4, act="relu", dtype="f16")
+        for plan in ("fused", "layered"):
+            for k in w.kernels(plan):
+                body = w.graph.kernel_source(*k).split('extern "C"')[-1]
+                assert "k_relu" not in body and "k_max" not in body
