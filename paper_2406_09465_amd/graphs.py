@@ -856,12 +856,29 @@ class _Rotary:
         self.b, self.batch, self.heads, self.kv, self.n, self.d, self.rot = b, batch, heads, kv_heads, n, d, rot
         self.pairs, self.axes, self.interleaved, self.packed = rot // 2, axes, interleaved, packed
         self.sizes = dict(batch=batch, heads=heads, kv_heads=kv_heads, n=n, d=d, rot=rot, axes=axes, interleaved=interleaved, packed=packed)
-        self.prims = []
+        self.prims, self.reads = [], {}
 
     def op(self, name, op, ins, dtype="f32", **attrs):
         self.b.op(name, op, ins, dtype, **attrs)
         self.prims.append(name)
+        self.reads[name] = ins
         return name
+
+    def fused(self, w, outs):
+        """One kernel; where no family takes the results together (neighbouring
+        pairs in heads of odd width, which no vector of the rotary kernel holds,
+        and results whose heads differ), one for each with what it needs."""
+        whole = (list(self.prims), outs)
+        if _one_kernel(w, whole):
+            return [whole]
+        kernels = []
+        for o in outs:
+            need = {o}
+            for p in reversed(self.prims):
+                if p in need:
+                    need.update(self.reads[p])
+            kernels.append(([p for p in self.prims if p in need], [o]))
+        return kernels
 
     def angles(self):
         b = self.b
@@ -914,7 +931,8 @@ class _Rotary:
 
 def rotary(batch=1, heads=8, kv_heads=None, n=1024, d=64, rot=None, axes=1, interleaved=False, packed=False, dtype="bf16", extra_outputs=()):
     """Rotary positions of queries and keys along one or several axes (time,
-    height, width), in one kernel.  Pair p of a token's head turns by the angle
+    height, width), in one kernel (neighbouring pairs in heads of odd width: one
+    for each result).  Pair p of a token's head turns by the angle
     a = positions[b, i, axis[p]] freq[p]:
 
       (x1, x2) -> (x1 cos a - x2 sin a, x2 cos a + x1 sin a)
@@ -949,7 +967,7 @@ def rotary(batch=1, heads=8, kv_heads=None, n=1024, d=64, rot=None, axes=1, inte
     a.turn("Qr", src[0], a.heads, False)
     a.turn("Kr", src[1], a.kv, False)
     w = _finish(b, "rotary", outs, a.sizes, extra_outputs)
-    w.plans["fused"] = [(list(a.prims), outs)]
+    w.plans["fused"] = a.fused(w, outs)
     return w
 
 
@@ -973,7 +991,7 @@ def rotary_grad(batch=1, heads=8, kv_heads=None, n=1024, d=64, rot=None, axes=1,
         a.op("dQKV", "concat", ["dQt", "dKt", "dVt"], dtype, axis=2)
         outs = ["dQKV"]
     w = _finish(b, "rotary_grad", outs, a.sizes, extra_outputs)
-    w.plans["fused"] = [(list(a.prims), outs)]
+    w.plans["fused"] = a.fused(w, outs)
     return w
 
 

@@ -7,8 +7,8 @@ import pytest
 
 from paper_2406_09465_amd import graphs
 
-from .test_gpu_vision_ops import _run
-from .test_vision_edges import check_poisoned, poisoned
+from .test_gpu_vision_ops import _check, _rot_case, _rot_want, _run
+from .test_vision_edges import ODD_HEADS, check_poisoned, poisoned
 
 pytestmark = pytest.mark.gpu
 
@@ -22,3 +22,17 @@ def test_a_group_that_is_no_number_stays_none(act, hh, dtype, plan):
     g = {**s, "mu": out["mu"].astype(np.float32), "r": out["r"].astype(np.float32)}
     out.update(_run(graphs.build("groupnorm_grad", **z), g, plan))
     check_poisoned(out, want, hit, dtype)
+
+
+@pytest.mark.parametrize("case", ODD_HEADS + [
+    dict(dtype="f16", batch=7, heads=4, kv_heads=2, n=1, d=64, axes=2, first=3000),      # next tokens
+    dict(dtype="f32", batch=2, heads=6, kv_heads=3, n=1, d=40, rot=24, packed=True),
+    dict(dtype="f32", batch=3, heads=2, kv_heads=2, n=1, d=16, interleaved=True, axes=3),
+], ids=str)
+def test_rotary_and_gradient(case):
+    """Heads that no rotary kernel takes, and single tokens of every type."""
+    c, x, s = _rot_case(case)
+    for name, want in zip(("rotary", "rotary_grad"), _rot_want(c, x)):
+        out = _run(graphs.build(name, **c), s)
+        assert set(out) == set(want)
+        _check(out, want, c["dtype"])

@@ -68,3 +68,26 @@ def test_relu_keeps_what_is_no_number_in_the_kernels():
             for k in w.kernels(plan):
                 body = w.graph.kernel_source(*k).split('extern "C"')[-1]
                 assert "k_relu" not in body and "k_max" not in body
+
+
+# ---- heads that no rotary kernel takes ----------------------------------------------
+
+# neighbouring pairs in heads of odd width with grouped queries: the results differ in their heads
+ODD_HEADS = [
+    dict(dtype="f32", batch=1, heads=8, kv_heads=4, n=5, d=9, rot=4, interleaved=True),
+    dict(dtype="f16", batch=2, heads=4, kv_heads=2, n=7, d=9, rot=8, interleaved=True, packed=True, axes=2),
+    dict(dtype="bf16", batch=3, heads=6, kv_heads=2, n=1, d=33, rot=32, interleaved=True, axes=3, first=70000),
+    dict(dtype="f32", batch=1, heads=2, kv_heads=2, n=3, d=5, rot=2, interleaved=True, packed=True),
+]
+
+
+@pytest.mark.parametrize("case", ODD_HEADS, ids=str)
+def test_neighbours_in_odd_heads_have_a_fused_plan(case):
+    c, x, _ = cases._rot_case(case)
+    for name, want in zip(("rotary", "rotary_grad"), cases._rot_want(c, x)):
+        w = graphs.build(name, **c)
+        p = w.plan("fused").compile()
+        assert p.num_kernels() <= len(w.output_names) and all(p.kernel_info(k)[0] == "pointwise" for k in range(p.num_kernels()))
+        out = run_unfused(_oracle_copy(w), {k: x[k] for k in w.input_names})
+        for k, (v, _) in want.items():
+            assert np.allclose(out[k], v, rtol=1e-12, atol=1e-12), k
