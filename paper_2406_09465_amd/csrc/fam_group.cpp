@@ -43,6 +43,7 @@ int64_t pow2floor(int64_t x) {
 constexpr int kRowsInFlight = 8;     // rows that a thread loads together
 constexpr int64_t kHandOver = 16;    // partial results that one workgroup adds where there are two levels
 constexpr int64_t kOneLevel = 64;    // and at most with one
+constexpr int64_t kLds = 160 * 1024; // of a workgroup
 
 struct GroupGen {
   const KInfo& ki;
@@ -307,7 +308,8 @@ struct GroupGen {
       const int64_t lines = B <= kOneLevel ? 1 : (B + kHandOver - 1) / kHandOver + 1;  // counters of a tile (allocation-free execution has 64 KiB of them)
       if (B > kHandOver * 32 || tiles * lines > 256 || B * tiles * ((int64_t)r0.size() * ((CT + 3) / 4 * 4)) * 4 * 17 / 16 > ((int64_t)16 << 20)) return false;
     }
-    return B * tiles * T < ((int64_t)1 << 32);
+    kind = Slab;
+    return lds().bytes() <= kLds && B * tiles * T < ((int64_t)1 << 32);
   }
 
   void stream_geometry(int threads, int64_t channels) {
@@ -346,10 +348,7 @@ struct GroupGen {
       if (B * S * T + (((int64_t)C + 16) * 4 * T) >= ((int64_t)1 << 32) || S >= ((int64_t)1 << 31)) bad("more threads than a launch holds");
       return;
     }
-    if (slab_geometry()) {
-      kind = Slab;
-      return;
-    }
+    if (slab_geometry()) return;
     if (!full_outs.empty() || !r0.empty()) bad("a map and sums over it that do not fit the registers of a workgroup");
     if (find_moments())
       kind = Moments;
@@ -388,6 +387,7 @@ struct GroupGen {
     U = (int)std::min<int64_t>(U, room);
     if (rows <= 2 * most && most <= room) U = (int)((rows + (rows + most - 1) / most - 1) / ((rows + most - 1) / most));
     if (B * tiles * S * T >= ((int64_t)1 << 32)) bad("more threads than a launch holds");
+    if (lds().bytes() > kLds) bad("sums of more channels than LDS holds");
   }
 
   // ---- code ------------------------------------------------------------------
@@ -855,10 +855,50 @@ struct GroupGen {
       << " + v) * 4);\n      *(f32x4*)(chan + v * 4) = t_;\n    }\n  }\n";
   }
 
-  void head(int64_t lds_red, int64_t lds_part, int64_t lds_chan) {
-    if (lds_red) s << "  __shared__ __attribute__((aligned(16))) float red[" << lds_red << "];\n";
-    if (lds_part) s << "  __shared__ float part[" << lds_part << "];\n";
-    if (lds_chan) s << "  __shared__ __attribute__((aligned(16))) float chan[" << lds_chan << "];\n  __shared__ float grp[" << std::max<int64_t>(1, r3.size()) * (CT / K) << "];\n";
+  // What a kernel of the kind takes of LDS (floats).
+  struct Lds {
+    int64_t red = 0, part = 0, chan = 0, grp = 0, mean = 0;
+    int64_t bytes() const { return (red + part + chan + grp + mean) * 4 + 64; }  // (and the flag of a hand-over, and what aligns)
+  };
+  Lds lds() const {
+    Lds l;
+    const int n = (int)r1.size();
+    switch (kind) {
+      case Slab: {
+        int64_t widest = 1;
+        for (const auto& p : passes()) {
+          widest = std::max<int64_t>(widest, p.size());
+          if (only_groups(p)) l.red = std::max(l.red, direct_floats((int)p.size()));
+        }
+        l.red = std::max({l.red, red_floats((int)widest), r0.empty() || B == 1 ? 0 : slice_floats((int64_t)r0.size() * CT4(), B)});
+        l.part = part_floats((int)widest);
+        l.chan = std::max<int64_t>({widest, (int64_t)r0.size(), (int64_t)r3.size()}) * CT4();
+        break;
+      }
+      case Sums:
+        l.red = std::max(red_floats(n), S > 1 ? slice_floats(n * CT4(), S) : 0);
+        l.part = part_floats(n);
+        l.chan = std::max<int64_t>(n, r3.size()) * CT4();
+        break;
+      case Moments:
+        // (chan is written when red has been read for the last time)
+        l.red = std::max({direct_floats(1), CT4(), 2 * ((CT / K + 3) / 4 * 4)});
+        l.mean = CT / K;
+        l.grp = CT / K;
+        break;
+      case Apply: return l;
+    }
+    if (kind != Moments) l.grp = std::max<int64_t>(1, r3.size()) * (CT / K);
+    return l;
+  }
+
+  void head() {
+    const Lds l = lds();
+    if (l.red) s << "  __shared__ __attribute__((aligned(16))) float red[" << l.red << "];\n";
+    if (l.part) s << "  __shared__ float part[" << l.part << "];\n";
+    if (l.chan) s << "  __shared__ __attribute__((aligned(16))) float chan[" << l.chan << "];\n";
+    if (l.mean) s << "  __shared__ float gmean[" << l.mean << "];\n  float* const chan = red;\n";
+    if (l.grp) s << "  __shared__ float grp[" << l.grp << "];\n";
     s << "  const int tid = threadIdx.x;\n";
     if (NJ == 1) {
       s << "  const int ly = tid / " << CVT << ";\n  const bool act = ly < " << LY << ";\n";
@@ -924,18 +964,18 @@ struct GroupGen {
     return b.o.str() + st.str();
   }
 
-  void gen_slab() {
+  // The sums over positions of each pass.
+  std::vector<std::vector<int>> passes() const {
     std::vector<std::vector<int>> pass(npass);
-    size_t widest = 1;
     for (int v : r1) pass[gen.at(v) - 1].push_back(v);
-    for (auto& p : pass) widest = std::max(widest, p.size());
+    return pass;
+  }
+
+  void gen_slab() {
+    const std::vector<std::vector<int>> pass = passes();
     const int64_t rowf = (int64_t)r0.size() * CT4();
-    int64_t red = red_floats((int)widest);
-    for (auto& p : pass)
-      if (only_groups(p)) red = std::max(red, direct_floats((int)p.size()));
-    red = std::max(red, r0.empty() || B == 1 ? 0 : slice_floats(rowf, B));
     s << "  const int b = blockIdx.x / " << tiles << ", ct0 = (int)(blockIdx.x % " << tiles << ") * " << CT << ";\n";
-    head(red, part_floats((int)widest), std::max<int64_t>({(int64_t)widest, (int64_t)r0.size(), (int64_t)r3.size()}) * CT4());
+    head();
     s << raw_decl() << "  const int row0 = " << first_row() << ";\n  {\n" << raw_load("row0", std::to_string(P)) << "  }\n";
     const std::string end = NJ == 1 ? "(act ? " + std::to_string(P) + " : 0)" : std::to_string(P);
     for (int k = 0; k < npass; ++k) {
@@ -1001,7 +1041,7 @@ struct GroupGen {
   void gen_sums() {
     const int64_t rowf = (int64_t)r1.size() * CT4();
     s << "  const int set = blockIdx.x / " << S << ", sp = blockIdx.x % " << S << ", b = set / " << tiles << ", ct0 = (set % " << tiles << ") * " << CT << ";\n";
-    head(std::max(red_floats((int)r1.size()), S > 1 ? slice_floats(rowf, S) : 0), part_floats((int)r1.size()), std::max<int64_t>(rowf, r3.size() * CT4()));
+    head();
     std::vector<int> targets;
     for (int v : r1) targets.push_back(nd(v).in[0]);
     s << raw_decl() << "  const int p1 = (sp + 1) * " << chunk << " < " << P << " ? (sp + 1) * " << chunk << " : " << P << ", lim = " << (NJ == 1 ? "act ? p1 : 0" : "p1") << ";\n";
@@ -1031,8 +1071,7 @@ struct GroupGen {
   void gen_moments() {
     const int64_t G = CT / K, G4 = (G + 3) / 4 * 4, rowf = 2 * G4;  // of the tile
     s << "  const int set = blockIdx.x / " << S << ", sp = blockIdx.x % " << S << ", b = set / " << tiles << ", ct0 = (set % " << tiles << ") * " << CT << ";\n";
-    head(direct_floats(1), 0, std::max(CT4(), rowf));
-    s << "  __shared__ float gmean[" << G << "];\n";
+    head();
     s << raw_decl() << "  const int p1 = (sp + 1) * " << chunk << " < " << P << " ? (sp + 1) * " << chunk << " : " << P << ", lim = " << (NJ == 1 ? "act ? p1 : 0" : "p1") << ";\n";
     s << "  int row0 = sp * " << chunk << " + " << first_row() << ";\n" << raw_load("row0", "p1");
     s << "  float mean[" << NJ << "][" << VEC << "] = {}, m2[" << NJ << "][" << VEC << "] = {}, cnt_ = 0.0f;\n";
@@ -1126,7 +1165,7 @@ struct GroupGen {
       s << "    return;\n  }\n";
     }
     s << "  const int b = blockIdx.x / " << S << ", sp = blockIdx.x % " << S << ", ct0 = 0;\n";
-    head(0, 0, 0);
+    head();
     set_fast_math(false);
     load_invariants(full_outs);
     set_fast_math(fast_full());

@@ -7,7 +7,8 @@ import pytest
 
 from paper_2406_09465_amd import graphs
 
-from .test_gpu_vision_ops import _check, _rot_case, _rot_want, _run
+from . import vision_ref as ref
+from .test_gpu_vision_ops import _check, _gn_inputs, _gn_sizes, _rot_case, _rot_want, _run
 from .test_vision_edges import ODD_HEADS, check_poisoned, poisoned
 
 pytestmark = pytest.mark.gpu
@@ -36,3 +37,23 @@ def test_rotary_and_gradient(case):
         out = _run(graphs.build(name, **c), s)
         assert set(out) == set(want)
         _check(out, want, c["dtype"])
+
+
+WIDE = [
+    ("f16", 1, 40, 41, 8192, 8192, "silu"),   # a channel to a group, split positions: the groups' numbers fill most of LDS
+    ("f32", 2, 33, 40, 8192, 4096, "relu"),
+    ("f32", 1, 50, 41, 8190, 8190, "none"),
+]
+
+
+@pytest.mark.parametrize("case", WIDE, ids=str)
+def test_wide_maps(case):
+    z = _gn_sizes(case)
+    x, s = _gn_inputs(*case[:5])
+    want = ref.groupnorm(x["X"], x["gamma"], x["beta"], z["groups"], 1e-5, z["act"], z["dtype"], x["dY"])
+    out = _run(graphs.build("groupnorm", **z), s, "layered")
+    _check(out, want, z["dtype"], ("mu", "r"))
+    g = {**s, "mu": out["mu"].astype(np.float32), "r": out["r"].astype(np.float32)}
+    back = _run(graphs.build("groupnorm_grad", **z), g, "layered")
+    _check(back, want, z["dtype"])
+    assert set(out) | set(back) == set(want)

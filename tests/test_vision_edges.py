@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 
 from oracle.graph import run_unfused
-from paper_2406_09465_amd import graphs
+from paper_2406_09465_amd import codeobj, graphs
 from tests import test_gpu_vision_ops as cases
 from tests import vision_ref as ref
 from tests.test_layer_ops import _oracle_copy
@@ -91,3 +91,43 @@ def test_neighbours_in_odd_heads_have_a_fused_plan(case):
         out = run_unfused(_oracle_copy(w), {k: x[k] for k in w.input_names})
         for k, (v, _) in want.items():
             assert np.allclose(out[k], v, rtol=1e-12, atol=1e-12), k
+
+
+# ---- what a kernel needs of a compute unit -------------------------------------------
+
+
+def _compiled(name, sizes, plan):
+    """(family, resources) of every kernel of a plan."""
+    p = graphs.build(name, **sizes).plan(plan).compile()
+    return [(p.kernel_info(k)[0], r) for k in range(p.num_kernels()) for r in codeobj.kernel_resources(p.kernel_code(k)).values()]
+
+
+@pytest.mark.parametrize("c,groups", [(8192, 8192), (8192, 4096), (8191, 8191), (8190, 2730)])
+@pytest.mark.parametrize("dtype,batch,hh", [("f16", 1, 100), ("f32", 2, 64), ("bf16", 2, 64)])
+def test_wide_maps_of_many_groups_compile(c, groups, dtype, batch, hh):
+    """As many groups as channels, up to the widest maps: the groups' numbers fit LDS."""
+    sizes = dict(batch=batch, hh=hh, ww=hh, c=c, groups=groups, dtype=dtype)
+    for name in ("groupnorm", "groupnorm_grad"):
+        for plan in ("fused", "layered"):
+            for family, r in _compiled(name, sizes, plan):
+                assert family == "group" and r["lds"] <= 160 * 1024
+
+
+def test_sums_that_lds_does_not_hold_are_refused():
+    """Five sums over the positions of 8192 channels (160 KiB of partial sums): no family, instead of an error of the compiler."""
+    for c, family in ((8192, "none"), (4096, "group")):
+        b = graphs._B("f32")
+        prims, outs = [], []
+        b.inp("X", (1, 3000, 1, c))
+        b.inp("mu", (1, 1, 1, c))
+        b.op("D", "sub", ["X", "mu"])
+        prims.append("D")
+        for i in range(5):
+            b.op(f"x{i}", "mul", ["D"], scalar=float(i + 1))
+            b.op(f"s{i}", "reduce_sum", [f"x{i}"], axis=1, keepdim=True)
+            prims += [f"x{i}", f"s{i}"]
+            outs.append(f"s{i}")
+        w = graphs._finish(b, "sums", outs, {})
+        kernel = [w.ids[p] for p in prims], [w.ids[o] for o in outs]
+        assert w.graph.family(*kernel) == family
+        assert w.graph.compile_candidate(*kernel) == (family != "none")
