@@ -248,6 +248,15 @@ struct GroupGen {
     LY = NJ == 1 ? (int)(T / CVT) : 1;
   }
 
+  // Workgroups of 1024 threads have 128 registers for each, half of what smaller
+  // ones have: fewer rows and partial results in flight, loops as they are written
+  // (spilling, the statistics of 1x64x64x5120 f32 took 48.7 us instead of 20.0, the
+  // gradient's sums of 1x64x65x7680 f32 72.3 instead of 69.5).
+  bool few_registers() const { return T > 512; }
+  std::string as_written() const { return few_registers() ? "#pragma unroll 1\n" : ""; }
+  // Rows of the maps in `words` registers.
+  int64_t rows_in(int64_t words) const { return std::max<int64_t>(1, words / (NJ * std::max(1, VEC * eb / 4) * std::max<int64_t>(1, xfull.size()))); }
+
   // Whether `nr` rows of `words` maps stay in a thread's registers beside the
   // fp32 values of a row and the channels' own (256 registers; 1024 threads have 128 each).
   bool slab_fits(int threads, int64_t nr, int vec, int words) const {
@@ -342,7 +351,7 @@ struct GroupGen {
       // batches, so that the channels' values are loaded for several rows
       const int64_t want = std::max<int64_t>(1, ((double)B * P * C * eb >= 67108864.0 ? 4096 : 2048) / B);
       chunk = std::max<int64_t>((P + want - 1) / want, 1);
-      U = (int)std::min<int64_t>(4, (chunk + LY - 1) / LY);
+      U = (int)std::min<int64_t>({4, (chunk + LY - 1) / LY, few_registers() ? rows_in(16) : 4});
       chunk = (chunk + (int64_t)LY * U - 1) / ((int64_t)LY * U) * ((int64_t)LY * U);
       S = (P + chunk - 1) / chunk;
       if (B * S * T + (((int64_t)C + 16) * 4 * T) >= ((int64_t)1 << 32) || S >= ((int64_t)1 << 31)) bad("more threads than a launch holds");
@@ -382,8 +391,8 @@ struct GroupGen {
     S = (P + chunk - 1) / chunk;
     // few rows: in as few batches as hold them evenly, one where it can be
     const int64_t rows = chunk / LY, most = kind == Moments ? 8 : 4;
-    // (as far as they fit registers beside the sums)
-    const int64_t room = std::max<int64_t>(1, 32 / std::max<int64_t>(1, (int64_t)NJ * VEC * eb / 4 * (int64_t)xfull.size()));
+    // (as far as they fit registers beside the sums, and the sums' operands)
+    const int64_t room = rows_in(few_registers() && kind == Sums ? 16 : 32);
     U = (int)std::min<int64_t>(U, room);
     if (rows <= 2 * most && most <= room) U = (int)((rows + (rows + most - 1) / most - 1) / ((rows + most - 1) / most));
     if (B * tiles * S * T >= ((int64_t)1 << 32)) bad("more threads than a launch holds");
@@ -841,7 +850,7 @@ struct GroupGen {
     s << "  {\n    const __amdgpu_buffer_rsrc_t r_ = __builtin_amdgcn_make_buffer_rsrc(hand + (i64)(" << from << ") * " << rowf << ", 0, 0x7fffffff, 0x00020000);\n"
       << "    const int m_ = " << m << ", zs = tid / " << step << ";\n";
     const int64_t RD = std::min<int64_t>(per, 16);
-    s << "    if (zs < " << ZS << ")\n      for (int v = tid % " << step << "; v < " << CQ << "; v += " << step << ") {\n        f32x4 t_ = {};\n";
+    s << "    if (zs < " << ZS << ")\n" << as_written() << "      for (int v = tid % " << step << "; v < " << CQ << "; v += " << step << ") {\n        f32x4 t_ = {};\n";
     s << (per > RD ? "#pragma unroll 1\n" : "") << "        for (int z0 = 0; z0 < " << per << "; z0 += " << RD << ") {\n          float4 q_[" << RD << "];\n#pragma unroll\n          for (int z = 0; z < " << RD
       << "; ++z) {\n            const int zz = zs * " << per << " + z0 + z;\n            q_[z] = coherent_load4(r_, (unsigned)((zz < m_ ? zz : m_ - 1) * " << rowf * 4
       << " + v * 16));\n          }\n#pragma unroll\n          for (int z = 0; z < " << RD << "; ++z)\n            if (zs * " << per << " + z0 + z < m_" << (per % RD ? " && z0 + z < " + std::to_string(per) : std::string())
@@ -940,6 +949,9 @@ struct GroupGen {
   // A thread's rows of its workgroup's part in batches, the first of which is loaded already.
   std::string stream(const std::string& work) const {
     std::ostringstream o;
+    // (where registers are few, the compiler is not to know how often the loop runs: it unrolls
+    // up to 32 rounds, whatever the loop's own pragma says, and spills)
+    if (few_registers()) o << "  asm volatile(\"\" : \"+" << (NJ == 1 ? "v" : "s") << "\"(lim));\n";
     o << "  while (row0 < lim) {\n" << work << "    row0 += " << (int64_t)U * LY << ";\n    if (row0 >= lim) break;\n" << raw_load("row0", "p1") << "  }\n";
     return o.str();
   }
@@ -1044,7 +1056,7 @@ struct GroupGen {
     head();
     std::vector<int> targets;
     for (int v : r1) targets.push_back(nd(v).in[0]);
-    s << raw_decl() << "  const int p1 = (sp + 1) * " << chunk << " < " << P << " ? (sp + 1) * " << chunk << " : " << P << ", lim = " << (NJ == 1 ? "act ? p1 : 0" : "p1") << ";\n";
+    s << raw_decl() << "  const int p1 = (sp + 1) * " << chunk << " < " << P << " ? (sp + 1) * " << chunk << " : " << P << ";\n  int lim = " << (NJ == 1 ? "act ? p1 : 0" : "p1") << ";\n";
     s << "  int row0 = sp * " << chunk << " + " << first_row() << ";\n" << raw_load("row0", "p1");
     load_invariants(targets);
     set_fast_math(fast_full());
@@ -1072,7 +1084,7 @@ struct GroupGen {
     const int64_t G = CT / K, G4 = (G + 3) / 4 * 4, rowf = 2 * G4;  // of the tile
     s << "  const int set = blockIdx.x / " << S << ", sp = blockIdx.x % " << S << ", b = set / " << tiles << ", ct0 = (set % " << tiles << ") * " << CT << ";\n";
     head();
-    s << raw_decl() << "  const int p1 = (sp + 1) * " << chunk << " < " << P << " ? (sp + 1) * " << chunk << " : " << P << ", lim = " << (NJ == 1 ? "act ? p1 : 0" : "p1") << ";\n";
+    s << raw_decl() << "  const int p1 = (sp + 1) * " << chunk << " < " << P << " ? (sp + 1) * " << chunk << " : " << P << ";\n  int lim = " << (NJ == 1 ? "act ? p1 : 0" : "p1") << ";\n";
     s << "  int row0 = sp * " << chunk << " + " << first_row() << ";\n" << raw_load("row0", "p1");
     s << "  float mean[" << NJ << "][" << VEC << "] = {}, m2[" << NJ << "][" << VEC << "] = {}, cnt_ = 0.0f;\n";
     const std::string x = "tof(x" + id(mo_x) + "[i][j]" + (VEC > 1 ? "[e]" : "") + ")";
@@ -1098,8 +1110,8 @@ struct GroupGen {
     s << "  __syncthreads();\n  for (int q = tid; q < " << G4 << "; q += " << T << ") {\n    chan[q] = q < " << G << " ? gmean[q] : 0.0f;\n    chan[" << G4 << " + q] = q < " << G
       << " ? grp[q] : 0.0f;\n  }\n  __syncthreads();\n";
     if (S > 1) {
-      // (sixteen means and squares of a lane in flight, 32 where a lane has a group to itself)
-      const int64_t one = std::max<int64_t>(32, std::min(kOneLevel, 16 * std::min<int64_t>(16, pow2floor(std::max<int64_t>(1, T / G)))));
+      // (sixteen means and squares of a lane in flight, 32 where a lane has a group to itself and registers allow)
+      const int64_t one = std::max<int64_t>(few_registers() ? 16 : 32, std::min(kOneLevel, 16 * std::min<int64_t>(16, pow2floor(std::max<int64_t>(1, T / G)))));
       const int64_t GS = S <= one ? S : kHandOver;
       hand_over(B * tiles, "set", S, "sp", rowf, one, [&](const std::string& from, const std::string& m, int64_t maxm, int level) {
         // rows (positions) of partial z: a split's, or those of a whole group of splits
@@ -1107,7 +1119,7 @@ struct GroupGen {
         const std::string first = level == 1 ? "(" + from + " + z)" : "z";
         const int64_t L = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(16, pow2floor(maxm)), pow2floor(std::max<int64_t>(1, T / G))));
         const int64_t nz = (maxm + L - 1) / L;
-        s << "  for (int q = tid; q < " << (G * L + T - 1) / T * T << "; q += " << T << ") {\n    const int gr_ = q / " << L << ", gr = gr_ < " << G << " ? gr_ : " << G - 1
+        s << as_written() << "  for (int q = tid; q < " << (G * L + T - 1) / T * T << "; q += " << T << ") {\n    const int gr_ = q / " << L << ", gr = gr_ < " << G << " ? gr_ : " << G - 1
           << ", l = q % " << L << ", m_ = " << m << ";\n    float a_[" << nz << "], b_[" << nz << "], n_[" << nz << "], t = 0.0f, n = 0.0f, v = 0.0f;\n";
         s << "    float* const p_ = hand + (i64)(" << from << ") * " << rowf << " + gr;\n";
         s << "#pragma unroll\n    for (int i = 0; i < " << nz << "; ++i) {\n      const int z_ = l + i * " << L << ", z = z_ < m_ ? z_ : m_ - 1;\n      a_[i] = coherent_load(p_ + (i64)z * " << rowf
@@ -1171,7 +1183,7 @@ struct GroupGen {
     set_fast_math(fast_full());
     const std::string body = results();
     s << raw_decl() << "  const int p1 = (sp + 1) * " << chunk << " < " << P << " ? (sp + 1) * " << chunk << " : " << P << ";\n";
-    s << "  for (int row0 = sp * " << chunk << " + " << (NJ == 1 ? "ly" : "0") << "; row0 < " << (NJ == 1 ? "(act ? p1 : 0)" : "p1") << "; row0 += " << (int64_t)U * LY << ") {\n"
+    s << as_written() << "  for (int row0 = sp * " << chunk << " + " << (NJ == 1 ? "ly" : "0") << "; row0 < " << (NJ == 1 ? "(act ? p1 : 0)" : "p1") << "; row0 += " << (int64_t)U * LY << ") {\n"
       << raw_load("row0", "p1") << row_loop("row0", "p1", body, store_rows()) << "  }\n";
     gk.grid[0] = (int)(B * S + rblk);
   }

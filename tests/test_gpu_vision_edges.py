@@ -43,6 +43,9 @@ WIDE = [
     ("f16", 1, 40, 41, 8192, 8192, "silu"),   # a channel to a group, split positions: the groups' numbers fill most of LDS
     ("f32", 2, 33, 40, 8192, 4096, "relu"),
     ("f32", 1, 50, 41, 8190, 8190, "none"),
+    ("f32", 2, 40, 40, 4288, 2144, "silu"),   # 1024 threads, several vectors to each
+    ("bf16", 1, 45, 41, 6395, 5, "relu"),     # and single elements
+    ("f32", 30, 20, 21, 4288, 64, "silu"),    # an image to a workgroup
 ]
 
 

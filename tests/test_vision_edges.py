@@ -131,3 +131,31 @@ def test_sums_that_lds_does_not_hold_are_refused():
         kernel = [w.ids[p] for p in prims], [w.ids[o] for o in outs]
         assert w.graph.family(*kernel) == family
         assert w.graph.compile_candidate(*kernel) == (family != "none")
+
+
+@pytest.mark.parametrize("name,dtype,batch,hh,ww,c,groups,act", [
+    ("groupnorm", "f32", 1, 64, 64, 7200, 16, "silu"),
+    ("groupnorm", "f32", 2, 64, 64, 4288, 2144, "relu"),       # more groups than threads
+    ("groupnorm", "f32", 1, 64, 64, 6395, 6395, "none"),
+    ("groupnorm", "f16", 1, 64, 64, 8191, 8191, "relu"),
+    ("groupnorm_grad", "f32", 1, 64, 64, 4288, 32, "silu"),
+    ("groupnorm_grad", "f32", 1, 64, 64, 6464, 32, "silu"),
+    ("groupnorm_grad", "f32", 300, 16, 17, 4100, 10, "silu"),
+    ("groupnorm_grad", "f32", 9, 64, 65, 7680, 32, "silu"),
+    ("groupnorm_grad", "f32", 1, 100, 100, 8192, 4096, "silu"),
+    ("groupnorm_grad", "f32", 300, 5, 3, 6395, 1, "relu"),
+    ("groupnorm_grad", "f32", 1, 64, 64, 2606, 2606, "silu"),
+    ("groupnorm_grad", "f16", 2, 64, 64, 6395, 5, "silu"),
+    ("groupnorm_grad", "bf16", 300, 16, 17, 8191, 8191, "relu"),
+    ("groupnorm_grad", "bf16", 300, 1, 7, 8191, 1, "silu"),
+    ("groupnorm_grad", "f16", 9, 100, 100, 7285, 7285, "silu"),
+    ("groupnorm_grad", "bf16", 1, 200, 150, 6395, 1279, "relu"),
+    ("groupnorm", "f32", 300, 30, 41, 4288, 64, "silu"),
+    ("groupnorm", "bf16", 2, 64, 64, 8192, 256, "silu"),
+], ids=str)
+def test_wide_maps_compile_without_spills(name, dtype, batch, hh, ww, c, groups, act):
+    """Workgroups of 1024 threads have 128 registers for each."""
+    sizes = dict(dtype=dtype, batch=batch, hh=hh, ww=ww, c=c, groups=groups, act=act)
+    for plan in ("fused", "layered"):
+        for family, r in _compiled(name, sizes, plan):
+            assert family == "group" and r["scratch"] == 0 and r["vgpr_spill"] == 0
