@@ -2,10 +2,12 @@
 what they take, against plain float64 forms with bounds counted from the
 definitions."""
 
+import random
+
 import numpy as np
 import pytest
 
-from paper_2406_09465_amd import graphs
+from paper_2406_09465_amd import graphs, search
 
 from . import vision_ref as ref
 from .test_gpu_vision_ops import _check, _gn_inputs, _gn_sizes, _rot_case, _rot_want, _run
@@ -60,3 +62,27 @@ def test_wide_maps(case):
     back = _run(graphs.build("groupnorm_grad", **z), g, "layered")
     _check(back, want, z["dtype"])
     assert set(out) | set(back) == set(want)
+
+
+@pytest.mark.parametrize("case", [("f32", 2, 3, 5, 12, 4, "silu"), ("f32", 3, 70, 40, 12, 3, "relu"), ("f32", 3, 70, 40, 12, 3, "silu")], ids=str)
+def test_gradients_with_an_activation_by_sampled_plans(case):
+    """Random valid plans of the gradient's graph, of the group family's kernels and single primitives."""
+    from paper_2406_09465_amd.runner import PlanRunner
+    z = _gn_sizes(case)
+    x, s = _gn_inputs(*case[:5])
+    want = ref.groupnorm(x["X"], x["gamma"], x["beta"], z["groups"], 1e-5, z["act"], z["dtype"], x["dY"])
+    s.update({k: want[k][0].astype(np.float32) for k in ("mu", "r")})
+    w = graphs.build("groupnorm_grad", **z)
+    cands = [c for c in w.graph.candidates(max_prims=6, max_outs=2, only_supported=True) if len(c[0]) == 1 or w.graph.family(*c) == "group"]
+    wide, few = [c for c in cands if len(c[0]) > 3], [c for c in cands if len(c[0]) <= 2]
+    view, rng = search.GraphView(w.graph), random.Random(7)
+    for i in range(2):
+        plan = search.random_plan(view, rng.sample(wide, min(len(wide), 60)) + few, rng)
+        made = {o for _, outs in plan for o in outs}
+        r = PlanRunner(w, kernels=plan + [([o], [o]) for o in w.graph.outputs() if o not in made])  # (views that are outputs)
+        fams = [r.plan.kernel_info(k)[0] for k in range(r.plan.num_kernels())]
+        print(f"\n[case] {case} plan {i}: {fams}", flush=True)
+        assert "group" in fams
+        out = r.run(s)
+        assert set(out) == {"dX", "dgamma", "dbeta"}
+        _check(out, want, z["dtype"])

@@ -7,6 +7,7 @@ import pytest
 
 from oracle.graph import run_unfused
 from paper_2406_09465_amd import codeobj, graphs
+from paper_2406_09465_amd._abi import KorchError
 from tests import test_gpu_vision_ops as cases
 from tests import vision_ref as ref
 from tests.test_layer_ops import _oracle_copy
@@ -159,3 +160,50 @@ def test_wide_maps_compile_without_spills(name, dtype, batch, hh, ww, c, groups,
     for plan in ("fused", "layered"):
         for family, r in _compiled(name, sizes, plan):
             assert family == "group" and r["scratch"] == 0 and r["vgpr_spill"] == 0
+
+
+# ---- what is refused, exactly ---------------------------------------------------------
+
+
+@pytest.mark.parametrize("c,groups,hh,first", [(8194, 2, 4, "none"), (8194, 2, 200, "none"), (8194, 34, 200, "none"), (8194, 34, 4, "group"), (8194, 8194, 4, "group"),
+                                               (8192, 2, 4, "group")])
+def test_past_the_widest_maps(c, groups, hh, first):
+    """Past 8192 channels no kernel streams a map; a small map's groups still fit registers, in one kernel of all."""
+    for name in ("groupnorm", "groupnorm_grad"):
+        w = graphs.build(name, hh=hh, ww=hh, c=c, groups=groups)
+        for plan in ("fused", "layered"):
+            fams = [w.graph.family(*k) for k in w.kernels(plan)]
+            if c == 8192:
+                assert fams == ["group", "group"]
+            elif plan == "fused" and first == "group":
+                assert fams == ["group"]
+            else:  # (what only applies statistics is a pointwise kernel's, too)
+                assert fams == [first, "pointwise" if name == "groupnorm" else "none"]
+            if "none" in fams:
+                with pytest.raises(KorchError) as e:
+                    w.plan(plan).compile()
+                assert e.value.code == -20
+        assert w.plan("unfused").num_kernels() > 15
+
+
+def test_names_of_the_results():
+    want = {"groupnorm": ["Y", "mu", "r"], "groupnorm_grad": ["dX", "dgamma", "dbeta"], "rotary": ["Qr", "Kr"], "rotary_grad": ["dQ", "dK"],
+            "grad_clip": ["norm", "C0", "C1"]}
+    for name, outs in want.items():
+        w = graphs.build(name)
+        assert w.output_names == outs
+        for plan in w.plans:
+            stored = [o for _, made in w.plans[plan] for o in made]
+            assert set(outs) <= set(stored)
+    assert graphs.build("rotary", packed=True).output_names == ["Qr", "Kr", "V"] and graphs.build("rotary_grad", packed=True).output_names == ["dQKV"]
+
+
+@pytest.mark.parametrize("count", [199, 200, 201, 400, 401, 650])
+def test_clipping_of_many_tensors(count):
+    """A norm and a product for every 200 tensors, and the norm of the parts' norms."""
+    w = graphs.build("grad_clip", shapes=[(3 + i % 5, 2) for i in range(count)], dtype="f16")
+    fams = [w.graph.family(*k) for k in w.kernels("fused")]
+    parts = -(-count // graphs.CLIP_TENSORS)
+    assert len(fams) == (2 if parts == 1 else 2 * parts + 1)
+    # (a product of one tensor alone is the pointwise family's)
+    assert fams == ["multi"] * (len(fams) - 1) + ["pointwise" if count % graphs.CLIP_TENSORS == 1 else "multi"]
