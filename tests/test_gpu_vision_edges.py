@@ -10,8 +10,8 @@ import pytest
 from paper_2406_09465_amd import graphs, search
 
 from . import vision_ref as ref
-from .test_gpu_vision_ops import _check, _gn_inputs, _gn_sizes, _rot_case, _rot_want, _run
-from .test_vision_edges import ODD_HEADS, check_poisoned, poisoned
+from .test_gpu_vision_ops import _check, _clip_case, _gn_inputs, _gn_sizes, _rot_case, _rot_want, _run
+from .test_vision_edges import ODD_HEADS, SPLITS, check_poisoned, poisoned, split_plan
 
 pytestmark = pytest.mark.gpu
 
@@ -86,3 +86,31 @@ def test_gradients_with_an_activation_by_sampled_plans(case):
         out = r.run(s)
         assert set(out) == {"dX", "dgamma", "dbeta"}
         _check(out, want, z["dtype"])
+
+
+@pytest.mark.parametrize("name,case,groups,families", SPLITS, ids=str)
+def test_turns_in_several_kernels(name, case, groups, families):
+    from paper_2406_09465_amd.runner import PlanRunner
+    c, x, s = _rot_case(case)
+    want = _rot_want(c, x)[name == "rotary_grad"]
+    w = graphs.build(name, **c)
+    out = PlanRunner(w, kernels=split_plan(w, groups)).run(s)
+    assert set(out) == set(want)
+    _check(out, want, c["dtype"])
+
+
+def test_clipping_in_place_one_tensor_past_a_part():
+    """201 gradients, the last one's product a kernel of its own, written over the gradients."""
+    import torch
+    from paper_2406_09465_amd.runner import PlanRunner
+    case = dict(shapes=[(7 + i % 9, 3) for i in range(200)] + [(1001, 3)], dtype="f16")
+    dt, x, s = _clip_case(case)
+    want = ref.clipped(list(x.values()), dt, 0.5, 1e-6)
+    r = PlanRunner(graphs.build("grad_clip", **case, max_norm=0.5), "fused")
+    r.set_inputs(s)
+    r.outs[1:] = r.ins
+    r.launch()
+    torch.cuda.synchronize()
+    assert ref.outside(r.outs[0].double().cpu().numpy(), *want["norm"], "f32") <= 2.0  # (norms of parts are rounded too)
+    for i, t in enumerate(r.outs[1:]):
+        assert ref.outside(t.double().cpu().numpy(), *want[f"C{i}"], "f16") <= 1.0, i

@@ -6,8 +6,8 @@ import numpy as np
 import pytest
 
 from oracle.graph import run_unfused
-from paper_2406_09465_amd import codeobj, graphs
-from paper_2406_09465_amd._abi import KorchError
+from paper_2406_09465_amd import codeobj, graphs, search
+from paper_2406_09465_amd._abi import KorchError, Plan
 from tests import test_gpu_vision_ops as cases
 from tests import vision_ref as ref
 from tests.test_layer_ops import _oracle_copy
@@ -207,3 +207,48 @@ def test_clipping_of_many_tensors(count):
     assert len(fams) == (2 if parts == 1 else 2 * parts + 1)
     # (a product of one tensor alone is the pointwise family's)
     assert fams == ["multi"] * (len(fams) - 1) + ["pointwise" if count % graphs.CLIP_TENSORS == 1 else "multi"]
+
+
+def split_plan(w, groups):
+    """A plan whose kernels store the given results, each computed from the inputs and what earlier kernels stored."""
+    view, stored, kernels = search.GraphView(w.graph), set(w.graph.inputs()), []
+
+    def is_stored(v):
+        return v in stored or (view.op[v] == "reshape" and is_stored(view.ins[v][0]))
+
+    for outs in groups:
+        outs = [w.ids[o] for o in outs]
+        need, walk = set(), list(outs)
+        while walk:
+            v = walk.pop()
+            if v not in need and not is_stored(v):
+                need.add(v)
+                walk += view.ins[v]
+        kernels.append((sorted(need), outs))
+        stored.update(outs)
+    return kernels
+
+
+PACKED = dict(dtype="f16", batch=2, heads=4, kv_heads=2, n=21, d=32, rot=24, axes=2, packed=True)
+NEIGHBOURS = dict(dtype="f32", batch=3, heads=4, kv_heads=2, n=13, d=16, axes=3, interleaved=True, first=1000)
+# (operator, sizes, results of each kernel, families)
+SPLITS = [
+    ("rotary", PACKED, [["co"], ["si"], ["Qr", "Kr", "V"]], ["pointwise", "pointwise", "rotary"]),
+    ("rotary", PACKED, [["Qt"], ["Kt"], ["V"], ["Qr", "Kr"]], ["pointwise", "pointwise", "pointwise", "rotary"]),
+    ("rotary", PACKED, [["Kr"], ["V"], ["Qr"]], ["rotary", "pointwise", "rotary"]),
+    ("rotary", dict(PACKED, batch=1, heads=1, kv_heads=1), [["place"], ["V", "Kr", "Qr"]], ["pointwise", "rotary"]),
+    ("rotary", NEIGHBOURS, [["place"], ["Qr", "Kr"]], ["pointwise", "rotary"]),
+    ("rotary", NEIGHBOURS, [["co_i"], ["si_i"], ["Qr"], ["Kr"]], ["pointwise"] * 4),  # (stored angles of neighbours)
+    ("rotary_grad", PACKED, [["dQ"], ["dK"], ["dQKV"]], ["rotary", "rotary", "pointwise"]),
+    ("rotary_grad", dict(PACKED, interleaved=True), [["dQ", "dK"], ["dQKV"]], ["rotary", "pointwise"]),
+    ("rotary_grad", dict(PACKED, interleaved=True), [["co"], ["si"], ["dQKV"]], ["pointwise"] * 3),
+    ("rotary_grad", NEIGHBOURS, [["dQ"], ["dK"]], ["rotary", "rotary"]),
+]
+
+
+@pytest.mark.parametrize("name,case,groups,families", SPLITS, ids=str)
+def test_turns_in_several_kernels_compile(name, case, groups, families):
+    c = {k: v for k, v in case.items() if k != "first"}
+    w = graphs.build(name, **c)
+    p = Plan(w.graph, split_plan(w, groups)).compile()
+    assert [p.kernel_info(k)[0] for k in range(p.num_kernels())] == families
