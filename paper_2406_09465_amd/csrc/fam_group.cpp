@@ -8,10 +8,12 @@
 //     ([B, 1, G, K] -> [B, 1, G, 1]) and over the images ([B, 1, G, K] -> [1, 1, G, K]);
 //   * reshapes that rename such tensors.
 //
-// HBM bound throughout (10 to 30 operations per element).  A thread keeps one
-// vector of channels for every row it visits, so what belongs to a channel or
-// its group is loaded and computed once per thread, and consecutive threads
-// read consecutive memory.  Kinds of kernels:
+// 10 to 30 operations per element: what applies statistics to a large map is
+// bound by HBM, what sums by HBM, the vector units (busy 64 to 73 % of the time
+// at 8x64x64x320 bf16 with silu) and the hand-over together, a small map by its
+// launch and its exchanges.  A thread keeps one vector of channels for every row
+// it visits, so what belongs to a channel or its group is loaded and computed
+// once per thread, and consecutive threads read consecutive memory.  Kinds of kernels:
 //   * slab: a workgroup owns whole groups of one image, whose rows stay in its
 //     registers in their own type: every pass over the positions (mean, then
 //     variance, then the result) after the first reads registers, and the map
@@ -20,7 +22,7 @@
 //     workgroup of an image adds the partial sums in order and computes what
 //     follows from them;
 //   * moments: means and variances of groups in one pass (per thread, rows in
-//     batches of eight whose mean and centred squares merge into the running
+//     batches of up to eight whose mean and centred squares merge into the running
 //     ones; then mean and M2 of threads and of workgroups merge likewise), so
 //     a mean far from zero costs the variance no bits;
 //   * apply: no sum over positions; rows are spread over the chip.
@@ -40,7 +42,6 @@ int64_t pow2floor(int64_t x) {
   return p;
 }
 
-constexpr int kRowsInFlight = 8;     // rows that a thread loads together
 constexpr int64_t kHandOver = 16;    // partial results that one workgroup adds where there are two levels
 constexpr int64_t kOneLevel = 64;    // and at most with one
 constexpr int64_t kLds = 160 * 1024; // of a workgroup
@@ -63,7 +64,8 @@ struct GroupGen {
   int mo_mu = -1, mo_var = -1, mo_x = -1;
   std::set<int> mo_nodes;
   // geometry
-  int VEC = 1, T = 256, NJ = 1, LY = 1, U = kRowsInFlight, NR = 1;
+  int VEC = 1, T = 256, NJ = 1, LY = 1, NR = 1;
+  int U = 1;                         // rows that a thread loads together
   int64_t CT = 0, CVT = 0, tiles = 1, S = 1, chunk = 0;
 
   GroupGen(const KInfo& k) : ki(k), g(k.g) {}
@@ -347,8 +349,11 @@ struct GroupGen {
     if (npass == 0) {
       kind = Apply;
       stream_geometry(256, C);
-      // about eight workgroups to a compute unit, a thread's rows in whole
-      // batches, so that the channels' values are loaded for several rows
+      // about eight workgroups to a compute unit, sixteen for maps from 64 MiB on, whose
+      // last workgroups would end apart (the gradient's of 8x128x128x256 bf16, 134 MB:
+      // 30.1 us, 32.3 with eight; of 4x416x416x64 f16, 89 MB: 41.2, 43.0; of 8x64x64x320,
+      // 21 MB: 11.6, 11.3); a thread's rows in whole batches, so that the channels'
+      // values are loaded for several rows
       const int64_t want = std::max<int64_t>(1, ((double)B * P * C * eb >= 67108864.0 ? 4096 : 2048) / B);
       chunk = std::max<int64_t>((P + want - 1) / want, 1);
       U = (int)std::min<int64_t>({4, (chunk + LY - 1) / LY, few_registers() ? rows_in(16) : 4});
@@ -475,6 +480,9 @@ struct GroupGen {
     }
     return "f" + id(v);
   }
+  // Maps of 16 bits take the hardware's approximations of the exponential and the
+  // quotient, also where only their sums are stored, in fp32: those are off by a
+  // few 2^-24 (and the exponent's rounding, |Z| 2^-24), the maps' own values by 2^-11 or 2^-8.
   bool fast_full() const { return eb == 2; }
 
   // Rows in registers in their own type.

@@ -1008,7 +1008,9 @@ def grad_clip(shapes=((768,), (768, 768)), dtype="bf16", dtypes=None, max_norm=1
     Inputs G0, G1, .. of ``shapes`` (and ``dtypes``, default ``dtype`` for all);
     outputs ``norm`` [1] (fp32) and C0, C1, .. of the inputs' shapes and types.
     C_i may share the memory of its own G_i (every kernel reads an element before
-    it writes it), as long as no two gradients lie in one memory.  The sum of
+    it writes it), as long as no two gradients lie in one memory.  Every tensor
+    begins on a multiple of 16 bytes, as for every plan (``KORCH_E_ALIGN``
+    otherwise): in one flat buffer of many gradients, pad their sizes to that.  The sum of
     squares is held in 64 bits by the fused plan, so neither 1e30 nor 1e-30
     leaves its range, and taken in a fixed order.
     A norm that is not a number leaves none in any gradient; an infinite one
